@@ -39,7 +39,14 @@ extern "C" {
 
 typedef struct gptq2d_factors_s* gptq2d_factors_t; /* opaque factor handle */
 
-typedef enum { GPTQ2D_F32 = 0, GPTQ2D_F64 = 1 } gptq2d_dtype;
+/* F16 and BF16 are types of the eight-bit operators' inputs and outputs (below);
+ * factorisation and rounding take F32 and F64. */
+typedef enum { GPTQ2D_F32 = 0, GPTQ2D_F64 = 1, GPTQ2D_F16 = 2, GPTQ2D_BF16 = 3 } gptq2d_dtype;
+
+/* What an eight-bit code stands for, before its scale: a floating-point number
+ * with four exponent and three mantissa bits (largest 448) or an integer (-127 ..
+ * 127). */
+typedef enum { GPTQ2D_E4M3 = 0, GPTQ2D_INT8 = 1 } gptq2d_code;
 
 typedef enum {
   GPTQ2D_OK = 0,
@@ -240,6 +247,86 @@ gptq2d_status gptq2d_round_batched(int count, const gptq2d_factors_t* f, gptq2d_
  * used `workspace` met one, OK otherwise. The flags are the batch's, not a
  * problem's: to find the problem, round it on its own. */
 gptq2d_status gptq2d_round_batched_check(const void* workspace, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Eight-bit blocks: the product that a rounded matrix is served with
+ *
+ * A block of 128 values x is held as eight-bit codes q and a scale s, x ~ s q.
+ * With fl the rounding to 32 bits, amax the block's largest magnitude and top
+ * the largest code (448 for e4m3, 127 for int8):
+ *   s = max(fl(amax fl(1 / top)), 2^-126), rounded up to a power of two where
+ *       asked (pow2); 1 for a block of zeros
+ *   q = the code nearest to fl(x fl(1 / s)) within +-top, ties to even
+ * A block that holds a NaN or an infinity gets scale NaN and codes 0: what
+ * reads it comes out as NaN. With pow2, integers up to 16 in magnitude (a
+ * rounded Z of at most five bits) are held exactly.
+ *
+ * Codes (e4m3) are bytes, row-major, ld a multiple of 16, the first row 16-byte
+ * aligned; the bytes from the last column up to the next multiple of 16 belong
+ * to the row as well (the quantiser sets them to 0, the products do not read
+ * them). Blocks are 1 x 128 ("rows": the scale of block b of row r at
+ * S[b * lds + r], lds >= rows) or 128 x 128 ("tiles": S[(r / 128) * lds +
+ * c / 128], lds >= ceil(cols / 128)); the last block of a row or column of
+ * blocks may be short. All sizes lie in [1, 2^24], a matrix in 2^37 entries.
+ * ------------------------------------------------------------------------- */
+
+/* Quantises X (rows x cols, F32, F16 or BF16) to e4m3 blocks of block_rows (1
+ * or 128) x 128. Q, S (nullable together): the codes of X and their scales. QT,
+ * ST (nullable together): those of X's transpose (cols x rows), whose blocks
+ * run along X's columns; both come from one pass over X. Enqueued on `stream`.
+ * Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_block_quantize(int64_t rows, int64_t cols, gptq2d_dtype dt, const void* X,
+                                    int64_t ldx, int block_rows, int pow2, void* Q, int64_t ldq,
+                                    float* S, int64_t lds, void* QT, int64_t ldqt, float* ST,
+                                    int64_t ldst, void* stream);
+
+/* Bytes of device workspace gptq2d_block_matmul needs (may be 0; 0 on bad sizes). */
+size_t gptq2d_block_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/* Enqueues C = A B^T for codes A (M x K, blocks of 1 x 128: SA) and B (N x K,
+ * blocks of b_block_rows (1 or 128) x 128: SB); C (M x N) has type dt. Each
+ * block's products are summed by themselves and enter the sum, which is held in
+ * 32 bits, with the block's two scales. For a 32-bit C the products are summed
+ * in 32 bits throughout; for a 16-bit C inside a block by the eight-bit matrix
+ * instruction, whose sum was measured to be off by 1.5e-5 of the sum of
+ * magnitudes (3e-4 at most, where few products tower over the others). The
+ * order of the sums is fixed: the same call gives the same bits. workspace: as
+ * sized above, 256-byte aligned, owned by the caller; overlapping calls need
+ * distinct ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_block_matmul(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
+                                  const float* SA, int64_t ldsa, const void* B, int64_t ldb,
+                                  const float* SB, int64_t ldsb, int b_block_rows, gptq2d_dtype dt,
+                                  void* C, int64_t ldc, void* workspace, size_t ws_bytes,
+                                  void* stream);
+
+/* Bytes of device workspace gptq2d_block_linear needs (0 on bad sizes). */
+size_t gptq2d_block_linear_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/* Enqueues Y = X W^T for X (M x K, type dt), quantised on the way to blocks of 1
+ * x 128 (pow2 as above), and W (N x K) held as e4m3 tiles of 128 x 128 (SW); Y
+ * (M x N) has type dt. The same Y as gptq2d_block_quantize and
+ * gptq2d_block_matmul give, up to the order of the sums. Errors: INVALID_ARG,
+ * WORKSPACE, HIP. */
+gptq2d_status gptq2d_block_linear(int64_t M, int64_t N, int64_t K, gptq2d_dtype dt, const void* X,
+                                  int64_t ldx, const void* W, int64_t ldw, const float* SW,
+                                  int64_t ldsw, int pow2, void* Y, int64_t ldy, void* workspace,
+                                  size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace gptq2d_block_linear_backward needs (0 on bad sizes). */
+size_t gptq2d_block_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/* Enqueues the gradients of that layer from dY (M x N, type dt): dX = dY W (M x
+ * K, type dt; nullable) with dY in blocks of 1 x 128 along N and WT (K x N) the
+ * e4m3 tiles of W's transpose, and dW = dY^T X (N x K, 32 bits; nullable) with
+ * both in blocks of 128 rows (tokens). X may be NULL without dW, WT and SWT
+ * without dX. The quantisations themselves are passed as the identity. Errors:
+ * INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq2d_dtype dt,
+                                           const void* dY, int64_t lddy, const void* X, int64_t ldx,
+                                           const void* WT, int64_t ldwt, const float* SWT,
+                                           int64_t ldswt, int pow2, void* dX, int64_t lddx,
+                                           float* dW, int64_t lddw, void* workspace,
+                                           size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Diagnostics

@@ -21,7 +21,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libgptq2d.so")
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "gptq2d.h")
 
-F32, F64 = 0, 1
+F32, F64, F16, BF16 = 0, 1, 2, 3
+E4M3, INT8 = 0, 1
 STATUS = {0: "OK", -1: "ERR_INVALID_ARG", -2: "ERR_SINGULAR", -3: "ERR_NONFINITE", -4: "ERR_OOM",
           -5: "ERR_HIP", -6: "ERR_WORKSPACE", -7: "ERR_OVERFLOW", -8: "ERR_TIMEOUT"}
 
@@ -71,6 +72,15 @@ def load():
         "gptq2d_round_batched_workspace_size": (sz, [i32, vp]),
         "gptq2d_round_batched": (i32, [i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "gptq2d_round_batched_check": (i32, [vp, vp]),
+        "gptq2d_block_quantize": (i32, [i64, i64, i32, vp, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "gptq2d_block_matmul_workspace_size": (sz, [i64, i64, i64]),
+        "gptq2d_block_matmul": (i32, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, sz,
+                                      vp]),
+        "gptq2d_block_linear_workspace_size": (sz, [i64, i64, i64]),
+        "gptq2d_block_linear": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, sz, vp]),
+        "gptq2d_block_linear_backward_workspace_size": (sz, [i64, i64, i64]),
+        "gptq2d_block_linear_backward": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64,
+                                               vp, i64, vp, sz, vp]),
         "gptq2d_status_string": (ctypes.c_char_p, [i32]),
         "gptq2d_last_error": (ctypes.c_char_p, []),
         "gptq2d_version": (i32, []),
@@ -416,6 +426,148 @@ def gptq2d_schedule_sweeps(m: int, n: int):
     rows = np.zeros((total, 2), dtype=np.int32)
     lib.gptq2d_schedule_sweeps(m, n, rows.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), total)
     return rows
+
+
+# ---------------------------------------------------------------------------
+# Eight-bit operators
+#
+# With prepare=True nothing is enqueued: the arguments are checked and laid out
+# once and a function of no arguments is returned that enqueues the call on the
+# stream given (or current) now, for loops over the same tensors.
+# ---------------------------------------------------------------------------
+
+_NARROW = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_CODES = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
+
+
+def _narrow(*tensors) -> int:
+    """The common dtype (float32, float16 or bfloat16) of the tensors given."""
+    kinds = {t.dtype for t in tensors if t is not None}
+    if len(kinds) != 1 or next(iter(kinds)) not in _NARROW:
+        raise TypeError(f"need tensors of one dtype out of float32, float16 and bfloat16, got {sorted(map(str, kinds))}")
+    return _NARROW[kinds.pop()]
+
+
+def _codes(t: torch.Tensor, rows: int, cols: int, what: str):
+    """Pointer and row stride of e4m3 codes, whose rows reach to a multiple of
+    16 columns (the stride has to be one, also of a single row)."""
+    if t.dtype != torch.float8_e4m3fn:
+        raise TypeError(f"{what} must be float8_e4m3fn")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    ld = _layout(t, rows, cols, what)
+    up = -(-cols // 16) * 16
+    if rows == 1:
+        ld = max(ld, up)
+    if ld % 16 or t.data_ptr() % 16:
+        raise ValueError(f"{what} needs rows on 16-byte boundaries, its row stride is {ld}")
+    if t.storage_offset() + (rows - 1) * ld + up > t.untyped_storage().nbytes():
+        raise ValueError(f"{what}: its rows must reach to a multiple of 16 columns")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _scales(t: torch.Tensor, rows: int, cols: int, what: str):
+    if t.dtype != torch.float32:
+        raise TypeError(f"{what} must be float32")
+    return _mat(t, rows, cols, what)
+
+
+def _space(workspace, need: int, what: str):
+    if need == 0:
+        return ctypes.c_void_p(0), 0
+    if workspace is None or not workspace.is_cuda:
+        raise ValueError(f"{what} needs a device workspace of {need} bytes")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _blocks(v: int) -> int:
+    return -(-v // 128)
+
+
+def _enqueue(name: str, args, keep, prepare: bool):
+    fn = getattr(load(), name)
+
+    def call(_keep=keep):  # the tensors live as long as the call can be made
+        st = fn(*args)
+        if st != 0:
+            _check(st, name)
+    if prepare:
+        return call
+    call()
+
+
+def gptq2d_block_quantize(X, Q, S, QT=None, ST=None, block_rows: int = 1, pow2: bool = False, stream=None,
+                          prepare=False):
+    """e4m3 codes and scales of X (Q, S) and of its transpose (QT, ST); either
+    pair may be None."""
+    rows, cols = X.shape
+    px, ldx = _mat(X, rows, cols, "X")
+    tile = block_rows != 1
+    q = s = qt = st = (ctypes.c_void_p(0), 0)
+    if Q is not None:
+        q = _codes(Q, rows, cols, "Q")
+        s = _scales(S, _blocks(rows) if tile else _blocks(cols), _blocks(cols) if tile else rows, "S")
+    if QT is not None:
+        qt = _codes(QT, cols, rows, "QT")
+        st = _scales(ST, _blocks(cols) if tile else _blocks(rows), _blocks(rows) if tile else cols, "ST")
+    args = (rows, cols, _narrow(X), px, ldx, block_rows, int(bool(pow2)), *q, *s, *qt, *st, _stream(stream))
+    return _enqueue("gptq2d_block_quantize", args, (X, Q, S, QT, ST), prepare)
+
+
+def gptq2d_block_matmul_workspace_size(M: int, N: int, K: int) -> int:
+    return int(load().gptq2d_block_matmul_workspace_size(M, N, K))
+
+
+def gptq2d_block_matmul(A, SA, B, SB, C, workspace=None, block_rows: int = 128, stream=None, prepare=False):
+    """C = A B^T for e4m3 codes A (M x K; SA: blocks x M) and B (N x K; SB: the
+    scales of blocks of block_rows x 128)."""
+    (M, K), N = A.shape, B.shape[0]
+    a, b = _codes(A, M, K, "A"), _codes(B, N, K, "B")
+    sa = _scales(SA, _blocks(K), M, "SA")
+    sb = _scales(SB, *((_blocks(K), N) if block_rows == 1 else (_blocks(N), _blocks(K))), "SB")
+    c = _mat(C, M, N, "C")
+    ws = _space(workspace, gptq2d_block_matmul_workspace_size(M, N, K), "gptq2d_block_matmul")
+    args = (M, N, K, *a, *sa, *b, *sb, block_rows, _narrow(C), *c, *ws, _stream(stream))
+    return _enqueue("gptq2d_block_matmul", args, (A, SA, B, SB, C, workspace), prepare)
+
+
+def gptq2d_block_linear_workspace_size(M: int, N: int, K: int) -> int:
+    return int(load().gptq2d_block_linear_workspace_size(M, N, K))
+
+
+def gptq2d_block_linear(X, W, SW, Y, workspace, pow2: bool = False, stream=None, prepare=False):
+    """Y = X W^T: X (M x K) quantised on the way, W (N x K) e4m3 tiles of 128 x 128."""
+    (M, K), N = X.shape, W.shape[0]
+    x, w, y = _mat(X, M, K, "X"), _codes(W, N, K, "W"), _mat(Y, M, N, "Y")
+    sw = _scales(SW, _blocks(N), _blocks(K), "SW")
+    ws = _space(workspace, gptq2d_block_linear_workspace_size(M, N, K), "gptq2d_block_linear")
+    args = (M, N, K, _narrow(X, Y), *x, *w, *sw, int(bool(pow2)), *y, *ws, _stream(stream))
+    return _enqueue("gptq2d_block_linear", args, (X, W, SW, Y, workspace), prepare)
+
+
+def gptq2d_block_linear_backward_workspace_size(M: int, N: int, K: int) -> int:
+    return int(load().gptq2d_block_linear_backward_workspace_size(M, N, K))
+
+
+def gptq2d_block_linear_backward(dY, X, WT, SWT, dX, dW, workspace, pow2: bool = False, stream=None, prepare=False):
+    """dX = dY W (dtype of dY) and dW = dY^T X (float32); either may be None. WT
+    (K x N): the e4m3 tiles of W's transpose."""
+    M, N = dY.shape
+    if dX is None and dW is None:
+        raise ValueError("neither dX nor dW is asked for")
+    K = (dX if dX is not None else dW).shape[1]
+    none = (ctypes.c_void_p(0), 0)
+    dy = _mat(dY, M, N, "dY")
+    x = wt = swt = dx = dw = none
+    if dX is not None:
+        wt, dx = _codes(WT, K, N, "WT"), _mat(dX, M, K, "dX")
+        swt = _scales(SWT, _blocks(K), _blocks(N), "SWT")
+    if dW is not None:
+        x, dw = _mat(X, M, K, "X"), _scales(dW, N, K, "dW")
+    dt = _narrow(dY, dX, X if dW is not None else None)
+    ws = _space(workspace, gptq2d_block_linear_backward_workspace_size(M, N, K), "gptq2d_block_linear_backward")
+    args = (M, N, K, dt, *dy, *x, *wt, *swt, int(bool(pow2)), *dx, *dw, *ws, _stream(stream))
+    return _enqueue("gptq2d_block_linear_backward", args, (dY, X, WT, SWT, dX, dW, workspace), prepare)
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,678 @@
+// Matrices in eight-bit floating point (e4m3) with a 32-bit scale for each
+// block of 128 values: the quantiser and the product
+//   C[m][n] = sum_b SA[b][m] SB[b][n] sum_{k in block b} A[m][k] B[n][k].
+#include <algorithm>
+#include <type_traits>
+
+#include "codes.hpp"
+
+namespace g2d {
+namespace {
+
+constexpr int kBlock = 128;
+
+// ---------------------------------------------------------------------------
+// Quantiser
+// ---------------------------------------------------------------------------
+
+struct QuantArgs {
+  int64_t rows, cols;
+  const void* X;
+  int64_t ldx;
+  uint8_t* Q;
+  int64_t ldq;
+  float* S;
+  int64_t lds;
+  uint8_t* QT;
+  int64_t ldqt;
+  float* ST;
+  int64_t ldst;
+  bool pow2, wide;
+};
+
+// Codes of the first n of eight columns; the rest up to the next multiple of
+// 16 is inside the row (its leading dimension is one) and becomes code 0.
+__device__ __forceinline__ void put8(uint8_t* p, u2 q) { *(u2*)p = q; }
+
+// Blocks of 1 x 128, 16 lanes each, eight values a lane.
+template <class T>
+__global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
+  const int64_t nb = (a.cols + kBlock - 1) / kBlock, total = a.rows * nb;
+  for (int64_t id = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); id < total; id += (int64_t)gridDim.x * 16) {
+    const int64_t row = id / nb, b = id - row * nb;
+    const int64_t c0 = b * kBlock + (threadIdx.x & 15) * 8;
+    const int n = (int)min((int64_t)8, a.cols - c0);
+    float x[8];
+    load8((const T*)a.X + row * a.ldx + c0, a.wide && n == 8, n, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, mag(x[i]));
+    m = group_max<16>(m);
+    const float s = block_scale(m, 1.0f / kTopE4M3, a.pow2);
+    const u2 q = code8<false>(x, 1.0f / s, bad_amax(m));
+    if (c0 < (a.cols + 15) / 16 * 16) put8(a.Q + row * a.ldq + c0, q);
+    if ((threadIdx.x & 15) == 0) a.S[b * a.lds + row] = s;
+  }
+}
+
+// One 128 x 128 tile per work group, read once: thread t holds the 8 x 8
+// values of rows 8 (t / 16) and columns 8 (t % 16). TILE: one scale for the
+// tile; otherwise one for each row (Q) and one for each column (QT).
+template <class T, bool TILE>
+__global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
+  __shared__ uint32_t colmax[16][kBlock + 4];
+  __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 16];
+  const int t = threadIdx.x, tr = t >> 4, tc = t & 15;
+  const int64_t nc = (a.cols + kBlock - 1) / kBlock, by = blockIdx.x / nc, bx = blockIdx.x - by * nc;
+  const int64_t r0 = by * kBlock, c0 = bx * kBlock;
+  const int64_t rows = a.rows - r0, cols = a.cols - c0;  // of the tile on
+  float x[8][8];
+  uint32_t rm[8], cm[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cm[i] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = 8 * tr + i;
+    const int n = r < rows ? (int)max((int64_t)0, min((int64_t)8, cols - 8 * tc)) : 0;
+    load8((const T*)a.X + (r0 + r) * a.ldx + c0 + 8 * tc, a.wide && n == 8, n, x[i]);
+    rm[i] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = mag(x[i][j]);
+      rm[i] = max(rm[i], m);
+      cm[j] = max(cm[j], m);
+    }
+  }
+  if constexpr (TILE) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, rm[i]);
+    m = group_max<64>(m);
+    if ((t & 63) == 0) colmax[0][t >> 6] = m;
+    __syncthreads();
+    m = max(max(colmax[0][0], colmax[0][1]), max(colmax[0][2], colmax[0][3]));
+    const float s = block_scale(m, 1.0f / kTopE4M3, a.pow2);
+    if (t == 0) {
+      if (a.Q) a.S[by * a.lds + bx] = s;
+      if (a.QT) a.ST[bx * a.ldst + by] = s;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rm[i] = cm[i] = m;
+  }
+  if (a.Q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = 8 * tr + i;
+      if constexpr (!TILE) rm[i] = group_max<16>(rm[i]);
+      const float s = block_scale(rm[i], 1.0f / kTopE4M3, a.pow2);
+      const u2 q = code8<false>(x[i], 1.0f / s, bad_amax(rm[i]));
+      if (r < rows) {
+        if (8 * tc < (cols + 15) / 16 * 16) put8(a.Q + (r0 + r) * a.ldq + c0 + 8 * tc, q);
+        if (!TILE && tc == 0) a.S[bx * a.lds + r0 + r] = s;
+      }
+    }
+  }
+  if (a.QT) {
+    if constexpr (!TILE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) colmax[tr][8 * tc + j] = cm[j];
+      __syncthreads();
+      if (t < kBlock) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = max(m, colmax[i][t]);
+        colmax[0][t] = m;
+        if (t < cols) a.ST[by * a.ldst + c0 + t] = block_scale(m, 1.0f / kTopE4M3, a.pow2);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cm[j] = colmax[0][8 * tc + j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float r = 1.0f / block_scale(cm[j], 1.0f / kTopE4M3, a.pow2);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = x[i][j];
+      *(u2*)&turned[8 * tc + j][8 * tr] = code8<false>(y, r, bad_amax(cm[j]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = t + 256 * i, c = e >> 3, k = (e & 7) * 16;
+      if (c < cols && k < rows) *(u4*)(a.QT + (c0 + c) * a.ldqt + r0 + k) = *(const u4*)&turned[c][k];
+    }
+  }
+}
+
+template <class T>
+void quantize_typed(const QuantArgs& a, bool tile, hipStream_t s) {
+  const int64_t nr = ceil_div(a.rows, kBlock), nc = ceil_div(a.cols, kBlock);
+  if (!tile && !a.QT) {
+    hipLaunchKernelGGL(k_quantize_rows<T>, dim3((unsigned)std::min<int64_t>(1 << 20, ceil_div(a.rows * nc, 16))), dim3(256), 0, s, a);
+  } else {
+    auto k = tile ? k_quantize_tile<T, true> : k_quantize_tile<T, false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(nc * nr)), dim3(256), 0, s, a);
+  }
+}
+
+void quantize(const QuantArgs& a, gptq2d_dtype dt, bool tile, hipStream_t s) {
+  with_type(dt, [&](auto* p) { quantize_typed<std::remove_pointer_t<decltype(p)>>(a, tile, s); });
+}
+
+// ---------------------------------------------------------------------------
+// Product
+// ---------------------------------------------------------------------------
+
+struct ProductArgs {
+  int M, N, K;        // Y (M x N) = X (M x K) W (N x K)^T
+  const uint8_t* W;   // N x K
+  int64_t ldw;
+  const float* SW;    // ROWS: [block][n], otherwise [n / 128][block]
+  int64_t ldsw;
+  const uint8_t* X;   // M x K
+  int64_t ldx;
+  const float* SX;    // [block][m]
+  int64_t ldsx;
+  void* Y;
+  int64_t ldy;
+  bool ywide;         // four consecutive results of a row are aligned to be stored at once
+  float* part;        // splits > 1: partial sums, [split][m][n]
+  int splits;
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 codes at p of which the first n are there (n may be anything), zeros after them
+__device__ __forceinline__ u4 tail16(const uint8_t* p, int n) {
+  if (n >= 16) return *(const u4*)p;
+  u4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < n) v[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  return v;
+}
+
+// One 128-deep step of an operand's R rows from row r0 on into LDS, row by row
+// (128 bytes each). Chunk c of 16 bytes of row r lies at chunk c ^ (r % 8), so
+// that sixteen rows read at the same k spread over the banks. Rows past the
+// last are the last one's (their products are not stored).
+template <int R, int THREADS>
+__device__ __forceinline__ void stage(uint8_t* dst, const uint8_t* src, int64_t ld, int r0, int rows, int K, int k0) {
+  const int t = threadIdx.x;
+  const bool whole = k0 + kBlock <= K;
+#pragma unroll
+  for (int i = 0; i < R * 8 / THREADS; ++i) {
+    const int e = t + i * THREADS, r = e >> 3, c = (e & 7) ^ (r & 7);
+    const uint8_t* p = src + (int64_t)min(r0 + r, rows - 1) * ld + k0 + 16 * c;
+    if (whole) {
+      uint8_t* base = dst + (i * THREADS + (t & ~63)) * 16;  // of the wave
+      __builtin_amdgcn_global_load_lds((const void*)p, (lds_void*)base, 16, 0, 0);
+    } else {
+      *(u4*)(dst + e * 16) = tail16(p, K - k0 - 16 * c);
+    }
+  }
+}
+
+__device__ __forceinline__ i8v frag(const uint8_t* tile, int row, int g) {
+  const u4 lo = *(const u4*)(tile + row * kBlock + ((2 * g) ^ (row & 7)) * 16);
+  const u4 hi = *(const u4*)(tile + row * kBlock + ((2 * g + 1) ^ (row & 7)) * 16);
+  return __builtin_bit_cast(i8v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// the lane's 32 codes as four operands of eight halves
+__device__ __forceinline__ void widen(i8v v, h8 h[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const h2 a = halves<false, false>(v[2 * i]), b = halves<false, true>(v[2 * i]);
+    const h2 c = halves<false, false>(v[2 * i + 1]), d = halves<false, true>(v[2 * i + 1]);
+    h[i] = h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+
+// The work group's tile, so that the groups of one XCD (dispatched round-robin
+// over eight) take neighbouring tiles: eight rows of tiles at a time, so both
+// operands' panels stay in its L2.
+__device__ __forceinline__ void tile_of(int id, int total, int tn, int tm, int& bn, int& bm) {
+  const int q = total / 8, r = total % 8, x = id % 8;
+  int w = x * q + min(x, r) + id / 8;
+  const int per = 8 * tn, grp = w / per, first = grp * 8, h = min(8, tm - first);
+  w -= grp * per;
+  bm = first + w % h;
+  bn = w / h;
+}
+
+template <class T>
+__device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
+  if (wide && n >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      *(f4*)p = v;
+    } else {
+      struct alignas(8) V { T v[4]; };
+      *(V*)p = V{{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+
+// BN x BM tile of Y^T per work group, WN x WM waves. The weights are the
+// instruction's row operand, so a lane's accumulator holds four consecutive n of
+// one m: its scale is one register for X and one uniform value for W.
+// Each 128-deep block is summed by itself and enters the accumulators with its scale.
+// EXACT: the codes are widened to halves (which hold them exactly) and summed
+// by the 16-bit instruction. The eight-bit one aligns its products to about
+// 14 bits below the largest (measured 1.5e-5 of the sum of magnitudes), which
+// is far below a 16-bit result's last place, but not below a 32-bit one's.
+template <class T, int BN, int BM, int WN, int WM, bool ROWS, bool EXACT>
+__global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn, int tm) {
+  constexpr int THREADS = 64 * WN * WM, TN = BN / WN / 16, TM = BM / WM / 16;
+  __shared__ __align__(16) uint8_t lw[2][BN * kBlock];
+  __shared__ __align__(16) uint8_t lx[2][BM * kBlock];
+  int bn, bm;
+  tile_of(blockIdx.x, gridDim.x, tn, tm, bn, bm);
+  const int n0 = bn * BN, m0 = bm * BM;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  const int wn = (w % WN) * (BN / WN), wm = (w / WN) * (BM / WM);
+  const int nb = (a.K + kBlock - 1) / kBlock;
+  const int b0 = (int)((int64_t)nb * blockIdx.y / a.splits), b1 = (int)((int64_t)nb * (blockIdx.y + 1) / a.splits);
+  f4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f4{0, 0, 0, 0};
+  // the scales of a block are loaded before its codes: loads come back in
+  // order, so a wait for the scales would be one for the codes otherwise
+  float sx[TM], nx[TM], u = 0, nu = 0;
+  f4 sw[TN], nw[TN];
+  auto next = [&](int b) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j) nx[j] = a.SX[b * a.ldsx + min(m0 + wm + 16 * j + c, a.M - 1)];
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) nw[i][e] = a.SW[b * a.ldsw + min(n0 + wn + 16 * i + 4 * g + e, a.N - 1)];
+    } else {
+      nu = a.SW[(int64_t)(min(n0 + wn, a.N - 1) / kBlock) * a.ldsw + b];
+    }
+    const int buf = (b - b0) & 1;
+    stage<BN, THREADS>(lw[buf], a.W, a.ldw, n0, a.N, a.K, b * kBlock);
+    stage<BM, THREADS>(lx[buf], a.X, a.ldx, m0, a.M, a.K, b * kBlock);
+  };
+  if (b0 < b1) next(b0);
+  for (int b = b0; b < b1; ++b) {
+    const int cur = (b - b0) & 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this block's codes are in LDS
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TM; ++j) sx[j] = nx[j];
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) sw[i] = nw[i];
+    } else {
+      u = nu;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) sx[j] *= u;
+    }
+    if (b + 1 < b1) next(b + 1);
+    if constexpr (EXACT) {
+      h8 fx[TM][4];
+#pragma unroll
+      for (int j = 0; j < TM; ++j) widen(frag(lx[cur], wm + 16 * j + c, g), fx[j]);
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        h8 fw[4];
+        widen(frag(lw[cur], wn + 16 * i + c, g), fw);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+          f4 p = {0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(fw[k], fx[j][k], p, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROWS ? p[e] * sw[i][e] : p[e], sx[j], acc[i][j][e]);
+        }
+      }
+    } else {
+      i8v fw[TN];
+#pragma unroll
+      for (int i = 0; i < TN; ++i) fw[i] = frag(lw[cur], wn + 16 * i + c, g);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) {
+        const i8v fx = frag(lx[cur], wm + 16 * j + c, g);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+          const f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx, f4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROWS ? p[e] * sw[i][e] : p[e], sx[j], acc[i][j][e]);
+        }
+      }
+    }
+  }
+  const bool joined = a.splits > 1;
+  float* part = a.part + (int64_t)blockIdx.y * a.M * a.N;
+  const bool wide = joined ? (a.N & 3) == 0 : a.ywide;
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int m = m0 + wm + 16 * j + c;
+    if (m >= a.M) continue;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      const int n = n0 + wn + 16 * i + 4 * g;
+      if (n >= a.N) continue;
+      if (joined)
+        put4(part + (int64_t)m * a.N + n, wide, a.N - n, acc[i][j]);
+      else
+        put4((T*)a.Y + (int64_t)m * a.ldy + n, wide, a.N - n, acc[i][j]);
+    }
+  }
+}
+
+// Few rows (M <= 16 TM): the weights are read once, straight into the
+// instruction's registers, 16 rows a work group; its eight waves take every
+// eighth block of 128 and add up in LDS in the order of the waves.
+template <class T, int TM, bool ROWS, bool EXACT>
+__global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
+  __shared__ f4 sum[8][TM][64];
+  const int n0 = blockIdx.x * 16, w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  const int nb = (a.K + kBlock - 1) / kBlock;
+  const uint8_t* pw = a.W + (int64_t)min(n0 + c, a.N - 1) * a.ldw + 32 * g;
+  f4 acc[TM];
+#pragma unroll
+  for (int j = 0; j < TM; ++j) acc[j] = f4{0, 0, 0, 0};
+  for (int b = w; b < nb; b += 8) {
+    const int left = a.K - b * kBlock - 32 * g;
+    auto load = [&](const uint8_t* p) {
+      u4 lo, hi;
+      if (left >= 32) {
+        lo = *(const u4*)(p + b * kBlock), hi = *(const u4*)(p + b * kBlock + 16);
+      } else {
+        lo = tail16(p + b * kBlock, left), hi = tail16(p + b * kBlock + 16, left - 16);
+      }
+      return __builtin_bit_cast(i8v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const i8v fw = load(pw);
+    f4 sw;
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sw[e] = a.SW[b * a.ldsw + min(n0 + 4 * g + e, a.N - 1)];
+    } else {
+      const float u = a.SW[(int64_t)(n0 / kBlock) * a.ldsw + b];
+      sw = f4{u, u, u, u};
+    }
+    h8 hw[4];
+    if constexpr (EXACT) widen(fw, hw);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = min(16 * j + c, a.M - 1);
+      const i8v fx = load(a.X + (int64_t)m * a.ldx + 32 * g);
+      const float sx = a.SX[b * a.ldsx + m];
+      f4 p = {0, 0, 0, 0};
+      if constexpr (EXACT) {
+        h8 hx[4];
+        widen(fx, hx);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[k], hx[k], p, 0, 0, 0);
+      } else {
+        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fx, p, 0, 0, 0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[e] * sw[e], sx, acc[j][e]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < TM; ++j) sum[w][j][l] = acc[j];
+  __syncthreads();
+  for (int j = w; j < TM; j += 8) {
+    f4 v = sum[0][j][l];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += sum[i][j][l];
+    const int m = 16 * j + c, n = n0 + 4 * g;
+    if (m < a.M && n < a.N) put4((T*)a.Y + (int64_t)m * a.ldy + n, a.ywide, a.N - n, v);
+  }
+}
+
+// adds the splits' partial sums in their order
+template <class T>
+__global__ __launch_bounds__(256) void k_join(ProductArgs a) {
+  const int64_t total = (int64_t)a.M * a.N;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+    float v = a.part[e];
+    for (int s = 1; s < a.splits; ++s) v += a.part[s * total + e];
+    const int64_t m = e / a.N;
+    ((T*)a.Y)[m * a.ldy + (e - m * a.N)] = (T)v;
+  }
+}
+
+// Which kernel and how many parts of K (the same for the workspace's size and the launch)
+struct Plan { int edge; int splits; };
+Plan plan(int64_t M, int64_t N, int64_t K) {
+  if (M <= 64) return {16, 1};
+  const int64_t nb = ceil_div(K, kBlock);
+  const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles, nb / 4, 16}));
+  return {128, (int)splits};
+}
+
+size_t part_bytes(const Plan& p, int64_t M, int64_t N) {
+  return p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0;
+}
+
+template <class T, bool ROWS>
+void product_typed(ProductArgs a, const Plan& p, hipStream_t s) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  if (p.edge == 16) {
+    const dim3 grid((a.N + 15) / 16);
+    if (a.M <= 16) hipLaunchKernelGGL((k_thin<T, 1, ROWS, EXACT>), grid, dim3(512), 0, s, a);
+    else if (a.M <= 32) hipLaunchKernelGGL((k_thin<T, 2, ROWS, EXACT>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_thin<T, 4, ROWS, EXACT>), grid, dim3(512), 0, s, a);
+    return;
+  }
+  const int tn = (a.N + 127) / 128, tm = (a.M + 127) / 128;
+  hipLaunchKernelGGL((k_product<T, 128, 128, 2, 2, ROWS, EXACT>), dim3(tn * tm, p.splits), dim3(256), 0, s, a, tn, tm);
+  if (p.splits > 1) {
+    const int64_t total = (int64_t)a.M * a.N;
+    hipLaunchKernelGGL(k_join<T>, dim3((unsigned)std::min<int64_t>(2048, ceil_div(total, 256))), dim3(256), 0, s, a);
+  }
+}
+
+void product(const ProductArgs& a, const Plan& p, bool rows, gptq2d_dtype dt, hipStream_t s) {
+  with_type(dt, [&](auto* t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (rows)
+      product_typed<T, true>(a, p, s);
+    else
+      product_typed<T, false>(a, p, s);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Arguments
+// ---------------------------------------------------------------------------
+
+constexpr int64_t kMaxDim = (int64_t)1 << 24;
+bool bad_dim(int64_t d) { return d < 1 || d > kMaxDim; }
+// more entries than the device holds (and than a launch's grid can cover)
+bool bad_area(int64_t r, int64_t c) { return r * c > (int64_t)1 << 37; }
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+bool bad_sizes(int64_t M, int64_t N, int64_t K) {
+  return bad_dim(M) || bad_dim(N) || bad_dim(K) || bad_area(M, N) || bad_area(M, K) || bad_area(N, K);
+}
+
+gptq2d_status check_codes(const void* Q, int64_t ldq, int64_t cols, const void* S, int64_t lds, int64_t least) {
+  if (!Q || !S) return refuse("codes or scales are NULL");
+  if (!aligned(Q, 16) || ldq % 16 != 0) return refuse("codes need 16-byte aligned rows");
+  if (ldq < cols || ldq > kMaxDim * 2) return refuse("leading dimension of the codes too small or too large");
+  if (!aligned(S, 4) || lds < least) return refuse("leading dimension of the scales too small");
+  return GPTQ2D_OK;
+}
+
+gptq2d_status check_matrix(const void* X, int64_t ldx, int64_t cols, gptq2d_dtype dt, const char* what) {
+  if (!X) return refuse(what);
+  if (ldx < cols) return refuse("leading dimension too small");
+  if (!aligned(X, elem_size(dt))) return refuse("a matrix is not aligned to its elements");
+  return GPTQ2D_OK;
+}
+
+gptq2d_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return GPTQ2D_OK;
+  if (!ws || have < need) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
+  if (!aligned(ws, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return GPTQ2D_OK;
+}
+
+// workspace regions of the layer's calls
+struct Region {
+  char* at;
+  template <class P>
+  P* take(size_t bytes) {
+    P* p = (P*)at;
+    at += up256(bytes);
+    return p;
+  }
+};
+int64_t code_ld(int64_t cols) { return ceil_div(cols, 16) * 16; }
+size_t code_bytes(int64_t rows, int64_t cols) { return up256((size_t)rows * code_ld(cols)); }
+size_t scale_bytes(int64_t rows, int64_t cols) { return up256((size_t)rows * ceil_div(cols, kBlock) * sizeof(float)); }
+
+ProductArgs product_args(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* SA, int64_t ldsa,
+                         const void* B, int64_t ldb, const float* SB, int64_t ldsb, void* C, int64_t ldc,
+                         gptq2d_dtype dt, const Plan& p, void* part) {
+  ProductArgs a = {};
+  a.M = (int)M, a.N = (int)N, a.K = (int)K;
+  a.X = (const uint8_t*)A, a.ldx = lda, a.SX = SA, a.ldsx = ldsa;
+  a.W = (const uint8_t*)B, a.ldw = ldb, a.SW = SB, a.ldsw = ldsb;
+  a.Y = C, a.ldy = ldc;
+  const size_t es = elem_size(dt);
+  a.ywide = aligned(C, 4 * es) && ldc % 4 == 0;
+  a.part = (float*)part, a.splits = p.splits;
+  return a;
+}
+
+}  // namespace
+}  // namespace g2d
+
+using namespace g2d;
+
+extern "C" {
+
+gptq2d_status gptq2d_block_quantize(int64_t rows, int64_t cols, gptq2d_dtype dt, const void* X, int64_t ldx,
+                                    int block_rows, int pow2, void* Q, int64_t ldq, float* S, int64_t lds, void* QT,
+                                    int64_t ldqt, float* ST, int64_t ldst, void* stream) {
+  if (bad_dim(rows) || bad_dim(cols)) return refuse("rows and cols must lie in [1, 2^24]");
+  if (bad_area(rows, cols)) return refuse("X has more than 2^37 entries");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  if (block_rows != 1 && block_rows != kBlock) return refuse("block_rows must be 1 or 128");
+  if (!Q && !QT) return refuse("neither codes nor transposed codes are asked for");
+  gptq2d_status st = check_matrix(X, ldx, cols, dt, "X is NULL");
+  const bool tile = block_rows != 1;
+  if (st == GPTQ2D_OK && Q) st = check_codes(Q, ldq, cols, S, lds, tile ? ceil_div(cols, kBlock) : rows);
+  if (st == GPTQ2D_OK && QT) st = check_codes(QT, ldqt, rows, ST, ldst, tile ? ceil_div(rows, kBlock) : cols);
+  if (st != GPTQ2D_OK) return st;
+  QuantArgs a = {rows, cols, X, ldx, (uint8_t*)Q, ldq, S, lds, (uint8_t*)QT, ldqt, ST, ldst, pow2 != 0,
+                 wide_rows(X, ldx, elem_size(dt))};
+  quantize(a, dt, tile, (hipStream_t)stream);
+  return launched("gptq2d_block_quantize");
+}
+
+size_t gptq2d_block_matmul_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (bad_sizes(M, N, K)) return 0;
+  return part_bytes(plan(M, N, K), M, N);
+}
+
+gptq2d_status gptq2d_block_matmul(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* SA,
+                                  int64_t ldsa, const void* B, int64_t ldb, const float* SB, int64_t ldsb,
+                                  int b_block_rows, gptq2d_dtype dt, void* C, int64_t ldc, void* workspace,
+                                  size_t ws_bytes, void* stream) {
+  if (bad_sizes(M, N, K)) return refuse("M, N and K must lie in [1, 2^24], each matrix in 2^37 entries");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  if (b_block_rows != 1 && b_block_rows != kBlock) return refuse("block_rows must be 1 or 128");
+  const bool rows = b_block_rows == 1;
+  gptq2d_status st = check_codes(A, lda, K, SA, ldsa, M);
+  if (st == GPTQ2D_OK) st = check_codes(B, ldb, K, SB, ldsb, rows ? N : ceil_div(K, kBlock));
+  if (st == GPTQ2D_OK) st = check_matrix(C, ldc, N, dt, "C is NULL");
+  const Plan p = plan(M, N, K);
+  if (st == GPTQ2D_OK) st = check_workspace(workspace, ws_bytes, part_bytes(p, M, N));
+  if (st != GPTQ2D_OK) return st;
+  product(product_args(M, N, K, A, lda, SA, ldsa, B, ldb, SB, ldsb, C, ldc, dt, p, workspace), p, rows, dt,
+          (hipStream_t)stream);
+  return launched("gptq2d_block_matmul");
+}
+
+size_t gptq2d_block_linear_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (bad_sizes(M, N, K)) return 0;
+  return code_bytes(M, K) + scale_bytes(M, K) + part_bytes(plan(M, N, K), M, N);
+}
+
+gptq2d_status gptq2d_block_linear(int64_t M, int64_t N, int64_t K, gptq2d_dtype dt, const void* X, int64_t ldx,
+                                  const void* W, int64_t ldw, const float* SW, int64_t ldsw, int pow2, void* Y,
+                                  int64_t ldy, void* workspace, size_t ws_bytes, void* stream) {
+  if (bad_sizes(M, N, K)) return refuse("M, N and K must lie in [1, 2^24], each matrix in 2^37 entries");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  gptq2d_status st = check_matrix(X, ldx, K, dt, "X is NULL");
+  if (st == GPTQ2D_OK) st = check_codes(W, ldw, K, SW, ldsw, ceil_div(K, kBlock));
+  if (st == GPTQ2D_OK) st = check_matrix(Y, ldy, N, dt, "Y is NULL");
+  if (st == GPTQ2D_OK) st = check_workspace(workspace, ws_bytes, gptq2d_block_linear_workspace_size(M, N, K));
+  if (st != GPTQ2D_OK) return st;
+  Region ws{(char*)workspace};
+  uint8_t* q = ws.take<uint8_t>(code_bytes(M, K));
+  float* sq = ws.take<float>(scale_bytes(M, K));
+  const Plan p = plan(M, N, K);
+  QuantArgs a = {M, K, X, ldx, q, code_ld(K), sq, M, nullptr, 0, nullptr, 0, pow2 != 0, wide_rows(X, ldx, elem_size(dt))};
+  quantize(a, dt, false, (hipStream_t)stream);
+  product(product_args(M, N, K, q, code_ld(K), sq, M, W, ldw, SW, ldsw, Y, ldy, dt, p, ws.at), p, false, dt,
+          (hipStream_t)stream);
+  return launched("gptq2d_block_linear");
+}
+
+size_t gptq2d_block_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (bad_sizes(M, N, K)) return 0;
+  return code_bytes(M, N) + scale_bytes(M, N) + code_bytes(N, M) + scale_bytes(N, M) + code_bytes(K, M) +
+         scale_bytes(K, M) + std::max(part_bytes(plan(M, K, N), M, K), part_bytes(plan(N, K, M), N, K));
+}
+
+gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq2d_dtype dt, const void* dY,
+                                           int64_t lddy, const void* X, int64_t ldx, const void* WT, int64_t ldwt,
+                                           const float* SWT, int64_t ldswt, int pow2, void* dX, int64_t lddx, float* dW,
+                                           int64_t lddw, void* workspace, size_t ws_bytes, void* stream) {
+  if (bad_sizes(M, N, K)) return refuse("M, N and K must lie in [1, 2^24], each matrix in 2^37 entries");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  if (!dX && !dW) return refuse("neither dX nor dW is asked for");
+  gptq2d_status st = check_matrix(dY, lddy, N, dt, "dY is NULL");
+  if (st == GPTQ2D_OK && dX) st = check_codes(WT, ldwt, N, SWT, ldswt, ceil_div(N, kBlock));
+  if (st == GPTQ2D_OK && dX) st = check_matrix(dX, lddx, K, dt, "dX is NULL");
+  if (st == GPTQ2D_OK && dW) st = check_matrix(X, ldx, K, dt, "X is NULL");
+  if (st == GPTQ2D_OK && dW) st = check_matrix(dW, lddw, K, GPTQ2D_F32, "dW is NULL");
+  if (st == GPTQ2D_OK) st = check_workspace(workspace, ws_bytes, gptq2d_block_linear_backward_workspace_size(M, N, K));
+  if (st != GPTQ2D_OK) return st;
+  Region ws{(char*)workspace};
+  uint8_t* qy = ws.take<uint8_t>(code_bytes(M, N));
+  float* sy = ws.take<float>(scale_bytes(M, N));
+  uint8_t* qyt = ws.take<uint8_t>(code_bytes(N, M));
+  float* syt = ws.take<float>(scale_bytes(N, M));
+  uint8_t* qxt = ws.take<uint8_t>(code_bytes(K, M));
+  float* sxt = ws.take<float>(scale_bytes(K, M));
+  const hipStream_t s = (hipStream_t)stream;
+  const size_t es = elem_size(dt);
+  // dY is read once for both products that it enters
+  QuantArgs a = {M, N, dY, lddy, dX ? qy : nullptr, code_ld(N), sy, M, dW ? qyt : nullptr, code_ld(M), syt, N,
+                 pow2 != 0, wide_rows(dY, lddy, es)};
+  quantize(a, dt, false, s);
+  if (dX) {
+    const Plan p = plan(M, K, N);
+    product(product_args(M, K, N, qy, code_ld(N), sy, M, WT, ldwt, SWT, ldswt, dX, lddx, dt, p, ws.at), p, false, dt, s);
+  }
+  if (dW) {
+    QuantArgs x = {M, K, X, ldx, nullptr, 0, nullptr, 0, qxt, code_ld(M), sxt, K, pow2 != 0, wide_rows(X, ldx, es)};
+    quantize(x, dt, false, s);
+    const Plan p = plan(N, K, M);
+    product(product_args(N, K, M, qyt, code_ld(M), syt, N, qxt, code_ld(M), sxt, K, dW, lddw, GPTQ2D_F32, p, ws.at), p,
+            true, GPTQ2D_F32, s);
+  }
+  return launched("gptq2d_block_linear_backward");
+}
+
+}  // extern "C"
