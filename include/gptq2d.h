@@ -329,6 +329,121 @@ gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq
                                            size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Eight-bit cache of keys and values, and the attention that reads it
+ *
+ * The cache holds `pages` pages of page_size tokens for `heads` key/value heads
+ * of `dim` elements, as four tensors owned by the caller: codes KC, VC (bytes,
+ * [page][head][token][dim]) and scales KS, VS (float, [page][head][token]), each
+ * contiguous and 16-byte aligned. A token's vector of one head is a block as
+ * above (without pow2): e4m3 or int8 codes and one scale. dim is a multiple of
+ * 16 up to 256, page_size one up to 4096; pages * page_size < 2^31, heads <=
+ * 4096. A slot is page * page_size + the token's place in the page.
+ * ------------------------------------------------------------------------- */
+
+/* Enqueues the quantisation of `tokens` tokens' keys K and values V (tokens x
+ * (heads dim), type F32, F16 or BF16) into the slots slots[0 .. tokens-1]
+ * (device). A slot that is negative or past the cache is skipped; a slot may
+ * appear once. Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_cache_append(int64_t tokens, int heads, int dim, gptq2d_dtype dt,
+                                  const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                  const int64_t* slots, gptq2d_code code, int64_t pages,
+                                  int page_size, void* KC, void* VC, float* KS, float* VS,
+                                  void* stream);
+
+/* Enqueues the way back: the values of the slots' vectors, s q rounded to dt, into
+ * K and V. A slot that is negative or past the cache gives zeros. Errors:
+ * INVALID_ARG, HIP. */
+gptq2d_status gptq2d_cache_read(int64_t tokens, int heads, int dim, gptq2d_dtype dt,
+                                const int64_t* slots, gptq2d_code code, int64_t pages,
+                                int page_size, const void* KC, const void* VC, const float* KS,
+                                const float* VS, void* K, int64_t ldk, void* V, int64_t ldv,
+                                void* stream);
+
+/* Enqueues the masks of gptq2d_tree_attention for trees given by parents (device,
+ * seqs x width): parents[b][t] < t is the drafted token that t follows; anything
+ * else means that it follows the context. Bit u of masks[b][t] is set for t and
+ * its ancestors. 1 <= width <= 64. Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_tree_masks(int64_t seqs, int width, const int32_t* parents, uint64_t* masks,
+                                void* stream);
+
+/* Bytes of device workspace gptq2d_tree_attention needs (may be 0; 0 on a bad shape). */
+size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, int kv_heads,
+                                            int dim);
+
+/* Enqueues attention over the cache (kv_heads heads). Sequence b's tokens 0, 1, ..
+ * lie in the pages table[b * ldt + 0], table[b * ldt + 1], .. (device int32,
+ * table_width entries a sequence): context[b] tokens (device), then the sequence's
+ * drafted ones, whose keys and values are in the cache as well. Row b * width + t
+ * of Q and O (type dt, heads * dim columns; query head h reads key/value head
+ * h / (heads / kv_heads)) belongs to drafted token t. It sees the whole context
+ * and the drafted tokens u whose bit is set in masks[b * width + t] (device; NULL:
+ * u <= t, a chain). drafts[b] (device; NULL: width) of the width tokens are there;
+ * the rows after them come out as zeros, and so does a row that sees nothing.
+ *   z = scale q.k, O = sum softmax(z) v
+ *   lse (nullable): log sum e^z of every row and head (-inf for a row of zeros),
+ *       seqs * width x heads.
+ * Sums and the softmax are held in 32 bits. Queries and probabilities enter the
+ * products as 16-bit floats (after scaling by a power of two), or as the sum of
+ * two where dt is F32. A context past the table's last page ends there; the
+ * tokens of an entry that names no page are absent. One token per sequence
+ * (width 1) is decoding. 1 <= width <= 64, seqs <= 65535. workspace: as sized
+ * above, 256-byte aligned, owned by the caller; overlapping calls need distinct
+ * ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_heads, int dim,
+                                    gptq2d_dtype dt, const void* Q, int64_t ldq, gptq2d_code code,
+                                    int64_t pages, int page_size, const void* KC, const void* VC,
+                                    const float* KS, const float* VS, const int32_t* table,
+                                    int64_t ldt, int64_t table_width, const int32_t* context,
+                                    const int32_t* drafts, const uint64_t* masks, float scale,
+                                    void* O, int64_t ldo, float* lse, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Log probabilities of given tokens: the score of a rounded model, and the
+ * gradient that its bases are made from
+ *
+ * For a row of logits x (vocab of them) and z = scale x: lse = log sum e^z, the
+ * given token's log probability z_y - lse, the entropy -sum p log p and the `top`
+ * largest logits. Sums are held in 32 bits. A logit of -inf has probability 0. A
+ * row of nothing else has lse = -inf, entropy 0 and log probabilities -inf; a row
+ * with a NaN or +inf comes out as NaN (its alternatives in order all the same, NaN
+ * first). rows <= 2^22, vocab <= 2^28, top <= 64, scale positive and finite.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of device workspace gptq2d_token_logprobs needs (may be 0; 0 on bad sizes). */
+size_t gptq2d_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int top);
+
+/* Enqueues the scores of X (rows x vocab, type F32, F16 or BF16).
+ *   target (nullable, device): the given token of every row. A negative one is
+ *       none: log probability 0. One past the vocabulary gives NaN.
+ *   logprob, entropy, lse (device, rows entries each).
+ *   ids, tops (device, rows x top, contiguous; NULL where top = 0): the largest
+ *       logits' tokens, largest first, the lower token first among equal ones, and
+ *       their log probabilities.
+ * The same call gives the same bits. workspace: as sized above, 256-byte aligned,
+ * owned by the caller; overlapping calls need distinct ones. Errors: INVALID_ARG,
+ * WORKSPACE, HIP. */
+gptq2d_status gptq2d_token_logprobs(int64_t rows, int64_t vocab, gptq2d_dtype dt, const void* X,
+                                    int64_t ldx, float scale, const int64_t* target, int top,
+                                    float* logprob, float* entropy, float* lse, int32_t* ids,
+                                    float* tops, void* workspace, size_t ws_bytes, void* stream);
+
+/* Enqueues dX (rows x vocab, type dt; may be X itself) = the gradient of the logits
+ * from g_logprob and g_entropy (device, rows entries; either may be NULL), the
+ * gradients of the log probabilities and entropies, with lse and entropy as the
+ * call above gave them (entropy is read with g_entropy only, target with g_logprob
+ * only):
+ *   dx = scale (g_logprob (1[y] - p) - g_entropy p (log p + entropy))
+ * A row without a target takes no part in g_logprob, a row of -inf has gradient 0,
+ * and one with a target past the vocabulary NaN. Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_token_logprobs_backward(int64_t rows, int64_t vocab, gptq2d_dtype dt,
+                                             const void* X, int64_t ldx, float scale,
+                                             const int64_t* target, const float* lse,
+                                             const float* entropy, const float* g_logprob,
+                                             const float* g_entropy, void* dX, int64_t lddx,
+                                             void* stream);
+
+/* ---------------------------------------------------------------------------
  * Diagnostics
  * ------------------------------------------------------------------------- */
 

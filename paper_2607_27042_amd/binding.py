@@ -81,6 +81,16 @@ def load():
         "gptq2d_block_linear_backward_workspace_size": (sz, [i64, i64, i64]),
         "gptq2d_block_linear_backward": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64,
                                                vp, i64, vp, sz, vp]),
+        "gptq2d_cache_append": (i32, [i64, i32, i32, i32, vp, i64, vp, i64, vp, i32, i64, i32, vp, vp, vp, vp, vp]),
+        "gptq2d_cache_read": (i32, [i64, i32, i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp]),
+        "gptq2d_tree_masks": (i32, [i64, i32, vp, vp, vp]),
+        "gptq2d_tree_attention_workspace_size": (sz, [i64, i32, i32, i32, i32]),
+        "gptq2d_tree_attention": (i32, [i64, i32, i32, i32, i32, i32, vp, i64, i32, i64, i32, vp, vp, vp, vp, vp, i64,
+                                        i64, vp, vp, vp, ctypes.c_float, vp, i64, vp, vp, sz, vp]),
+        "gptq2d_token_logprobs_workspace_size": (sz, [i64, i64, i32]),
+        "gptq2d_token_logprobs": (i32, [i64, i64, i32, vp, i64, ctypes.c_float, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "gptq2d_token_logprobs_backward": (i32, [i64, i64, i32, vp, i64, ctypes.c_float, vp, vp, vp, vp, vp, vp, i64,
+                                                 vp]),
         "gptq2d_status_string": (ctypes.c_char_p, [i32]),
         "gptq2d_last_error": (ctypes.c_char_p, []),
         "gptq2d_version": (i32, []),
@@ -568,6 +578,129 @@ def gptq2d_block_linear_backward(dY, X, WT, SWT, dX, dW, workspace, pow2: bool =
     ws = _space(workspace, gptq2d_block_linear_backward_workspace_size(M, N, K), "gptq2d_block_linear_backward")
     args = (M, N, K, dt, *dy, *x, *wt, *swt, int(bool(pow2)), *dx, *dw, *ws, _stream(stream))
     return _enqueue("gptq2d_block_linear_backward", args, (dY, X, WT, SWT, dX, dW, workspace), prepare)
+
+
+def _cache(KC, VC, KS, VS):
+    """(code, pages, heads, page_size, dim) and the pointers of a cache."""
+    if KC.dtype not in _CODES or VC.dtype != KC.dtype:
+        raise TypeError("KC and VC must be float8_e4m3fn or both int8")
+    if KC.dim() != 4 or VC.shape != KC.shape:
+        raise ValueError("KC and VC must be [pages, heads, page_size, dim]")
+    if KS.dtype != torch.float32 or VS.dtype != torch.float32:
+        raise TypeError("KS and VS must be float32")
+    if KS.shape != KC.shape[:3] or VS.shape != KC.shape[:3]:
+        raise ValueError("KS and VS must be [pages, heads, page_size]")
+    for t in (KC, VC, KS, VS):
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("the cache's tensors must be contiguous device tensors")
+    pages, heads, page, dim = KC.shape
+    return _CODES[KC.dtype], pages, heads, page, dim, (_ptr(KC), _ptr(VC), _ptr(KS), _ptr(VS))
+
+
+def _ints(t, shape, dtype, what: str):
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous device tensor of shape {tuple(shape)}")
+    return _ptr(t)
+
+
+def gptq2d_cache_append(K, V, slots, KC, VC, KS, VS, stream=None, prepare=False):
+    """K and V (tokens x (heads dim)) into the cache's slots (int64)."""
+    code, pages, heads, page, dim, tensors = _cache(KC, VC, KS, VS)
+    tokens = K.shape[0]
+    k, v = _mat(K, tokens, heads * dim, "K"), _mat(V, tokens, heads * dim, "V")
+    args = (tokens, heads, dim, _narrow(K, V), *k, *v, _ints(slots, (tokens,), torch.int64, "slots"), code, pages, page,
+            *tensors, _stream(stream))
+    return _enqueue("gptq2d_cache_append", args, (K, V, slots, KC, VC, KS, VS), prepare)
+
+
+def gptq2d_cache_read(slots, KC, VC, KS, VS, K, V, stream=None, prepare=False):
+    """The values of the cache's slots into K and V (tokens x (heads dim))."""
+    code, pages, heads, page, dim, tensors = _cache(KC, VC, KS, VS)
+    tokens = K.shape[0]
+    k, v = _mat(K, tokens, heads * dim, "K"), _mat(V, tokens, heads * dim, "V")
+    args = (tokens, heads, dim, _narrow(K, V), _ints(slots, (tokens,), torch.int64, "slots"), code, pages, page,
+            *tensors, *k, *v, _stream(stream))
+    return _enqueue("gptq2d_cache_read", args, (slots, KC, VC, KS, VS, K, V), prepare)
+
+
+def gptq2d_tree_masks(parents, masks, stream=None, prepare=False):
+    """masks (int64 bits, [seqs, width]) of the trees given by parents (int32)."""
+    seqs, width = parents.shape
+    args = (seqs, width, _ints(parents, (seqs, width), torch.int32, "parents"),
+            _ints(masks, (seqs, width), torch.int64, "masks"), _stream(stream))
+    return _enqueue("gptq2d_tree_masks", args, (parents, masks), prepare)
+
+
+def gptq2d_tree_attention_workspace_size(seqs: int, width: int, heads: int, kv_heads: int, dim: int) -> int:
+    return int(load().gptq2d_tree_attention_workspace_size(seqs, width, heads, kv_heads, dim))
+
+
+def gptq2d_tree_attention(Q, KC, VC, KS, VS, table, context, drafts, masks, scale: float, O, lse, workspace,
+                          stream=None, prepare=False):
+    """Attention of the drafted tokens (rows of Q and O, seqs * width x (heads
+    dim)) over the pages table[b] (int32) of each sequence: context[b] (int32)
+    tokens, then drafts[b] (int32; None: width) drafted ones, seen by masks
+    (int64 bits, [seqs, width]; None: a chain). lse (float32, seqs * width x heads)
+    may be None."""
+    code, pages, kv, page, dim, tensors = _cache(KC, VC, KS, VS)
+    seqs, rows = context.shape[0], Q.shape[0]
+    if seqs < 1 or rows % seqs or Q.shape[1] % (kv * dim):
+        raise ValueError(f"Q must be seqs * width x (heads dim) for {seqs} sequences and {kv} kv heads of {dim}")
+    width, heads = rows // seqs, Q.shape[1] // dim
+    q, o = _mat(Q, rows, heads * dim, "Q"), _mat(O, rows, heads * dim, "O")
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise TypeError("table must be an int32 matrix")
+    tab = _mat(table, seqs, table.shape[1], "table")
+    n = None if drafts is None else _ints(drafts, (seqs,), torch.int32, "drafts")
+    m = None if masks is None else _ints(masks, (seqs, width), torch.int64, "masks")
+    if lse is not None:
+        _scales(lse, rows, heads, "lse")
+        if not lse.is_contiguous():
+            raise ValueError("lse must be contiguous")
+    ws = _space(workspace, gptq2d_tree_attention_workspace_size(seqs, width, heads, kv, dim), "gptq2d_tree_attention")
+    args = (seqs, width, heads, kv, dim, _narrow(Q, O), *q, code, pages, page, *tensors, *tab, table.shape[1],
+            _ints(context, (seqs,), torch.int32, "context"), n, m, float(scale), *o, _ptr(lse), *ws, _stream(stream))
+    return _enqueue("gptq2d_tree_attention", args, (Q, KC, VC, KS, VS, table, context, drafts, masks, O, lse, workspace),
+                    prepare)
+
+
+def gptq2d_token_logprobs_workspace_size(rows: int, vocab: int, top: int) -> int:
+    return int(load().gptq2d_token_logprobs_workspace_size(rows, vocab, top))
+
+
+def gptq2d_token_logprobs(X, target, scale: float, logprob, entropy, lse, ids=None, tops=None, workspace=None,
+                          stream=None, prepare=False):
+    """Of every row of logits X: the log probability of target (int64; None: none
+    given), entropy and log-sum-exp (float32) under scale X, and the largest
+    logits' tokens ids (int32) with their log probabilities tops (float32), both
+    rows x top or None."""
+    rows, vocab = X.shape
+    x = _mat(X, rows, vocab, "X")
+    y = None if target is None else _ints(target, (rows,), torch.int64, "target")
+    out = [_ints(t, (rows,), torch.float32, w) for t, w in ((logprob, "logprob"), (entropy, "entropy"), (lse, "lse"))]
+    top, best = 0, [None, None]
+    if ids is not None:
+        top = ids.shape[1]
+        best = [_ints(ids, (rows, top), torch.int32, "ids"), _ints(tops, (rows, top), torch.float32, "tops")]
+    ws = _space(workspace, gptq2d_token_logprobs_workspace_size(rows, vocab, top), "gptq2d_token_logprobs")
+    args = (rows, vocab, _narrow(X), *x, float(scale), y, top, *out, *best, *ws, _stream(stream))
+    return _enqueue("gptq2d_token_logprobs", args, (X, target, logprob, entropy, lse, ids, tops, workspace), prepare)
+
+
+def gptq2d_token_logprobs_backward(X, target, scale: float, lse, entropy, g_logprob, g_entropy, dX, stream=None,
+                                   prepare=False):
+    """dX (may be X) from the gradients of the log probabilities and of the
+    entropies (float32; either may be None), with lse and entropy of the forward
+    call."""
+    rows, vocab = X.shape
+    x, d = _mat(X, rows, vocab, "X"), _mat(dX, rows, vocab, "dX")
+    y = None if target is None else _ints(target, (rows,), torch.int64, "target")
+    v = [None if t is None else _ints(t, (rows,), torch.float32, w)
+         for t, w in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy"))]
+    args = (rows, vocab, _narrow(X, dX), *x, float(scale), y, *v, *d, _stream(stream))
+    return _enqueue("gptq2d_token_logprobs_backward", args, (X, target, lse, entropy, g_logprob, g_entropy, dX), prepare)
 
 
 # ---------------------------------------------------------------------------

@@ -8,7 +8,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = [os.path.join(PKG, "csrc", f) for f in ("api.hip", "factor.hip", "sweep.hip", "noalloc.hip", "block.hip")]
+SRC = [os.path.join(PKG, "csrc", f) for f in ("api.hip", "factor.hip", "sweep.hip", "noalloc.hip", "block.hip", "cache.hip",
+                                                "tree.hip", "score.hip")]
 HDR = [os.path.join(PKG, "csrc", f) for f in ("device.hpp", "internal.hpp", "codes.hpp")] + [
     os.path.join(ROOT, "include", "gptq2d.h")]
 LIB = os.path.join(PKG, "lib", "libgptq2d.so")

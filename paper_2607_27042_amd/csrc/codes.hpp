@@ -169,6 +169,22 @@ inline bool wide_rows(const void* p, int64_t ld, size_t es) {
 }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The cache's shape and tensors. Slots stay below 2^31 (quotients by the page
+// size are taken in 32 bits).
+inline gptq2d_status check_cache(int heads, int dim, gptq2d_code code, int64_t pages, int page_size, const void* KC,
+                                 const void* VC, const void* KS, const void* VS) {
+  if (heads < 1 || heads > 4096) return refuse("heads must lie in [1, 4096]");
+  if (dim < 16 || dim > 256 || dim % 16 != 0) return refuse("dim must be a multiple of 16 in [16, 256]");
+  if (code != GPTQ2D_E4M3 && code != GPTQ2D_INT8) return refuse("bad code");
+  if (page_size < 16 || page_size > 4096 || page_size % 16 != 0)
+    return refuse("page_size must be a multiple of 16 in [16, 4096]");
+  if (pages < 1 || pages > (int64_t)0x7fffffff / page_size) return refuse("the cache must hold 1 to 2^31 - 1 tokens");
+  if (!KC || !VC || !KS || !VS) return refuse("a tensor of the cache is NULL");
+  if (!aligned(KC, 16) || !aligned(VC, 16) || !aligned(KS, 16) || !aligned(VS, 16))
+    return refuse("the cache's tensors must be 16-byte aligned");
+  return GPTQ2D_OK;
+}
+
 // calls f with a null pointer of the element type of dt (F32, F16 or BF16)
 template <class F>
 inline void with_type(gptq2d_dtype dt, F&& f) {

@@ -1,0 +1,471 @@
+// Log probabilities of given tokens, with the entropy and the top alternatives,
+// and their gradient.
+//
+// For a row of logits x and z = a x (a = 1 / temperature):
+//   lse = log sum e^z, lp = z_y - lse, H = lse - sum p z, p = e^(z - lse)
+//   dx = a (g_lp (1[y] - p) - g_H p (log p + H))
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "codes.hpp"
+
+namespace g2d {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kVec = 16;                    // elements of a thread and step
+constexpr int kChunk = kThreads * kVec;     // of a work group
+constexpr int kMaxTop = 64;
+constexpr int kHeld = kThreads;             // candidates kept between steps
+constexpr int kMaxParts = 64;               // parts of a row
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLog2E = 1.44269504088896341f;
+
+struct ScoreArgs {
+  int64_t rows;
+  int vocab, top, parts;
+  const void* X;
+  int64_t ldx;
+  float a, a2;  // a and a log2 e
+  const int64_t* target;
+  float *logprob, *entropy, *lse;
+  int32_t* ids;
+  float* tops;
+  float* stat;       // parts > 1: the Sums of each part
+  uint64_t* keys;    // parts > 1: top keys of each part
+};
+
+// A candidate as one number that orders as wanted: larger values first (NaN
+// above all), the lower index first among equal ones (-0 = 0). No key is 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t i) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - i); }
+__device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
+}
+
+// The best of a work group's candidates, with room for a whole step's.
+struct Pool {
+  uint64_t key[kHeld + kChunk];
+  uint64_t best[kThreads];
+  uint64_t limit;  // candidates below it are none of the best
+  int count;
+};
+
+// Rank of each thread's key among the group's (0 for the largest); equal keys
+// (0: none) take their thread's order.
+__device__ __forceinline__ int rank_in(Pool& p, uint64_t mine) {
+  const int t = threadIdx.x;
+  p.best[t] = mine;
+  __syncthreads();
+  int r = 0;
+#pragma unroll 8
+  for (int i = 0; i < kThreads; ++i) {
+    const uint64_t k = p.best[i];
+    r += k > mine || (k == mine && i < t);
+  }
+  return r;
+}
+
+// Brings the candidates down to kHeld, keeping the `top` best: the top-th of
+// the threads' largest is a limit that at least `top` candidates reach, and at
+// most top / 256 of them all (a quarter) lie above it.
+__device__ __forceinline__ void shrink(Pool& p, int top) {
+  const int t = threadIdx.x;
+  __syncthreads();
+  while (p.count > kHeld) {
+    const int n = p.count;
+    uint64_t mine[(kHeld + kChunk) / kThreads], most = 0;
+#pragma unroll
+    for (int i = 0; i < (kHeld + kChunk) / kThreads; ++i) {
+      mine[i] = t + i * kThreads < n ? p.key[t + i * kThreads] : 0;
+      most = max(most, mine[i]);
+    }
+    const int r = rank_in(p, most);
+    if (r == top - 1) p.limit = most;
+    if (t == 0) p.count = 0;
+    __syncthreads();
+    const uint64_t limit = p.limit;
+#pragma unroll
+    for (int i = 0; i < (kHeld + kChunk) / kThreads; ++i)
+      if (mine[i] >= limit && mine[i] != 0) p.key[atomicAdd(&p.count, 1)] = mine[i];
+    __syncthreads();
+  }
+}
+
+// The thread's rank-th best key ends up at out[rank] for rank < top.
+template <class F>
+__device__ __forceinline__ void final_ranks(Pool& p, int top, F&& out) {
+  shrink(p, top);
+  const uint64_t mine = (int)threadIdx.x < p.count ? p.key[threadIdx.x] : 0;
+  const int r = rank_in(p, mine);
+  if (r < top) out(r, mine);
+}
+
+// Running sums of a thread or more over logits of which m is the largest:
+// s1 = sum 2^(a2 (x - m)), s2 = sum (x - m) 2^(a2 (x - m)). Differences are taken
+// before anything is scaled: those of near logits are exact, and a logit of the
+// type's lowest value cannot overflow.
+struct Sums {
+  float m, s1, s2;
+};
+__device__ __forceinline__ void move_to(Sums& s, float m, float a2) {
+  if (s.m != -INFINITY) {
+    const float d = s.m - m, f = __builtin_amdgcn_exp2f(a2 * d);
+    // f = 0: what was summed is below the new terms' last place
+    s.s2 = f == 0.0f ? 0.0f : f * fmaf(s.s1, d, s.s2);
+    s.s1 *= f;
+  }
+  s.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float a2) {
+  if (a.m >= b.m)
+    move_to(b, a.m, a2);
+  else
+    move_to(a, b.m, a2);
+  return Sums{a.m, a.s1 + b.s1, a.s2 + b.s2};
+}
+__device__ __forceinline__ Sums wave_join(Sums s, float a2) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const Sums o{__shfl_xor(s.m, d), __shfl_xor(s.s1, d), __shfl_xor(s.s2, d)};
+    s = (threadIdx.x & d) ? join(o, s, a2) : join(s, o, a2);  // the same order in both lanes
+  }
+  return s;
+}
+
+// Sixteen elements from index e on of a row of n; those outside are -inf
+// (e may be negative: the row is read from the 16-byte boundary before it on).
+template <class T>
+__device__ __forceinline__ void load16(const T* x, int64_t e, int64_t n, float v[kVec]) {
+  constexpr int W = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < kVec; i += W) {
+    if (e + i >= 0 && e + i + W <= n) {
+      struct alignas(16) V { T v[W]; };
+      const V a = *(const V*)(x + e + i);
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i + j] = (float)a.v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i + j] = e + i + j >= 0 && e + i + j < n ? (float)x[e + i + j] : -INFINITY;
+    }
+  }
+}
+
+struct Out {
+  float lse, entropy;
+};
+__device__ __forceinline__ Out finish(const ScoreArgs& a, Sums s) {
+  // every logit -inf: the sum is empty
+  if (s.m == -INFINITY && s.s1 == 0.0f) return {-INFINITY, 0.0f};
+  const float l = logf(s.s1), h = l - a.a * (s.s2 / s.s1);
+  return {fmaf(s.m, a.a, l), h < 0.0f ? 0.0f : h};
+}
+
+__device__ __forceinline__ float logprob_of(float z, float lse) {
+  return z == -INFINITY && lse == lse ? -INFINITY : z - lse;
+}
+
+template <class T>
+__device__ __forceinline__ float target_logprob(const ScoreArgs& a, int64_t row, float lse) {
+  if (!a.target) return 0.0f;
+  const int64_t y = a.target[row];
+  if (y < 0) return 0.0f;
+  if (y >= a.vocab) return __uint_as_float(0x7fc00000u);
+  return logprob_of((float)((const T*)a.X)[row * a.ldx + y] * a.a, lse);
+}
+
+// One work group per part of a row, one pass. Each thread sums relative to its
+// own largest logit so far, which moves rarely after the first steps. At the end
+// s1 >= 1 and s2 <= 0, so the entropy log s1 - s2 / s1 cancels nothing.
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
+  __shared__ Sums wave[kThreads / 64];
+  __shared__ typename std::conditional<TOP, Pool, int>::type pool;
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - row * a.parts);
+  const T* x = (const T*)a.X + row * a.ldx;
+  const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));  // elements from the boundary before the row to it
+  const int64_t steps = (a.vocab + lead + kChunk - 1) / kChunk;
+  const int64_t first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
+  Sums s{-INFINITY, 0.0f, 0.0f};
+  if constexpr (TOP) {
+    if (t == 0) pool.count = 0, pool.limit = 0;
+    __syncthreads();
+  }
+  float next[kVec];
+  if (first < last) load16(x, first * kChunk + t * kVec - lead, a.vocab, next);
+  for (int64_t c = first; c < last; ++c) {
+    float v[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = next[i];
+    const int64_t at = c * kChunk + t * kVec - lead;
+    if (c + 1 < last) load16(x, at + kChunk, a.vocab, next);
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i < kVec; ++i) m = fmaxf(m, v[i]);
+    float low = v[0];
+#pragma unroll
+    for (int i = 1; i < kVec; ++i) low = fminf(low, v[i]);
+    if (m > s.m) move_to(s, m, a.a2);
+    bool odd = false;  // a NaN, which maxima drop
+    if (low > -1e37f && s.m < 1e37f) {
+      // differences are finite; a NaN enters the sums by itself
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float d = v[i] - s.m, e = __builtin_amdgcn_exp2f(d * a.a2);
+        s.s1 += e;
+        s.s2 = fmaf(e, d, s.s2);
+      }
+      odd = s.s1 != s.s1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        odd |= v[i] != v[i];
+        if (v[i] == -INFINITY) continue;
+        // 2^(a2 d) is 0 long before d reaches the clamp
+        const float d = fmaxf(v[i] - s.m, -3e38f), e = __builtin_amdgcn_exp2f(d * a.a2);
+        s.s1 += e;
+        s.s2 = fmaf(e, d, s.s2);
+      }
+      if (odd) s.s1 = s.s2 = __uint_as_float(0x7fc00000u);
+    }
+    if constexpr (TOP) {
+      if (c == first) {
+        // the limit of the start: the top-th of the threads' largest
+        uint64_t most = 0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (at + i >= 0 && at + i < a.vocab) most = max(most, key_of(v[i], (uint32_t)(at + i)));
+        if (rank_in(pool, most) == a.top - 1) pool.limit = most;
+        __syncthreads();
+      }
+      const uint64_t limit = pool.limit;
+      const uint32_t lo = (uint32_t)(limit >> 32);
+      if (odd || order_of(m) >= lo) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const uint64_t k = key_of(v[i], (uint32_t)(at + i));
+          if (k >= limit && at + i >= 0 && at + i < a.vocab) pool.key[atomicAdd(&pool.count, 1)] = k;
+        }
+      }
+      __syncthreads();
+      if (pool.count > kHeld) shrink(pool, a.top);
+      __syncthreads();
+    }
+  }
+  s = wave_join(s, a.a2);
+  if ((t & 63) == 0) wave[t >> 6] = s;
+  __syncthreads();
+  s = join(join(wave[0], wave[1], a.a2), join(wave[2], wave[3], a.a2), a.a2);
+  if (a.parts > 1) {
+    if (t == 0) ((f4*)a.stat)[blockIdx.x] = f4{s.m, s.s1, s.s2, 0.0f};
+    if constexpr (TOP)
+      final_ranks(pool, a.top, [&](int r, uint64_t k) { a.keys[(int64_t)blockIdx.x * a.top + r] = k; });
+    return;
+  }
+  const Out o = finish(a, s);
+  if (t == 0) {
+    a.lse[row] = o.lse;
+    a.entropy[row] = o.entropy;
+    a.logprob[row] = target_logprob<T>(a, row, o.lse);
+  }
+  if constexpr (TOP)
+    final_ranks(pool, a.top, [&](int r, uint64_t k) {
+      a.ids[row * a.top + r] = (int32_t)key_index(k);
+      a.tops[row * a.top + r] = logprob_of(key_value(k) * a.a, o.lse);
+    });
+}
+
+// One work group per row: its parts' sums, and the best of their best.
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
+  __shared__ typename std::conditional<TOP, Pool, int>::type pool;
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  Sums s{-INFINITY, 0.0f, 0.0f};
+  const int l = t & 63;
+  if (l < a.parts) {
+    const f4 st = ((const f4*)a.stat)[row * a.parts + l];
+    s = Sums{st[0], st[1], st[2]};
+  }
+  s = wave_join(s, a.a2);
+  const Out o = finish(a, s);
+  if (t == 0) {
+    a.lse[row] = o.lse;
+    a.entropy[row] = o.entropy;
+    a.logprob[row] = target_logprob<T>(a, row, o.lse);
+  }
+  if constexpr (TOP) {
+    const int n = a.parts * a.top;  // at most kMaxParts kMaxTop = kChunk
+    if (t == 0) pool.count = n, pool.limit = 0;
+    for (int i = t; i < n; i += kThreads) pool.key[i] = a.keys[row * n + i];
+    final_ranks(pool, a.top, [&](int r, uint64_t k) {
+      a.ids[row * a.top + r] = (int32_t)key_index(k);
+      a.tops[row * a.top + r] = logprob_of(key_value(k) * a.a, o.lse);
+    });
+  }
+}
+
+struct GradArgs {
+  int64_t rows;
+  int vocab, parts;
+  const void* X;
+  int64_t ldx;
+  float a, a2;
+  const int64_t* target;
+  const float *lse, *entropy, *gl, *gh;
+  void* D;
+  int64_t ldd;
+};
+
+// One pass, element by element. Rows of logits and gradients that start at the
+// same distance from a 16-byte boundary are moved in 16-byte pieces.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
+  constexpr int W = 16 / sizeof(T);
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - row * a.parts);
+  const T* x = (const T*)a.X + row * a.ldx;
+  T* d = (T*)a.D + row * a.ldd;
+  const float lse = a.lse[row];
+  const float gl = a.gl ? a.gl[row] : 0.0f, gh = a.gh ? a.gh[row] : 0.0f;
+  const float H = gh != 0.0f ? a.entropy[row] : 0.0f;
+  const int64_t y = a.target ? a.target[row] : -1;
+  const bool given = y >= 0 && y < a.vocab;
+  const float g = given ? gl : y >= a.vocab ? gl * __uint_as_float(0x7fc00000u) : 0.0f;
+  const float l2 = lse * kLog2E;
+  auto one = [&](float v, int64_t i) {
+    const float q = fmaf(v, a.a2, -l2);  // log2 p
+    const float p = __builtin_amdgcn_exp2f(q);
+    float r = -p * (g + gh * (fmaxf(q, -1000.0f) * kLn2 + H));
+    if (i == y) r += g;
+    // a row without a finite logit has no gradient
+    return lse == -INFINITY ? 0.0f : a.a * r;
+  };
+  const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));
+  const bool wide = (((uintptr_t)x ^ (uintptr_t)d) & 15) == 0;
+  const int64_t n = a.vocab + lead, per = (n + a.parts - 1) / a.parts;
+  const int64_t span = (per + kThreads * W - 1) / (kThreads * W) * (kThreads * W);
+  const int64_t end = min(n, span * (part + 1));
+  for (int64_t e = span * part + threadIdx.x * W; e < end; e += kThreads * W) {
+    const int64_t i0 = e - lead;
+    if (wide && i0 >= 0 && i0 + W <= a.vocab) {
+      struct alignas(16) V { T v[W]; };
+      const V in = *(const V*)(x + i0);
+      V out;
+#pragma unroll
+      for (int j = 0; j < W; ++j) out.v[j] = (T)one((float)in.v[j], i0 + j);
+      *(V*)(d + i0) = out;
+    } else {
+      for (int j = 0; j < W; ++j)
+        if (i0 + j >= 0 && i0 + j < a.vocab) d[i0 + j] = (T)one((float)x[i0 + j], i0 + j);
+    }
+  }
+}
+
+// Parts of a row: as many as give the device about four work groups a compute
+// unit, but no part of less than two steps.
+int part_count(int64_t rows, int64_t vocab) {
+  const int64_t want = ceil_div(1024, rows), room = std::max<int64_t>(1, vocab / (2 * kChunk));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, room, kMaxParts}));
+}
+
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+size_t stat_bytes(int64_t rows, int parts) { return up256((size_t)rows * parts * 4 * sizeof(float)); }
+size_t score_bytes(int64_t rows, int64_t vocab, int top) {
+  const int parts = part_count(rows, vocab);
+  return parts == 1 ? 0 : stat_bytes(rows, parts) + up256((size_t)rows * parts * top * sizeof(uint64_t));
+}
+
+bool bad_sizes(int64_t rows, int64_t vocab) {
+  return rows < 0 || rows > (int64_t)1 << 22 || vocab < 1 || vocab > (int64_t)1 << 28;
+}
+
+}  // namespace
+}  // namespace g2d
+
+using namespace g2d;
+
+extern "C" {
+
+size_t gptq2d_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int top) {
+  if (bad_sizes(rows, vocab) || rows == 0 || top < 0 || top > kMaxTop) return 0;
+  return score_bytes(rows, vocab, top);
+}
+
+gptq2d_status gptq2d_token_logprobs(int64_t rows, int64_t vocab, gptq2d_dtype dt, const void* X, int64_t ldx,
+                                    float scale, const int64_t* target, int top, float* logprob, float* entropy,
+                                    float* lse, int32_t* ids, float* tops, void* workspace, size_t ws_bytes,
+                                    void* stream) {
+  if (bad_sizes(rows, vocab)) return refuse("rows must lie in [0, 2^22], vocab in [1, 2^28]");
+  if (top < 0 || top > kMaxTop || top > vocab) return refuse("top must lie in [0, 64] and not exceed vocab");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  if (!(scale > 0.0f) || !isfinite(scale)) return refuse("scale must be positive and finite");
+  if (rows == 0) return GPTQ2D_OK;
+  if (!X || !logprob || !entropy || !lse) return refuse("X, logprob, entropy or lse is NULL");
+  if (top > 0 && (!ids || !tops)) return refuse("ids or tops is NULL");
+  if (ldx < vocab) return refuse("leading dimension too small");
+  if (!aligned(X, elem_size(dt)) || !aligned(target, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+      !aligned(lse, 4) || !aligned(ids, 4) || !aligned(tops, 4))
+    return refuse("an argument is not aligned to its elements");
+  const size_t need = score_bytes(rows, vocab, top);
+  if (need > 0 && (!workspace || ws_bytes < need)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
+  if (need > 0 && !aligned(workspace, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const int parts = part_count(rows, vocab);
+  ScoreArgs a = {rows, (int)vocab, top, parts, X, ldx, scale, scale * kLog2E, target, logprob, entropy, lse, ids, tops,
+                 (float*)workspace, (uint64_t*)((char*)workspace + stat_bytes(rows, parts))};
+  const hipStream_t s = (hipStream_t)stream;
+  with_type(dt, [&](auto* p) {
+    using T = std::remove_pointer_t<decltype(p)>;
+    const dim3 grid((unsigned)(rows * parts));
+    if (top > 0)
+      hipLaunchKernelGGL((k_score<T, true>), grid, dim3(kThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_score<T, false>), grid, dim3(kThreads), 0, s, a);
+    if (parts > 1) {
+      if (top > 0)
+        hipLaunchKernelGGL((k_score_join<T, true>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_score_join<T, false>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+    }
+  });
+  return launched("gptq2d_token_logprobs");
+}
+
+gptq2d_status gptq2d_token_logprobs_backward(int64_t rows, int64_t vocab, gptq2d_dtype dt, const void* X, int64_t ldx,
+                                             float scale, const int64_t* target, const float* lse, const float* entropy,
+                                             const float* g_logprob, const float* g_entropy, void* dX, int64_t lddx,
+                                             void* stream) {
+  if (bad_sizes(rows, vocab)) return refuse("rows must lie in [0, 2^22], vocab in [1, 2^28]");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  if (!(scale > 0.0f) || !isfinite(scale)) return refuse("scale must be positive and finite");
+  if (!g_logprob && !g_entropy) return refuse("no gradient is given");
+  if (rows == 0) return GPTQ2D_OK;
+  if (!X || !dX || !lse) return refuse("X, dX or lse is NULL");
+  if (g_logprob && !target) return refuse("g_logprob needs the targets");
+  if (g_entropy && !entropy) return refuse("g_entropy needs the entropy");
+  if (ldx < vocab || lddx < vocab) return refuse("leading dimension too small");
+  const size_t es = elem_size(dt);
+  if (!aligned(X, es) || !aligned(dX, es) || !aligned(target, 8) || !aligned(lse, 4) || !aligned(entropy, 4) ||
+      !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
+    return refuse("an argument is not aligned to its elements");
+  GradArgs a = {rows, (int)vocab, 1, X, ldx, scale, scale * kLog2E, target, lse, entropy, g_logprob, g_entropy, dX, lddx};
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, rows), ceil_div(vocab, 4096)));
+  with_type(dt, [&](auto* p) {
+    using T = std::remove_pointer_t<decltype(p)>;
+    hipLaunchKernelGGL(k_score_grad<T>, dim3((unsigned)(rows * a.parts)), dim3(kThreads), 0, (hipStream_t)stream, a);
+  });
+  return launched("gptq2d_token_logprobs_backward");
+}
+
+}  // extern "C"

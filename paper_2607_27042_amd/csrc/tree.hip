@@ -1,0 +1,561 @@
+// Attention of a tree of drafted tokens (one token: decoding) over a paged
+// eight-bit cache.
+//
+// Sequence b has context[b] tokens in the cache and then its drafted ones. A
+// drafted token t sees the whole context and the drafted tokens u whose bit is
+// set in mask[b][t]. With keys k = ks ck and values v = vs cv (codes and scales),
+//   z = scale ks (q . ck),  o = sum_x softmax(z)_x vs_x cv_x,  lse = log sum e^z.
+#include <math.h>
+
+#include <algorithm>
+
+#include "codes.hpp"
+
+namespace g2d {
+namespace {
+
+constexpr int kStep = 32;        // tokens a wave takes at a time
+constexpr int kWaves = 4;
+constexpr int kMaxSplits = 64;
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLog2E = 1.44269504088896341f;
+
+struct TreeArgs {
+  int seqs, width, kv, group, dim, rows;  // rows = width * group: queries of a sequence that share a kv head
+  gptq2d_dtype dt;
+  const void* Q;
+  int64_t ldq;
+  const uint8_t *KC, *VC;
+  const float *KS, *VS;
+  int64_t pages;
+  int page, page16;
+  uint64_t magic;  // floor(2^32 / page16) + 1
+  const int32_t* table;
+  int64_t ldt;
+  int64_t capacity;  // tokens that a row of the table covers
+  const int32_t *context, *drafts;
+  const uint64_t* mask;
+  float scale;  // times log2 e
+  void* O;
+  int64_t ldo;
+  float* lse;
+  int splits, rowblocks;
+  float* part;  // splits > 1: [sequence][kv head][row][split][dim padded], then {m, l} likewise
+};
+
+__device__ __forceinline__ float load_as_float(const void* p, gptq2d_dtype dt, int64_t i) {
+  if (dt == GPTQ2D_F32) return ((const float*)p)[i];
+  if (dt == GPTQ2D_F16) return (float)((const _Float16*)p)[i];
+  return (float)((const bf16*)p)[i];
+}
+__device__ __forceinline__ void store_float(void* p, gptq2d_dtype dt, int64_t i, float v) {
+  if (dt == GPTQ2D_F32) ((float*)p)[i] = v;
+  else if (dt == GPTQ2D_F16) ((_Float16*)p)[i] = (_Float16)v;
+  else ((bf16*)p)[i] = (bf16)v;
+}
+
+// over the four lanes that share l % 16
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// One wave's 32 tokens as they lie in the cache. A lane (c = l % 16, g = l / 16)
+// holds of the keys a quarter (g) of token c of each 16-token row, and of the
+// values sixteenth c of tokens 4 g .. 4 g + 3 of each row: both are what the
+// matrix instruction takes as its row operand once widened, with no exchange
+// between lanes (the order in which it sums is free, as long as both operands
+// agree).
+template <int DP>
+struct Tokens {
+  u4 k[2][DP / 64];
+  uint32_t v[2][4][DP / 64];
+  f4 ks[2], vs[2];
+  bool there[2];
+};
+
+template <int DP>
+__device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, const int32_t* table, int hkv, int64_t tok,
+                                      int64_t end, int c, int g) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t t = tok + 16 * h;
+    int64_t entry = -1;
+    uint32_t off = 0;
+    if (t < end) {
+      const uint32_t t16 = (uint32_t)(t >> 4);
+      const uint32_t pg = (uint32_t)((t16 * a.magic) >> 32);  // exact: t16 page16 < 2^32
+      off = (t16 - pg * a.page16) * 16;
+      entry = table[pg];
+    }
+    // an entry that names no page: its tokens are absent
+    x.there[h] = entry >= 0 && entry < a.pages;
+    if (x.there[h]) {
+      const int64_t at = (entry * a.kv + hkv) * a.page + off;
+      const uint8_t* pk = a.KC + (at + c) * a.dim;
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i) {
+        const int d = g * (DP / 4) + 16 * i;
+        x.k[h][i] = d < a.dim ? *(const u4*)(pk + d) : u4{0, 0, 0, 0};
+      }
+      const uint8_t* pv = a.VC + (at + 4 * g) * a.dim + c * (DP / 16);
+      const bool in = c * (DP / 16) < a.dim;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (DP == 64) {
+          x.v[h][i][0] = in ? *(const uint32_t*)(pv + i * a.dim) : 0;
+        } else if constexpr (DP == 128) {
+          const u2 w = in ? *(const u2*)(pv + i * a.dim) : u2{0, 0};
+          x.v[h][i][0] = w[0], x.v[h][i][1] = w[1];
+        } else {
+          const u4 w = in ? *(const u4*)(pv + i * a.dim) : u4{0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[h][i][e] = w[e];
+        }
+      }
+      x.ks[h] = *(const f4*)(a.KS + at + 4 * g);
+      x.vs[h] = *(const f4*)(a.VS + at + 4 * g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i) x.k[h][i] = u4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
+      x.ks[h] = x.vs[h] = f4{0, 0, 0, 0};
+    }
+  }
+}
+
+// 16 QT queries of one kv head and sequence over one part of its tokens. Scores
+// and outputs are transposed (tokens and dimensions are the instruction's rows,
+// queries its columns), so a lane's values all belong to one query: maximum,
+// sum and rescaling are its own, and the scores leave the first product in the
+// registers where the second one takes them.
+// Codes are widened to halves, exactly. A query is scaled by a power of two so
+// that its largest element is in [1, 2) and rounded to halves (which a 16-bit
+// query survives, but for elements below 2^-14 of the largest); probabilities
+// are taken times vs over the largest vs so far (as a power of two), so they
+// lie in [0, 1]. Queries are kept as ZQ halves (two of them, 22 bits, for 32-bit
+// queries), probabilities as ZP (one, rounded by 2^-11 at most, where the result
+// is rounded by 2^-8 after it).
+template <bool INT8, int DP, int QT, int ZQ, int ZP>
+__global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
+  constexpr int KS = DP / 32, NT = DP / 16;
+  __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
+  __shared__ float lo[kWaves][16][DP + 4];
+  const int split = blockIdx.x, hkv = blockIdx.y / a.rowblocks, rb = blockIdx.y % a.rowblocks, b = blockIdx.z;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  const int64_t ctx = min((int64_t)max(a.context[b], 0), a.capacity);
+  const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
+  const int64_t total = min(ctx + drafted, a.capacity);
+  const int64_t per = (((total + a.splits - 1) / a.splits) + kWaves * kStep - 1) / (kWaves * kStep) * (kWaves * kStep);
+  const int64_t begin = split * per, end = min(total, begin + per);
+  const int32_t* table = a.table + b * a.ldt;
+
+  h8 q[QT][KS][ZQ];
+  float qs[QT], m[QT], sum[QT];
+  uint64_t sees[QT];
+  f4 o[QT][NT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = (rb * QT + t) * 16 + c, tok = r / a.group, head = hkv * a.group + r % a.group;
+    const bool live = r < a.rows;
+    const int64_t at = ((int64_t)b * a.width + tok) * a.ldq + (int64_t)head * a.dim;
+    float x[DP / 4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < DP / 4; ++i) {
+      const int d = g * (DP / 4) + i;
+      x[i] = live && d < a.dim ? load_as_float(a.Q, a.dt, at + d) : 0.0f;
+      top = max(top, mag(x[i]));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    uint32_t e = min(top & 0x7f800000u, 253u << 23);
+    if (e == 0 || bad_amax(top)) e = 127u << 23;
+    // (a scale of zero is taken as queries of zero, so that qs stays positive)
+    const float down = a.scale == 0.0f ? 0.0f : copysignf(__uint_as_float((254u << 23) - e), a.scale);
+    qs[t] = fmaxf(fabsf(a.scale) * __uint_as_float(e), 0x1p-126f);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float y = x[8 * s + i] * down;
+        q[t][s][0][i] = (_Float16)y;
+        if constexpr (ZQ == 2) q[t][s][1][i] = (_Float16)(y - (float)q[t][s][0][i]);
+      }
+    sees[t] = !live ? 0 : a.mask ? a.mask[(int64_t)b * a.width + tok] : ((uint64_t)2 << tok) - 1;
+    m[t] = -INFINITY, sum[t] = 0;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) o[t][j] = f4{0, 0, 0, 0};
+  }
+  float vref = 0x1p-120f;  // a power of two, at least the largest value scale so far
+
+  Tokens<DP> x, y;
+  int64_t tok = begin + w * kStep;
+  if (tok < end) fetch(y, a, table, hkv, tok, end, c, g);
+  for (; tok < end; tok += kWaves * kStep) {
+    x = y;
+    if (tok + kWaves * kStep < end) fetch(y, a, table, hkv, tok + kWaves * kStep, end, c, g);
+    // scores
+    f4 z[QT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      h8 kf[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const uint32_t w0 = x.k[h][s / 2][2 * (s & 1)], w1 = x.k[h][s / 2][2 * (s & 1) + 1];
+        const h2 p0 = halves<INT8, false>(w0), p1 = halves<INT8, true>(w0);
+        const h2 p2 = halves<INT8, false>(w1), p3 = halves<INT8, true>(w1);
+        kf[s] = h8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        f4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = ZQ - 1; e >= 0; --e)
+#pragma unroll
+          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[s], q[t][s][e], acc, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[t][h][i] = acc[i];
+      }
+    }
+    const bool edge = tok + kStep > min(ctx, end) || !x.there[0] || !x.there[1];
+    // bit 4 h + i: token tok + 16 h + 4 g + i is seen by query t
+    uint32_t ok[QT];
+    if (edge) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) ok[t] = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t p = tok + 16 * h + 4 * g + i;
+          const bool in = x.there[h] && p < end;
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const bool s = in && (p < ctx || ((sees[t] >> (p - ctx)) & 1));
+            ok[t] |= (uint32_t)s << (4 * h + i);
+          }
+          if (!in) {  // whatever lies there, it must not meet a zero probability
+            x.vs[h][i] = 0;
+#pragma unroll
+            for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
+          }
+        }
+    }
+    // the value scales' power of two
+    float vmax = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vmax = fmaxf(vmax, x.vs[h][i]);
+    vmax = quad_max(vmax);
+    float vold = vref;
+    if (vmax > vref && vmax <= 0x1p126f) vref = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
+    const float vinv = __uint_as_float((254u << 23) - __float_as_uint(vref));
+    // probabilities
+    h8 p[QT][ZP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float top = m[t];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float s = z[t][h][i] * x.ks[h][i];
+          top = fmaxf(top, edge && !((ok[t] >> (4 * h + i)) & 1) ? -INFINITY : s);
+        }
+      top = quad_max(top);
+      const float base = top == -INFINITY ? 0.0f : top;
+      const float fade = __builtin_amdgcn_exp2f((m[t] - base) * qs[t]);
+      float part = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // the maximum is taken off before the query's scale comes in
+          float e = __builtin_amdgcn_exp2f((z[t][h][i] * x.ks[h][i] - base) * qs[t]);
+          float y = e * (x.vs[h][i] * vinv);
+          if (edge && !((ok[t] >> (4 * h + i)) & 1)) e = y = 0;
+          part += e;
+          p[t][0][4 * h + i] = (_Float16)y;
+          if constexpr (ZP == 2) p[t][1][4 * h + i] = (_Float16)(y - (float)p[t][0][4 * h + i]);
+        }
+      sum[t] = sum[t] * fade + part;
+      m[t] = top;
+      const float f = fade * (vold * vinv);
+      if (__any(f != 1.0f)) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) o[t][j] *= f;
+      }
+    }
+    // values
+#pragma unroll
+    for (int e = 0; e < DP / 64; ++e) {
+      h8 vf[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const uint32_t lo2 = __builtin_amdgcn_perm(x.v[h][i + 1][e], x.v[h][i][e], 0x05010400u);
+          const uint32_t hi2 = __builtin_amdgcn_perm(x.v[h][i + 1][e], x.v[h][i][e], 0x07030602u);
+          const h2 d0 = halves<INT8, false>(lo2), d1 = halves<INT8, true>(lo2);
+          const h2 d2 = halves<INT8, false>(hi2), d3 = halves<INT8, true>(hi2);
+          vf[0][4 * h + i] = d0[0], vf[0][4 * h + i + 1] = d0[1];
+          vf[1][4 * h + i] = d1[0], vf[1][4 * h + i + 1] = d1[1];
+          vf[2][4 * h + i] = d2[0], vf[2][4 * h + i + 1] = d2[1];
+          vf[3][4 * h + i] = d3[0], vf[3][4 * h + i + 1] = d3[1];
+        }
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int s = ZP - 1; s >= 0; --s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            o[t][4 * e + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], p[t][s], o[t][4 * e + j], 0, 0, 0);
+    }
+  }
+
+  // the waves' parts, in their order
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    sum[t] = quad_sum(sum[t]);
+    m[t] *= qs[t];  // the same in every lane of a query
+    if (g == 0) lm[w][16 * t + c] = m[t], ll[w][16 * t + c] = sum[t];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    {
+      float top = lm[0][16 * t + c];
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) top = fmaxf(top, lm[i][16 * t + c]);
+      const float f = vref * (top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - top));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) lo[w][c][(4 * g + i) * NT + j] = o[t][j][i] * f;
+    }
+    __syncthreads();
+    const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * NT;
+    const int r = (rb * QT + t) * 16 + qr;
+    if (r < a.rows) {
+      float top = lm[0][16 * t + qr], L = 0;
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) top = fmaxf(top, lm[i][16 * t + qr]);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i)
+        L += ll[i][16 * t + qr] * (top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(lm[i][16 * t + qr] - top));
+      float v[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        v[j] = lo[0][qr][d0 + j];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) v[j] += lo[i][qr][d0 + j];
+      }
+      if (a.splits == 1) {
+        const int tk = r / a.group, head = hkv * a.group + r % a.group;
+        const int64_t row = (int64_t)b * a.width + tk;
+        const bool none = L == 0.0f || tk >= drafted;
+        const float inv = none ? 0.0f : 1.0f / L;
+        if (d0 < a.dim) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            store_float(a.O, a.dt, row * a.ldo + (int64_t)head * a.dim + d0 + j, none ? 0.0f : v[j] * inv);
+        }
+        if (a.lse && d0 == 0)
+          a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
+      } else {
+        const int64_t at = (((int64_t)b * a.kv + hkv) * a.rows + r) * a.splits + split;
+        float* ml = a.part + (int64_t)a.seqs * a.kv * a.rows * a.splits * DP;
+        if (L != 0.0f) {
+#pragma unroll
+          for (int j = 0; j < NT; j += 4) *(f4*)(a.part + at * DP + d0 + j) = f4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+        }
+        if (d0 == 0) ml[2 * at] = top, ml[2 * at + 1] = L;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// One wave per query: the splits' parts in their order.
+template <int DP>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.seqs * a.kv * a.rows;
+  if (id >= all) return;
+  const int l = threadIdx.x & 63;
+  const int64_t bh = id / a.rows;
+  const int r = (int)(id - bh * a.rows), hkv = (int)(bh % a.kv), b = (int)(bh / a.kv);
+  const float* ml = a.part + all * a.splits * DP + 2 * id * a.splits;
+  const float ms = l < a.splits ? ml[2 * l] : -INFINITY, ls = l < a.splits ? ml[2 * l + 1] : 0.0f;
+  float top = ms;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
+  float L = 0, v[DP / 64];
+#pragma unroll
+  for (int e = 0; e < DP / 64; ++e) v[e] = 0;
+  for (int s = 0; s < a.splits; ++s) {
+    const float ps = __shfl(ls, s), fs = __shfl(f, s);
+    if (ps == 0.0f) continue;
+    L += ps * fs;
+    const float* p = a.part + (id * a.splits + s) * DP;
+#pragma unroll
+    for (int e = 0; e < DP / 64; ++e) v[e] += p[64 * e + l] * fs;
+  }
+  const int tk = r / a.group, head = hkv * a.group + r % a.group;
+  const int64_t row = (int64_t)b * a.width + tk;
+  const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
+  const bool none = L == 0.0f || tk >= drafted;
+#pragma unroll
+  for (int e = 0; e < DP / 64; ++e)
+    if (64 * e + l < a.dim)
+      store_float(a.O, a.dt, row * a.ldo + (int64_t)head * a.dim + 64 * e + l, none ? 0.0f : v[e] / L);
+  if (a.lse && l == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
+}
+
+// bits of a token's ancestors and itself; a parent that is not an earlier token is none
+__global__ __launch_bounds__(256) void k_tree_masks(int64_t count, int width, const int32_t* parents, uint64_t* masks) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count * width) return;
+  const int64_t b = i / width;
+  int t = (int)(i - b * width);
+  uint64_t m = (uint64_t)1 << t;
+  for (;;) {
+    const int p = parents[b * width + t];
+    if (p < 0 || p >= t) break;
+    m |= (uint64_t)1 << p;
+    t = p;
+  }
+  masks[i] = m;
+}
+
+int padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+
+// Queries a work group takes, in tiles of 16: more of them share each read of
+// the cache, as far as their accumulators fit the registers.
+int query_tiles(int rows, int dim) {
+  const int most = padded(dim) == 256 ? 2 : 4;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+}
+
+// Parts that a sequence's tokens are split into: as many as give the device
+// about four work groups a compute unit.
+int split_count(int64_t seqs, int rows, int kv, int dim) {
+  const int64_t groups = seqs * kv * ceil_div(rows, 16 * query_tiles(rows, dim));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(1024, groups)));
+}
+
+size_t part_bytes(int64_t seqs, int rows, int kv, int dim) {
+  const int s = split_count(seqs, rows, kv, dim);
+  return s == 1 ? 0 : (size_t)seqs * kv * rows * s * (padded(dim) + 2) * sizeof(float);
+}
+
+template <bool INT8, int DP, int QT, int ZQ, int ZP>
+void launch(const TreeArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_tree<INT8, DP, QT, ZQ, ZP>), dim3(a.splits, a.kv * a.rowblocks, a.seqs), dim3(64 * kWaves), 0, s, a);
+}
+template <bool INT8, int DP, int ZQ, int ZP>
+void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
+  if (tiles == 1) launch<INT8, DP, 1, ZQ, ZP>(a, s);
+  else if (tiles == 2) launch<INT8, DP, 2, ZQ, ZP>(a, s);
+  else if constexpr (DP != 256) launch<INT8, DP, 4, ZQ, ZP>(a, s);
+  if (a.splits > 1) {
+    const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
+    hipLaunchKernelGGL(k_tree_join<DP>, dim3((unsigned)ceil_div(all, 4)), dim3(256), 0, s, a);
+  }
+}
+template <bool INT8, int DP>
+void launch_type(const TreeArgs& a, int tiles, hipStream_t s) {
+  if (a.dt == GPTQ2D_F32) launch_tiles<INT8, DP, 2, 2>(a, tiles, s);
+  else if (a.dt == GPTQ2D_F16) launch_tiles<INT8, DP, 1, 2>(a, tiles, s);
+  else launch_tiles<INT8, DP, 1, 1>(a, tiles, s);
+}
+template <bool INT8>
+void launch_dim(const TreeArgs& a, int tiles, hipStream_t s) {
+  if (a.dim <= 64) launch_type<INT8, 64>(a, tiles, s);
+  else if (a.dim <= 128) launch_type<INT8, 128>(a, tiles, s);
+  else launch_type<INT8, 256>(a, tiles, s);
+}
+
+bool bad_shape(int64_t seqs, int width, int heads, int kv_heads, int dim) {
+  return seqs < 1 || seqs > 65535 || width < 1 || width > 64 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads ||
+         heads > 4096 || heads % kv_heads != 0 || dim < 16 || dim > 256 || dim % 16 != 0;
+}
+
+}  // namespace
+}  // namespace g2d
+
+using namespace g2d;
+
+extern "C" {
+
+gptq2d_status gptq2d_tree_masks(int64_t seqs, int width, const int32_t* parents, uint64_t* masks, void* stream) {
+  if (seqs < 0 || seqs > 65535) return refuse("seqs must lie in [0, 65535]");
+  if (width < 1 || width > 64) return refuse("width must lie in [1, 64]");
+  if (seqs == 0) return GPTQ2D_OK;
+  if (!parents || !masks) return refuse("parents or masks are NULL");
+  if (!aligned(parents, 4) || !aligned(masks, 8)) return refuse("parents or masks are not aligned");
+  hipLaunchKernelGGL(k_tree_masks, dim3((unsigned)ceil_div(seqs * width, 256)), dim3(256), 0, (hipStream_t)stream, seqs,
+                     width, parents, masks);
+  return launched("gptq2d_tree_masks");
+}
+
+size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, int kv_heads, int dim) {
+  if (bad_shape(seqs, width, heads, kv_heads, dim)) return 0;
+  return part_bytes(seqs, width * (heads / kv_heads), kv_heads, dim);
+}
+
+gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_heads, int dim, gptq2d_dtype dt,
+                                    const void* Q, int64_t ldq, gptq2d_code code, int64_t pages, int page_size,
+                                    const void* KC, const void* VC, const float* KS, const float* VS,
+                                    const int32_t* table, int64_t ldt, int64_t table_width, const int32_t* context,
+                                    const int32_t* drafts, const uint64_t* masks, float scale, void* O, int64_t ldo,
+                                    float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  if (bad_shape(seqs, width, heads, kv_heads, dim))
+    return refuse("bad shape: 1 <= seqs <= 65535, 1 <= width <= 64, heads a multiple of kv_heads (up to 4096 of up to "
+                  "1024), dim a multiple of 16 up to 256");
+  if (!narrow_dtype(dt)) return refuse("bad dtype");
+  gptq2d_status st = check_cache(kv_heads, dim, code, pages, page_size, KC, VC, KS, VS);
+  if (st != GPTQ2D_OK) return st;
+  if (!Q || !O || !table || !context) return refuse("Q, O, table or context are NULL");
+  const int64_t cols = (int64_t)heads * dim;
+  if (ldq < cols || ldo < cols) return refuse("leading dimension too small");
+  if (table_width < 1 || ldt < table_width || table_width > ((int64_t)1 << 28) / page_size)
+    return refuse("the page table must cover 1 to 2^28 tokens a sequence");
+  const size_t es = elem_size(dt);
+  if (!aligned(Q, es) || !aligned(O, es) || !aligned(table, 4) || !aligned(context, 4) || !aligned(drafts, 4) ||
+      !aligned(masks, 8) || !aligned(lse, 4))
+    return refuse("an argument is not aligned to its elements");
+  if (!isfinite(scale)) return refuse("scale is not finite");
+  const int rows = width * (heads / kv_heads);
+  const size_t need = part_bytes(seqs, rows, kv_heads, dim);
+  if (need > 0 && (!workspace || ws_bytes < need)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
+  if (need > 0 && !aligned(workspace, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  TreeArgs a = {};
+  a.seqs = (int)seqs, a.width = width, a.kv = kv_heads, a.group = heads / kv_heads, a.dim = dim, a.rows = rows;
+  a.dt = dt, a.Q = Q, a.ldq = ldq;
+  a.KC = (const uint8_t*)KC, a.VC = (const uint8_t*)VC, a.KS = KS, a.VS = VS;
+  a.pages = pages, a.page = page_size, a.page16 = page_size / 16, a.magic = ((uint64_t)1 << 32) / a.page16 + 1;
+  a.table = table, a.ldt = ldt, a.capacity = table_width * page_size;
+  a.context = context, a.drafts = drafts, a.mask = masks;
+  a.scale = scale * kLog2E;
+  a.O = O, a.ldo = ldo, a.lse = lse, a.part = (float*)workspace;
+  const int tiles = query_tiles(rows, dim);
+  a.rowblocks = (int)ceil_div(rows, 16 * tiles);
+  a.splits = (int)std::min<int64_t>(split_count(seqs, rows, kv_heads, dim), ceil_div(a.capacity, kWaves * kStep));
+  if (code == GPTQ2D_INT8)
+    launch_dim<true>(a, tiles, (hipStream_t)stream);
+  else
+    launch_dim<false>(a, tiles, (hipStream_t)stream);
+  return launched("gptq2d_tree_attention");
+}
+
+}  // extern "C"

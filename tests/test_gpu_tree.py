@@ -1,0 +1,371 @@
+"""Tree attention over the eight-bit cache through the C ABI against the plain
+64-bit form, in which a masked token takes no part at all (its values are not
+multiplied by zero).
+
+Bounds. With z off by dz, a softmax-weighted mean of v is off by 2 dz sum p |v|.
+  dz <= (dim + 8) 2^-24 max scale sum |q k| (32-bit sums, 22-bit or exact
+        queries) + 2^-20 (the exponential)
+  probabilities: 2^-12 of themselves (16-bit types) or 2^-21 (32-bit), and
+        2^-24 of the largest |v| for each of the tokens where they are below the
+        halves' normal range
+  result: half a unit of its last place.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2607_27042_amd import binding
+
+import eightbit as eb
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+class Case:
+    """Random cache, tables, queries and trees. Codes and scales outside the
+    tokens in use are NaN (-128)."""
+
+    def __init__(self, contexts, width, kv, group, dim, page, code, dtype, seed=0, drafts=None, chain=False,
+                 masks=None, spare=2, peaked=1.0):
+        g = _gen(seed)
+        self.width, self.kv, self.group, self.dim, self.page, self.code, self.dtype = (
+            width, kv, group, dim, page, code, dtype)
+        self.contexts, self.seqs = contexts, len(contexts)
+        self.drafts, self.peaked = drafts, peaked
+        n = [c + width for c in contexts]
+        need = [-(-t // page) for t in n]
+        self.pages = sum(need) + spare
+        order = torch.randperm(self.pages, generator=g, device="cuda")
+        self.table = torch.full((self.seqs, max(need) + 1), -1, dtype=torch.int32, device="cuda")
+        fill = 0x7F if code == "e4m3" else 0x80
+        shape = (self.pages, kv, page)
+        self.C = [torch.full(shape + (dim,), fill, dtype=torch.uint8, device="cuda").view(CODE[code]) for _ in range(2)]
+        self.S = [torch.full(shape, float("nan"), device="cuda") for _ in range(2)]
+        self.kv_values = []
+        at = 0
+        for b in range(self.seqs):
+            pages = order[at:at + need[b]]
+            at += need[b]
+            self.table[b, :need[b]] = pages.int()
+            pair = []
+            for i in range(2):
+                x = torch.randn(n[b], kv, dim, generator=g, device="cuda", dtype=torch.float64)
+                x *= torch.exp2(torch.randint(-3, 4, (n[b], kv, 1), generator=g, device="cuda").double())
+                if i == 0:
+                    x *= peaked
+                s = eb.scale_of(x.abs().amax(-1), code)
+                q = eb.codes_of(x, s[..., None], code)
+                pair.append(q * s[..., None])
+                t = torch.arange(n[b], device="cuda")
+                slot_page, off = pages[t // page], t % page
+                codes = q.float().to(CODE[code]).view(torch.uint8) if code == "e4m3" else q.to(torch.int8).view(
+                    torch.uint8)
+                self.C[i].view(torch.uint8)[slot_page, :, off] = codes
+                self.S[i][slot_page, :, off] = s.float()
+            self.kv_values.append(pair)
+        heads = kv * group
+        self.Q = torch.randn(self.seqs * width, heads * dim, generator=g, device="cuda").to(eb.DTYPE[dtype])
+        self.scale = 1.0 / math.sqrt(dim)
+        parent = torch.stack([torch.arange(-1, width - 1)] + [
+            torch.tensor([int(torch.randint(-1, max(t, 1), (1,), generator=torch.Generator().manual_seed(seed + 7 * t + b)))
+                          if t else -1 for t in range(width)]) for b in range(1, self.seqs)]).int().cuda()
+        self.parents = parent if not chain else torch.arange(-1, width - 1).int().cuda().repeat(self.seqs, 1)
+        self.masks = masks
+        if masks is None and not chain:
+            self.masks = torch.empty(self.seqs, width, dtype=torch.int64, device="cuda")
+            binding.gptq2d_tree_masks(self.parents.contiguous(), self.masks)
+        self.context = torch.tensor(contexts, dtype=torch.int32, device="cuda")
+
+    def sees(self, b):
+        w = self.width
+        if self.masks is None:
+            return torch.tril(torch.ones(w, w, dtype=torch.bool, device="cuda"))
+        m = self.masks[b]
+        return torch.stack([((m >> u) & 1).bool() for u in range(w)], 1)
+
+    def run(self, Q=None, O=None, stream=None):
+        heads = self.kv * self.group
+        Q = self.Q if Q is None else Q
+        O = torch.full(self.Q.shape, 55.0, dtype=self.Q.dtype, device="cuda") if O is None else O
+        lse = torch.full((self.seqs * self.width, heads), 55.0, device="cuda")
+        need = binding.gptq2d_tree_attention_workspace_size(self.seqs, self.width, heads, self.kv, self.dim)
+        ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+        drafts = None if self.drafts is None else torch.tensor(self.drafts, dtype=torch.int32, device="cuda")
+        binding.gptq2d_tree_attention(Q, *self.C, *self.S, self.table, self.context, drafts, self.masks, self.scale, O,
+                                      lse, ws, stream=stream)
+        return O, lse
+
+    def reference(self, skip=()):
+        """(o, lse, bound of o, bound of lse); tokens in skip (sequence, position) are absent."""
+        w, heads, dim = self.width, self.kv * self.group, self.dim
+        o = torch.zeros(self.seqs, w, heads, dim, dtype=torch.float64, device="cuda")
+        lse = torch.full((self.seqs, w, heads), -math.inf, dtype=torch.float64, device="cuda")
+        bo, bl = torch.zeros_like(o), torch.zeros_like(lse)
+        q = self.Q.double().view(self.seqs, w, heads, dim)
+        for b in range(self.seqs):
+            n = w if self.drafts is None else self.drafts[b]
+            ctx = self.contexts[b]
+            tree = self.sees(b)
+            for t in range(n):
+                keep = torch.cat([torch.ones(ctx, dtype=torch.bool, device="cuda"), tree[t, :n]])
+                for s, x in skip:
+                    if s == b:
+                        keep[x] = False
+                idx = keep.nonzero()[:, 0]
+                if len(idx) == 0:
+                    continue
+                k = self.kv_values[b][0][idx].repeat_interleave(self.group, 1)
+                v = self.kv_values[b][1][idx].repeat_interleave(self.group, 1)
+                z = self.scale * (k * q[b, t]).sum(-1)  # tokens x heads
+                zm = abs(self.scale) * (k * q[b, t]).abs().sum(-1).amax(0)
+                p = torch.softmax(z, 0)
+                o[b, t] = (p.unsqueeze(-1) * v).sum(0)
+                lse[b, t] = torch.logsumexp(z, 0)
+                dz = (dim + 8) * 2.0 ** -24 * zm + 2.0 ** -20
+                rel = 2 * dz + (2.0 ** -21 if self.dtype == "f32" else 2.0 ** -12)
+                bo[b, t] = (o[b, t].abs() * eb.HALF_ULP[self.dtype] * 1.01 + (p.unsqueeze(-1) * v.abs()).sum(0) * rel[:, None]
+                            + len(idx) * 2.0 ** -24 * v.abs().amax() + 1e-30)
+                bl[b, t] = dz + 2.0 ** -22 * (1 + lse[b, t].abs())
+        return o.view(self.seqs * w, -1), lse.view(-1, heads), bo.view(self.seqs * w, -1), bl.view(-1, heads)
+
+    def check(self, O, lse, skip=()):
+        o, l, bo, bl = self.reference(skip)
+        err = (O.double() - o).abs()
+        assert (err <= bo).all(), f"output: {int((~(err <= bo)).sum())} off, worst {float((err / (bo + 1e-300)).max())} bounds"
+        assert torch.equal(torch.isinf(lse), torch.isinf(l))
+        fin = ~torch.isinf(l)
+        assert ((lse.double() - l).abs() <= bl)[fin].all()
+        # errors are mostly far below their bounds, as long as the scores' own rounding is
+        if self.peaked > 1:
+            return
+        rms = float(err.pow(2).mean().sqrt() / (o.pow(2).mean().sqrt() + 1e-30))
+        assert rms <= {"f32": 1e-5, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[self.dtype], rms
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("contexts,width,kv,group,dim,page", [
+    ([0], 1, 1, 1, 16, 16), ([1], 1, 2, 1, 64, 16), ([31, 32, 33], 1, 1, 4, 128, 16), ([0, 5, 700], 3, 2, 3, 80, 48),
+    ([1000, 17], 16, 2, 1, 64, 64), ([300, 0, 64], 33, 1, 2, 96, 16), ([200], 64, 1, 3, 128, 32), ([90, 130], 64, 2, 1, 256, 16),
+    ([3000], 1, 1, 8, 192, 128), ([4096, 4095], 2, 1, 16, 128, 4096), ([5000], 5, 3, 5, 32, 64)])
+def test_attention(contexts, width, kv, group, dim, page, dtype, code):
+    print(f"[tree] {contexts} width {width} heads {kv}x{group} dim {dim} page {page} {dtype} {code}", flush=True)
+    c = Case(contexts, width, kv, group, dim, page, code, dtype, seed=len(contexts) + dim)
+    O, lse = c.run()
+    c.check(O, lse)
+    O2, lse2 = c.run()
+    assert torch.equal(O, O2) and torch.equal(lse, lse2), "the same call gave other bits"
+
+
+@pytest.mark.parametrize("contexts,width", [([100, 0, 37], 7), ([513], 64)])
+def test_chain_is_the_default_mask(contexts, width):
+    c = Case(contexts, width, 2, 2, 64, 16, "e4m3", "bf16", seed=3, chain=True)
+    O, lse = c.run()
+    c.check(O, lse)
+    c.masks = torch.empty(len(contexts), width, dtype=torch.int64, device="cuda")
+    binding.gptq2d_tree_masks(c.parents.contiguous(), c.masks)
+    O2, lse2 = c.run()
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def test_masks_follow_parents():
+    parents = torch.tensor([[-1, 0, 0, 1, 3, 2, -1, 6], [-1, -5, 1, 7, 4, 2, 5, 100]], dtype=torch.int32, device="cuda")
+    masks = torch.empty(2, 8, dtype=torch.int64, device="cuda")
+    binding.gptq2d_tree_masks(parents, masks)
+    want = [[1, 3, 5, 11, 27, 37, 64, 192], [1, 2, 6, 8, 16, 38, 102, 128]]
+    assert masks.tolist() == want
+    wide = torch.arange(-1, 63, dtype=torch.int32, device="cuda").view(1, 64)
+    masks = torch.empty(1, 64, dtype=torch.int64, device="cuda")
+    binding.gptq2d_tree_masks(wide, masks)
+    assert masks.tolist()[0] == [(1 << (t + 1)) - 1 if t < 62 else (1 << 63) - 1 if t == 62 else -1 for t in range(64)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_see_nothing(dtype):
+    """No context and an empty mask: zeros and -inf; bits past the drafted
+    tokens and the rows after them count for nothing."""
+    masks = torch.zeros(3, 9, dtype=torch.int64, device="cuda")
+    masks[0, 2] = 0b101
+    masks[0, 8] = -1
+    masks[1, 0] = -(1 << 63)
+    masks[2] = -1
+    c = Case([0, 0, 40], 9, 2, 2, 64, 16, "int8", dtype, masks=masks, drafts=[9, 4, 0])
+    O, lse = c.run()
+    c.check(O, lse)
+    O = O.view(3, 9, -1)
+    assert (O[0, 0] == 0).all() and (O[0, 2] != 0).any() and (O[1] == 0).all() and (O[2] == 0).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+def test_nothing_masked_takes_part(code):
+    """A drafted token with NaN keys and values reaches those that see it only;
+    so does one in the context."""
+    c = Case([50, 20], 6, 2, 2, 64, 16, code, "f16", seed=5)
+    O0, _ = c.run()
+    # token 3 of the tree of sequence 0 is not finite, in kv head 1
+    p, off = int(c.table[0, 53 // 16]), 53 % 16
+    for S in c.S:
+        S[p, 1, off] = float("nan")
+    for C in c.C:
+        C.view(torch.uint8)[p, 1, off] = 0
+    O, _ = c.run()
+    hit = c.sees(0)[:, 3]
+    O, O0 = O.view(2, 6, 4, 64), O0.view(2, 6, 4, 64)
+    assert hit.any() and not hit.all()
+    assert torch.isnan(O[0, hit][:, 2:]).all() and torch.equal(O[0, ~hit], O0[0, ~hit])
+    assert torch.equal(O[0, :, :2], O0[0, :, :2]) and torch.equal(O[1], O0[1])
+
+
+def test_tables_that_end_or_name_no_page():
+    c = Case([70, 100], 4, 1, 2, 64, 16, "e4m3", "bf16", seed=9)
+    # a page of the context missing: its tokens are absent
+    c.table[0, 2] = -1
+    c.table[1, 1] = c.pages
+    O, lse = c.run()
+    c.check(O, lse, skip=[(0, x) for x in range(32, 48)] + [(1, x) for x in range(16, 32)])
+    # a context past the table's end stops there
+    c = Case([60], 4, 1, 2, 64, 16, "e4m3", "bf16", seed=9)
+    O, lse = c.run()
+    c.table = c.table[:, :4].contiguous()
+    c.context += 4
+    c.contexts = [64]
+    c.drafts = [0]
+    O2, lse2 = c.run()
+    assert (O2 == 0).all()
+    c.context += 1000000
+    c.drafts = None
+    O3, lse3 = c.run()  # 64 tokens of context, no room for the drafted ones
+    c.contexts, c.drafts = [64], None
+    k, v = c.kv_values[0]
+    z = c.scale * torch.einsum("tkd,rkgd->rkgt", k, c.Q.double().view(4, 1, 2, 64))
+    want = torch.softmax(z, -1) @ v.permute(1, 0, 2).unsqueeze(0)
+    assert ((O3.double().view(4, 1, 2, 64) - want).abs() <= 2.0 ** -7 * v.abs().amax()).all()
+    c.context.fill_(-3)  # no tokens before the tree
+    O4, _ = c.run()
+    assert torch.isfinite(O4.float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_peaked_and_wide_scores(dtype):
+    """Keys a hundred times larger: one token takes nearly all, and the running
+    maximum moves late."""
+    c = Case([2000], 3, 2, 2, 128, 16, "e4m3", dtype, seed=11, peaked=100.0)
+    O, lse = c.run()
+    c.check(O, lse)
+    # queries over the type's whole range
+    c = Case([200], 3, 2, 2, 64, 16, "e4m3", dtype, seed=12)
+    c.Q *= torch.exp2(torch.randint(-12, 5, c.Q.shape, device="cuda", generator=_gen(1)).float()).to(c.Q.dtype)
+    O, lse = c.run()
+    c.check(O, lse)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.25, 1e-30, 3.0])
+def test_scales(scale):
+    c = Case([90, 0], 3, 2, 2, 64, 16, "int8", "f32", seed=13)
+    c.scale = scale
+    O, lse = c.run()
+    c.check(O, lse)
+
+
+def test_strides_streams_and_graph():
+    c = Case([500, 60], 5, 2, 2, 64, 16, "int8", "bf16", seed=2)
+    want, lse = c.run()
+    buf = torch.full((10, 4 * 64 + 9), 3.0, dtype=torch.bfloat16, device="cuda")
+    q = buf[:, 9:]
+    q.copy_(c.Q)
+    out = torch.full((10, 4 * 64 + 5), 3.0, dtype=torch.bfloat16, device="cuda")
+    c.run(Q=q, O=out[:, 1:257])
+    assert torch.equal(out[:, 1:257], want) and (out[:, 257:] == 3).all() and (out[:, 0] == 3).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        O, _ = c.run()
+    side.synchronize()
+    assert torch.equal(O, want)
+    O, l2 = torch.empty_like(want), torch.empty_like(lse)
+    ws = torch.empty(max(256, binding.gptq2d_tree_attention_workspace_size(2, 5, 4, 2, 64)), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.gptq2d_tree_attention(c.Q, *c.C, *c.S, c.table, c.context, None, c.masks, c.scale, O, l2, ws)
+    for seed in (1, 2, 3):
+        c.Q.copy_(torch.randn(c.Q.shape, generator=_gen(seed), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _ = c.run()
+        assert torch.equal(O, want)
+
+
+def test_append_then_attend():
+    """Keys and values written by the library itself, one token at a time."""
+    kv, dim, page = 2, 64, 16
+    c = Case([0], 1, kv, 2, dim, page, "e4m3", "bf16", seed=1, spare=5)
+    c.table = torch.tensor([[3, 0, 5]], dtype=torch.int32, device="cuda")
+    ks, vs = [], []
+    for n in range(40):
+        k, v = (torch.randn(1, kv * dim, generator=_gen(100 + 2 * n + i), device="cuda").bfloat16() for i in range(2))
+        slot = c.table[0, n // page].long() * page + n % page
+        binding.gptq2d_cache_append(k, v, slot.view(1), *c.C, *c.S)
+        for x, l in ((k, ks), (v, vs)):
+            t = x.double().view(1, kv, dim)
+            s = eb.scale_of(t.abs().amax(-1))
+            l.append(eb.codes_of(t, s[..., None]) * s[..., None])
+        c.kv_values = [[torch.cat(ks), torch.cat(vs)]]
+        c.contexts, c.context = [n], torch.tensor([n], dtype=torch.int32, device="cuda")
+        O, lse = c.run()
+        c.check(O, lse)
+
+
+def test_offsets_past_32_bits():
+    """A cache whose codes reach past 2^32 bytes; the sequence lies in its last pages."""
+    pages, kv, page, dim = 70000, 4, 64, 256
+    C = [torch.zeros(pages, kv, page, dim, dtype=torch.int8, device="cuda") for _ in range(2)]
+    S = [torch.ones(pages, kv, page, device="cuda") for _ in range(2)]
+    small = Case([150], 2, kv, 1, dim, page, "int8", "f32", seed=4)
+    want, lse = small.run()
+    for b in range(small.table.shape[1]):
+        if int(small.table[0, b]) >= 0:
+            for big, own in ((C, small.C), (S, small.S)):
+                for i in range(2):
+                    big[i][pages - 1 - 7 * b] = own[i][int(small.table[0, b])]
+            small.table[0, b] = pages - 1 - 7 * b
+    small.C, small.S = C, S
+    O, l2 = small.run()
+    assert torch.equal(O, want) and torch.equal(lse, l2)
+
+
+def test_refusals():
+    c = Case([20], 2, 1, 2, 64, 16, "int8", "bf16")
+    O, lse = torch.empty_like(c.Q), torch.empty(2, 2, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    call = lambda **k: binding.gptq2d_tree_attention(**{**dict(
+        Q=c.Q, KC=c.C[0], VC=c.C[1], KS=c.S[0], VS=c.S[1], table=c.table, context=c.context, drafts=None, masks=c.masks,
+        scale=c.scale, O=O, lse=lse, workspace=ws), **k})
+    call()
+    with pytest.raises(TypeError, match="one dtype"):
+        call(O=O.float())
+    with pytest.raises(ValueError, match="Q must be"):
+        call(Q=c.Q[:, :100])
+    with pytest.raises(TypeError, match="table must be"):
+        call(table=c.table.long())
+    with pytest.raises(TypeError, match="context must be"):
+        call(context=c.context.long())
+    with pytest.raises(ValueError, match="masks must be"):
+        call(masks=c.masks[:, :1])
+    with pytest.raises(ValueError, match="lse must be"):
+        call(lse=lse[:1])
+    with pytest.raises(binding.Gptq2dError, match="scale is not finite"):
+        call(scale=float("nan"))
+    with pytest.raises(binding.Gptq2dError, match="ERR_WORKSPACE"):
+        call(workspace=ws[:256])
+    with pytest.raises(binding.Gptq2dError, match="bad shape"):
+        q = c.Q.repeat(33, 1)
+        call(Q=q, O=torch.empty_like(q), masks=None, lse=None)
