@@ -32,36 +32,58 @@ struct TreeArgs {
   uint64_t magic;  // floor(2^32 / page16) + 1
   const int32_t* table;
   int64_t ldt;
-  int64_t capacity;  // tokens that a row of the table covers
+  int capacity;  // tokens that a row of the table covers
   const int32_t *context, *drafts;
   const uint64_t* mask;
   float scale;  // times log2 e
   void* O;
   int64_t ldo;
+  bool qwide, owide;  // rows of Q and O start on 16-byte boundaries
   float* lse;
   int splits, rowblocks;
   float* part;  // splits > 1: [sequence][kv head][row][split][dim padded], then {m, l} likewise
 };
 
-__device__ __forceinline__ float load_as_float(const void* p, gptq2d_dtype dt, int64_t i) {
-  if (dt == GPTQ2D_F32) return ((const float*)p)[i];
-  if (dt == GPTQ2D_F16) return (float)((const _Float16*)p)[i];
-  return (float)((const bf16*)p)[i];
+// eight elements of type dt from element i on; wide: they are 16-byte aligned
+__device__ __forceinline__ void load8_as(const void* p, gptq2d_dtype dt, int64_t i, bool wide, float x[8]) {
+  if (dt == GPTQ2D_F32) load8((const float*)p + i, wide, 8, x);
+  else if (dt == GPTQ2D_F16) load8((const _Float16*)p + i, wide, 8, x);
+  else load8((const bf16*)p + i, wide, 8, x);
 }
-__device__ __forceinline__ void store_float(void* p, gptq2d_dtype dt, int64_t i, float v) {
-  if (dt == GPTQ2D_F32) ((float*)p)[i] = v;
-  else if (dt == GPTQ2D_F16) ((_Float16*)p)[i] = (_Float16)v;
-  else ((bf16*)p)[i] = (bf16)v;
+// N (4 or a multiple of 8) results; wide: aligned to their size, at most 16 bytes
+template <int N, class T>
+__device__ __forceinline__ void store_n(T* p, bool wide, const float* v) {
+  if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) store8(p + i, wide, 8, v + i);
+  } else if (wide) {
+    struct alignas(4 * sizeof(T)) V { T v[4]; };
+    *(V*)p = V{{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = (T)v[i];
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_as(void* p, gptq2d_dtype dt, int64_t i, bool wide, const float* v) {
+  if (dt == GPTQ2D_F32) store_n<N>((float*)p + i, wide, v);
+  else if (dt == GPTQ2D_F16) store_n<N>((_Float16*)p + i, wide, v);
+  else store_n<N>((bf16*)p + i, wide, v);
 }
 
-// over the four lanes that share l % 16
+// over the four lanes that share l % 16, in every lane: the instructions swap
+// halves (rows of 16) of two registers
 __device__ __forceinline__ float quad_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  const u2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float quad_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  const u2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const u2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // One wave's 32 tokens as they lie in the cache. A lane (c = l % 16, g = l / 16)
@@ -78,56 +100,58 @@ struct Tokens {
   bool there[2];
 };
 
-template <int DP>
-__device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, const int32_t* table, int hkv, int64_t tok,
-                                      int64_t end, int c, int g) {
+// The table's entries of a wave's next 32 tokens (uniform, looked up ahead of
+// the tokens themselves); an entry that names no page, or tokens from `end` on: -1
+struct Entry {
+  int32_t page[2], off[2];
+};
+__device__ __forceinline__ Entry look_up(const TreeArgs& a, const int32_t* table, int tok, int end) {
+  Entry r;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int64_t t = tok + 16 * h;
-    int64_t entry = -1;
-    uint32_t off = 0;
-    if (t < end) {
-      const uint32_t t16 = (uint32_t)(t >> 4);
-      const uint32_t pg = (uint32_t)((t16 * a.magic) >> 32);  // exact: t16 page16 < 2^32
-      off = (t16 - pg * a.page16) * 16;
-      entry = table[pg];
+    const bool in = tok + 16 * h < end;
+    const uint32_t t16 = in ? (uint32_t)(tok >> 4) + h : 0;
+    const uint32_t pg = (uint32_t)((t16 * a.magic) >> 32);  // exact: t16 page16 < 2^32
+    r.off[h] = (t16 - pg * a.page16) * 16;
+    const int32_t e = table[pg];
+    r.page[h] = in && e >= 0 && e < a.pages ? e : -1;
+  }
+  return r;
+}
+
+// Tokens that are not there are read from page 0 and masked later.
+template <int DP>
+__device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, Entry e, int hkv, int c, int g) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    x.there[h] = e.page[h] >= 0;
+    const int64_t at = ((int64_t)max(e.page[h], 0) * a.kv + hkv) * a.page + e.off[h];
+    const uint8_t* pk = a.KC + at * a.dim;
+    const uint8_t* pv = a.VC + at * a.dim;
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) {
+      // past the end of a vector: any of it (the query is 0 there)
+      const int d = g * (DP / 4) + 16 * i;
+      x.k[h][i] = *(const u4*)(pk + (uint32_t)(c * a.dim + (d < a.dim ? d : 0)));
     }
-    // an entry that names no page: its tokens are absent
-    x.there[h] = entry >= 0 && entry < a.pages;
-    if (x.there[h]) {
-      const int64_t at = (entry * a.kv + hkv) * a.page + off;
-      const uint8_t* pk = a.KC + (at + c) * a.dim;
+    // past the end: any of it (the results are not stored)
+    const int d = c * (DP / 16) < a.dim ? c * (DP / 16) : 0;
 #pragma unroll
-      for (int i = 0; i < DP / 64; ++i) {
-        const int d = g * (DP / 4) + 16 * i;
-        x.k[h][i] = d < a.dim ? *(const u4*)(pk + d) : u4{0, 0, 0, 0};
+    for (int i = 0; i < 4; ++i) {
+      const uint8_t* p = pv + (uint32_t)((4 * g + i) * a.dim + d);
+      if constexpr (DP == 64) {
+        x.v[h][i][0] = *(const uint32_t*)p;
+      } else if constexpr (DP == 128) {
+        const u2 w = *(const u2*)p;
+        x.v[h][i][0] = w[0], x.v[h][i][1] = w[1];
+      } else {
+        const u4 w = *(const u4*)p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.v[h][i][j] = w[j];
       }
-      const uint8_t* pv = a.VC + (at + 4 * g) * a.dim + c * (DP / 16);
-      const bool in = c * (DP / 16) < a.dim;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (DP == 64) {
-          x.v[h][i][0] = in ? *(const uint32_t*)(pv + i * a.dim) : 0;
-        } else if constexpr (DP == 128) {
-          const u2 w = in ? *(const u2*)(pv + i * a.dim) : u2{0, 0};
-          x.v[h][i][0] = w[0], x.v[h][i][1] = w[1];
-        } else {
-          const u4 w = in ? *(const u4*)(pv + i * a.dim) : u4{0, 0, 0, 0};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x.v[h][i][e] = w[e];
-        }
-      }
-      x.ks[h] = *(const f4*)(a.KS + at + 4 * g);
-      x.vs[h] = *(const f4*)(a.VS + at + 4 * g);
-    } else {
-#pragma unroll
-      for (int i = 0; i < DP / 64; ++i) x.k[h][i] = u4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
-      x.ks[h] = x.vs[h] = f4{0, 0, 0, 0};
     }
+    x.ks[h] = *(const f4*)(a.KS + at + 4 * g);
+    x.vs[h] = *(const f4*)(a.VS + at + 4 * g);
   }
 }
 
@@ -144,18 +168,23 @@ __device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, const in
 // queries), probabilities as ZP (one, rounded by 2^-11 at most, where the result
 // is rounded by 2^-8 after it).
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
-__global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
   __shared__ float lo[kWaves][16][DP + 4];
   const int split = blockIdx.x, hkv = blockIdx.y / a.rowblocks, rb = blockIdx.y % a.rowblocks, b = blockIdx.z;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, g = l >> 4;
-  const int64_t ctx = min((int64_t)max(a.context[b], 0), a.capacity);
+  const int ctx = min(max(a.context[b], 0), a.capacity);
   const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
-  const int64_t total = min(ctx + drafted, a.capacity);
-  const int64_t per = (((total + a.splits - 1) / a.splits) + kWaves * kStep - 1) / (kWaves * kStep) * (kWaves * kStep);
-  const int64_t begin = split * per, end = min(total, begin + per);
+  const int total = min(ctx + drafted, a.capacity);
+  const int per = (((total + a.splits - 1) / a.splits) + kWaves * kStep - 1) / (kWaves * kStep) * (kWaves * kStep);
+  const int begin = split * per, end = min(total, begin + per);
   const int32_t* table = a.table + b * a.ldt;
+
+  Tokens<DP> x, y;
+  int tok = begin + w * kStep;
+  Entry e = look_up(a, table, tok, end), e2 = look_up(a, table, tok + kWaves * kStep, end);
+  if (tok < end) fetch(x, a, e, hkv, c, g);
 
   h8 q[QT][KS][ZQ];
   float qs[QT], m[QT], sum[QT];
@@ -163,17 +192,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
   f4 o[QT][NT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int r = (rb * QT + t) * 16 + c, tok = r / a.group, head = hkv * a.group + r % a.group;
+    const int r = (rb * QT + t) * 16 + c, tq = r / a.group, head = hkv * a.group + r % a.group;
     const bool live = r < a.rows;
-    const int64_t at = ((int64_t)b * a.width + tok) * a.ldq + (int64_t)head * a.dim;
-    float x[DP / 4];
+    const int64_t at = ((int64_t)b * a.width + tq) * a.ldq + (int64_t)head * a.dim;
+    float f[DP / 4];
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < DP / 4; ++i) {
-      const int d = g * (DP / 4) + i;
-      x[i] = live && d < a.dim ? load_as_float(a.Q, a.dt, at + d) : 0.0f;
-      top = max(top, mag(x[i]));
+    for (int s = 0; s < KS; ++s) {
+      const int d = g * (DP / 4) + 8 * s;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[8 * s + i] = 0.0f;
+      if (live && d < a.dim) load8_as(a.Q, a.dt, at + d, a.qwide, f + 8 * s);
     }
+#pragma unroll
+    for (int i = 0; i < DP / 4; ++i) top = max(top, mag(f[i]));
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     uint32_t e = min(top & 0x7f800000u, 253u << 23);
@@ -185,23 +217,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = x[8 * s + i] * down;
-        q[t][s][0][i] = (_Float16)y;
-        if constexpr (ZQ == 2) q[t][s][1][i] = (_Float16)(y - (float)q[t][s][0][i]);
+        const float v = f[8 * s + i] * down;
+        q[t][s][0][i] = (_Float16)v;
+        if constexpr (ZQ == 2) q[t][s][1][i] = (_Float16)(v - (float)q[t][s][0][i]);
       }
-    sees[t] = !live ? 0 : a.mask ? a.mask[(int64_t)b * a.width + tok] : ((uint64_t)2 << tok) - 1;
+    sees[t] = !live ? 0 : a.mask ? a.mask[(int64_t)b * a.width + tq] : ((uint64_t)2 << tq) - 1;
     m[t] = -INFINITY, sum[t] = 0;
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[t][j] = f4{0, 0, 0, 0};
   }
   float vref = 0x1p-120f;  // a power of two, at least the largest value scale so far
 
-  Tokens<DP> x, y;
-  int64_t tok = begin + w * kStep;
-  if (tok < end) fetch(y, a, table, hkv, tok, end, c, g);
-  for (; tok < end; tok += kWaves * kStep) {
-    x = y;
-    if (tok + kWaves * kStep < end) fetch(y, a, table, hkv, tok + kWaves * kStep, end, c, g);
+  auto step = [&](Tokens<DP>& x, int tok) {
     // scores
     f4 z[QT][2];
 #pragma unroll
@@ -235,7 +262,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int64_t p = tok + 16 * h + 4 * g + i;
+          const int p = tok + 16 * h + 4 * g + i;
           const bool in = x.there[h] && p < end;
 #pragma unroll
           for (int t = 0; t < QT; ++t) {
@@ -250,46 +277,54 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
         }
     }
     // the value scales' power of two
-    float vmax = 0;
+    float vmax = 0, fade = 1;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) vmax = fmaxf(vmax, x.vs[h][i]);
-    vmax = quad_max(vmax);
-    float vold = vref;
-    if (vmax > vref && vmax <= 0x1p126f) vref = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
+    if (__any(vmax > vref)) {
+      vmax = fminf(quad_max(vmax), 0x1p126f);
+      const float up = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
+      fade = vref * __uint_as_float((254u << 23) - __float_as_uint(up));
+      vref = up;
+    }
     const float vinv = __uint_as_float((254u << 23) - __float_as_uint(vref));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) x.vs[h] *= vinv;
     // probabilities
     h8 p[QT][ZP];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float top = m[t];
+      float top = -INFINITY;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float s = z[t][h][i] * x.ks[h][i];
-          top = fmaxf(top, edge && !((ok[t] >> (4 * h + i)) & 1) ? -INFINITY : s);
+          z[t][h][i] *= x.ks[h][i];
+          top = fmaxf(top, edge && !((ok[t] >> (4 * h + i)) & 1) ? -INFINITY : z[t][h][i]);
         }
-      top = quad_max(top);
-      const float base = top == -INFINITY ? 0.0f : top;
-      const float fade = __builtin_amdgcn_exp2f((m[t] - base) * qs[t]);
-      float part = 0;
+      float f = fade;
+      // the maximum of a query seldom moves after its first tokens
+      if (__any(top > m[t])) {
+        top = fmaxf(quad_max(top), m[t]);
+        const float base = top == -INFINITY ? 0.0f : top, d = __builtin_amdgcn_exp2f((m[t] - base) * qs[t]);
+        sum[t] *= d;
+        f *= d;
+        m[t] = top;
+      }
+      const float base = m[t] == -INFINITY ? 0.0f : m[t];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // the maximum is taken off before the query's scale comes in
-          float e = __builtin_amdgcn_exp2f((z[t][h][i] * x.ks[h][i] - base) * qs[t]);
-          float y = e * (x.vs[h][i] * vinv);
+          float e = __builtin_amdgcn_exp2f((z[t][h][i] - base) * qs[t]);
+          float y = e * x.vs[h][i];
           if (edge && !((ok[t] >> (4 * h + i)) & 1)) e = y = 0;
-          part += e;
+          sum[t] += e;
           p[t][0][4 * h + i] = (_Float16)y;
           if constexpr (ZP == 2) p[t][1][4 * h + i] = (_Float16)(y - (float)p[t][0][4 * h + i]);
         }
-      sum[t] = sum[t] * fade + part;
-      m[t] = top;
-      const float f = fade * (vold * vinv);
       if (__any(f != 1.0f)) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) o[t][j] *= f;
@@ -320,6 +355,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
           for (int j = 0; j < 4; ++j)
             o[t][4 * e + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], p[t][s], o[t][4 * e + j], 0, 0, 0);
     }
+  };
+  // the tokens of the step after this one are on their way, the table's entries
+  // of the one after that
+  constexpr int kStride = kWaves * kStep;
+  while (tok < end) {
+    e = look_up(a, table, tok + 2 * kStride, end);
+    if (tok + kStride < end) fetch(y, a, e2, hkv, c, g);
+    step(x, tok);
+    tok += kStride;
+    if (tok >= end) break;
+    e2 = look_up(a, table, tok + 2 * kStride, end);
+    if (tok + kStride < end) fetch(x, a, e, hkv, c, g);
+    step(y, tok);
+    tok += kStride;
   }
 
   // the waves' parts, in their order
@@ -363,12 +412,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree(TreeArgs a) {
         const int tk = r / a.group, head = hkv * a.group + r % a.group;
         const int64_t row = (int64_t)b * a.width + tk;
         const bool none = L == 0.0f || tk >= drafted;
-        const float inv = none ? 0.0f : 1.0f / L;
-        if (d0 < a.dim) {
+        const float inv = 1.0f / L;
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-            store_float(a.O, a.dt, row * a.ldo + (int64_t)head * a.dim + d0 + j, none ? 0.0f : v[j] * inv);
-        }
+        for (int j = 0; j < NT; ++j) v[j] = none ? 0.0f : v[j] * inv;
+        if (d0 < a.dim) store_as<NT>(a.O, a.dt, row * a.ldo + (int64_t)head * a.dim + d0, a.owide, v);
         if (a.lse && d0 == 0)
           a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
       } else {
@@ -402,22 +449,28 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   float L = 0, v[DP / 64];
 #pragma unroll
   for (int e = 0; e < DP / 64; ++e) v[e] = 0;
+#pragma clang loop unroll_count(8)
   for (int s = 0; s < a.splits; ++s) {
     const float ps = __shfl(ls, s), fs = __shfl(f, s);
-    if (ps == 0.0f) continue;
     L += ps * fs;
-    const float* p = a.part + (id * a.splits + s) * DP;
+    const float* p = a.part + (id * a.splits + s) * DP + (DP / 64) * l;
 #pragma unroll
-    for (int e = 0; e < DP / 64; ++e) v[e] += p[64 * e + l] * fs;
+    for (int e = 0; e < DP / 64; ++e) v[e] += ps == 0.0f ? 0.0f : p[e] * fs;  // an empty part is not written
   }
   const int tk = r / a.group, head = hkv * a.group + r % a.group;
   const int64_t row = (int64_t)b * a.width + tk;
   const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
   const bool none = L == 0.0f || tk >= drafted;
 #pragma unroll
-  for (int e = 0; e < DP / 64; ++e)
-    if (64 * e + l < a.dim)
-      store_float(a.O, a.dt, row * a.ldo + (int64_t)head * a.dim + 64 * e + l, none ? 0.0f : v[e] / L);
+  for (int e = 0; e < DP / 64; ++e) {
+    const int d = (DP / 64) * l + e;
+    const int64_t at = row * a.ldo + (int64_t)head * a.dim + d;
+    const float y = none ? 0.0f : v[e] / L;
+    if (d >= a.dim) continue;
+    if (a.dt == GPTQ2D_F32) ((float*)a.O)[at] = y;
+    else if (a.dt == GPTQ2D_F16) ((_Float16*)a.O)[at] = (_Float16)y;
+    else ((bf16*)a.O)[at] = (bf16)y;
+  }
   if (a.lse && l == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
 }
 
@@ -544,9 +597,10 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
   a.dt = dt, a.Q = Q, a.ldq = ldq;
   a.KC = (const uint8_t*)KC, a.VC = (const uint8_t*)VC, a.KS = KS, a.VS = VS;
   a.pages = pages, a.page = page_size, a.page16 = page_size / 16, a.magic = ((uint64_t)1 << 32) / a.page16 + 1;
-  a.table = table, a.ldt = ldt, a.capacity = table_width * page_size;
+  a.table = table, a.ldt = ldt, a.capacity = (int)(table_width * page_size);
   a.context = context, a.drafts = drafts, a.mask = masks;
   a.scale = scale * kLog2E;
+  a.qwide = wide_rows(Q, ldq, es), a.owide = wide_rows(O, ldo, es);
   a.O = O, a.ldo = ldo, a.lse = lse, a.part = (float*)workspace;
   const int tiles = query_tiles(rows, dim);
   a.rowblocks = (int)ceil_div(rows, 16 * tiles);
