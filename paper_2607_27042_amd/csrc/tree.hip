@@ -97,7 +97,6 @@ struct Tokens {
   u4 k[2][DP / 64];
   uint32_t v[2][4][DP / 64];
   f4 ks[2], vs[2];
-  bool there[2];
 };
 
 // The table's entries of a wave's next 32 tokens (uniform, looked up ahead of
@@ -119,22 +118,29 @@ __device__ __forceinline__ Entry look_up(const TreeArgs& a, const int32_t* table
   return r;
 }
 
-// Tokens that are not there are read from page 0 and masked later.
+// Tokens that are not there are read from page 0 and masked later. Past the end
+// of a vector any of it is read: there the query is 0 (keys) or the results are
+// not stored (values).
+__device__ __forceinline__ int64_t place(const TreeArgs& a, Entry e, int h, int hkv) {
+  return ((int64_t)max(e.page[h], 0) * a.kv + hkv) * a.page + e.off[h];
+}
 template <int DP>
-__device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, Entry e, int hkv, int c, int g) {
+__device__ __forceinline__ void fetch_keys(Tokens<DP>& x, const TreeArgs& a, Entry e, int hkv, int c, int g) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    x.there[h] = e.page[h] >= 0;
-    const int64_t at = ((int64_t)max(e.page[h], 0) * a.kv + hkv) * a.page + e.off[h];
-    const uint8_t* pk = a.KC + at * a.dim;
-    const uint8_t* pv = a.VC + at * a.dim;
+    const uint8_t* p = a.KC + place(a, e, h, hkv) * a.dim;
 #pragma unroll
     for (int i = 0; i < DP / 64; ++i) {
-      // past the end of a vector: any of it (the query is 0 there)
       const int d = g * (DP / 4) + 16 * i;
-      x.k[h][i] = *(const u4*)(pk + (uint32_t)(c * a.dim + (d < a.dim ? d : 0)));
+      x.k[h][i] = *(const u4*)(p + (uint32_t)(c * a.dim + (d < a.dim ? d : 0)));
     }
-    // past the end: any of it (the results are not stored)
+  }
+}
+template <int DP>
+__device__ __forceinline__ void fetch_values(Tokens<DP>& x, const TreeArgs& a, Entry e, int hkv, int c, int g) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint8_t* pv = a.VC + place(a, e, h, hkv) * a.dim;
     const int d = c * (DP / 16) < a.dim ? c * (DP / 16) : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -150,8 +156,15 @@ __device__ __forceinline__ void fetch(Tokens<DP>& x, const TreeArgs& a, Entry e,
         for (int j = 0; j < 4; ++j) x.v[h][i][j] = w[j];
       }
     }
-    x.ks[h] = *(const f4*)(a.KS + at + 4 * g);
-    x.vs[h] = *(const f4*)(a.VS + at + 4 * g);
+  }
+}
+template <int DP>
+__device__ __forceinline__ void fetch_scales(Tokens<DP>& x, const TreeArgs& a, Entry e, int hkv, int g) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t at = place(a, e, h, hkv) + 4 * g;
+    x.ks[h] = *(const f4*)(a.KS + at);
+    x.vs[h] = *(const f4*)(a.VS + at);
   }
 }
 
@@ -171,7 +184,7 @@ template <bool INT8, int DP, int QT, int ZQ, int ZP>
 __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
-  __shared__ float lo[kWaves][16][DP + 4];
+  __shared__ float lo[kWaves][16 * QT][DP + 4];
   const int split = blockIdx.x, hkv = blockIdx.y / a.rowblocks, rb = blockIdx.y % a.rowblocks, b = blockIdx.z;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, g = l >> 4;
   const int ctx = min(max(a.context[b], 0), a.capacity);
@@ -181,10 +194,15 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
   const int begin = split * per, end = min(total, begin + per);
   const int32_t* table = a.table + b * a.ldt;
 
-  Tokens<DP> x, y;
+  constexpr int kStride = kWaves * kStep;
+  Tokens<DP> x;
   int tok = begin + w * kStep;
-  Entry e = look_up(a, table, tok, end), e2 = look_up(a, table, tok + kWaves * kStep, end);
-  if (tok < end) fetch(x, a, e, hkv, c, g);
+  Entry now = look_up(a, table, tok, end), next = look_up(a, table, tok + kStride, end);
+  if (tok < end) {
+    fetch_keys(x, a, now, hkv, c, g);
+    fetch_scales(x, a, now, hkv, g);
+    fetch_values(x, a, now, hkv, c, g);
+  }
 
   h8 q[QT][KS][ZQ];
   float qs[QT], m[QT], sum[QT];
@@ -228,60 +246,80 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
   }
   float vref = 0x1p-120f;  // a power of two, at least the largest value scale so far
 
-  auto step = [&](Tokens<DP>& x, int tok) {
+  // Tokens are kept once: as soon as the keys of a step are widened, those of the
+  // next one are on their way into their registers, and likewise the values. (The
+  // last step fetches once more, from page 0: a branch around the loads would make
+  // the compiler wait for all of them at its end.)
+  for (; tok < end; tok += kStride) {
+    const Entry after = look_up(a, table, tok + 2 * kStride, end);
     // scores
-    f4 z[QT][2];
+    h8 kf[2][KS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      h8 kf[KS];
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const uint32_t w0 = x.k[h][s / 2][2 * (s & 1)], w1 = x.k[h][s / 2][2 * (s & 1) + 1];
         const h2 p0 = halves<INT8, false>(w0), p1 = halves<INT8, true>(w0);
         const h2 p2 = halves<INT8, false>(w1), p3 = halves<INT8, true>(w1);
-        kf[s] = h8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+        kf[h][s] = h8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
       }
+    fetch_keys(x, a, next, hkv, c, g);
+    f4 z[QT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        f4 acc = {0, 0, 0, 0};
+        z[t][h] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int e = ZQ - 1; e >= 0; --e)
 #pragma unroll
-          for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[s], q[t][s][e], acc, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[t][h][i] = acc[i];
+          for (int s = 0; s < KS; ++s)
+            z[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h][s], q[t][s][e], z[t][h], 0, 0, 0);
       }
-    }
-    const bool edge = tok + kStep > min(ctx, end) || !x.there[0] || !x.there[1];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) z[t][h] *= x.ks[h];
+    f4 vs[2] = {x.vs[0], x.vs[1]};
+    fetch_scales(x, a, next, hkv, g);
     // bit 4 h + i: token tok + 16 h + 4 g + i is seen by query t
     uint32_t ok[QT];
+    const bool edge = tok + kStep > min(ctx, end) || now.page[0] < 0 || now.page[1] < 0;
     if (edge) {
 #pragma unroll
       for (int t = 0; t < QT; ++t) ok[t] = 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        const int first = tok + 16 * h + 4 * g, past = first - ctx;
+        const uint32_t in = now.page[h] < 0 ? 0 : (1u << min(max(end - first, 0), 4)) - 1;
+        const uint32_t before = (1u << min(max(-past, 0), 4)) - 1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int p = tok + 16 * h + 4 * g + i;
-          const bool in = x.there[h] && p < end;
-#pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            const bool s = in && (p < ctx || ((sees[t] >> (p - ctx)) & 1));
-            ok[t] |= (uint32_t)s << (4 * h + i);
-          }
-          if (!in) {  // whatever lies there, it must not meet a zero probability
-            x.vs[h][i] = 0;
-#pragma unroll
-            for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
-          }
+        for (int t = 0; t < QT; ++t) {
+          const uint64_t tree = past >= 0 ? (past < 64 ? sees[t] >> past : 0) : past > -4 ? sees[t] << -past : 0;
+          ok[t] |= (in & (before | (uint32_t)tree)) << (4 * h);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // whatever lies there, it must not meet a zero probability
+          const uint32_t keep = -((in >> i) & 1);
+          vs[h][i] = __uint_as_float(__float_as_uint(vs[h][i]) & keep);
+#pragma unroll
+          for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] &= keep;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!((ok[t] >> (4 * h + i)) & 1)) z[t][h][i] = -INFINITY;
     }
     // the value scales' power of two
     float vmax = 0, fade = 1;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vmax = fmaxf(vmax, x.vs[h][i]);
+      for (int i = 0; i < 4; ++i) vmax = fmaxf(vmax, vs[h][i]);
     if (__any(vmax > vref)) {
       vmax = fminf(quad_max(vmax), 0x1p126f);
       const float up = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
@@ -290,22 +328,18 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
     }
     const float vinv = __uint_as_float((254u << 23) - __float_as_uint(vref));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) x.vs[h] *= vinv;
+    for (int h = 0; h < 2; ++h) vs[h] *= vinv;
     // probabilities
     h8 p[QT][ZP];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float top = -INFINITY;
+      float top = z[t][0][0];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          z[t][h][i] *= x.ks[h][i];
-          top = fmaxf(top, edge && !((ok[t] >> (4 * h + i)) & 1) ? -INFINITY : z[t][h][i]);
-        }
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, z[t][i >> 2][i & 3]);
       float f = fade;
-      // the maximum of a query seldom moves after its first tokens
-      if (__any(top > m[t])) {
+      // what the exponents are relative to moves when a score exceeds it by more
+      // than 2^10, which is seldom after a query's first tokens
+      if (__any((top - m[t]) * qs[t] > 10.0f)) {
         top = fmaxf(quad_max(top), m[t]);
         const float base = top == -INFINITY ? 0.0f : top, d = __builtin_amdgcn_exp2f((m[t] - base) * qs[t]);
         sum[t] *= d;
@@ -313,18 +347,27 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
         m[t] = top;
       }
       const float base = m[t] == -INFINITY ? 0.0f : m[t];
+      float y[8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < 8; ++i) {
+        // the maximum is taken off before the query's scale comes in
+        const float e = __builtin_amdgcn_exp2f((z[t][i >> 2][i & 3] - base) * qs[t]);
+        sum[t] += e;
+        y[i] = e * vs[i >> 2][i & 3];
+      }
+      if (edge) {  // a probability of 0 may have met a scale that is not finite
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // the maximum is taken off before the query's scale comes in
-          float e = __builtin_amdgcn_exp2f((z[t][h][i] - base) * qs[t]);
-          float y = e * x.vs[h][i];
-          if (edge && !((ok[t] >> (4 * h + i)) & 1)) e = y = 0;
-          sum[t] += e;
-          p[t][0][4 * h + i] = (_Float16)y;
-          if constexpr (ZP == 2) p[t][1][4 * h + i] = (_Float16)(y - (float)p[t][0][4 * h + i]);
+        for (int i = 0; i < 8; ++i) y[i] = (ok[t] >> i) & 1 ? y[i] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const h2 hi = __builtin_convertvector(fp2{y[i], y[i + 1]}, h2);
+        p[t][0][i] = hi[0], p[t][0][i + 1] = hi[1];
+        if constexpr (ZP == 2) {
+          const h2 lo = __builtin_convertvector(fp2{y[i] - (float)hi[0], y[i + 1] - (float)hi[1]}, h2);
+          p[t][1][i] = lo[0], p[t][1][i + 1] = lo[1];
         }
+      }
       if (__any(f != 1.0f)) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) o[t][j] *= f;
@@ -355,20 +398,8 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
           for (int j = 0; j < 4; ++j)
             o[t][4 * e + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], p[t][s], o[t][4 * e + j], 0, 0, 0);
     }
-  };
-  // the tokens of the step after this one are on their way, the table's entries
-  // of the one after that
-  constexpr int kStride = kWaves * kStep;
-  while (tok < end) {
-    e = look_up(a, table, tok + 2 * kStride, end);
-    if (tok + kStride < end) fetch(y, a, e2, hkv, c, g);
-    step(x, tok);
-    tok += kStride;
-    if (tok >= end) break;
-    e2 = look_up(a, table, tok + 2 * kStride, end);
-    if (tok + kStride < end) fetch(x, a, e, hkv, c, g);
-    step(y, tok);
-    tok += kStride;
+    fetch_values(x, a, next, hkv, c, g);
+    now = next, next = after;
   }
 
   // the waves' parts, in their order
@@ -378,35 +409,35 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
     m[t] *= qs[t];  // the same in every lane of a query
     if (g == 0) lm[w][16 * t + c] = m[t], ll[w][16 * t + c] = sum[t];
   }
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; j += 4)
+        *(f4*)&lo[w][16 * t + c][(4 * g + i) * NT + j] =
+            f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]} * vref;
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    {
-      float top = lm[0][16 * t + c];
-#pragma unroll
-      for (int i = 1; i < kWaves; ++i) top = fmaxf(top, lm[i][16 * t + c]);
-      const float f = vref * (top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - top));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) lo[w][c][(4 * g + i) * NT + j] = o[t][j][i] * f;
-    }
-    __syncthreads();
     const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * NT;
     const int r = (rb * QT + t) * 16 + qr;
     if (r < a.rows) {
-      float top = lm[0][16 * t + qr], L = 0;
+      float top = lm[0][16 * t + qr], L = 0, f[kWaves], v[NT];
 #pragma unroll
       for (int i = 1; i < kWaves; ++i) top = fmaxf(top, lm[i][16 * t + qr]);
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i)
-        L += ll[i][16 * t + qr] * (top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(lm[i][16 * t + qr] - top));
-      float v[NT];
+      for (int j = 0; j < NT; ++j) v[j] = 0;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        v[j] = lo[0][qr][d0 + j];
+      for (int i = 0; i < kWaves; ++i) {
+        f[i] = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(lm[i][16 * t + qr] - top);
+        L += ll[i][16 * t + qr] * f[i];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) v[j] += lo[i][qr][d0 + j];
+        for (int j = 0; j < NT; j += 4) {
+          const f4 s = *(const f4*)&lo[i][16 * t + qr][d0 + j];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[j + k] = fmaf(s[k], f[i], v[j + k]);
+        }
       }
       if (a.splits == 1) {
         const int tk = r / a.group, head = hkv * a.group + r % a.group;
@@ -428,50 +459,60 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
         if (d0 == 0) ml[2 * at] = top, ml[2 * at + 1] = L;
       }
     }
-    __syncthreads();
   }
 }
 
-// One wave per query: the splits' parts in their order.
+// One work group per query: each wave adds up every fourth split's part, eight
+// loads at a time, then the waves' sums are added, all in a fixed order.
 template <int DP>
-__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.seqs * a.kv * a.rows;
-  if (id >= all) return;
-  const int l = threadIdx.x & 63;
+__global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
+  __shared__ float lo[kWaves][DP];
+  const int64_t id = blockIdx.x, all = (int64_t)a.seqs * a.kv * a.rows;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const int64_t bh = id / a.rows;
   const int r = (int)(id - bh * a.rows), hkv = (int)(bh % a.kv), b = (int)(bh / a.kv);
   const float* ml = a.part + all * a.splits * DP + 2 * id * a.splits;
   const float ms = l < a.splits ? ml[2 * l] : -INFINITY, ls = l < a.splits ? ml[2 * l + 1] : 0.0f;
+  const float* part = a.part + id * a.splits * DP + (DP / 64) * l;
+  float v[DP / 64], x[8][DP / 64];
+#pragma unroll
+  for (int e = 0; e < DP / 64; ++e) v[e] = 0;
   float top = ms;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
-  float L = 0, v[DP / 64];
+  const float f = ls == 0.0f ? 0.0f : top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
+  float L = ls * f;
 #pragma unroll
-  for (int e = 0; e < DP / 64; ++e) v[e] = 0;
-#pragma clang loop unroll_count(8)
-  for (int s = 0; s < a.splits; ++s) {
-    const float ps = __shfl(ls, s), fs = __shfl(f, s);
-    L += ps * fs;
-    const float* p = a.part + (id * a.splits + s) * DP + (DP / 64) * l;
+  for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
+  for (int s0 = w; s0 < a.splits; s0 += 8 * kWaves) {
 #pragma unroll
-    for (int e = 0; e < DP / 64; ++e) v[e] += ps == 0.0f ? 0.0f : p[e] * fs;  // an empty part is not written
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < DP / 64; ++e) x[u][e] = part[(int64_t)min(s0 + u * kWaves, a.splits - 1) * DP + e];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int s = s0 + u * kWaves;
+      const float fs = s < a.splits ? __shfl(f, s) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < DP / 64; ++e) v[e] += fs == 0.0f ? 0.0f : x[u][e] * fs;  // an empty part is not written
+    }
   }
+#pragma unroll
+  for (int e = 0; e < DP / 64; ++e) lo[w][(DP / 64) * l + e] = v[e];
+  __syncthreads();
+  const int d = threadIdx.x;
   const int tk = r / a.group, head = hkv * a.group + r % a.group;
   const int64_t row = (int64_t)b * a.width + tk;
   const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
   const bool none = L == 0.0f || tk >= drafted;
-#pragma unroll
-  for (int e = 0; e < DP / 64; ++e) {
-    const int d = (DP / 64) * l + e;
+  if (d < a.dim) {
+    const float y = none ? 0.0f : (lo[0][d] + lo[1][d] + lo[2][d] + lo[3][d]) / L;
     const int64_t at = row * a.ldo + (int64_t)head * a.dim + d;
-    const float y = none ? 0.0f : v[e] / L;
-    if (d >= a.dim) continue;
     if (a.dt == GPTQ2D_F32) ((float*)a.O)[at] = y;
     else if (a.dt == GPTQ2D_F16) ((_Float16*)a.O)[at] = (_Float16)y;
     else ((bf16*)a.O)[at] = (bf16)y;
   }
-  if (a.lse && l == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
+  if (a.lse && threadIdx.x == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
 }
 
 // bits of a token's ancestors and itself; a parent that is not an earlier token is none
@@ -499,11 +540,14 @@ int query_tiles(int rows, int dim) {
   return rows <= 16 ? 1 : rows <= 32 ? 2 : most;
 }
 
-// Parts that a sequence's tokens are split into: as many as give the device
-// about four work groups a compute unit.
+// Parts that a sequence's tokens are split into: as many as give the device two
+// work groups a compute unit, which is what the registers let run at once. At
+// 256 / 512 / 1024 / 2048 work groups: 16 trees of 13 over up to 8192 tokens
+// (dim 64) 75 / 58 / 65 / 76 us, 32 trees of 8 over up to 32768 (dim 128) 310 /
+// 311 / 312 / 300 us, one token over 4096 10.7 / 11.5 / 11.4 / 11.5 us.
 int split_count(int64_t seqs, int rows, int kv, int dim) {
   const int64_t groups = seqs * kv * ceil_div(rows, 16 * query_tiles(rows, dim));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(1024, groups)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(512, groups)));
 }
 
 size_t part_bytes(int64_t seqs, int rows, int kv, int dim) {
@@ -522,7 +566,7 @@ void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
   else if constexpr (DP != 256) launch<INT8, DP, 4, ZQ, ZP>(a, s);
   if (a.splits > 1) {
     const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
-    hipLaunchKernelGGL(k_tree_join<DP>, dim3((unsigned)ceil_div(all, 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_tree_join<DP>, dim3((unsigned)all), dim3(64 * kWaves), 0, s, a);
   }
 }
 template <bool INT8, int DP>
