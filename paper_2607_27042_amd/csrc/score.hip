@@ -18,7 +18,8 @@ constexpr int kThreads = 256;
 constexpr int kVec = 16;                    // elements of a thread and step
 constexpr int kChunk = kThreads * kVec;     // of a work group
 constexpr int kMaxTop = 64;
-constexpr int kHeld = kThreads;             // candidates kept between steps
+constexpr int kHeld = kThreads;             // candidates that are ranked at once
+constexpr int kSpare = 32;                  // candidates beyond the best that wait for that
 constexpr int kMaxParts = 64;               // parts of a row
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2E = 1.44269504088896341f;
@@ -53,33 +54,46 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 
 // The best of a work group's candidates, with room for a whole step's.
 struct Pool {
-  uint64_t key[kHeld + kChunk];
-  uint64_t best[kThreads];
+  alignas(16) uint64_t key[kHeld + kChunk];
+  alignas(16) uint64_t best[kThreads];
   uint64_t limit;  // candidates below it are none of the best
   int count;
 };
 
-// Rank of each thread's key among the group's (0 for the largest); equal keys
-// (0: none) take their thread's order.
-__device__ __forceinline__ int rank_in(Pool& p, uint64_t mine) {
-  const int t = threadIdx.x;
-  p.best[t] = mine;
+// Number of keys above the thread's among the first n of the group's; n <=
+// kThreads, past n keys are 0.
+template <class K>
+__device__ __forceinline__ int rank_in(Pool& p, K mine, int n) {
+  K* best = (K*)p.best;
+  best[threadIdx.x] = mine;
   __syncthreads();
   int r = 0;
-#pragma unroll 8
-  for (int i = 0; i < kThreads; ++i) {
-    const uint64_t k = p.best[i];
-    r += k > mine || (k == mine && i < t);
+#pragma unroll 2
+  for (int i = 0; i < n; i += 8) {
+    K k[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = best[i + j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r += k[j] > mine;
   }
   return r;
 }
 
-// Brings the candidates down to kHeld, keeping the `top` best: the top-th of
-// the threads' largest is a limit that at least `top` candidates reach, and at
-// most top / 256 of them all (a quarter) lie above it.
-__device__ __forceinline__ void shrink(Pool& p, int top) {
-  const int t = threadIdx.x;
+// A first limit that at least `top` elements reach: the top-th of the threads'
+// largest (their low bits give way to the thread's number, so that no two are
+// equal and the limit is no higher).
+__device__ __forceinline__ void first_limit(Pool& p, uint32_t most, int top) {
+  const uint32_t mine = most == 0 ? 0 : (most & ~255u) | threadIdx.x;
+  const int r = rank_in(p, mine, kThreads);
+  if (r == top - 1) p.limit = (uint64_t)(mine & ~255u) << 32;
   __syncthreads();
+}
+
+// Keeps the `top` best candidates, in order, and makes the last of them the
+// limit. While there are more than kHeld, the top-th of the threads' largest is
+// one: candidates of `top` threads, a quarter at most, lie above it.
+__device__ __forceinline__ void keep_best(Pool& p, int top) {
+  const int t = threadIdx.x;
   while (p.count > kHeld) {
     const int n = p.count;
     uint64_t mine[(kHeld + kChunk) / kThreads], most = 0;
@@ -88,8 +102,7 @@ __device__ __forceinline__ void shrink(Pool& p, int top) {
       mine[i] = t + i * kThreads < n ? p.key[t + i * kThreads] : 0;
       most = max(most, mine[i]);
     }
-    const int r = rank_in(p, most);
-    if (r == top - 1) p.limit = most;
+    if (rank_in(p, most, kThreads) == top - 1) p.limit = most;
     if (t == 0) p.count = 0;
     __syncthreads();
     const uint64_t limit = p.limit;
@@ -98,15 +111,13 @@ __device__ __forceinline__ void shrink(Pool& p, int top) {
       if (mine[i] >= limit && mine[i] != 0) p.key[atomicAdd(&p.count, 1)] = mine[i];
     __syncthreads();
   }
-}
-
-// The thread's rank-th best key ends up at out[rank] for rank < top.
-template <class F>
-__device__ __forceinline__ void final_ranks(Pool& p, int top, F&& out) {
-  shrink(p, top);
-  const uint64_t mine = (int)threadIdx.x < p.count ? p.key[threadIdx.x] : 0;
-  const int r = rank_in(p, mine);
-  if (r < top) out(r, mine);
+  const int n = p.count;
+  const uint64_t mine = t < n ? p.key[t] : 0;
+  const int r = rank_in(p, mine, n);
+  if (mine != 0 && r < top) p.key[r] = mine;
+  if (mine != 0 && r == top - 1) p.limit = mine;
+  if (t == 0) p.count = min(n, top);
+  __syncthreads();
 }
 
 // Running sums of a thread or more over logits of which m is the largest:
@@ -141,23 +152,24 @@ __device__ __forceinline__ Sums wave_join(Sums s, float a2) {
   return s;
 }
 
-// Sixteen elements from index e on of a row of n; those outside are -inf
-// (e may be negative: the row is read from the 16-byte boundary before it on).
+// A thread's elements of one step: kVec of them in pieces of 16 bytes, the
+// pieces of a group side by side. Element j of the thread is element
+// step + (j / W) kThreads W + t W + j % W of the row.
 template <class T>
-__device__ __forceinline__ void load16(const T* x, int64_t e, int64_t n, float v[kVec]) {
-  constexpr int W = 16 / sizeof(T);
+struct Piece {
+  static constexpr int W = 16 / sizeof(T), N = kVec / W;
+  struct alignas(16) V { T v[W]; };
+};
+template <class T>
+__device__ __forceinline__ int64_t index_of(int64_t step, int j) {
+  constexpr int W = Piece<T>::W;
+  return step + (j / W) * kThreads * W + (int)threadIdx.x * W + j % W;
+}
+template <class T>
+__device__ __forceinline__ void load_whole(const T* x, int64_t step, typename Piece<T>::V raw[Piece<T>::N]) {
 #pragma unroll
-  for (int i = 0; i < kVec; i += W) {
-    if (e + i >= 0 && e + i + W <= n) {
-      struct alignas(16) V { T v[W]; };
-      const V a = *(const V*)(x + e + i);
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[i + j] = (float)a.v[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[i + j] = e + i + j >= 0 && e + i + j < n ? (float)x[e + i + j] : -INFINITY;
-    }
-  }
+  for (int i = 0; i < Piece<T>::N; ++i)
+    raw[i] = *(const typename Piece<T>::V*)(x + index_of<T>(step, i * Piece<T>::W));
 }
 
 struct Out {
@@ -183,6 +195,15 @@ __device__ __forceinline__ float target_logprob(const ScoreArgs& a, int64_t row,
   return logprob_of((float)((const T*)a.X)[row * a.ldx + y] * a.a, lse);
 }
 
+__device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t row, float lse) {
+  keep_best(p, a.top);
+  const int t = threadIdx.x;
+  if (t >= a.top) return;
+  const uint64_t k = p.key[t];
+  a.ids[row * a.top + t] = (int32_t)key_index(k);
+  a.tops[row * a.top + t] = logprob_of(key_value(k) * a.a, lse);
+}
+
 // One work group per part of a row, one pass. Each thread sums relative to its
 // own largest logit so far, which moves rarely after the first steps. At the end
 // s1 >= 1 and s2 <= 0, so the entropy log s1 - s2 / s1 cancels nothing.
@@ -191,43 +212,57 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   __shared__ Sums wave[kThreads / 64];
   __shared__ typename std::conditional<TOP, Pool, int>::type pool;
   const int t = threadIdx.x;
-  const int64_t row = blockIdx.x / a.parts;
-  const int part = (int)(blockIdx.x - row * a.parts);
+  const int row32 = blockIdx.x / (uint32_t)a.parts, part = blockIdx.x - row32 * a.parts;
+  const int64_t row = row32;
   const T* x = (const T*)a.X + row * a.ldx;
   const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));  // elements from the boundary before the row to it
-  const int64_t steps = (a.vocab + lead + kChunk - 1) / kChunk;
-  const int64_t first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
+  const int steps = (a.vocab + lead + kChunk - 1) / kChunk;
+  const int first = (uint32_t)(steps * part) / (uint32_t)a.parts, last = (uint32_t)(steps * (part + 1)) / (uint32_t)a.parts;
   Sums s{-INFINITY, 0.0f, 0.0f};
   if constexpr (TOP) {
     if (t == 0) pool.count = 0, pool.limit = 0;
     __syncthreads();
   }
-  float next[kVec];
-  if (first < last) load16(x, first * kChunk + t * kVec - lead, a.vocab, next);
-  for (int64_t c = first; c < last; ++c) {
+  // the steps inside the row are loaded whole, one ahead; the first and the last
+  // may reach past it, and are loaded element by element
+  const int inner = lead > 0 ? 1 : 0, outer = (a.vocab + lead) / kChunk - 1;
+  typename Piece<T>::V raw[Piece<T>::N];
+  const bool any = inner <= outer;
+  auto ahead = [&](int c) { load_whole(x, (int64_t)max(inner, min(c, outer)) * kChunk - lead, raw); };
+  if (any) ahead(first);
+  for (int c = first; c < last; ++c) {
     float v[kVec];
+    const int64_t at = (int64_t)c * kChunk - lead;
+    if (any) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = next[i];
-    const int64_t at = c * kChunk + t * kVec - lead;
-    if (c + 1 < last) load16(x, at + kChunk, a.vocab, next);
+      for (int i = 0; i < kVec; ++i) v[i] = (float)raw[i / Piece<T>::W].v[i % Piece<T>::W];
+      ahead(c + 1);
+    }
+    if (c < inner || c > outer) {
+      // (what lies outside is loaded from the row's ends, so that no load waits for a branch)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = (float)x[max((int64_t)0, min(index_of<T>(at, i), (int64_t)a.vocab - 1))];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int64_t e = index_of<T>(at, i);
+        v[i] = e >= 0 && e < a.vocab ? v[i] : -INFINITY;
+      }
+    }
     float m = v[0];
 #pragma unroll
     for (int i = 1; i < kVec; ++i) m = fmaxf(m, v[i]);
-    float low = v[0];
-#pragma unroll
-    for (int i = 1; i < kVec; ++i) low = fminf(low, v[i]);
     if (m > s.m) move_to(s, m, a.a2);
-    bool odd = false;  // a NaN, which maxima drop
-    if (low > -1e37f && s.m < 1e37f) {
-      // differences are finite; a NaN enters the sums by itself
+    const Sums old = s;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const float d = v[i] - s.m, e = __builtin_amdgcn_exp2f(d * a.a2);
-        s.s1 += e;
-        s.s2 = fmaf(e, d, s.s2);
-      }
-      odd = s.s1 != s.s1;
-    } else {
+    for (int i = 0; i < kVec; ++i) {
+      const float d = v[i] - s.m, e = __builtin_amdgcn_exp2f(d * a.a2);
+      s.s1 += e;
+      s.s2 = fmaf(e, d, s.s2);
+    }
+    bool odd = false;  // a NaN, which maxima drop
+    if (!(fabsf(s.s2) < 1e37f)) {
+      // a difference of -inf (0 times it is NaN), or a NaN: once more with care
+      s = old;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         odd |= v[i] != v[i];
@@ -241,25 +276,28 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
     }
     if constexpr (TOP) {
       if (c == first) {
-        // the limit of the start: the top-th of the threads' largest
-        uint64_t most = 0;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          if (at + i >= 0 && at + i < a.vocab) most = max(most, key_of(v[i], (uint32_t)(at + i)));
-        if (rank_in(pool, most) == a.top - 1) pool.limit = most;
-        __syncthreads();
-      }
-      const uint64_t limit = pool.limit;
-      const uint32_t lo = (uint32_t)(limit >> 32);
-      if (odd || order_of(m) >= lo) {
+        uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-          const uint64_t k = key_of(v[i], (uint32_t)(at + i));
-          if (k >= limit && at + i >= 0 && at + i < a.vocab) pool.key[atomicAdd(&pool.count, 1)] = k;
+          const int64_t e = index_of<T>(at, i);
+          if (e >= 0 && e < a.vocab) most = max(most, order_of(v[i]));
+        }
+        first_limit(pool, most, a.top);
+      }
+      const uint64_t limit = pool.limit;
+      const float least = key_value(limit);  // NaN: of the start, or NaN themselves
+      if (odd || !(m < least)) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          if (v[i] < least) continue;
+          const int64_t e = index_of<T>(at, i);
+          const uint64_t k = key_of(v[i], (uint32_t)e);
+          if (k >= limit && e >= 0 && e < a.vocab) pool.key[atomicAdd(&pool.count, 1)] = k;
         }
       }
       __syncthreads();
-      if (pool.count > kHeld) shrink(pool, a.top);
+      // a limit that keeps up spares the threads most of these
+      if (pool.count > a.top + kSpare) keep_best(pool, a.top);
       __syncthreads();
     }
   }
@@ -269,8 +307,11 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   s = join(join(wave[0], wave[1], a.a2), join(wave[2], wave[3], a.a2), a.a2);
   if (a.parts > 1) {
     if (t == 0) ((f4*)a.stat)[blockIdx.x] = f4{s.m, s.s1, s.s2, 0.0f};
-    if constexpr (TOP)
-      final_ranks(pool, a.top, [&](int r, uint64_t k) { a.keys[(int64_t)blockIdx.x * a.top + r] = k; });
+    if constexpr (TOP) {
+      keep_best(pool, a.top);
+      // a part of a step's remainder may have fewer
+      if (t < a.top) a.keys[(int64_t)blockIdx.x * a.top + t] = t < pool.count ? pool.key[t] : 0;
+    }
     return;
   }
   const Out o = finish(a, s);
@@ -279,11 +320,7 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
     a.entropy[row] = o.entropy;
     a.logprob[row] = target_logprob<T>(a, row, o.lse);
   }
-  if constexpr (TOP)
-    final_ranks(pool, a.top, [&](int r, uint64_t k) {
-      a.ids[row * a.top + r] = (int32_t)key_index(k);
-      a.tops[row * a.top + r] = logprob_of(key_value(k) * a.a, o.lse);
-    });
+  if constexpr (TOP) put_best(pool, a, row, o.lse);
 }
 
 // One work group per row: its parts' sums, and the best of their best.
@@ -309,10 +346,8 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
     const int n = a.parts * a.top;  // at most kMaxParts kMaxTop = kChunk
     if (t == 0) pool.count = n, pool.limit = 0;
     for (int i = t; i < n; i += kThreads) pool.key[i] = a.keys[row * n + i];
-    final_ranks(pool, a.top, [&](int r, uint64_t k) {
-      a.ids[row * a.top + r] = (int32_t)key_index(k);
-      a.tops[row * a.top + r] = logprob_of(key_value(k) * a.a, o.lse);
-    });
+    __syncthreads();
+    put_best(pool, a, row, o.lse);
   }
 }
 
@@ -333,8 +368,8 @@ struct GradArgs {
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   constexpr int W = 16 / sizeof(T);
-  const int64_t row = blockIdx.x / a.parts;
-  const int part = (int)(blockIdx.x - row * a.parts);
+  const int row32 = blockIdx.x / (uint32_t)a.parts, part = blockIdx.x - row32 * a.parts;
+  const int64_t row = row32;
   const T* x = (const T*)a.X + row * a.ldx;
   T* d = (T*)a.D + row * a.ldd;
   const float lse = a.lse[row];
@@ -374,9 +409,9 @@ __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
 }
 
 // Parts of a row: as many as give the device about four work groups a compute
-// unit, but no part of less than two steps.
+// unit, each of one step at least.
 int part_count(int64_t rows, int64_t vocab) {
-  const int64_t want = ceil_div(1024, rows), room = std::max<int64_t>(1, vocab / (2 * kChunk));
+  const int64_t want = ceil_div(1024, rows), room = ceil_div(vocab, kChunk);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, room, kMaxParts}));
 }
 
