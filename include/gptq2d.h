@@ -267,7 +267,8 @@ gptq2d_status gptq2d_round_batched_check(const void* workspace, void* stream);
  * them). Blocks are 1 x 128 ("rows": the scale of block b of row r at
  * S[b * lds + r], lds >= rows) or 128 x 128 ("tiles": S[(r / 128) * lds +
  * c / 128], lds >= ceil(cols / 128)); the last block of a row or column of
- * blocks may be short. All sizes lie in [1, 2^24], a matrix in 2^37 entries.
+ * blocks may be short. All sizes lie in [1, 2^22], leading dimensions of codes in
+ * 2^23, a matrix in 2^37 entries.
  * ------------------------------------------------------------------------- */
 
 /* Quantises X (rows x cols, F32, F16 or BF16) to e4m3 blocks of block_rows (1
