@@ -1,7 +1,6 @@
 // Matrices in eight-bit floating point (e4m3) with a 32-bit scale for each
 // block of 128 values: the quantiser and the product
 //   C[m][n] = sum_b SA[b][m] SB[b][n] sum_{k in block b} A[m][k] B[n][k].
-#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -11,6 +10,9 @@ namespace g2d {
 namespace {
 
 constexpr int kBlock = 128;
+// rows that the product quantises by itself: at 4096 x 4096 1 / 2 / 4 rows took 5.3 /
+// 6.6 / 8.1 us, against 7.8 us after a launch of the quantiser
+constexpr int kFusedRows = 2;
 
 // ---------------------------------------------------------------------------
 // Quantiser
@@ -171,8 +173,9 @@ struct ProductArgs {
   int64_t ldw;
   const float* SW;    // ROWS: [block][n], otherwise [n / 128][block]
   int64_t ldsw;
-  const uint8_t* X;   // M x K
+  const void* X;      // M x K: codes (unless the kernel quantises by itself)
   int64_t ldx;
+  bool pow2;          // what it quantises has scales of powers of two
   const float* SX;    // [block][m]
   int64_t ldsx;
   void* Y;
@@ -266,8 +269,8 @@ __device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
     if constexpr (sizeof(T) == 4) {
       *(f4*)p = v;
     } else {
-      struct alignas(8) V { T v[4]; };
-      *(V*)p = V{{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+      typedef T V __attribute__((ext_vector_type(4)));
+      *(u2*)p = __builtin_bit_cast(u2, V{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
     }
   } else {
 #pragma unroll
@@ -296,7 +299,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   int bn, bm;
   tile_of(blockIdx.x, gridDim.x, tn, tm, bn, bm);
   const int n0 = bn * BN, m0 = bm * BM;
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, g = l >> 4;
   const int wn = (w % WN) * (BN / WN), wm = (w / WN) * (BM / WM);
   const int nb = (a.K + kBlock - 1) / kBlock;
   const int b0 = (int)((int64_t)nb * blockIdx.y / a.splits), b1 = (int)((int64_t)nb * (blockIdx.y + 1) / a.splits);
@@ -308,12 +311,13 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   Stage<BN, THREADS> gw;
   Stage<BM, THREADS> gx;
   gw.init(a.W, a.ldw, n0, a.N);
-  gx.init(a.X, a.ldx, m0, a.M);
-  const bool xs = !ROWS || threadIdx.x < BM;
-  const float* ps = xs ? a.SX + min(m0 + (int)threadIdx.x % BM, a.M - 1) : a.SW + min(n0 + (int)threadIdx.x - BM, a.N - 1);
+  gx.init((const uint8_t*)a.X, a.ldx, m0, a.M);
+  const bool xs = !ROWS || w < BM / 64;  // (whole waves)
+  const float* ps = xs ? a.SX : a.SW;
   const int64_t psl = xs ? a.ldsx : a.ldsw;
+  const uint32_t pse = xs ? min(m0 + (int)threadIdx.x % BM, a.M - 1) : min(n0 + (int)threadIdx.x - BM, a.N - 1);
   auto scales = [&](int b, float* ms) {
-    __builtin_amdgcn_global_load_lds((const void*)(ps + b * psl), (lds_void*)(ms + (threadIdx.x & ~63)), 4, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(ps + b * psl + pse), (lds_void*)(ms + (threadIdx.x & ~63)), 4, 0, 0);
   };
   // the i-th of `parts` shares of a whole block's loads
   constexpr int LOADS = Stage<BN, THREADS>::N + Stage<BM, THREADS>::N;
@@ -438,57 +442,136 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   }
 }
 
+// largest over the wave, in every lane
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xf, 0xf, true));  // rows of 16 rotated by 1, 2, 4, 8
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true));
+  const u2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const u2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
+}
+
 // Few rows (M <= 16 TM): the weights are read once, straight into the
 // instruction's registers, 16 rows a work group; its eight waves take every
-// eighth block of 128 and add up in LDS in the order of the waves.
-template <class T, int TM, bool ROWS, bool EXACT>
+// eighth block of 128, the loads of four of them at once, and add up in LDS in
+// the order of the waves.
+// FUSED (rows of X, at least M; 0: X is codes): X comes as it is, and each wave
+// quantises the blocks it takes, two values a lane (K and ldx are even), through
+// LDS of its own. Every work group does that for itself, which for few rows costs
+// less than a launch before this one.
+template <class T, int TM, bool ROWS, bool EXACT, int FUSED>
 __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
+  constexpr int U = 4;
   __shared__ f4 sum[8][TM][64];
-  const int n0 = blockIdx.x * 16, w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  __shared__ __align__(16) uint8_t own[FUSED ? 8 : 1][U][FUSED ? FUSED : 1][kBlock];
+  const int n0 = blockIdx.x * 16, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nb = (a.K + kBlock - 1) / kBlock;
   const uint8_t* pw = a.W + (int64_t)min(n0 + c, a.N - 1) * a.ldw;
   f4 acc[TM];
 #pragma unroll
   for (int j = 0; j < TM; ++j) acc[j] = f4{0, 0, 0, 0};
-  for (int b = w; b < nb; b += 8) {
+  // pieces 2 g and 2 g + 1 of a row's block; those past the end of the row are
+  // read from the block's start, and masked once they are there
+  auto load = [&](const uint8_t* row, int b) {
+    const uint8_t* p = row + b * kBlock;
     const int left = a.K - b * kBlock;
-    auto load = [&](const uint8_t* p) {  // the row's codes from 32 g on
-      u4 lo, hi;
-      p += b * kBlock;
-      if (left >= kBlock) {
-        lo = *(const u4*)(p + 32 * g), hi = *(const u4*)(p + 32 * g + 16);
-      } else {
-        lo = tail16(p, 2 * g, left), hi = tail16(p, 2 * g + 1, left);
-      }
-      return __builtin_bit_cast(i8v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    const i8v fw = load(pw);
-    f4 sw;
-    if constexpr (ROWS) {
+    const u4 lo = *(const u4*)(p + (32 * g < left ? 32 * g : 0)), hi = *(const u4*)(p + (32 * g + 16 < left ? 32 * g + 16 : 0));
+    return __builtin_bit_cast(i8v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto mask = [&](i8v& v, int b) {
+    const int left = a.K - b * kBlock - 32 * g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sw[e] = a.SW[b * a.ldsw + min(n0 + 4 * g + e, a.N - 1)];
-    } else {
-      const float u = a.SW[(int64_t)(n0 / kBlock) * a.ldsw + b];
-      sw = f4{u, u, u, u};
+    for (int i = 0; i < 8; ++i) {
+      const int keep = min(max(left - 4 * i, 0), 4);
+      v[i] &= keep == 4 ? -1 : (1 << (8 * keep)) - 1;
     }
-    h8 hw[4];
-    if constexpr (EXACT) widen(fw, hw);
+  };
+  for (int b0 = w; b0 < nb; b0 += 8 * U) {
+    i8v fw[U], fx[U][TM];
+    f4 sw[U];
+    struct alignas(2 * sizeof(T)) Pair { T v[2]; };
+    Pair raw[U][FUSED ? FUSED : 1];
+    float sx[U][TM];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int m = min(16 * j + c, a.M - 1);
-      const i8v fx = load(a.X + (int64_t)m * a.ldx);
-      const float sx = a.SX[b * a.ldsx + m];
-      f4 p = {0, 0, 0, 0};
-      if constexpr (EXACT) {
-        h8 hx[4];
-        widen(fx, hx);
+    for (int u = 0; u < U; ++u) {
+      const int b = min(b0 + 8 * u, nb - 1);
+      fw[u] = load(pw, b);
+      if constexpr (ROWS) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[k], hx[k], p, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) sw[u][e] = a.SW[b * a.ldsw + min(n0 + 4 * g + e, a.N - 1)];
       } else {
-        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fx, p, 0, 0, 0, 0, 0, 0);
+        const float v = a.SW[(int64_t)(n0 / kBlock) * a.ldsw + b];
+        sw[u] = f4{v, v, v, v};
       }
+      if constexpr (FUSED) {
+        const int k = min(b * kBlock + 2 * l, a.K - 2);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[e] * sw[e], sx, acc[j][e]);
+        for (int m = 0; m < FUSED; ++m)
+          raw[u][m] = *(const Pair*)((const T*)a.X + (int64_t)min(m, a.M - 1) * a.ldx + k);
+      } else {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+          const int m = min(16 * j + c, a.M - 1);
+          fx[u][j] = load((const uint8_t*)a.X + (int64_t)m * a.ldx, b);
+          sx[u][j] = a.SX[b * a.ldsx + m];
+        }
+      }
+    }
+    if constexpr (FUSED) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = min(b0 + 8 * u, nb - 1) * kBlock + 2 * l < a.K;
+#pragma unroll
+        for (int m = 0; m < FUSED; ++m) {
+          if (m >= a.M) break;
+          const float x = in ? (float)raw[u][m].v[0] : 0.0f, y = in ? (float)raw[u][m].v[1] : 0.0f;
+          const uint32_t top = wave_max(max(mag(x), mag(y)));
+          const float s = block_scale(top, 1.0f / kTopE4M3, a.pow2), r = 1.0f / s;
+          const uint32_t q = bad_amax(top) ? 0 : code4<false>(x * r, y * r, 0.0f, 0.0f);
+          *(uint16_t*)&own[w][u][m][2 * l] = (uint16_t)q;
+          if (m == 0 || m == min(c, a.M - 1)) sx[u][0] = s;
+        }
+      }
+      // (the wave reads what it wrote itself: LDS keeps its order)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const u4* p = (const u4*)&own[w][u][min(c, a.M - 1)][32 * g];
+        const u4 lo = p[0], hi = p[1];
+        fx[u][0] = __builtin_bit_cast(i8v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int b = b0 + 8 * u;
+      if (b >= nb) break;
+      if ((b + 1) * kBlock > a.K) {
+        mask(fw[u], b);
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+          if (!FUSED) mask(fx[u][j], b);
+      }
+      h8 hw[4];
+      if constexpr (EXACT) widen(fw[u], hw);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) {
+        f4 p = {0, 0, 0, 0};
+        if constexpr (EXACT) {
+          h8 hx[4];
+          widen(fx[u][j], hx);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[k], hx[k], p, 0, 0, 0);
+        } else {
+          p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[u], fx[u][j], p, 0, 0, 0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[e] * sw[u][e], sx[u][j], acc[j][e]);
+      }
     }
   }
 #pragma unroll
@@ -515,14 +598,24 @@ __global__ __launch_bounds__(256) void k_join(ProductArgs a) {
   }
 }
 
-// Which kernel and how many parts of K (the same for the workspace's size and the launch)
+// Which kernel (edge of a work group's tile; 16: few rows) and how many parts of K
+// (the same for the workspace's size and the launch).
 struct Plan { int edge; int splits; };
 Plan plan(int64_t M, int64_t N, int64_t K) {
-  if (M <= 64) return {16, 1};
+  if (M <= 32) return {16, 1};
   const int64_t nb = ceil_div(K, kBlock);
-  if (ceil_div(M, 256) * ceil_div(N, 256) >= (getenv("BIG") ? atoi(getenv("BIG")) : 200)) return {256, 1};
-  const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles, nb / 4, 16}));
+  auto tiles = [&](int64_t e) { return ceil_div(M, e) * ceil_div(N, e); };
+  // A 256 x 256 tile has a compute unit to itself, two of 128 x 128 share one; a
+  // round of them takes 65 and 39 us at K = 4096. 8192 x 11008: 6 rounds of 388 us
+  // against 11 of 430 us; 2047 x 4096 at K = 11008: 253 us (half the units idle)
+  // against 132 us.
+  if (5 * ceil_div(tiles(256), 256) <= 3 * ceil_div(tiles(128), 512)) return {256, 1};
+  // tiles of 128 do not give every second unit one: 64 x 64
+  if (tiles(128) < 128 && tiles(64) <= 256) {
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles(64), nb / 8, 16}));
+    return {64, (int)splits};
+  }
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles(128), nb / 4, 16}));
   return {128, (int)splits};
 }
 
@@ -542,18 +635,19 @@ void product_typed(ProductArgs a, const Plan& p, hipStream_t s) {
   constexpr bool EXACT = sizeof(T) == 4;
   if (p.edge == 16) {
     const dim3 grid((a.N + 15) / 16);
-    if (a.M <= 16) hipLaunchKernelGGL((k_thin<T, 1, ROWS, EXACT>), grid, dim3(512), 0, s, a);
-    else if (a.M <= 32) hipLaunchKernelGGL((k_thin<T, 2, ROWS, EXACT>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_thin<T, 4, ROWS, EXACT>), grid, dim3(512), 0, s, a);
+    if (a.M <= 16) hipLaunchKernelGGL((k_thin<T, 1, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_thin<T, 2, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
     return;
   }
-  if constexpr (!EXACT) {
+  if (p.edge == 64) {
+    launch_product<T, 64, 64, 2, 2, ROWS, EXACT>(a, s);
+  } else if constexpr (EXACT) {
+    launch_product<T, 128, 128, 2, 2, ROWS, EXACT>(a, s);
+  } else {
     if (p.edge == 256)
       launch_product<T, 256, 256, 2, 4, ROWS, EXACT>(a, s);
     else
       launch_product<T, 128, 128, 2, 2, ROWS, EXACT>(a, s);
-  } else {
-    launch_product<T, 128, 128, 2, 2, ROWS, EXACT>(a, s);
   }
   if (p.splits > 1) {
     const int64_t total = (int64_t)a.M * a.N;
@@ -629,7 +723,7 @@ ProductArgs product_args(int64_t M, int64_t N, int64_t K, const void* A, int64_t
                          gptq2d_dtype dt, const Plan& p, void* part) {
   ProductArgs a = {};
   a.M = (int)M, a.N = (int)N, a.K = (int)K;
-  a.X = (const uint8_t*)A, a.ldx = lda, a.SX = SA, a.ldsx = ldsa;
+  a.X = A, a.ldx = lda, a.SX = SA, a.ldsx = ldsa;
   a.W = (const uint8_t*)B, a.ldw = ldb, a.SW = SB, a.ldsw = ldsb;
   a.Y = C, a.ldy = ldc;
   const size_t es = elem_size(dt);
@@ -703,10 +797,20 @@ gptq2d_status gptq2d_block_linear(int64_t M, int64_t N, int64_t K, gptq2d_dtype 
   if (st == GPTQ2D_OK) st = check_matrix(Y, ldy, N, dt, "Y is NULL");
   if (st == GPTQ2D_OK) st = check_workspace(workspace, ws_bytes, gptq2d_block_linear_workspace_size(M, N, K));
   if (st != GPTQ2D_OK) return st;
+  const Plan p = plan(M, N, K);
+  if (M <= kFusedRows && K % 2 == 0 && ldx % 2 == 0 && aligned(X, 2 * elem_size(dt))) {
+    ProductArgs a = product_args(M, N, K, X, ldx, nullptr, 0, W, ldw, SW, ldsw, Y, ldy, dt, p, nullptr);
+    a.pow2 = pow2 != 0;
+    with_type(dt, [&](auto* t) {
+      using T = std::remove_pointer_t<decltype(t)>;
+      auto k = M == 1 ? k_thin<T, 1, false, sizeof(T) == 4, 1> : k_thin<T, 1, false, sizeof(T) == 4, kFusedRows>;
+      hipLaunchKernelGGL(k, dim3((unsigned)ceil_div(N, 16)), dim3(512), 0, (hipStream_t)stream, a);
+    });
+    return launched("gptq2d_block_linear");
+  }
   Region ws{(char*)workspace};
   uint8_t* q = ws.take<uint8_t>(code_bytes(M, K));
   float* sq = ws.take<float>(scale_bytes(M, K));
-  const Plan p = plan(M, N, K);
   QuantArgs a = {M, K, X, ldx, q, code_ld(K), sq, M, nullptr, 0, nullptr, 0, pow2 != 0, wide_rows(X, ldx, elem_size(dt))};
   quantize(a, dt, false, (hipStream_t)stream);
   product(product_args(M, N, K, q, code_ld(K), sq, M, W, ldw, SW, ldsw, Y, ldy, dt, p, ws.at), p, false, dt,

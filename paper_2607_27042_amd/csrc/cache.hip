@@ -23,14 +23,15 @@ struct CacheArgs {
   bool wide;
 };
 
-// the vector's place in the cache, or -1 for a slot that is none
-__device__ __forceinline__ int64_t place(const CacheArgs& a, int64_t token, int head) {
-  const int64_t s = a.slots[token];
-  if (s < 0 || s >= a.total) return -1;
-  const uint32_t slot = (uint32_t)s;
+// a vector's place in the cache, or -1 for a slot that is none (without branches:
+// the loads of several are not to wait for one another)
+__device__ __forceinline__ int64_t place(const CacheArgs& a, int64_t s, int head) {
+  const bool none = s < 0 || s >= a.total;
+  const uint32_t slot = none ? 0 : (uint32_t)s;
   uint32_t q = __umulhi(slot, a.magic);  // slot < 2^31: at most one too large
-  if (q * a.page > slot) --q;
-  return ((int64_t)q * a.heads + head) * a.page + (slot - q * a.page);
+  q -= q * a.page > slot;
+  const int64_t at = ((int64_t)q * a.heads + head) * a.page + (slot - q * a.page);
+  return none ? -1 : at;
 }
 
 // L lanes hold a vector, eight values each (dim <= 8 L)
@@ -38,7 +39,7 @@ template <class T, int L, bool INT8>
 __global__ __launch_bounds__(256) void k_append(CacheArgs a) {
   const int lane = threadIdx.x % L, head = blockIdx.y;
   const int64_t token = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int64_t at = token < a.tokens ? place(a, token, head) : -1;
+  const int64_t at = token < a.tokens ? place(a, a.slots[token], head) : -1;
   const bool active = at >= 0 && 8 * lane < a.dim;
   const bool key = blockIdx.z == 0;
   float x[8];
@@ -55,36 +56,63 @@ __global__ __launch_bounds__(256) void k_append(CacheArgs a) {
   if (lane == 0) (key ? a.KS : a.VS)[at] = s;
 }
 
+// L lanes hold a vector, sixteen values each (dim <= 16 L), and four vectors one
+// after the other: slot, codes and value wait for one another, so that the reads
+// of four of them are on their way at once (32768 tokens x 8 heads x 128, int8 to
+// 16 bits: 92 us one by one with eight values a lane).
 template <class T, int L, bool INT8>
 __global__ __launch_bounds__(256) void k_read(CacheArgs a) {
-  const int lane = threadIdx.x % L, head = blockIdx.y;
-  const int64_t token = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  if (token >= a.tokens || 8 * lane >= a.dim) return;
-  const bool key = blockIdx.z == 0;
-  const int64_t at = place(a, token, head);
-  float x[8];
+  constexpr int V = 4, P = 256 / L;  // vectors of a lane, of a work group at a time
+  const int lane = threadIdx.x % L;
+  const bool key = blockIdx.y == 0;
+  const uint32_t all = (uint32_t)(a.tokens * a.heads), first = blockIdx.x * (P * V) + threadIdx.x / L;
+  if (16 * lane >= a.dim) return;
+  int64_t at[V];
+  u4 q[V];
+  float s[V];
+  uint32_t token[V];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-  if (at >= 0) {
-    const u2 q = *(const u2*)((key ? a.KC : a.VC) + at * a.dim + 8 * lane);
-    const float s = (key ? a.KS : a.VS)[at];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const h2 lo = halves<INT8, false>(q[i]), hi = halves<INT8, true>(q[i]);
-      x[4 * i] = (float)lo[0] * s, x[4 * i + 1] = (float)lo[1] * s;
-      x[4 * i + 2] = (float)hi[0] * s, x[4 * i + 3] = (float)hi[1] * s;
-    }
+  for (int v = 0; v < V; ++v) {
+    token[v] = min(first + v * P, all - 1) / (uint32_t)a.heads;
+    at[v] = a.slots[token[v]];
   }
-  store8((T*)(key ? a.K : a.V) + token * (key ? a.ldk : a.ldv) + (int64_t)head * a.dim + 8 * lane, a.wide, 8, x);
+#pragma unroll
+  for (int v = 0; v < V; ++v) at[v] = place(a, at[v], (int)(min(first + v * P, all - 1) - token[v] * a.heads));
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int64_t from = max(at[v], (int64_t)0);
+    q[v] = *(const u4*)((key ? a.KC : a.VC) + from * a.dim + 16 * lane);
+    s[v] = (key ? a.KS : a.VS)[from];
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const uint32_t vec = first + v * P;
+    if (vec >= all) break;
+    T* p = (T*)(key ? a.K : a.V) + token[v] * (key ? a.ldk : a.ldv) + (int64_t)(vec - token[v] * a.heads) * a.dim + 16 * lane;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const h2 lo = halves<INT8, false>(q[v][i]), hi = halves<INT8, true>(q[v][i]);
+      x[4 * i] = (float)lo[0] * s[v], x[4 * i + 1] = (float)lo[1] * s[v];
+      x[4 * i + 2] = (float)hi[0] * s[v], x[4 * i + 3] = (float)hi[1] * s[v];
+    }
+    if (at[v] < 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    }
+    store8(p, a.wide, 8, x);
+    store8(p + 8, a.wide, 8, x + 8);
+  }
 }
 
+// lanes of a vector when writing (8 values each) and reading (16)
 template <class T, int L, bool INT8>
 void launch(const CacheArgs& a, bool append, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div(a.tokens, 256 / L), a.heads, 2);
   if (append)
-    hipLaunchKernelGGL((k_append<T, L, INT8>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_append<T, L, INT8>), dim3((unsigned)ceil_div(a.tokens, 256 / L), a.heads, 2), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_read<T, L, INT8>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_read<T, L / 2, INT8>), dim3((unsigned)ceil_div(a.tokens * a.heads, 4 * 256 / (L / 2)), 2),
+                       dim3(256), 0, s, a);
 }
 
 template <class T, bool INT8>
@@ -100,7 +128,8 @@ gptq2d_status cache_call(int64_t tokens, int heads, int dim, gptq2d_dtype dt, vo
                          void* VC, float* KS, float* VS, bool append, hipStream_t s, const char* name) {
   const gptq2d_status st = check_cache(heads, dim, code, pages, page_size, KC, VC, KS, VS);
   if (st != GPTQ2D_OK) return st;
-  if (tokens < 0 || tokens > (int64_t)1 << 26) return refuse("tokens must lie in [0, 2^26]");
+  if (tokens < 0 || tokens > (int64_t)1 << 26 || tokens * heads > (int64_t)1 << 30)
+    return refuse("tokens must lie in [0, 2^26], and tokens x heads in 2^30");
   if (!narrow_dtype(dt)) return refuse("bad dtype");
   if (tokens == 0) return GPTQ2D_OK;
   if (!K || !V || !slots) return refuse("K, V or slots are NULL");

@@ -97,10 +97,10 @@ __device__ __forceinline__ void load8(const T* p, bool wide, int n, float x[8]) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
     } else {
-      struct alignas(16) V { T v[8]; };
-      const V a = *(const V*)p;
+      typedef T V __attribute__((ext_vector_type(8)));
+      const V a = __builtin_bit_cast(V, *(const u4*)p);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (float)a.v[i];
+      for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
     }
   } else {
 #pragma unroll
@@ -114,11 +114,13 @@ __device__ __forceinline__ void store8(T* p, bool wide, int n, const float x[8])
       *(f4*)p = f4{x[0], x[1], x[2], x[3]};
       *(f4*)(p + 4) = f4{x[4], x[5], x[6], x[7]};
     } else {
-      struct alignas(16) V { T v[8]; };
+      // one piece of 16 bytes: element by element the compiler would share the
+      // stores with the other branch, and write eight times as often
+      typedef T V __attribute__((ext_vector_type(8)));
       V a;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a.v[i] = (T)x[i];
-      *(V*)p = a;
+      for (int i = 0; i < 8; ++i) a[i] = (T)x[i];
+      *(u4*)p = __builtin_bit_cast(u4, a);
     }
   } else {
 #pragma unroll

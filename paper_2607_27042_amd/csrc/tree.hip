@@ -57,8 +57,12 @@ __device__ __forceinline__ void store_n(T* p, bool wide, const float* v) {
 #pragma unroll
     for (int i = 0; i < N; i += 8) store8(p + i, wide, 8, v + i);
   } else if (wide) {
-    struct alignas(4 * sizeof(T)) V { T v[4]; };
-    *(V*)p = V{{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+    if constexpr (sizeof(T) == 4) {
+      *(f4*)p = f4{v[0], v[1], v[2], v[3]};
+    } else {
+      typedef T V __attribute__((ext_vector_type(4)));
+      *(u2*)p = __builtin_bit_cast(u2, V{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) p[i] = (T)v[i];
@@ -181,7 +185,7 @@ __device__ __forceinline__ void fetch_scales(Tokens<DP>& x, const TreeArgs& a, E
 // queries), probabilities as ZP (one, rounded by 2^-11 at most, where the result
 // is rounded by 2^-8 after it).
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
-__global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
   __shared__ float lo[kWaves][16 * QT][DP + 4];
@@ -206,7 +210,6 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
 
   h8 q[QT][KS][ZQ];
   float qs[QT], m[QT], sum[QT];
-  uint64_t sees[QT];
   f4 o[QT][NT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -239,7 +242,6 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
         q[t][s][0][i] = (_Float16)v;
         if constexpr (ZQ == 2) q[t][s][1][i] = (_Float16)(v - (float)q[t][s][0][i]);
       }
-    sees[t] = !live ? 0 : a.mask ? a.mask[(int64_t)b * a.width + tq] : ((uint64_t)2 << tq) - 1;
     m[t] = -INFINITY, sum[t] = 0;
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[t][j] = f4{0, 0, 0, 0};
@@ -286,8 +288,13 @@ __global__ __launch_bounds__(64 * kWaves, DP * QT <= 256 ? 2 : 1) void k_tree(Tr
     uint32_t ok[QT];
     const bool edge = tok + kStep > min(ctx, end) || now.page[0] < 0 || now.page[1] < 0;
     if (edge) {
+      uint64_t sees[QT];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) ok[t] = 0;
+      for (int t = 0; t < QT; ++t) {
+        const int tq = min((rb * QT + t) * 16 + c, a.rows - 1) / a.group;
+        sees[t] = a.mask ? a.mask[(int64_t)b * a.width + tq] : ((uint64_t)2 << tq) - 1;
+        ok[t] = 0;
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int first = tok + 16 * h + 4 * g, past = first - ctx;
@@ -534,10 +541,11 @@ __global__ __launch_bounds__(256) void k_tree_masks(int64_t count, int width, co
 int padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 // Queries a work group takes, in tiles of 16: more of them share each read of
-// the cache, as far as their accumulators fit the registers.
-int query_tiles(int rows, int dim) {
-  const int most = padded(dim) == 256 ? 2 : 4;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+// the cache, as far as they and their accumulators fit the registers (a kernel
+// that spills is not built: two tiles of 32-bit queries of 256 gave wrong results).
+int query_tiles(int rows, int dim, bool f32) {
+  const int most = f32 ? (padded(dim) == 256 ? 1 : 2) : padded(dim) == 256 ? 2 : 4;
+  return std::min(most, rows <= 16 ? 1 : rows <= 32 ? 2 : 4);
 }
 
 // Parts that a sequence's tokens are split into: as many as give the device two
@@ -546,7 +554,7 @@ int query_tiles(int rows, int dim) {
 // (dim 64) 75 / 58 / 65 / 76 us, 32 trees of 8 over up to 32768 (dim 128) 310 /
 // 311 / 312 / 300 us, one token over 4096 10.7 / 11.5 / 11.4 / 11.5 us.
 int split_count(int64_t seqs, int rows, int kv, int dim) {
-  const int64_t groups = seqs * kv * ceil_div(rows, 16 * query_tiles(rows, dim));
+  const int64_t groups = seqs * kv * ceil_div(rows, 16 * query_tiles(rows, dim, false));
   return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(512, groups)));
 }
 
@@ -561,9 +569,13 @@ void launch(const TreeArgs& a, hipStream_t s) {
 }
 template <bool INT8, int DP, int ZQ, int ZP>
 void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
-  if (tiles == 1) launch<INT8, DP, 1, ZQ, ZP>(a, s);
-  else if (tiles == 2) launch<INT8, DP, 2, ZQ, ZP>(a, s);
-  else if constexpr (DP != 256) launch<INT8, DP, 4, ZQ, ZP>(a, s);
+  if (tiles == 1) {
+    launch<INT8, DP, 1, ZQ, ZP>(a, s);
+  } else if (tiles == 2) {
+    if constexpr (DP != 256 || ZQ == 1) launch<INT8, DP, 2, ZQ, ZP>(a, s);
+  } else {
+    if constexpr (DP != 256 && ZQ == 1) launch<INT8, DP, 4, ZQ, ZP>(a, s);
+  }
   if (a.splits > 1) {
     const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
     hipLaunchKernelGGL(k_tree_join<DP>, dim3((unsigned)all), dim3(64 * kWaves), 0, s, a);
@@ -646,7 +658,7 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
   a.scale = scale * kLog2E;
   a.qwide = wide_rows(Q, ldq, es), a.owide = wide_rows(O, ldo, es);
   a.O = O, a.ldo = ldo, a.lse = lse, a.part = (float*)workspace;
-  const int tiles = query_tiles(rows, dim);
+  const int tiles = query_tiles(rows, dim, dt == GPTQ2D_F32);
   a.rowblocks = (int)ceil_div(rows, 16 * tiles);
   a.splits = (int)std::min<int64_t>(split_count(seqs, rows, kv_heads, dim), ceil_div(a.capacity, kWaves * kStep));
   if (code == GPTQ2D_INT8)
