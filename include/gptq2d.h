@@ -387,7 +387,8 @@ size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, 
  * products as 16-bit floats (after scaling by a power of two), or as the sum of
  * two where dt is F32. A context past the table's last page ends there; the
  * tokens of an entry that names no page are absent. One token per sequence
- * (width 1) is decoding. 1 <= width <= 64, seqs <= 65535. workspace: as sized
+ * (width 1) is decoding. 1 <= width <= 64, seqs <= 65535, seqs * width * heads <=
+ * 2^24, kv_heads <= 1024. workspace: as sized
  * above, 256-byte aligned, owned by the caller; overlapping calls need distinct
  * ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
 gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_heads, int dim,

@@ -469,21 +469,23 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
   }
 }
 
-// One work group per query: each wave adds up every fourth split's part, eight
-// loads at a time, then the waves' sums are added, all in a fixed order.
-template <int DP>
+// G waves per query: each adds up every G-th split's part, eight loads at a time,
+// then the waves' sums are added, all in a fixed order.
+template <int DP, int G>
 __global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
-  __shared__ float lo[kWaves][DP];
-  const int64_t id = blockIdx.x, all = (int64_t)a.seqs * a.kv * a.rows;
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
-  const int64_t bh = id / a.rows;
-  const int r = (int)(id - bh * a.rows), hkv = (int)(bh % a.kv), b = (int)(bh / a.kv);
-  const float* ml = a.part + all * a.splits * DP + 2 * id * a.splits;
+  constexpr int E = DP / 64;  // elements of a lane
+  __shared__ float lo[G][DP];
+  const int wave = threadIdx.x >> 6, w = wave % G, l = threadIdx.x & 63;
+  const uint32_t all = (uint32_t)a.seqs * a.kv * a.rows, id = blockIdx.x * (kWaves / G) + wave / G;
+  if (id >= all) return;  // (G = 1, or a whole work group)
+  const uint32_t bh = id / (uint32_t)a.rows, b = bh / (uint32_t)a.kv;
+  const int r = id - bh * a.rows, hkv = bh - b * a.kv;
+  const float* ml = a.part + (int64_t)all * a.splits * DP + 2 * (int64_t)id * a.splits;
   const float ms = l < a.splits ? ml[2 * l] : -INFINITY, ls = l < a.splits ? ml[2 * l + 1] : 0.0f;
-  const float* part = a.part + id * a.splits * DP + (DP / 64) * l;
-  float v[DP / 64], x[8][DP / 64];
+  const float* part = a.part + (int64_t)id * a.splits * DP + E * l;
+  float v[E], x[8][E];
 #pragma unroll
-  for (int e = 0; e < DP / 64; ++e) v[e] = 0;
+  for (int e = 0; e < E; ++e) v[e] = 0;
   float top = ms;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -491,35 +493,43 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
   float L = ls * f;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
-  for (int s0 = w; s0 < a.splits; s0 += 8 * kWaves) {
+  for (int s0 = w; s0 < a.splits; s0 += 8 * G) {
 #pragma unroll
     for (int u = 0; u < 8; ++u)
 #pragma unroll
-      for (int e = 0; e < DP / 64; ++e) x[u][e] = part[(int64_t)min(s0 + u * kWaves, a.splits - 1) * DP + e];
+      for (int e = 0; e < E; ++e) x[u][e] = part[(int64_t)min(s0 + u * G, a.splits - 1) * DP + e];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int s = s0 + u * kWaves;
+      const int s = s0 + u * G;
       const float fs = s < a.splits ? __shfl(f, s) : 0.0f;
 #pragma unroll
-      for (int e = 0; e < DP / 64; ++e) v[e] += fs == 0.0f ? 0.0f : x[u][e] * fs;  // an empty part is not written
+      for (int e = 0; e < E; ++e) v[e] += fs == 0.0f ? 0.0f : x[u][e] * fs;  // an empty part is not written
     }
   }
+  if constexpr (G > 1) {
 #pragma unroll
-  for (int e = 0; e < DP / 64; ++e) lo[w][(DP / 64) * l + e] = v[e];
-  __syncthreads();
-  const int d = threadIdx.x;
+    for (int e = 0; e < E; ++e) lo[w][E * l + e] = v[e];
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 1; i < G; ++i) v[e] += lo[i][E * l + e];
+  }
   const int tk = r / a.group, head = hkv * a.group + r % a.group;
   const int64_t row = (int64_t)b * a.width + tk;
   const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
   const bool none = L == 0.0f || tk >= drafted;
-  if (d < a.dim) {
-    const float y = none ? 0.0f : (lo[0][d] + lo[1][d] + lo[2][d] + lo[3][d]) / L;
-    const int64_t at = row * a.ldo + (int64_t)head * a.dim + d;
-    if (a.dt == GPTQ2D_F32) ((float*)a.O)[at] = y;
-    else if (a.dt == GPTQ2D_F16) ((_Float16*)a.O)[at] = (_Float16)y;
-    else ((bf16*)a.O)[at] = (bf16)y;
+  const int64_t at = row * a.ldo + (int64_t)head * a.dim + E * l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (E * l + e >= a.dim) break;
+    const float y = none ? 0.0f : v[e] / L;
+    if (a.dt == GPTQ2D_F32) ((float*)a.O)[at + e] = y;
+    else if (a.dt == GPTQ2D_F16) ((_Float16*)a.O)[at + e] = (_Float16)y;
+    else ((bf16*)a.O)[at + e] = (bf16)y;
   }
-  if (a.lse && threadIdx.x == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
+  if (a.lse && l == 0) a.lse[row * (a.kv * a.group) + head] = none ? -INFINITY : (top + log2f(L)) * kLn2;
 }
 
 // bits of a token's ancestors and itself; a parent that is not an earlier token is none
@@ -576,10 +586,11 @@ void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
   } else {
     if constexpr (DP != 256 && ZQ == 1) launch<INT8, DP, 4, ZQ, ZP>(a, s);
   }
-  if (a.splits > 1) {
-    const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
-    hipLaunchKernelGGL(k_tree_join<DP>, dim3((unsigned)all), dim3(64 * kWaves), 0, s, a);
-  }
+  const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
+  if (a.splits > 8)
+    hipLaunchKernelGGL((k_tree_join<DP, kWaves>), dim3((unsigned)all), dim3(64 * kWaves), 0, s, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL((k_tree_join<DP, 1>), dim3((unsigned)ceil_div(all, kWaves)), dim3(64 * kWaves), 0, s, a);
 }
 template <bool INT8, int DP>
 void launch_type(const TreeArgs& a, int tiles, hipStream_t s) {
@@ -596,7 +607,7 @@ void launch_dim(const TreeArgs& a, int tiles, hipStream_t s) {
 
 bool bad_shape(int64_t seqs, int width, int heads, int kv_heads, int dim) {
   return seqs < 1 || seqs > 65535 || width < 1 || width > 64 || kv_heads < 1 || kv_heads > 1024 || heads < kv_heads ||
-         heads > 4096 || heads % kv_heads != 0 || dim < 16 || dim > 256 || dim % 16 != 0;
+         heads > 4096 || heads % kv_heads != 0 || seqs * heads * width > (int64_t)1 << 24 || dim < 16 || dim > 256 || dim % 16 != 0;
 }
 
 }  // namespace
@@ -630,7 +641,7 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
                                     float* lse, void* workspace, size_t ws_bytes, void* stream) {
   if (bad_shape(seqs, width, heads, kv_heads, dim))
     return refuse("bad shape: 1 <= seqs <= 65535, 1 <= width <= 64, heads a multiple of kv_heads (up to 4096 of up to "
-                  "1024), dim a multiple of 16 up to 256");
+                  "1024), seqs x width x heads up to 2^24, dim a multiple of 16 up to 256");
   if (!narrow_dtype(dt)) return refuse("bad dtype");
   gptq2d_status st = check_cache(kv_heads, dim, code, pages, page_size, KC, VC, KS, VS);
   if (st != GPTQ2D_OK) return st;
