@@ -17,6 +17,7 @@ namespace {
 constexpr int kStep = 32;        // tokens a wave takes at a time
 constexpr int kWaves = 4;
 constexpr int kMaxSplits = 64;
+constexpr int kBalanced = 256;   // sequences whose lengths a work group looks at
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2E = 1.44269504088896341f;
 
@@ -40,7 +41,8 @@ struct TreeArgs {
   int64_t ldo;
   bool qwide, owide;  // rows of Q and O start on 16-byte boundaries
   float* lse;
-  int splits, rowblocks;
+  int splits, rowblocks;  // parts that a sequence may have
+  int mean;               // parts that one of mean length is to have
   float* part;  // splits > 1: [sequence][kv head][row][split][dim padded], then {m, l} likewise
 };
 
@@ -172,6 +174,28 @@ __device__ __forceinline__ void fetch_scales(Tokens<DP>& x, const TreeArgs& a, E
   }
 }
 
+// Tokens of a part: the same for all sequences, so that the work groups of long and
+// short ones take alike, as far as the longest one's parts suffice; whole steps.
+// (32 trees of 8, lengths between 8192 and 32768: 278 us, in equal numbers of parts
+// 311 us; 16 trees of 13, lengths between 2048 and 8192: 57 and 54 us.)
+__device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) {
+  int per = (total + a.splits - 1) / a.splits;
+  if (a.splits > 1 && a.seqs <= kBalanced) {
+    int n[kBalanced / 64];
+#pragma unroll
+    for (int i = 0; i < kBalanced / 64; ++i) n[i] = a.context[min(l + 64 * i, a.seqs - 1)];
+    float sum = 0;  // (a mean, so 32 bits will do)
+#pragma unroll
+    for (int i = 0; i < kBalanced / 64; ++i)
+      sum += l + 64 * i < a.seqs ? (float)(min(max(n[i], 0), a.capacity) + a.width) : 0.0f;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    per = max(per, (int)(sum / (a.seqs * (a.mean - 0.5f))));  // half a part is lost to whole ones
+  }
+  constexpr int whole = kWaves * kStep;
+  return __builtin_amdgcn_readfirstlane((per + whole - 1) / whole * whole);
+}
+
 // 16 QT queries of one kv head and sequence over one part of its tokens. Scores
 // and outputs are transposed (tokens and dimensions are the instruction's rows,
 // queries its columns), so a lane's values all belong to one query: maximum,
@@ -189,13 +213,23 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
   __shared__ float lo[kWaves][16 * QT][DP + 4];
-  const int split = blockIdx.x, hkv = blockIdx.y / a.rowblocks, rb = blockIdx.y % a.rowblocks, b = blockIdx.z;
+  // parts are the slowest index: work groups go round the XCDs by their number, and
+  // the last parts, which few sequences have, are not to meet on a few of them
+  const int hkv = blockIdx.x / a.rowblocks, rb = blockIdx.x % a.rowblocks, b = blockIdx.y, split = blockIdx.z;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, c = l & 15, g = l >> 4;
   const int ctx = min(max(a.context[b], 0), a.capacity);
   const int drafted = a.drafts ? min(max(a.drafts[b], 0), a.width) : a.width;
   const int total = min(ctx + drafted, a.capacity);
-  const int per = (((total + a.splits - 1) / a.splits) + kWaves * kStep - 1) / (kWaves * kStep) * (kWaves * kStep);
+  const int per = part_length(a, total, l);
   const int begin = split * per, end = min(total, begin + per);
+  if (begin >= end && a.splits > 1) {  // no such part
+    float* ml = a.part + (int64_t)a.seqs * a.kv * a.rows * a.splits * DP;
+    for (int r = rb * 16 * QT + threadIdx.x; r < min((rb + 1) * 16 * QT, a.rows); r += 64 * kWaves) {
+      const int64_t at = (((int64_t)b * a.kv + hkv) * a.rows + r) * a.splits + split;
+      ml[2 * at] = -INFINITY, ml[2 * at + 1] = 0.0f;
+    }
+    return;
+  }
   const int32_t* table = a.table + b * a.ldt;
 
   constexpr int kStride = kWaves * kStep;
@@ -321,17 +355,34 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
           for (int i = 0; i < 4; ++i)
             if (!((ok[t] >> (4 * h + i)) & 1)) z[t][h][i] = -INFINITY;
     }
-    // the value scales' power of two
-    float vmax = 0, fade = 1;
+    // What the exponents and the value scales are relative to moves when a score
+    // exceeds it by more than 2^10, or a value scale at all, which is seldom after
+    // the first tokens. The value scales' reference is a power of two.
+    float vmax = 0, top[QT];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 8; ++i) vmax = fmaxf(vmax, vs[i >> 2][i & 3]);
+    bool moves = vmax > vref;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vmax = fmaxf(vmax, vs[h][i]);
-    if (__any(vmax > vref)) {
-      vmax = fminf(quad_max(vmax), 0x1p126f);
+    for (int t = 0; t < QT; ++t) {
+      top[t] = z[t][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], z[t][i >> 2][i & 3]);
+      moves |= (top[t] - m[t]) * qs[t] > 10.0f;
+    }
+    if (__any(moves)) {
+      vmax = fminf(fmaxf(quad_max(vmax), vref), 0x1p126f);
       const float up = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
-      fade = vref * __uint_as_float((254u << 23) - __float_as_uint(up));
+      const float fade = vref * __uint_as_float((254u << 23) - __float_as_uint(up));
       vref = up;
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        top[t] = fmaxf(quad_max(top[t]), m[t]);
+        const float d = __builtin_amdgcn_exp2f((m[t] - (top[t] == -INFINITY ? 0.0f : top[t])) * qs[t]);
+        sum[t] *= d;
+        m[t] = top[t];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) o[t][j] *= fade * d;
+      }
     }
     const float vinv = __uint_as_float((254u << 23) - __float_as_uint(vref));
 #pragma unroll
@@ -340,19 +391,6 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
     h8 p[QT][ZP];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float top = z[t][0][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, z[t][i >> 2][i & 3]);
-      float f = fade;
-      // what the exponents are relative to moves when a score exceeds it by more
-      // than 2^10, which is seldom after a query's first tokens
-      if (__any((top - m[t]) * qs[t] > 10.0f)) {
-        top = fmaxf(quad_max(top), m[t]);
-        const float base = top == -INFINITY ? 0.0f : top, d = __builtin_amdgcn_exp2f((m[t] - base) * qs[t]);
-        sum[t] *= d;
-        f *= d;
-        m[t] = top;
-      }
       const float base = m[t] == -INFINITY ? 0.0f : m[t];
       float y[8];
 #pragma unroll
@@ -374,10 +412,6 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
           const h2 lo = __builtin_convertvector(fp2{y[i] - (float)hi[0], y[i + 1] - (float)hi[1]}, h2);
           p[t][1][i] = lo[0], p[t][1][i + 1] = lo[1];
         }
-      }
-      if (__any(f != 1.0f)) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j) o[t][j] *= f;
       }
     }
     // values
@@ -568,14 +602,20 @@ int split_count(int64_t seqs, int rows, int kv, int dim) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(512, groups)));
 }
 
-size_t part_bytes(int64_t seqs, int rows, int kv, int dim) {
+// parts that the longest sequence may have: up to twice the mean's
+int slot_count(int64_t seqs, int rows, int kv, int dim) {
   const int s = split_count(seqs, rows, kv, dim);
+  return s == 1 || seqs == 1 ? s : std::min(2 * s, kMaxSplits);
+}
+
+size_t part_bytes(int64_t seqs, int rows, int kv, int dim) {
+  const int s = slot_count(seqs, rows, kv, dim);
   return s == 1 ? 0 : (size_t)seqs * kv * rows * s * (padded(dim) + 2) * sizeof(float);
 }
 
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
 void launch(const TreeArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_tree<INT8, DP, QT, ZQ, ZP>), dim3(a.splits, a.kv * a.rowblocks, a.seqs), dim3(64 * kWaves), 0, s, a);
+  hipLaunchKernelGGL((k_tree<INT8, DP, QT, ZQ, ZP>), dim3(a.kv * a.rowblocks, a.seqs, a.splits), dim3(64 * kWaves), 0, s, a);
 }
 template <bool INT8, int DP, int ZQ, int ZP>
 void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
@@ -584,7 +624,7 @@ void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
   } else if (tiles == 2) {
     if constexpr (DP != 256 || ZQ == 1) launch<INT8, DP, 2, ZQ, ZP>(a, s);
   } else {
-    if constexpr (DP != 256 && ZQ == 1) launch<INT8, DP, 4, ZQ, ZP>(a, s);
+    if constexpr (DP != 256 && ZQ == 1 && (DP != 64 || ZP == 2)) launch<INT8, DP, 4, ZQ, ZP>(a, s);
   }
   const int64_t all = (int64_t)a.seqs * a.kv * a.rows;
   if (a.splits > 8)
@@ -595,7 +635,8 @@ void launch_tiles(const TreeArgs& a, int tiles, hipStream_t s) {
 template <bool INT8, int DP>
 void launch_type(const TreeArgs& a, int tiles, hipStream_t s) {
   if (a.dt == GPTQ2D_F32) launch_tiles<INT8, DP, 2, 2>(a, tiles, s);
-  else if (a.dt == GPTQ2D_F16) launch_tiles<INT8, DP, 1, 2>(a, tiles, s);
+  // (the kernel for four tiles of 64 and one half spills)
+  else if (a.dt == GPTQ2D_F16 || (DP == 64 && tiles == 4)) launch_tiles<INT8, DP, 1, 2>(a, tiles, s);
   else launch_tiles<INT8, DP, 1, 1>(a, tiles, s);
 }
 template <bool INT8>
@@ -671,7 +712,8 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
   a.O = O, a.ldo = ldo, a.lse = lse, a.part = (float*)workspace;
   const int tiles = query_tiles(rows, dim, dt == GPTQ2D_F32);
   a.rowblocks = (int)ceil_div(rows, 16 * tiles);
-  a.splits = (int)std::min<int64_t>(split_count(seqs, rows, kv_heads, dim), ceil_div(a.capacity, kWaves * kStep));
+  a.mean = split_count(seqs, rows, kv_heads, dim);
+  a.splits = (int)std::min<int64_t>(slot_count(seqs, rows, kv_heads, dim), ceil_div(a.capacity, kWaves * kStep));
   if (code == GPTQ2D_INT8)
     launch_dim<true>(a, tiles, (hipStream_t)stream);
   else
