@@ -7,13 +7,17 @@ missing library is an error, never a fallback.
 
 The functions named like the C entry points take and return the same things,
 with torch tensors in place of device pointers and Python ints in place of
-handles. ``Factors`` and ``round_matrix`` are conveniences built from them.
+handles. ``Factors`` and ``round_matrix`` are conveniences built from them, and
+``Blocks``, ``Cache``, ``block_*``, ``tree_masks`` and ``token_logprobs*`` those of
+the eight-bit operators: they allocate outputs and workspaces as they go.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
+from typing import NamedTuple
 
 import torch
 
@@ -793,3 +797,166 @@ def factor_batched(factors, As, Bs, check=True, stream=None, workspace=None):
     gptq2d_factor_batched(handles, As, Bs, ws, stream, shapes=[(f.m, f.n) for f in factors])
     if check:
         gptq2d_factor_batched_check(handles, stream)
+
+
+def _on(stream):
+    """Memory that a call on `stream` uses is taken for that stream, so that none
+    of it goes to other work while the call may still run."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _bytes(n: int) -> torch.Tensor:
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=torch.cuda.current_device())
+
+
+class Blocks(NamedTuple):
+    """A rows x cols matrix in e4m3 blocks of block_rows x 128: codes (rows on
+    16-byte boundaries) and 32-bit scales (block_rows 1: [blocks, rows], 128:
+    [row blocks, column blocks])."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    block_rows: int
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int = 128):
+        dev = torch.cuda.current_device()
+        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=dev)[:, :cols]
+        shape = (_blocks(cols), rows) if block_rows == 1 else (_blocks(rows), _blocks(cols))
+        return cls(codes, torch.empty(shape, dtype=torch.float32, device=dev), block_rows)
+
+    def values(self) -> torch.Tensor:
+        """What the codes stand for, in 32 bits."""
+        rows, cols = self.codes.shape
+        s = self.scales.T if self.block_rows == 1 else self.scales.repeat_interleave(128, 0)[:rows]
+        return self.codes.float() * s.repeat_interleave(128, 1)[:, :cols]
+
+
+def block_quantize(X: torch.Tensor, block_rows: int = 128, pow2: bool = False, transposed: bool = False,
+                   stream=None) -> Blocks:
+    """X (or its transpose, whose blocks run along X's columns) in e4m3 blocks."""
+    rows, cols = X.shape
+    with _on(stream):
+        out = Blocks.empty(*((cols, rows) if transposed else (rows, cols)), block_rows)
+        pair = (None, None, out.codes, out.scales) if transposed else (out.codes, out.scales)
+        gptq2d_block_quantize(X, *pair, block_rows=block_rows, pow2=pow2)
+    return out
+
+
+def block_matmul(A: Blocks, B: Blocks, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """A B^T; A in blocks of 1 x 128."""
+    if A.block_rows != 1:
+        raise ValueError("A must be in blocks of 1 x 128")
+    (M, K), N = A.codes.shape, B.codes.shape[0]
+    with _on(stream):
+        C = torch.empty((M, N), dtype=dtype, device=A.codes.device)
+        gptq2d_block_matmul(A.codes, A.scales, B.codes, B.scales, C,
+                            _bytes(gptq2d_block_matmul_workspace_size(M, N, K)), block_rows=B.block_rows)
+    return C
+
+
+def block_linear(X: torch.Tensor, W: Blocks, pow2: bool = False, stream=None) -> torch.Tensor:
+    """X W^T for W in tiles of 128 x 128; X is quantised on the way."""
+    (M, K), N = X.shape, W.codes.shape[0]
+    if W.block_rows != 128:
+        raise ValueError("W must be in tiles of 128 x 128")
+    with _on(stream):
+        Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
+        gptq2d_block_linear(X, W.codes, W.scales, Y, _bytes(gptq2d_block_linear_workspace_size(M, N, K)), pow2=pow2)
+    return Y
+
+
+def block_linear_backward(dY: torch.Tensor, X: torch.Tensor, WT: Blocks, pow2: bool = False, stream=None):
+    """(dX, dW) of block_linear; WT: block_quantize(W, transposed=True)."""
+    (M, N), K = dY.shape, X.shape[1]
+    if WT.block_rows != 128:
+        raise ValueError("WT must be in tiles of 128 x 128")
+    with _on(stream):
+        dX = torch.empty((M, K), dtype=dY.dtype, device=dY.device)
+        dW = torch.empty((N, K), dtype=torch.float32, device=dY.device)
+        ws = _bytes(gptq2d_block_linear_backward_workspace_size(M, N, K))
+        gptq2d_block_linear_backward(dY, X, WT.codes, WT.scales, dX, dW, ws, pow2=pow2)
+    return dX, dW
+
+
+class Cache:
+    """A paged eight-bit cache of keys and values (code: torch.float8_e4m3fn or
+    torch.int8). Pages are the caller's to hand out: table (int32, sequences x
+    pages) names each sequence's."""
+
+    def __init__(self, pages: int, heads: int, page_size: int, dim: int, code=torch.float8_e4m3fn):
+        dev = torch.cuda.current_device()
+        self.heads, self.page_size, self.dim = heads, page_size, dim
+        self.KC, self.VC = (torch.zeros((pages, heads, page_size, dim), dtype=torch.uint8, device=dev).view(code)
+                            for _ in range(2))
+        self.KS, self.VS = (torch.ones((pages, heads, page_size), device=dev) for _ in range(2))
+
+    @property
+    def tensors(self):
+        return self.KC, self.VC, self.KS, self.VS
+
+    def slots(self, table: torch.Tensor, first: torch.Tensor, count: int) -> torch.Tensor:
+        """The slots (int64, sequences * count) of positions first[b] .. first[b] +
+        count - 1 of every sequence; -1 past its pages."""
+        at = first.long().unsqueeze(1) + torch.arange(count, device=table.device)
+        page = at // self.page_size
+        entry = table.long().gather(1, page.clamp(max=table.shape[1] - 1))
+        slot = entry * self.page_size + at % self.page_size
+        return torch.where((page < table.shape[1]) & (entry >= 0), slot, -1).reshape(-1)
+
+    def append(self, K, V, slots, stream=None) -> None:
+        gptq2d_cache_append(K, V, slots, *self.tensors, stream=stream)
+
+    def read(self, slots, dtype=torch.bfloat16, stream=None):
+        with _on(stream):
+            K, V = (torch.empty((slots.shape[0], self.heads * self.dim), dtype=dtype, device=slots.device)
+                    for _ in range(2))
+            gptq2d_cache_read(slots, *self.tensors, K, V)
+        return K, V
+
+    def attend(self, Q, table, context, masks=None, drafts=None, scale=None, stream=None):
+        """(O, lse) of gptq2d_tree_attention; scale defaults to dim^-1/2."""
+        seqs, heads = context.shape[0], Q.shape[1] // self.dim
+        with _on(stream):
+            O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            lse = torch.empty((Q.shape[0], heads), dtype=torch.float32, device=Q.device)
+            ws = _bytes(gptq2d_tree_attention_workspace_size(seqs, Q.shape[0] // seqs, heads, self.heads, self.dim))
+            gptq2d_tree_attention(Q, *self.tensors, table, context, drafts, masks,
+                                  self.dim ** -0.5 if scale is None else scale, O, lse, ws)
+        return O, lse
+
+
+def tree_masks(parents: torch.Tensor, stream=None) -> torch.Tensor:
+    """Masks (int64 bits) of trees of drafted tokens, from their parents (int32)."""
+    with _on(stream):
+        masks = torch.empty(parents.shape, dtype=torch.int64, device=parents.device)
+        gptq2d_tree_masks(parents, masks)
+    return masks
+
+
+class Scores(NamedTuple):
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    ids: torch.Tensor | None
+    tops: torch.Tensor | None
+
+
+def token_logprobs(X: torch.Tensor, target=None, scale: float = 1.0, top: int = 0, stream=None) -> Scores:
+    """Scores of every row of logits X; ids and tops: the `top` largest."""
+    rows, vocab = X.shape
+    with _on(stream):
+        out = [torch.empty(rows, dtype=torch.float32, device=X.device) for _ in range(3)]
+        best = [torch.empty((rows, top), dtype=dt, device=X.device) if top else None
+                for dt in (torch.int32, torch.float32)]
+        gptq2d_token_logprobs(X, target, scale, *out, *best,
+                              _bytes(gptq2d_token_logprobs_workspace_size(rows, vocab, top)))
+    return Scores(*out, *best)
+
+
+def token_logprobs_backward(X: torch.Tensor, target, scores: Scores, g_logprob=None, g_entropy=None, scale: float = 1.0,
+                            stream=None) -> torch.Tensor:
+    """The gradient of the logits from those of the log probabilities and entropies."""
+    with _on(stream):
+        dX = torch.empty_like(X, memory_format=torch.contiguous_format)
+        gptq2d_token_logprobs_backward(X, target, scale, scores.lse, scores.entropy, g_logprob, g_entropy, dX)
+    return dX
