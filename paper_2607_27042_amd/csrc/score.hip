@@ -68,13 +68,14 @@ __device__ __forceinline__ int rank_in(Pool& p, K mine, int n) {
   best[threadIdx.x] = mine;
   __syncthreads();
   int r = 0;
-#pragma unroll 2
-  for (int i = 0; i < n; i += 8) {
-    K k[8];
+  // (128 bytes are read at once: the reads are to wait for one another seldom)
+  constexpr int U = 128 / sizeof(K);
+  for (int i = 0; i < n; i += U) {
+    K k[U];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) k[j] = best[i + j];
+    for (int j = 0; j < U; ++j) k[j] = best[i + j];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r += k[j] > mine;
+    for (int j = 0; j < U; ++j) r += k[j] > mine;
   }
   return r;
 }
@@ -196,7 +197,6 @@ __device__ __forceinline__ float target_logprob(const ScoreArgs& a, int64_t row,
 }
 
 __device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t row, float lse) {
-  keep_best(p, a.top);
   const int t = threadIdx.x;
   if (t >= a.top) return;
   const uint64_t k = p.key[t];
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
       }
       __syncthreads();
       // a limit that keeps up spares the threads most of these
-      if (pool.count > a.top + kSpare) keep_best(pool, a.top);
+      if (pool.count > a.top + kSpare || c + 1 == last) keep_best(pool, a.top);
       __syncthreads();
     }
   }
@@ -308,7 +308,6 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   if (a.parts > 1) {
     if (t == 0) ((f4*)a.stat)[blockIdx.x] = f4{s.m, s.s1, s.s2, 0.0f};
     if constexpr (TOP) {
-      keep_best(pool, a.top);
       // a part of a step's remainder may have fewer
       if (t < a.top) a.keys[(int64_t)blockIdx.x * a.top + t] = t < pool.count ? pool.key[t] : 0;
     }
@@ -347,6 +346,7 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
     if (t == 0) pool.count = n, pool.limit = 0;
     for (int i = t; i < n; i += kThreads) pool.key[i] = a.keys[row * n + i];
     __syncthreads();
+    keep_best(pool, a.top);
     put_best(pool, a, row, o.lse);
   }
 }
