@@ -263,8 +263,8 @@ gptq2d_status gptq2d_round_batched_check(const void* workspace, void* stream);
  *
  * Codes (e4m3) are bytes, row-major, ld a multiple of 16, the first row 16-byte
  * aligned; the bytes from the last column up to the next multiple of 16 belong
- * to the row as well (the quantiser sets them to 0, the products do not read
- * them). Blocks are 1 x 128 ("rows": the scale of block b of row r at
+ * to the row as well, in the last row too (the quantiser sets them to 0; the
+ * products read them, but their values do not matter). Blocks are 1 x 128 ("rows": the scale of block b of row r at
  * S[b * lds + r], lds >= rows) or 128 x 128 ("tiles": S[(r / 128) * lds +
  * c / 128], lds >= ceil(cols / 128)); the last block of a row or column of
  * blocks may be short. All sizes lie in [1, 2^22], leading dimensions of codes in
@@ -344,7 +344,8 @@ gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq
 /* Enqueues the quantisation of `tokens` tokens' keys K and values V (tokens x
  * (heads dim), type F32, F16 or BF16) into the slots slots[0 .. tokens-1]
  * (device). A slot that is negative or past the cache is skipped; a slot may
- * appear once. Errors: INVALID_ARG, HIP. */
+ * appear once. At most 2^26 tokens and 2^30 tokens x heads a call, of this and of
+ * gptq2d_cache_read. Errors: INVALID_ARG, HIP. */
 gptq2d_status gptq2d_cache_append(int64_t tokens, int heads, int dim, gptq2d_dtype dt,
                                   const void* K, int64_t ldk, const void* V, int64_t ldv,
                                   const int64_t* slots, gptq2d_code code, int64_t pages,

@@ -37,7 +37,10 @@ struct QuantArgs {
 // 16 is inside the row (its leading dimension is one) and becomes code 0.
 __device__ __forceinline__ void put8(uint8_t* p, u2 q) { *(u2*)p = q; }
 
-// Blocks of 1 x 128, 16 lanes each, eight values a lane.
+// Blocks of 1 x 128, 16 lanes each, eight values a lane: one 16-byte load of a
+// 16-bit type, the largest magnitude over the 16 lanes without LDS, one 8-byte
+// store. Bound by its bytes: 8192 x 4096 bf16 25.9 us, 3.9 TB/s read and written
+// (a large copy reaches 4.9).
 template <class T>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
   const int64_t nb = (a.cols + kBlock - 1) / kBlock, total = a.rows * nb;
@@ -60,7 +63,10 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
 
 // One 128 x 128 tile per work group, read once: thread t holds the 8 x 8
 // values of rows 8 (t / 16) and columns 8 (t % 16). TILE: one scale for the
-// tile; otherwise one for each row (Q) and one for each column (QT).
+// tile; otherwise one for each row (Q) and one for each column (QT). Codes of the
+// transpose are turned through LDS, so that both directions store whole pieces.
+// Bound by its bytes, with the exchange through LDS not hidden: 2047 x 11008 bf16 to
+// both 31.0 us, 3.0 TB/s; 2047 x 4096 to the transpose 10.8 us, 2.4 TB/s.
 template <class T, bool TILE>
 __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
   __shared__ uint32_t colmax[16][kBlock + 4];
@@ -287,6 +293,15 @@ __device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
 // by the 16-bit instruction. The eight-bit one aligns its products to about
 // 14 bits below the largest (measured 1.5e-5 of the sum of magnitudes), which
 // is far below a 16-bit result's last place, but not below a 32-bit one's.
+//
+// The whole of a block's codes comes into LDS while the one before it is multiplied.
+// Measured, by tile: 256 x 256 at 8192 x 11008 x 4096 bf16 about 420 us (1.76 PFLOP/s),
+// of which the scales' multiply-adds are 110 (they share the issue slots, not the
+// matrix unit) and the loads 65; 128 x 128 at 2047 x 4096 x 11008 131 us (1.41
+// PFLOP/s), EXACT and ROWS at 11008 x 4096 x 2047 215 us (0.86, of the 1.1 that a
+// product of 16-bit matrices reaches); 64 x 64 at 333 x 1000 x 700 6.8 us, which is
+// six blocks' latency. Tiles of 32 x 32 of the instruction were no faster (437
+// against 428 us at 128 x 128).
 template <class T, int BN, int BM, int WN, int WM, bool ROWS, bool EXACT>
 __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn, int tm) {
   constexpr int THREADS = 64 * WN * WM, TN = BN / WN / 16, TM = BM / WM / 16;
@@ -462,9 +477,10 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 // quantises the blocks it takes, two values a lane (K and ldx are even), through
 // LDS of its own. Every work group does that for itself, which for few rows costs
 // less than a launch before this one.
+// Bound by the weights' bytes and one memory latency: 1 x 4096 x 4096 5.8 us, 2.9 TB/s.
 template <class T, int TM, bool ROWS, bool EXACT, int FUSED>
 __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
-  constexpr int U = 4;
+  constexpr int U = TM == 1 ? 4 : 2;  // (with four, two of these work groups do not fit a compute unit's registers)
   __shared__ f4 sum[8][TM][64];
   __shared__ __align__(16) uint8_t own[FUSED ? 8 : 1][U][FUSED ? FUSED : 1][kBlock];
   const int n0 = blockIdx.x * 16, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
@@ -586,7 +602,8 @@ __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
   }
 }
 
-// adds the splits' partial sums in their order
+// Adds the splits' partial sums in their order. A split costs 8 bytes a result here,
+// which a product of few tiles has to spare.
 template <class T>
 __global__ __launch_bounds__(256) void k_join(ProductArgs a) {
   const int64_t total = (int64_t)a.M * a.N;
@@ -602,16 +619,24 @@ __global__ __launch_bounds__(256) void k_join(ProductArgs a) {
 // (the same for the workspace's size and the launch).
 struct Plan { int edge; int splits; };
 Plan plan(int64_t M, int64_t N, int64_t K) {
-  if (M <= 32) return {16, 1};
   const int64_t nb = ceil_div(K, kBlock);
+  // Few rows, against 64 x 64 tiles, at 4096 x 4096: 16 rows 6.4 and 10.2 us, 32 rows
+  // 8.8 and 9.8; with more of the weights a second tile of rows, read from the caches
+  // by every work group, costs more than the tiles' join (32 x 11008 x 4096 19.2 and
+  // 17.7 us, 32 x 4096 x 11008 20.3 and 17.6; 16 rows 13.7 and 17.3).
+  if (M <= 16 || (M <= 32 && N <= 8192 && nb <= 32)) return {16, 1};
   auto tiles = [&](int64_t e) { return ceil_div(M, e) * ceil_div(N, e); };
   // A 256 x 256 tile has a compute unit to itself, two of 128 x 128 share one; a
   // round of them takes 65 and 39 us at K = 4096. 8192 x 11008: 6 rounds of 388 us
   // against 11 of 430 us; 2047 x 4096 at K = 11008: 253 us (half the units idle)
   // against 132 us.
   if (5 * ceil_div(tiles(256), 256) <= 3 * ceil_div(tiles(128), 512)) return {256, 1};
-  // tiles of 128 do not give every second unit one: 64 x 64
-  if (tiles(128) < 128 && tiles(64) <= 256) {
+  // Tiles of 128 that do not fill the device, along a short K or where they are few: 64 x
+  // 64, which need not be split, or less. 700 x 1500 at K = 1500 8.6 us against 16.8, at
+  // 4096 24 against 22, at 11008 66 against 32; 2048 x 2048 at K = 1500 15.6 against
+  // 27, at 4096 30 against 35, at 6000 51 against 48; 333 x 1000 at K = 700 5.7
+  // against 8.2.
+  if ((tiles(128) <= 256 && nb <= 32) || (tiles(128) < 128 && tiles(64) <= 256)) {
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles(64), nb / 8, 16}));
     return {64, (int)splits};
   }
@@ -641,7 +666,7 @@ void product_typed(ProductArgs a, const Plan& p, hipStream_t s) {
   }
   if (p.edge == 64) {
     launch_product<T, 64, 64, 2, 2, ROWS, EXACT>(a, s);
-  } else if constexpr (EXACT) {
+  } else if constexpr (EXACT) {  // (widened operands of 256 x 256 do not fit the registers)
     launch_product<T, 128, 128, 2, 2, ROWS, EXACT>(a, s);
   } else {
     if (p.edge == 256)

@@ -207,6 +207,11 @@ __device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t ro
 // One work group per part of a row, one pass. Each thread sums relative to its
 // own largest logit so far, which moves rarely after the first steps. At the end
 // s1 >= 1 and s2 <= 0, so the entropy log s1 - s2 / s1 cancels nothing.
+// TOP: an element below the limit (the top-th best so far) is none of the best; the
+// first step sets a limit that few pass, so ranking is seldom. Bound by its bytes:
+// 4096 x 128000 bf16 with top 8 225 us, 4.7 TB/s; 2047 x 50257 55 us, 3.7 TB/s, whose
+// rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 11 us: two
+// rankings of a step's candidates (without top 4.4 us).
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   __shared__ Sums wave[kThreads / 64];
@@ -322,7 +327,8 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   if constexpr (TOP) put_best(pool, a, row, o.lse);
 }
 
-// One work group per row: its parts' sums, and the best of their best.
+// One work group per row: its parts' sums, and the best of their best. One row of
+// eight parts 5.6 us with top 20, 3.2 us without.
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
   __shared__ typename std::conditional<TOP, Pool, int>::type pool;
@@ -364,7 +370,8 @@ struct GradArgs {
 };
 
 // One pass, element by element. Rows of logits and gradients that start at the
-// same distance from a 16-byte boundary are moved in 16-byte pieces.
+// same distance from a 16-byte boundary are moved in 16-byte pieces. Bound by its
+// bytes: 2047 x 50257 bf16 96 us, 4.3 TB/s read and written.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   constexpr int W = 16 / sizeof(T);
@@ -408,10 +415,12 @@ __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   }
 }
 
-// Parts of a row: as many as give the device about four work groups a compute
-// unit, each of one step at least.
+// Parts of a row: as many as give every compute unit a work group, each of one step
+// at least. At 256 / 512 / 1024 work groups: 700 rows of 32000 bf16 13.4 / 13.3 / 19.7
+// us, 256 of 128000 f32 23.1 / 27.9 / 30.5, 130 of 50257 bf16 with top 20 26.3 / 25.4 /
+// 29.2, 64 of 128000 12.5 / 12.2 / 13.5 (more parts are more to join).
 int part_count(int64_t rows, int64_t vocab) {
-  const int64_t want = ceil_div(1024, rows), room = ceil_div(vocab, kChunk);
+  const int64_t want = ceil_div(256, rows), room = ceil_div(vocab, kChunk);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, room, kMaxParts}));
 }
 
