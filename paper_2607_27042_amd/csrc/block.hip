@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
     const int64_t c0 = b * kBlock + (threadIdx.x & 15) * 8;
     const int n = (int)min((int64_t)8, a.cols - c0);
     float x[8];
-    load8((const T*)a.X + row * a.ldx + c0, a.wide && n == 8, n, x);
+    load8((const T*)a.X + row * a.ldx + c0, a.wide && n == 8, n, x, (const T*)a.X);
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, mag(x[i]));
@@ -66,10 +66,11 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a) {
 // tile; otherwise one for each row (Q) and one for each column (QT). Codes of the
 // transpose are turned through LDS, so that both directions store whole pieces.
 // Bound by its bytes, with the exchange through LDS not hidden: 2047 x 11008 bf16 to
-// both 31.0 us, 3.0 TB/s; 2047 x 4096 to the transpose 10.8 us, 2.4 TB/s.
+// both 25.3 us, 3.6 TB/s; 2047 x 4096 to the transpose 9.4 us, 2.7 TB/s; a few tiles
+// 5 us (one way), 7.5 us (both).
 template <class T, bool TILE>
 __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
-  __shared__ uint32_t colmax[16][kBlock + 4];
+  __shared__ __align__(16) uint32_t colmax[4][kBlock + 4];
   __shared__ __align__(16) uint8_t turned[kBlock][kBlock + 16];
   const int t = threadIdx.x, tr = t >> 4, tc = t & 15;
   const int64_t nc = (a.cols + kBlock - 1) / kBlock, by = blockIdx.x / nc, bx = blockIdx.x - by * nc;
@@ -79,11 +80,28 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
   uint32_t rm[8], cm[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) cm[i] = 0;
+  // one way for the whole tile, so that no row's loads wait for another's (2405 x 768
+  // bf16 10.6 us with a choice in each row)
+  if (a.wide && (cols >= kBlock || cols % 8 == 0)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const T* p = (const T*)a.X + (r0 + min((int64_t)8 * tr + i, rows - 1)) * a.ldx + c0;
+      load8(p + (8 * tc < cols ? 8 * tc : 0), true, 8, x[i], p);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[i][j] = 8 * tr + i < rows && 8 * tc < cols ? x[i][j] : 0.0f;
+  } else {
+    const int n = (int)max((int64_t)0, min((int64_t)8, cols - 8 * tc));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = 8 * tr + i;
+      load8((const T*)a.X + (r0 + r) * a.ldx + c0 + 8 * tc, false, r < rows ? n : 0, x[i], (const T*)a.X);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int64_t r = 8 * tr + i;
-    const int n = r < rows ? (int)max((int64_t)0, min((int64_t)8, cols - 8 * tc)) : 0;
-    load8((const T*)a.X + (r0 + r) * a.ldx + c0 + 8 * tc, a.wide && n == 8, n, x[i]);
     rm[i] = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -124,12 +142,15 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
   if (a.QT) {
     if constexpr (!TILE) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) colmax[tr][8 * tc + j] = cm[j];
+      for (int j = 0; j < 8; ++j) {  // over the wave's 32 rows
+        cm[j] = quad_max(cm[j]);
+        if ((tr & 3) == 0) colmax[tr >> 2][8 * tc + j] = cm[j];
+      }
       __syncthreads();
       if (t < kBlock) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m = max(m, colmax[i][t]);
+        for (int i = 0; i < 4; ++i) m = max(m, colmax[i][t]);
         colmax[0][t] = m;
         if (t < cols) a.ST[by * a.ldst + c0 + t] = block_scale(m, 1.0f / kTopE4M3, a.pow2);
       }
@@ -143,13 +164,14 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantArgs a) {
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = x[i][j];
-      *(u2*)&turned[8 * tc + j][8 * tr] = code8<false>(y, r, bad_amax(cm[j]));
+      // (16-byte pieces of column c lie at piece ^ (c / 16): lanes meet twice in a bank, not eight times)
+      *(u2*)&turned[8 * tc + j][8 * (tr ^ (tc & 14))] = code8<false>(y, r, bad_amax(cm[j]));
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int e = t + 256 * i, c = e >> 3, k = (e & 7) * 16;
-      if (c < cols && k < rows) *(u4*)(a.QT + (c0 + c) * a.ldqt + r0 + k) = *(const u4*)&turned[c][k];
+      if (c < cols && k < rows) *(u4*)(a.QT + (c0 + c) * a.ldqt + r0 + k) = *(const u4*)&turned[c][k ^ (c >> 4) * 16];
     }
   }
 }
@@ -479,18 +501,6 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
     store((T*)a.Y, a.ldy, a.ywide);
 }
 
-// largest over the wave, in every lane
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xf, 0xf, true));  // rows of 16 rotated by 1, 2, 4, 8
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true));
-  const u2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max(a[0], a[1]);
-  const u2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max(b[0], b[1]);
-}
-
 // Few rows (M <= 16 TM): the weights are read once, straight into the
 // instruction's registers, 16 rows a work group; its eight waves take every
 // eighth block of 128, the loads of four of them at once, and add up in LDS in
@@ -567,7 +577,7 @@ __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
         for (int m = 0; m < FUSED; ++m) {
           if (m >= a.M) break;
           const float x = in ? (float)raw[u][m].v[0] : 0.0f, y = in ? (float)raw[u][m].v[1] : 0.0f;
-          const uint32_t top = wave_max(max(mag(x), mag(y)));
+          const uint32_t top = group_max<64>(max(mag(x), mag(y)));
           const float s = block_scale(top, 1.0f / kTopE4M3, a.pow2), r = 1.0f / s;
           const uint32_t q = bad_amax(top) ? 0 : code4<false>(x * r, y * r, 0.0f, 0.0f);
           *(uint16_t*)&own[w][u][m][2 * l] = (uint16_t)q;

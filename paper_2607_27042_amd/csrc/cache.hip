@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void k_append(CacheArgs a) {
   const bool key = blockIdx.z == 0;
   float x[8];
   const T* p = (const T*)(key ? a.K : a.V) + token * (key ? a.ldk : a.ldv) + (int64_t)head * a.dim + 8 * lane;
-  load8(p, a.wide && active, active ? 8 : 0, x);
+  load8(p, a.wide && active, active ? 8 : 0, x, (const T*)(key ? a.K : a.V));
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, mag(x[i]));

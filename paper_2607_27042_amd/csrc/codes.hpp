@@ -88,9 +88,11 @@ __device__ __forceinline__ h2 halves(uint32_t w) {
 }
 
 // Eight consecutive elements at p as floats; `wide`: p is 16-byte aligned and
-// all eight are there, otherwise the first n are read one by one, the rest 0.
+// all eight are there, otherwise the first n (which may be none) are read one by
+// one, the rest are 0. (For those the last one is read, or what lies at `any`: a
+// branch around a load would make the next one wait for it.)
 template <class T>
-__device__ __forceinline__ void load8(const T* p, bool wide, int n, float x[8]) {
+__device__ __forceinline__ void load8(const T* p, bool wide, int n, float x[8], const T* any) {
   if (wide) {
     if constexpr (sizeof(T) == 4) {
       const f4 a = *(const f4*)p, b = *(const f4*)(p + 4);
@@ -103,8 +105,11 @@ __device__ __forceinline__ void load8(const T* p, bool wide, int n, float x[8]) 
       for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
     }
   } else {
+    const T* q = n > 0 ? p : any;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? (float)p[i] : 0.0f;
+    for (int i = 0; i < 8; ++i) x[i] = (float)q[min(i, max(n - 1, 0))];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? x[i] : 0.0f;
   }
 }
 template <class T>
@@ -129,12 +134,32 @@ __device__ __forceinline__ void store8(T* p, bool wide, int n, const float x[8])
   }
 }
 
-// over groups of L consecutive lanes (L a power of two), in every lane
+// over groups of L consecutive lanes (L a power of two), in every lane, without LDS:
+// lanes 1 and 2 away, then 8 and 16 lanes mirrored, then rows of 16 and halves swapped
 template <int L>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  static_assert(L >= 4 && L <= 64, "4 to 64 lanes");
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));
+  if constexpr (L >= 8) v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));
+  if constexpr (L >= 16) v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));
+  if constexpr (L >= 32) {
+    const u2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+  }
+  if constexpr (L == 64) {
+    const u2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(b[0], b[1]);
+  }
   return v;
+}
+
+// over the four lanes that share lane % 16, in every lane
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  const u2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const u2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
 }
 
 // ---------------------------------------------------------------------------

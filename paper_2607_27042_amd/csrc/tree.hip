@@ -48,9 +48,9 @@ struct TreeArgs {
 
 // eight elements of type dt from element i on; wide: they are 16-byte aligned
 __device__ __forceinline__ void load8_as(const void* p, gptq2d_dtype dt, int64_t i, bool wide, float x[8]) {
-  if (dt == GPTQ2D_F32) load8((const float*)p + i, wide, 8, x);
-  else if (dt == GPTQ2D_F16) load8((const _Float16*)p + i, wide, 8, x);
-  else load8((const bf16*)p + i, wide, 8, x);
+  if (dt == GPTQ2D_F32) load8((const float*)p + i, wide, 8, x, (const float*)p);
+  else if (dt == GPTQ2D_F16) load8((const _Float16*)p + i, wide, 8, x, (const _Float16*)p);
+  else load8((const bf16*)p + i, wide, 8, x, (const bf16*)p);
 }
 // N (4 or a multiple of 8) results; wide: aligned to their size, at most 16 bytes
 template <int N, class T>
