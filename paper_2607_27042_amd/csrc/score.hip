@@ -61,32 +61,46 @@ struct Pool {
 };
 
 // Number of keys above the thread's among the first n of the group's; n <=
-// kThreads, past n keys are 0.
-template <class K>
-__device__ __forceinline__ int rank_in(Pool& p, K mine, int n) {
-  K* best = (K*)p.best;
-  best[threadIdx.x] = mine;
+// kThreads, past n keys are 0 (and their threads' ranks are not wanted).
+__device__ __forceinline__ int rank_in(Pool& p, uint64_t mine, int n) {
+  p.best[threadIdx.x] = mine;
   __syncthreads();
   int r = 0;
+  if ((int)(threadIdx.x & ~63) >= n) return r;  // (whole waves)
   // (128 bytes are read at once: the reads are to wait for one another seldom)
-  constexpr int U = 128 / sizeof(K);
-  for (int i = 0; i < n; i += U) {
-    K k[U];
+  for (int i = 0; i < n; i += 16) {
+    uint64_t k[16];
 #pragma unroll
-    for (int j = 0; j < U; ++j) k[j] = best[i + j];
+    for (int j = 0; j < 16; ++j) k[j] = p.best[i + j];
 #pragma unroll
-    for (int j = 0; j < U; ++j) r += k[j] > mine;
+    for (int j = 0; j < 16; ++j) r += k[j] > mine;
   }
   return r;
 }
 
-// A first limit that at least `top` elements reach: the top-th of the threads'
-// largest (their low bits give way to the thread's number, so that no two are
-// equal and the limit is no higher).
+// A first limit that at least `top` elements reach, from the largest of each lane
+// (whose low bits give way to the lane's number, so that no two of a wave are equal and
+// the limit is no higher): the least of the four waves' of rank top / 4, or the greatest
+// of the waves' of rank top (rows that leave waves without elements). It is found without
+// LDS, whose reads would take longer than all else of a row of a few steps.
 __device__ __forceinline__ void first_limit(Pool& p, uint32_t most, int top) {
-  const uint32_t mine = most == 0 ? 0 : (most & ~255u) | threadIdx.x;
-  const int r = rank_in(p, mine, kThreads);
-  if (r == top - 1) p.limit = (uint64_t)(mine & ~255u) << 32;
+  const uint32_t mine = most == 0 ? 0 : (most & ~63u) | (threadIdx.x & 63);
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
+  // where there are fewer elements no lane has the rank, or one without an element: 0
+  auto of_rank = [&](int r) {
+    const uint64_t at = __ballot(above == r);
+    const uint32_t k = at == 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(at));
+    return (uint64_t)(k & ~63u) << 32;
+  };
+  const int w = threadIdx.x >> 6;
+  const uint64_t quarter = of_rank((top - 1) / 4), whole = of_rank(top - 1);
+  if ((threadIdx.x & 63) == 0) p.best[w] = quarter, p.best[4 + w] = whole;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    p.limit = max(min(min(p.best[0], p.best[1]), min(p.best[2], p.best[3])),
+                  max(max(p.best[4], p.best[5]), max(p.best[6], p.best[7])));
   __syncthreads();
 }
 
@@ -209,9 +223,9 @@ __device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t ro
 // s1 >= 1 and s2 <= 0, so the entropy log s1 - s2 / s1 cancels nothing.
 // TOP: an element below the limit (the top-th best so far) is none of the best; the
 // first step sets a limit that few pass, so ranking is seldom. Bound by its bytes:
-// 4096 x 128000 bf16 with top 8 225 us, 4.7 TB/s; 2047 x 50257 55 us, 3.7 TB/s, whose
-// rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 11 us: two
-// rankings of a step's candidates (without top 4.4 us).
+// 4096 x 128000 bf16 with top 8 222 us, 4.7 TB/s; 2047 x 50257 50 us, 4.1 TB/s, whose
+// rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 9.5 us: the
+// first limit and one ranking of candidates (without top 4.4 us).
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   __shared__ Sums wave[kThreads / 64];
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
 }
 
 // One work group per row: its parts' sums, and the best of their best. One row of
-// eight parts 5.6 us with top 20, 3.2 us without.
+// eight parts 5.4 us with top 20, 3.2 us without.
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
   __shared__ typename std::conditional<TOP, Pool, int>::type pool;
@@ -371,7 +385,7 @@ struct GradArgs {
 
 // One pass, element by element. Rows of logits and gradients that start at the
 // same distance from a 16-byte boundary are moved in 16-byte pieces. Bound by its
-// bytes: 2047 x 50257 bf16 96 us, 4.3 TB/s read and written.
+// bytes: 2047 x 50257 bf16 93 us, 4.4 TB/s read and written.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   constexpr int W = 16 / sizeof(T);
