@@ -330,7 +330,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   // four arrays, not two of two: the compiler then knows that the loads into the
   // next block's do not touch what is being read
   __shared__ __align__(16) uint8_t w0[BN * kBlock], w1[BN * kBlock], x0[BM * kBlock], x1[BM * kBlock];
-  // a block's scales, one a thread: X's BM, then W's BN (ROWS)
+  // A block's scales, one a thread: X's BM, then those of W's BN rows, which come this
+  // way also where they are one: read for the step from memory it costs 4 % of a
+  // large product.
   __shared__ __align__(16) float s0[THREADS], s1[THREADS];
   static_assert(BM + BN <= THREADS, "one scale a thread");
   int bn, bm;
@@ -349,12 +351,12 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   Stage<BM, THREADS> gx;
   gw.init(a.W, a.ldw, n0, a.N);
   gx.init((const uint8_t*)a.X, a.ldx, m0, a.M);
-  const bool xs = !ROWS || w < BM / 64;  // (whole waves)
-  const float* ps = xs ? a.SX : a.SW;
-  const int64_t psl = xs ? a.ldsx : a.ldsw;
-  const uint32_t pse = xs ? min(m0 + (int)threadIdx.x % BM, a.M - 1) : min(n0 + (int)threadIdx.x - BM, a.N - 1);
+  const bool xs = w < BM / 64;  // (whole waves)
+  const int at = xs ? min(m0 + (int)threadIdx.x, a.M - 1) : min(n0 + (int)threadIdx.x - BM, a.N - 1);
+  const float* ps = xs ? a.SX + at : ROWS ? a.SW + at : a.SW + at / kBlock * a.ldsw;
+  const int64_t psl = xs ? a.ldsx : ROWS ? a.ldsw : 1;
   auto scales = [&](int b, float* ms) {
-    __builtin_amdgcn_global_load_lds((const void*)(ps + b * psl + pse), (lds_void*)(ms + (threadIdx.x & ~63)), 4, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(ps + b * psl), (lds_void*)(ms + (threadIdx.x & ~63)), 4, 0, 0);
   };
   // the i-th of `parts` shares of a whole block's loads
   constexpr int LOADS = Stage<BN, THREADS>::N + Stage<BM, THREADS>::N;
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this block's codes and scales are in LDS
     __syncthreads();
     float sx[TM];
-    const float u = ROWS ? 1.0f : a.SW[(int64_t)(min(n0 + wn, a.N - 1) / kBlock) * a.ldsw + b];
+    const float u = ROWS ? 1.0f : ls[BM + wn];
 #pragma unroll
     for (int j = 0; j < TM; ++j) sx[j] = ls[wm + 16 * j + c] * u;
     if (SPREAD || b + 1 < b1) scales(b + 1, ms);
