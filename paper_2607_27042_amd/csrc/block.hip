@@ -317,13 +317,14 @@ __device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
 // is far below a 16-bit result's last place, but not below a 32-bit one's.
 //
 // The whole of a block's codes comes into LDS while the one before it is multiplied.
-// Measured, by tile: 256 x 256 at 8192 x 11008 x 4096 bf16 about 420 us (1.76 PFLOP/s),
-// of which the scales' multiply-adds are 110 (they share the issue slots, not the
-// matrix unit) and the loads 65; 128 x 128 at 2047 x 4096 x 11008 131 us (1.41
-// PFLOP/s), EXACT and ROWS at 11008 x 4096 x 2047 215 us (0.86, of the 1.1 that a
-// product of 16-bit matrices reaches); 64 x 64 at 333 x 1000 x 700 6.8 us, which is
-// six blocks' latency. Tiles of 32 x 32 of the instruction were no faster (437
-// against 428 us at 128 x 128).
+// Measured, by tile: 256 x 256 at 8192 x 11008 x 4096 bf16 356 us (2.07 PFLOP/s; a large
+// library product reaches 2.67); what bounds it are issue slots: when it took 387, it
+// took 278 without the scales' multiply-adds and 322 without its loads. 128 x 128 at
+// 2048 x 4096 x 11008 94 us (1.97 PFLOP/s), EXACT and ROWS at 11008 x 4096 x 2047 215 us
+// (0.86, of the 1.1 that a large product of 16-bit matrices reaches); 64 x 64 at 333 x
+// 1000 x 700 6.8 us, which is six blocks' latency (with the loads of three blocks on
+// their way no less). Tiles of 32 x 32 of the instruction were no faster (437 against 428
+// us at 128 x 128).
 template <class T, int BN, int BM, int WN, int WM, bool ROWS, bool EXACT>
 __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn, int tm) {
   constexpr int THREADS = 64 * WN * WM, TN = BN / WN / 16, TM = BM / WM / 16;
@@ -660,11 +661,11 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
   // 17.7 us, 32 x 4096 x 11008 20.3 and 17.6; 16 rows 13.7 and 17.3).
   if (M <= 16 || (M <= 32 && N <= 8192 && nb <= 32)) return {16, 1};
   auto tiles = [&](int64_t e) { return ceil_div(M, e) * ceil_div(N, e); };
-  // A 256 x 256 tile has a compute unit to itself, two of 128 x 128 share one; a
-  // round of them takes 65 and 39 us at K = 4096. 8192 x 11008: 6 rounds of 388 us
-  // against 11 of 430 us; 2047 x 4096 at K = 11008: 253 us (half the units idle)
-  // against 132 us.
-  if (5 * ceil_div(tiles(256), 256) <= 3 * ceil_div(tiles(128), 512)) return {256, 1};
+  // A 256 x 256 tile has a compute unit to itself, two of 128 x 128 share one; rounds of
+  // them take 60 and 36 us at K = 4096. 8192 x 11008: 6 rounds, 356 us, against 11, 390
+  // us; 4096 x 4096 64 and 74 us; 6000 x 6000: 3 rounds, 172 us, against 5, 164 us; 2048 x
+  // 4096: 60 us (half the units idle) against 44.
+  if (5 * ceil_div(tiles(256), 256) < 3 * ceil_div(tiles(128), 512)) return {256, 1};
   // Tiles of 128 that do not fill the device, along a short K or where they are few: 64 x
   // 64, which need not be split, or less. 700 x 1500 at K = 1500 8.6 us against 16.8, at
   // 4096 24 against 22, at 11008 66 against 32; 2048 x 2048 at K = 1500 15.6 against

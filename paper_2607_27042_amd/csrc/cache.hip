@@ -36,7 +36,7 @@ __device__ __forceinline__ int64_t place(const CacheArgs& a, int64_t s, int head
 
 // L lanes hold a vector, eight values each (dim <= 8 L): one read, the largest
 // magnitude over the lanes, one write. Bound by its bytes: 32768 tokens x 8 heads x
-// 128 from 16 bits 55 us, 3.7 TB/s read and written; 64 tokens 3 us.
+// 128 from 16 bits 52 us, 3.9 TB/s read and written; 64 tokens 2.6 us.
 template <class T, int L, bool INT8>
 __global__ __launch_bounds__(256) void k_append(CacheArgs a) {
   const int lane = threadIdx.x % L, head = blockIdx.y;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void k_append(CacheArgs a) {
 // after the other: slot, codes and value wait for one another, so that the reads
 // of four of them are on their way at once (32768 tokens x 8 heads x 128, int8 to
 // 16 bits: 92 us one by one with eight values a lane, now 33.5 us, 6.1 TB/s, the
-// codes partly from the last-level cache; 64 tokens 3.9 us, of which the chain of
+// codes partly from the last-level cache; 64 tokens 3.7 us, of which the chain of
 // three reads is most: with one vector a lane they take 2.8 us, but the call, which
 // a launch's latency bounds, no less).
 template <class T, int L, bool INT8>

@@ -214,8 +214,9 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // which is what bounds long contexts: 32 trees of 8 (4 queries a head) over up to
 // 32768 tokens (dim 128) 277 us, 5.1 TB/s of cache. With 52 queries a head, 16 trees
 // of 13 over up to 8192 (dim 64, f16) 55 us, the cache's bytes are 19 us of it and
-// the instructions of the softmax and of widening the codes bound it; one token over
-// 4096 8.0 us, where a step's latency does.
+// the instructions of the softmax and of widening the codes bound it (some 24 us of
+// issue slots, 7 us of the matrix unit); one token over 4096 8.0 us, where a step's
+// latency does.
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
 __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
