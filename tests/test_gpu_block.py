@@ -157,6 +157,22 @@ def test_product(M, N, K, dtype):
         assert (buf[:, N + 1:] == -9.0).all()
 
 
+# few rows of large weights, tiles of 128 with K in parts and whole, tiles of 256, each with a short last block
+LARGE = [(20, 8300, 300), (32, 500, 4200), (1100, 1030, 4300), (2000, 2300, 385), (3900, 2901, 200), (3900, 2816, 512)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_large_products(M, N, K, dtype):
+    test_product(M, N, K, dtype)
+
+
+@pytest.mark.parametrize("M,N,K", [(2000, 2300, 385), (3900, 2901, 200)])
+@pytest.mark.parametrize("br", [1, 128])
+def test_large_products_pass_on_what_is_not_finite(M, N, K, br):
+    test_product_passes_on_what_is_not_finite(M, N, K, br)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 40, 300), (70, 200, 200)])
 @pytest.mark.parametrize("br", [1, 128])
 def test_product_passes_on_what_is_not_finite(M, N, K, br):
