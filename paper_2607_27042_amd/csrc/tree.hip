@@ -289,6 +289,8 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[t][j] = f4{0, 0, 0, 0};
   }
+  float minus = -1.0f;  // (unknown to the compiler, which would make a multiply-add with it a subtraction)
+  asm("" : "+s"(minus));
   float vref = 0x1p-120f;  // a power of two, at least the largest value scale so far
 
   // Tokens are kept once: as soon as the keys of a step are widened, those of the
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
       top[t] = z[t][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], z[t][i >> 2][i & 3]);
-      moves |= (top[t] - m[t]) * qs[t] > 10.0f;
+      moves |= fmaf(top[t], qs[t], -m[t]) > 10.0f;
     }
     if (__any(moves)) {
       vmax = fminf(fmaxf(quad_max(vmax), vref), 0x1p126f);
@@ -385,8 +387,8 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
       vref = up;
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        top[t] = fmaxf(quad_max(top[t]), m[t]);
-        const float d = __builtin_amdgcn_exp2f((m[t] - (top[t] == -INFINITY ? 0.0f : top[t])) * qs[t]);
+        top[t] = fmaxf(quad_max(top[t]) * qs[t], m[t]);
+        const float d = __builtin_amdgcn_exp2f(m[t] - (top[t] == -INFINITY ? 0.0f : top[t]));
         sum[t] *= d;
         m[t] = top[t];
 #pragma unroll
@@ -404,8 +406,8 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        // the maximum is taken off before the query's scale comes in
-        const float e = __builtin_amdgcn_exp2f((z[t][i >> 2][i & 3] - base) * qs[t]);
+        // (one rounding, of the difference; any reference would do)
+        const float e = __builtin_amdgcn_exp2f(fmaf(z[t][i >> 2][i & 3], qs[t], -base));
         sum[t] += e;
         y[i] = e * vs[i >> 2][i & 3];
       }
@@ -418,8 +420,8 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
         const h2 hi = __builtin_convertvector(fp2{y[i], y[i + 1]}, h2);
         p[t][0][i] = hi[0], p[t][0][i + 1] = hi[1];
         if constexpr (ZP == 2) {
-          const h2 lo = __builtin_convertvector(fp2{y[i] - (float)hi[0], y[i + 1] - (float)hi[1]}, h2);
-          p[t][1][i] = lo[0], p[t][1][i + 1] = lo[1];
+          // y - hi as one instruction that reads halves and writes them
+          p[t][1][i] = (_Float16)fmaf((float)hi[0], minus, y[i]), p[t][1][i + 1] = (_Float16)fmaf((float)hi[1], minus, y[i + 1]);
         }
       }
     }
@@ -456,7 +458,6 @@ __global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) vo
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     sum[t] = quad_sum(sum[t]);
-    m[t] *= qs[t];  // the same in every lane of a query
     if (g == 0) lm[w][16 * t + c] = m[t], ll[w][16 * t + c] = sum[t];
   }
 #pragma unroll
