@@ -21,6 +21,9 @@ constexpr int kBalanced = 256;   // sequences whose lengths a work group looks a
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2E = 1.44269504088896341f;
 
+// work groups of k_tree that a compute unit's registers and LDS are to hold at once
+constexpr int groups_a_unit(int dp, int tiles) { return dp < 256 && dp * tiles <= 256 ? 2 : 1; }
+
 struct TreeArgs {
   int seqs, width, kv, group, dim, rows;  // rows = width * group: queries of a sequence that share a kv head
   gptq2d_dtype dt;
@@ -213,12 +216,12 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // waves at the end. One kv head's tokens are read once for all queries that share it,
 // which is what bounds long contexts: 32 trees of 8 (4 queries a head) over up to
 // 32768 tokens (dim 128) 277 us, 5.1 TB/s of cache. With 52 queries a head, 16 trees
-// of 13 over up to 8192 (dim 64, f16) 55 us, the cache's bytes are 19 us of it and
-// the instructions of the softmax and of widening the codes bound it (some 24 us of
+// of 13 over up to 8192 (dim 64, f16) 52 us, the cache's bytes are 19 us of it and
+// the instructions of the softmax and of widening the codes bound it (some 20 us of
 // issue slots, 7 us of the matrix unit); one token over 4096 8.0 us, where a step's
 // latency does.
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
-__global__ __launch_bounds__(64 * kWaves, DP < 256 && DP * QT <= 256 ? 2 : 1) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
   __shared__ float lo[kWaves][16 * QT][DP + 4];
@@ -603,14 +606,20 @@ int query_tiles(int rows, int dim, bool f32) {
   return std::min(most, rows <= 16 ? 1 : rows <= 32 ? 2 : 4);
 }
 
-// Parts that a sequence's tokens are split into: as many as give the device two
-// work groups a compute unit, which is what the registers let run at once. At
-// 256 / 512 / 1024 / 2048 work groups: 16 trees of 13 over up to 8192 tokens
-// (dim 64) 75 / 58 / 65 / 76 us, 32 trees of 8 over up to 32768 (dim 128) 310 /
-// 311 / 312 / 300 us, one token over 4096 10.7 / 11.5 / 11.4 / 11.5 us.
+// Parts that a sequence's tokens are split into: as many as run at once. Where a work
+// group has a compute unit to itself, one more than fit would take a second round: 12
+// trees of 5 (dim 256, 96 work groups a part, 256 at once) 61 us in 2 parts, 81 in 3, 85
+// in 6; 20 of 40 over 308 tokens (240) 17 us whole, 35 in 2. Where two share one, a few
+// more than fit do no harm: 40 tokens over 8000 (320 work groups a part, 512 at once) 116
+// us whole, 98 in 2 parts, 95 in 3; 32 of 2 x 16 queries a head over 853 (416) 26 us
+// whole, 38 in 2; 16 of 13 over 8192 (128) 60 / 59 / 59 / 70 us in 2 / 3 / 4 / 6; 32 of 8
+// over 32768 (256) 302 / 287 / 306 us in 1 / 2 / 4. (10 trees of 32 x 8 queries a head, 80
+// and 256 at once: 170 us in 3 parts, 155 in 7, 181 in 8.)
 int split_count(int64_t seqs, int rows, int kv, int dim) {
-  const int64_t groups = seqs * kv * ceil_div(rows, 16 * query_tiles(rows, dim, false));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, ceil_div(512, groups)));
+  const int tiles = query_tiles(rows, dim, false), a_unit = groups_a_unit(padded(dim), tiles);
+  const int64_t groups = seqs * kv * ceil_div(rows, 16 * tiles);
+  const int64_t fit = a_unit == 1 ? 256 / groups : (512 + 2 * groups / 5) / groups;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, fit));
 }
 
 // parts that the longest sequence may have: up to twice the mean's
