@@ -515,7 +515,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
 // Bound by the weights' bytes and one memory latency: 1 x 4096 x 4096 5.8 us, 2.9 TB/s.
 template <class T, int TM, bool ROWS, bool EXACT, int FUSED>
 __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
-  constexpr int U = TM == 1 ? 4 : 2;  // (with four, two of these work groups do not fit a compute unit's registers)
+  constexpr int U = TM == 1 ? 4 : TM == 2 ? 2 : 1;  // (with more, two work groups do not fit a compute unit's registers)
   __shared__ f4 sum[8][TM][64];
   __shared__ __align__(16) uint8_t own[FUSED ? 8 : 1][U][FUSED ? FUSED : 1][kBlock];
   const int n0 = blockIdx.x * 16, l = threadIdx.x & 63, c = l & 15, g = l >> 4;
@@ -658,8 +658,11 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
   // Few rows, against 64 x 64 tiles, at 4096 x 4096: 16 rows 6.4 and 10.2 us, 32 rows
   // 8.8 and 9.8; with more of the weights a second tile of rows, read from the caches
   // by every work group, costs more than the tiles' join (32 x 11008 x 4096 19.2 and
-  // 17.7 us, 32 x 4096 x 11008 20.3 and 17.6; 16 rows 13.7 and 17.3).
-  if (M <= 16 || (M <= 32 && N <= 8192 && nb <= 32)) return {16, 1};
+  // 17.7 us, 32 x 4096 x 11008 20.3 and 17.6; 16 rows 13.7 and 17.3). Four tiles of rows leave
+  // registers for one block at a time, so K is to be short: 44 x 1536 x 2238 5.5 and 9.4
+  // us, 64 x 2048 x 2048 7.7 and 8.2, 64 x 4096 x 4096 12.8 and 10.4, 33 x 1000 x 11008
+  // 20.8 and 10.9.
+  if (M <= 16 || (M <= 32 && N <= 8192 && nb <= 32) || (M <= 64 && N <= 4096 && nb <= 20)) return {16, 1};
   auto tiles = [&](int64_t e) { return ceil_div(M, e) * ceil_div(N, e); };
   // A 256 x 256 tile has a compute unit to itself, two of 128 x 128 share one; rounds of
   // them take 60 and 36 us at K = 4096. 8192 x 11008: 6 rounds, 356 us, against 11, 390
@@ -696,7 +699,8 @@ void product_typed(ProductArgs a, const Plan& p, hipStream_t s) {
   if (p.edge == 16) {
     const dim3 grid((a.N + 15) / 16);
     if (a.M <= 16) hipLaunchKernelGGL((k_thin<T, 1, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_thin<T, 2, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
+    else if (a.M <= 32) hipLaunchKernelGGL((k_thin<T, 2, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_thin<T, 4, ROWS, EXACT, 0>), grid, dim3(512), 0, s, a);
     return;
   }
   if (p.edge == 64) {
