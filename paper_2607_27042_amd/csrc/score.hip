@@ -242,8 +242,8 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
     if (t == 0) pool.count = 0, pool.limit = 0;
     __syncthreads();
   }
-  // the steps inside the row are loaded whole, one ahead; the first and the last
-  // may reach past it, and are loaded element by element
+  // the steps inside the row are loaded whole, one ahead; the first and the last may
+  // reach past it
   const int inner = lead > 0 ? 1 : 0, outer = (a.vocab + lead) / kChunk - 1;
   typename Piece<T>::V raw[Piece<T>::N];
   const bool any = inner <= outer;
@@ -258,13 +258,30 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
       ahead(c + 1);
     }
     if (c < inner || c > outer) {
-      // (what lies outside is loaded from the row's ends, so that no load waits for a branch)
+      // pieces inside the row are loaded whole (for the others the row's first is, so that
+      // no load waits for a branch), those at its ends element by element
+      constexpr int W = Piece<T>::W, N = Piece<T>::N;
+      const int64_t begin = lead > 0 ? W - lead : 0;
+      typename Piece<T>::V some[N] = {};
+      if (begin + W <= a.vocab) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) v[i] = (float)x[max((int64_t)0, min(index_of<T>(at, i), (int64_t)a.vocab - 1))];
+        for (int i = 0; i < N; ++i) {
+          const int64_t e = index_of<T>(at, i * W);
+          some[i] = *(const typename Piece<T>::V*)(x + (e >= 0 && e + W <= a.vocab ? e : begin));
+        }
+      }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const int64_t e = index_of<T>(at, i);
-        v[i] = e >= 0 && e < a.vocab ? v[i] : -INFINITY;
+      for (int i = 0; i < N; ++i) {
+        const int64_t e = index_of<T>(at, i * W);
+        const bool inside = e >= 0 && e + W <= a.vocab;
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[i * W + j] = inside ? (float)some[i].v[j] : -INFINITY;
+        if (!inside && e + W > 0 && e < a.vocab) {
+#pragma unroll
+          for (int j = 0; j < W; ++j) v[i * W + j] = (float)x[max((int64_t)0, min(e + j, (int64_t)a.vocab - 1))];
+#pragma unroll
+          for (int j = 0; j < W; ++j) v[i * W + j] = e + j >= 0 && e + j < a.vocab ? v[i * W + j] : -INFINITY;
+        }
       }
     }
     float m = v[0];
