@@ -224,7 +224,7 @@ __device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t ro
 // TOP: an element below the limit (the top-th best so far) is none of the best; the
 // first step sets a limit that few pass, so ranking is seldom. Bound by its bytes:
 // 4096 x 128000 bf16 with top 8 222 us, 4.7 TB/s; 2047 x 50257 50 us, 4.1 TB/s, whose
-// rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 9.5 us: the
+// rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 9.0 us: the
 // first limit and one ranking of candidates (without top 4.4 us).
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
@@ -402,7 +402,7 @@ struct GradArgs {
 
 // One pass, element by element. Rows of logits and gradients that start at the
 // same distance from a 16-byte boundary are moved in 16-byte pieces. Bound by its
-// bytes: 2047 x 50257 bf16 93 us, 4.4 TB/s read and written.
+// bytes: 2047 x 50257 bf16 96 us, 4.3 TB/s read and written.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   constexpr int W = 16 / sizeof(T);
