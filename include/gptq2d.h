@@ -384,6 +384,11 @@ size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, 
  *   z = scale q.k, O = sum softmax(z) v
  *   lse (nullable): log sum e^z of every row and head (-inf for a row of zeros),
  *       seqs * width x heads.
+ * A drafted token's keys and values, whatever they hold, reach only the rows that
+ * see it; one with a NaN code among its values is NaN as a whole to those. A
+ * token's part in a row, probability times value scale, counts down to about 2^-29 of
+ * the row's largest probability times the largest value scale that it sees (of a few
+ * tokens around it).
  * Sums and the softmax are held in 32 bits. Queries and probabilities enter the
  * products as 16-bit floats (after scaling by a power of two), or as the sum of
  * two where dt is F32. A context past the table's last page ends there; the

@@ -95,6 +95,15 @@ __device__ __forceinline__ float quad_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// log2 of a value scale, rounded up, plus kLevel, in bits 8 to 15: products of e^z and
+// value scales reach 2^5 then, and 2^15 before a reference moves, which halves hold, and
+// stay normal halves down to 2^-19. Scales below 2^-80 count as that, or the sum of the
+// exponentials could overflow.
+constexpr float kLevel = 132.0f;
+__device__ __forceinline__ uint32_t value_level(float v) {
+  return max((__float_as_uint(v) + 0x7fffffu) >> 23, 52u) << 8;
+}
+
 // One wave's 32 tokens as they lie in the cache. A lane (c = l % 16, g = l / 16)
 // holds of the keys a quarter (g) of token c of each 16-token row, and of the
 // values sixteenth c of tokens 4 g .. 4 g + 3 of each row: both are what the
@@ -207,8 +216,8 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // Codes are widened to halves, exactly. A query is scaled by a power of two so
 // that its largest element is in [1, 2) and rounded to halves (which a 16-bit
 // query survives, but for elements below 2^-14 of the largest); probabilities
-// are taken times vs over the largest vs so far (as a power of two), so they
-// lie in [0, 1]. Queries are kept as ZQ halves (two of them, 22 bits, for 32-bit
+// are taken times vs, relative to the query's largest such product so far (a bound
+// of it: the largest score times the largest vs of a step), and so is their sum. Queries are kept as ZQ halves (two of them, 22 bits, for 32-bit
 // queries), probabilities as ZP (one, rounded by 2^-11 at most, where the result
 // is rounded by 2^-8 after it).
 //
@@ -294,7 +303,6 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
   }
   float minus = -1.0f;  // (unknown to the compiler, which would make a multiply-add with it a subtraction)
   asm("" : "+s"(minus));
-  float vref = 0x1p-120f;  // a power of two, at least the largest value scale so far
 
   // Tokens are kept once: as soon as the keys of a step are widened, those of the
   // next one are on their way into their registers, and likewise the values. (The
@@ -302,6 +310,26 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
   // the compiler wait for all of them at its end.)
   for (; tok < end; tok += kStride) {
     const Entry after = look_up(a, table, tok + 2 * kStride, end);
+    if constexpr (!INT8) {
+      if (tok + kStep > ctx) {
+        // A drafted token whose values hold a NaN code is NaN as a whole, by its scale: a
+        // code would reach the queries that do not see it, as 0 times NaN.
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < DP / 64; ++e) top |= (x.v[h][i][e] & 0x7f7f7f7fu) + 0x01010101u;
+            top = tok + 16 * h + 4 * g + i >= ctx ? top & 0x80808080u : 0;
+            if (group_max<16>(top) != 0) {
+              x.vs[h][i] = __uint_as_float(0x7fc00000u);
+#pragma unroll
+              for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
+            }
+          }
+      }
+    }
     // scores
     h8 kf[2][KS];
 #pragma unroll
@@ -332,7 +360,8 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
       for (int h = 0; h < 2; ++h) z[t][h] *= x.ks[h];
     f4 vs[2] = {x.vs[0], x.vs[1]};
     fetch_scales(x, a, next, hkv, g);
-    // bit 4 h + i: token tok + 16 h + 4 g + i is seen by query t
+    // bit 4 h + i: token tok + 16 h + 4 g + i is seen by query t; bits 8 to 15: the level
+    // of the value scales that it sees
     uint32_t ok[QT];
     const bool edge = tok + kStep > min(ctx, end) || now.page[0] < 0 || now.page[1] < 0;
     if (edge) {
@@ -368,39 +397,45 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (!((ok[t] >> (4 * h + i)) & 1)) z[t][h][i] = -INFINITY;
-    }
-    // What the exponents and the value scales are relative to moves when a score
-    // exceeds it by more than 2^10, or a value scale at all, which is seldom after
-    // the first tokens. The value scales' reference is a power of two.
-    float vmax = 0, top[QT];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) vmax = fmaxf(vmax, vs[i >> 2][i & 3]);
-    bool moves = vmax > vref;
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      top[t] = z[t][0][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], z[t][i >> 2][i & 3]);
-      moves |= fmaf(top[t], qs[t], -m[t]) > 10.0f;
-    }
-    if (__any(moves)) {
-      vmax = fminf(fmaxf(quad_max(vmax), vref), 0x1p126f);
-      const float up = __uint_as_float((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u);
-      const float fade = vref * __uint_as_float((254u << 23) - __float_as_uint(up));
-      vref = up;
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        top[t] = fmaxf(quad_max(top[t]) * qs[t], m[t]);
-        const float d = __builtin_amdgcn_exp2f(m[t] - (top[t] == -INFINITY ? 0.0f : top[t]));
-        sum[t] *= d;
-        m[t] = top[t];
+        float most = 0;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) o[t][j] *= fade * d;
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, (ok[t] >> i) & 1 ? vs[i >> 2][i & 3] : 0.0f);
+        ok[t] |= value_level(most);
       }
     }
-    const float vinv = __uint_as_float((254u << 23) - __float_as_uint(vref));
+    // A query's reference m moves when the largest score it sees, times the largest
+    // value scale it sees, exceeds it by more than 2^10, which is seldom after the
+    // first tokens. A value that it does not see, however large, does not move it.
+    if (!edge) {
+      float most = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) vs[h] *= vinv;
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, vs[i >> 2][i & 3]);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) ok[t] = value_level(most);
+    }
+    auto most = [&](int t) {
+      float v = z[t][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) v = fmaxf(v, z[t][i >> 2][i & 3]);
+      return v;
+    };
+    auto level = [&](int t) { return (float)((ok[t] >> 8) & 0xff); };
+    bool moves = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) moves |= fmaf(most(t), qs[t], level(t)) - m[t] > kLevel + 10.0f;
+    if (__any(moves)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float top = fmaxf(quad_max(most(t)) * qs[t] + (quad_max(level(t)) - kLevel), m[t]);
+        const float d = __builtin_amdgcn_exp2f(m[t] - (top == -INFINITY ? 0.0f : top));
+        sum[t] *= d;
+        m[t] = top;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) o[t][j] *= d;
+      }
+    }
     // probabilities
     h8 p[QT][ZP];
 #pragma unroll
@@ -470,7 +505,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
 #pragma unroll
       for (int j = 0; j < NT; j += 4)
         *(f4*)&lo[w][16 * t + c][(4 * g + i) * NT + j] =
-            f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]} * vref;
+            f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < QT; ++t) {

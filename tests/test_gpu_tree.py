@@ -225,6 +225,39 @@ def test_nothing_masked_takes_part(code):
     assert torch.equal(O[0, :, :2], O0[0, :, :2]) and torch.equal(O[1], O0[1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("code,group,dim", [("e4m3", 2, 64), ("int8", 10, 64), ("e4m3", 6, 128), ("int8", 1, 256)])
+@pytest.mark.parametrize("what", ["large", "infinite", "codes"])
+def test_values_that_are_not_seen_change_nothing(what, code, group, dim, dtype):
+    """A drafted token whose values are large (2^100), infinite or NaN codes: the queries that do
+    not see it keep their results to the usual bounds, those that see it do not hide it (where its
+    probability is within 2^-20 of the largest: halves hold its part then)."""
+    c = Case([50, 20, 0], 6, 2, group, dim, 16, code, dtype, seed=11)
+    p, off = int(c.table[0, 53 // 16]), 53 % 16
+    if what == "codes":
+        if code == "int8":
+            pytest.skip("every int8 code is a number")
+        c.C[1].view(torch.uint8)[p, 1, off, dim - 1] = 0xFF
+    else:
+        c.S[1][p, 1, off] = 2.0 ** 100 if what == "large" else math.inf
+    O, lse = c.run()
+    o, l, bo, bl = c.reference()
+    hit = torch.zeros(3, 6, 2, group, 1, dtype=torch.bool, device="cuda")
+    hit[0, :, 1, :, 0] = c.sees(0)[:, 3, None]
+    err = ((O.double() - o).abs() <= bo).view(3, 6, 2, group, dim)
+    assert hit.any() and err.logical_or(hit).all()
+    k, q = c.kv_values[0][0][:, 1], c.Q.double().view(3, 6, 2, group, dim)[0, :, 1]
+    z = c.scale * torch.einsum("tgd,xd->tgx", q.cpu(), k.cpu())
+    sees = torch.cat([torch.ones(6, 50, dtype=torch.bool), c.sees(0).cpu()], 1)
+    z = z.masked_fill(~sees[:, None], -math.inf)
+    counts = z[..., 53] > z.amax(-1) - 20 * math.log(2)
+    seen = O.float().view(3, 6, 2, group, dim)[0, :, 1].cpu()[counts]
+    assert len(seen) > 0 and (~(seen.abs() < 1e4)).any(-1).all()
+    if what == "large":
+        near = (lse.double() - l).abs() <= bl + 2.0 ** -24 * 128
+        assert near.all()
+
+
 def test_tables_that_end_or_name_no_page():
     c = Case([70, 100], 4, 1, 2, 64, 16, "e4m3", "bf16", seed=9)
     # a page of the context missing: its tokens are absent
