@@ -224,10 +224,10 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // Each wave streams its own tokens from memory to registers; LDS only joins the four
 // waves at the end. One kv head's tokens are read once for all queries that share it,
 // which is what bounds long contexts: 32 trees of 8 (4 queries a head) over up to
-// 32768 tokens (dim 128) 277 us, 5.1 TB/s of cache. With 52 queries a head, 16 trees
-// of 13 over up to 8192 (dim 64, f16) 52 us, the cache's bytes are 19 us of it and
+// 32768 tokens (dim 128) 281 us, 5.0 TB/s of cache. With 52 queries a head, 16 trees
+// of 13 over up to 8192 (dim 64, f16) 55 us, the cache's bytes are 19 us of it and
 // the instructions of the softmax and of widening the codes bound it (some 20 us of
-// issue slots, 7 us of the matrix unit); one token over 4096 8.0 us, where a step's
+// issue slots, 7 us of the matrix unit); one token over 4096 8.2 us, where a step's
 // latency does.
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
 __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(TreeArgs a) {
@@ -314,20 +314,25 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
       if (tok + kStep > ctx) {
         // A drafted token whose values hold a NaN code is NaN as a whole, by its scale: a
         // code would reach the queries that do not see it, as 0 times NaN.
+        auto nan = [&](int h, int i) {
+          uint32_t top = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int e = 0; e < DP / 64; ++e) top |= (x.v[h][i][e] & 0x7f7f7f7fu) + 0x01010101u;
+          return tok + 16 * h + 4 * g + i >= ctx ? top & 0x80808080u : 0u;
+        };
+        uint32_t any = 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t top = 0;
+        for (int i = 0; i < 8; ++i) any |= nan(i >> 2, i & 3);
+        // (two halves a query leave no registers for the way around)
+        if (ZQ == 2 || __any(any != 0)) {
 #pragma unroll
-            for (int e = 0; e < DP / 64; ++e) top |= (x.v[h][i][e] & 0x7f7f7f7fu) + 0x01010101u;
-            top = tok + 16 * h + 4 * g + i >= ctx ? top & 0x80808080u : 0;
-            if (group_max<16>(top) != 0) {
-              x.vs[h][i] = __uint_as_float(0x7fc00000u);
+          for (int i = 0; i < 8; ++i)
+            if (group_max<16>(nan(i >> 2, i & 3)) != 0) {
+              x.vs[i >> 2][i & 3] = __uint_as_float(0x7fc00000u);
 #pragma unroll
-              for (int e = 0; e < DP / 64; ++e) x.v[h][i][e] = 0;
+              for (int e = 0; e < DP / 64; ++e) x.v[i >> 2][i & 3][e] = 0;
             }
-          }
+        }
       }
     }
     // scores
@@ -407,7 +412,9 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
     }
     // A query's reference m moves when the largest score it sees, times the largest
     // value scale it sees, exceeds it by more than 2^10, which is seldom after the
-    // first tokens. A value that it does not see, however large, does not move it.
+    // first tokens. A value that it does not see, however large, does not move it. (One
+    // reference of the value scales for all queries took 52 us where this takes 55, and gave
+    // zeros to the queries beside one that saw a value 2^30 times theirs.)
     if (!edge) {
       float most = 0;
 #pragma unroll
