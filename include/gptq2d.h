@@ -412,9 +412,11 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
  *
  * For a row of logits x (vocab of them) and z = scale x: lse = log sum e^z, the
  * given token's log probability z_y - lse, the entropy -sum p log p and the `top`
- * largest logits. Sums are held in 32 bits. A logit of -inf has probability 0. A
- * row of nothing else has lse = -inf, entropy 0 and log probabilities -inf; a row
- * with a NaN or +inf comes out as NaN (its alternatives in order all the same, NaN
+ * largest logits. Sums are held in 32 bits and taken, like all but lse, of
+ * differences to the row's largest logit: what a row's logits have in common costs
+ * no accuracy. A logit of -inf has probability 0. A row of nothing else has lse =
+ * -inf, entropy 0 and log probabilities -inf; a row with a NaN or +inf comes out as
+ * NaN (its alternatives in order all the same, NaN
  * first). rows <= 2^22, vocab <= 2^28, top <= 64, scale positive and finite.
  * ------------------------------------------------------------------------- */
 

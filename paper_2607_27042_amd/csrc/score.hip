@@ -4,6 +4,8 @@
 // For a row of logits x and z = a x (a = 1 / temperature):
 //   lse = log sum e^z, lp = z_y - lse, H = lse - sum p z, p = e^(z - lse)
 //   dx = a (g_lp (1[y] - p) - g_H p (log p + H))
+// All of them but lse are functions of the differences to the row's largest logit, and
+// are computed from these.
 #include <math.h>
 
 #include <algorithm>
@@ -187,35 +189,36 @@ __device__ __forceinline__ void load_whole(const T* x, int64_t step, typename Pi
     raw[i] = *(const typename Piece<T>::V*)(x + index_of<T>(step, i * Piece<T>::W));
 }
 
+// m, l: the largest logit and the logarithm of the sum relative to it
 struct Out {
-  float lse, entropy;
+  float lse, entropy, m, l;
 };
 __device__ __forceinline__ Out finish(const ScoreArgs& a, Sums s) {
   // every logit -inf: the sum is empty
-  if (s.m == -INFINITY && s.s1 == 0.0f) return {-INFINITY, 0.0f};
+  if (s.m == -INFINITY && s.s1 == 0.0f) return {-INFINITY, 0.0f, 0.0f, 0.0f};
   const float l = logf(s.s1), h = l - a.a * (s.s2 / s.s1);
-  return {fmaf(s.m, a.a, l), h < 0.0f ? 0.0f : h};
+  return {fmaf(s.m, a.a, l), h < 0.0f ? 0.0f : h, s.m, l};
 }
 
-__device__ __forceinline__ float logprob_of(float z, float lse) {
-  return z == -INFINITY && lse == lse ? -INFINITY : z - lse;
-}
+// From the difference to the largest logit, as the sums are: a x - lse would be
+// rounded at the size of lse (32000 equal logits of -1e9 would have probability 1).
+__device__ __forceinline__ float logprob_of(float x, float a, Out o) { return fmaf(x - o.m, a, -o.l); }
 
 template <class T>
-__device__ __forceinline__ float target_logprob(const ScoreArgs& a, int64_t row, float lse) {
+__device__ __forceinline__ float target_logprob(const ScoreArgs& a, int64_t row, Out o) {
   if (!a.target) return 0.0f;
   const int64_t y = a.target[row];
   if (y < 0) return 0.0f;
   if (y >= a.vocab) return __uint_as_float(0x7fc00000u);
-  return logprob_of((float)((const T*)a.X)[row * a.ldx + y] * a.a, lse);
+  return logprob_of((float)((const T*)a.X)[row * a.ldx + y], a.a, o);
 }
 
-__device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t row, float lse) {
+__device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t row, Out o) {
   const int t = threadIdx.x;
   if (t >= a.top) return;
   const uint64_t k = p.key[t];
   a.ids[row * a.top + t] = (int32_t)key_index(k);
-  a.tops[row * a.top + t] = logprob_of(key_value(k) * a.a, lse);
+  a.tops[row * a.top + t] = logprob_of(key_value(k), a.a, o);
 }
 
 // One work group per part of a row, one pass. Each thread sums relative to its
@@ -353,9 +356,9 @@ __global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
   if (t == 0) {
     a.lse[row] = o.lse;
     a.entropy[row] = o.entropy;
-    a.logprob[row] = target_logprob<T>(a, row, o.lse);
+    a.logprob[row] = target_logprob<T>(a, row, o);
   }
-  if constexpr (TOP) put_best(pool, a, row, o.lse);
+  if constexpr (TOP) put_best(pool, a, row, o);
 }
 
 // One work group per row: its parts' sums, and the best of their best. One row of
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
   if (t == 0) {
     a.lse[row] = o.lse;
     a.entropy[row] = o.entropy;
-    a.logprob[row] = target_logprob<T>(a, row, o.lse);
+    a.logprob[row] = target_logprob<T>(a, row, o);
   }
   if constexpr (TOP) {
     const int n = a.parts * a.top;  // at most kMaxParts kMaxTop = kChunk
@@ -384,7 +387,7 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
     for (int i = t; i < n; i += kThreads) pool.key[i] = a.keys[row * n + i];
     __syncthreads();
     keep_best(pool, a.top);
-    put_best(pool, a, row, o.lse);
+    put_best(pool, a, row, o);
   }
 }
 
