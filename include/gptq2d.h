@@ -442,7 +442,7 @@ gptq2d_status gptq2d_token_logprobs(int64_t rows, int64_t vocab, gptq2d_dtype dt
  * from g_logprob and g_entropy (device, rows entries; either may be NULL), the
  * gradients of the log probabilities and entropies, with lse and entropy as the
  * call above gave them (entropy is read with g_entropy only, target with g_logprob
- * only):
+ * only; where lse is past +-128, the row is summed again instead):
  *   dx = scale (g_logprob (1[y] - p) - g_entropy p (log p + entropy))
  * A row without a target takes no part in g_logprob, a row of -inf has gradient 0,
  * and one with a target past the vocabulary NaN. Errors: INVALID_ARG, HIP. */

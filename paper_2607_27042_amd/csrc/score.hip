@@ -401,42 +401,81 @@ struct GradArgs {
   const float *lse, *entropy, *gl, *gh;
   void* D;
   int64_t ldd;
+  bool shared;  // the gradients share memory with the logits
 };
+
+// Past it lse, a 32-bit number, is off by more than 2^-18, and p by as much of itself.
+constexpr float kNear = 128.0f;
 
 // One pass, element by element. Rows of logits and gradients that start at the
 // same distance from a 16-byte boundary are moved in 16-byte pieces. Bound by its
 // bytes: 2047 x 50257 bf16 96 us, 4.3 TB/s read and written.
+// A row whose lse is far from zero (or not a 32-bit number at all) is summed again
+// first, relative to its largest logit. Every part of a row does that for itself; where
+// one part's gradients would take the place of logits that another has yet to
+// sum, the first part takes the whole row.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   constexpr int W = 16 / sizeof(T);
+  struct alignas(16) V { T v[W]; };
+  __shared__ Sums wave[kThreads / 64];
   const int row32 = blockIdx.x / (uint32_t)a.parts, part = blockIdx.x - row32 * a.parts;
   const int64_t row = row32;
   const T* x = (const T*)a.X + row * a.ldx;
   T* d = (T*)a.D + row * a.ldd;
   const float lse = a.lse[row];
+  const bool far = fabsf(lse) > kNear, whole = far && a.shared;
+  if (whole && part > 0) return;
   const float gl = a.gl ? a.gl[row] : 0.0f, gh = a.gh ? a.gh[row] : 0.0f;
   const float H = gh != 0.0f ? a.entropy[row] : 0.0f;
   const int64_t y = a.target ? a.target[row] : -1;
   const bool given = y >= 0 && y < a.vocab;
   const float g = given ? gl : y >= a.vocab ? gl * __uint_as_float(0x7fc00000u) : 0.0f;
-  const float l2 = lse * kLog2E;
+  const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));
+  const int64_t n = a.vocab + lead;
+  float m = 0.0f, l = lse;  // log p = a (x - m) - l
+  if (far) {
+    Sums s{-INFINITY, 0.0f, 0.0f};
+    auto add = [&](float v) {
+      if (v > s.m) {
+        s.s1 *= __builtin_amdgcn_exp2f((s.m - v) * a.a2);
+        s.m = v;
+      }
+      if (v != -INFINITY) s.s1 += __builtin_amdgcn_exp2f((v - s.m) * a.a2);
+    };
+    for (int64_t e = threadIdx.x * W; e < n; e += kThreads * W) {
+      const int64_t i0 = e - lead;
+      if (i0 >= 0 && i0 + W <= a.vocab) {
+        const V in = *(const V*)(x + i0);
+#pragma unroll
+        for (int j = 0; j < W; ++j) add((float)in.v[j]);
+      } else {
+        for (int j = 0; j < W; ++j)
+          if (i0 + j >= 0 && i0 + j < a.vocab) add((float)x[i0 + j]);
+      }
+    }
+    s = wave_join(s, a.a2);
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = join(join(wave[0], wave[1], a.a2), join(wave[2], wave[3], a.a2), a.a2);
+    m = s.m, l = logf(s.s1);
+  }
   auto one = [&](float v, int64_t i) {
-    const float q = fmaf(v, a.a2, -l2);  // log2 p
-    const float p = __builtin_amdgcn_exp2f(q);
-    float r = -p * (g + gh * (fmaxf(q, -1000.0f) * kLn2 + H));
+    const float q = fmaf(v - m, a.a, -l);
+    const float p = __builtin_amdgcn_exp2f(q * kLog2E);
+    float r = -p * (g + gh * (fmaxf(q, -700.0f) + H));
     if (i == y) r += g;
     // a row without a finite logit has no gradient
-    return lse == -INFINITY ? 0.0f : a.a * r;
+    return m == -INFINITY ? 0.0f : a.a * r;
   };
-  const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));
   const bool wide = (((uintptr_t)x ^ (uintptr_t)d) & 15) == 0;
-  const int64_t n = a.vocab + lead, per = (n + a.parts - 1) / a.parts;
+  const int parts = whole ? 1 : a.parts;
+  const int64_t per = (n + parts - 1) / parts;
   const int64_t span = (per + kThreads * W - 1) / (kThreads * W) * (kThreads * W);
   const int64_t end = min(n, span * (part + 1));
   for (int64_t e = span * part + threadIdx.x * W; e < end; e += kThreads * W) {
     const int64_t i0 = e - lead;
     if (wide && i0 >= 0 && i0 + W <= a.vocab) {
-      struct alignas(16) V { T v[W]; };
       const V in = *(const V*)(x + i0);
       V out;
 #pragma unroll
@@ -537,7 +576,9 @@ gptq2d_status gptq2d_token_logprobs_backward(int64_t rows, int64_t vocab, gptq2d
   if (!aligned(X, es) || !aligned(dX, es) || !aligned(target, 8) || !aligned(lse, 4) || !aligned(entropy, 4) ||
       !aligned(g_logprob, 4) || !aligned(g_entropy, 4))
     return refuse("an argument is not aligned to its elements");
-  GradArgs a = {rows, (int)vocab, 1, X, ldx, scale, scale * kLog2E, target, lse, entropy, g_logprob, g_entropy, dX, lddx};
+  GradArgs a = {rows, (int)vocab, 1, X, ldx, scale, scale * kLog2E, target, lse, entropy, g_logprob, g_entropy, dX, lddx,
+                (uintptr_t)X < (uintptr_t)dX + ((rows - 1) * lddx + vocab) * es &&
+                    (uintptr_t)dX < (uintptr_t)X + ((rows - 1) * ldx + vocab) * es};
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, rows), ceil_div(vocab, 4096)));
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
