@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void k_score_grad(GradArgs a) {
   if (whole && part > 0) return;
   const float gl = a.gl ? a.gl[row] : 0.0f, gh = a.gh ? a.gh[row] : 0.0f;
   const float H = gh != 0.0f ? a.entropy[row] : 0.0f;
-  const int64_t y = a.target ? a.target[row] : -1;
+  const int64_t y = a.gl ? a.target[row] : -1;  // (past the vocabulary it would make NaN of the entropy's part too)
   const bool given = y >= 0 && y < a.vocab;
   const float g = given ? gl : y >= a.vocab ? gl * __uint_as_float(0x7fc00000u) : 0.0f;
   const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));
