@@ -591,9 +591,11 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int s = s0 + u * G;
-      const float fs = s < a.splits ? __shfl(f, s) : 0.0f;
+      const float fs = __shfl(f, s & 63);
+      // an empty part is not written; one far below the best is, and may hold a NaN
+      const bool there = s < a.splits && __shfl(ls, s & 63) != 0.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += fs == 0.0f ? 0.0f : x[u][e] * fs;  // an empty part is not written
+      for (int e = 0; e < E; ++e) v[e] += there ? x[u][e] * fs : 0.0f;
     }
   }
   if constexpr (G > 1) {
