@@ -291,6 +291,13 @@ __device__ __forceinline__ void tile_of(int id, int total, int tn, int tm, int& 
   bn = w / h;
 }
 
+// acc + p a b for two scales, wherever the result is in range. Where one scale is below
+// one and the other is not, their product is as well; otherwise p may take them one by one.
+__device__ __forceinline__ float add_scaled(float p, float a, float b, float acc) {
+  const bool first = (fabsf(a) >= 1.0f) != (fabsf(b) >= 1.0f);
+  return fmaf(p * (first ? a * b : a), first ? 1.0f : b, acc);
+}
+
 template <class T>
 __device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
   if (wide && n >= 4) {
@@ -350,12 +357,16 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
     for (int j = 0; j < TM; ++j) acc[i][j] = f4{0, 0, 0, 0};
   Stage<BN, THREADS> gw;
   Stage<BM, THREADS> gx;
-  gw.init(a.W, a.ldw, n0, a.N);
-  gx.init((const uint8_t*)a.X, a.ldx, m0, a.M);
   const bool xs = w < BM / 64;  // (whole waves)
-  const int at = xs ? min(m0 + (int)threadIdx.x, a.M - 1) : min(n0 + (int)threadIdx.x - BM, a.N - 1);
-  const float* ps = xs ? a.SX + at : ROWS ? a.SW + at : a.SW + at / kBlock * a.ldsw;
   const int64_t psl = xs ? a.ldsx : ROWS ? a.ldsw : 1;
+  const float* ps;
+  auto init = [&](int n, int m) {
+    gw.init(a.W, a.ldw, n, a.N);
+    gx.init((const uint8_t*)a.X, a.ldx, m, a.M);
+    const int at = xs ? min(m + (int)threadIdx.x, a.M - 1) : min(n + (int)threadIdx.x - BM, a.N - 1);
+    ps = xs ? a.SX + at : ROWS ? a.SW + at : a.SW + at / kBlock * a.ldsw;
+  };
+  init(n0, m0);
   auto scales = [&](int b, float* ms) {
     __builtin_amdgcn_global_load_lds((const void*)(ps + b * psl), (lds_void*)(ms + (threadIdx.x & ~63)), 4, 0, 0);
   };
@@ -377,10 +388,13 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
   };
   // block b, which lies in lw, lx and ls, while the next one comes into mw, mx and
   // ms. SPREAD: it is whole, and its loads are spread over this one's products
-  // (issued at once they hold up every wave until the memory pipeline has taken them)
+  // (issued at once they hold up every wave until the memory pipeline has taken them).
+  // CARE: sums are scaled one scale at a time where the product of the two, or one of
+  // them, could leave the range; otherwise `rare` tells of scales where that may be.
+  bool rare = false;
   auto step = [&](int b, const uint8_t* lw, const uint8_t* lx, const float* ls, uint8_t* mw, uint8_t* mx, float* ms,
-                  auto spread) {
-    constexpr bool SPREAD = decltype(spread)::value;
+                  auto spread, auto care) {
+    constexpr bool SPREAD = decltype(spread)::value, CARE = decltype(care)::value;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this block's codes and scales are in LDS
     __syncthreads();
     float sx[TM];
@@ -398,7 +412,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
     auto scaled = [&](int i, int j, f4 p) {
       if (ROWS && j == 0) sw = *(const f4*)&ls[BM + wn + 16 * i + 4 * g];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROWS ? p[e] * sw[e] : p[e], sx[j], acc[i][j][e]);
+      for (int e = 0; e < 4; ++e)
+        acc[i][j][e] = CARE ? add_scaled(p[e], ROWS ? sw[e] : u, ls[wm + 16 * j + c], acc[i][j][e])
+                            : fmaf(ROWS ? p[e] * sw[e] : p[e], sx[j], acc[i][j][e]);
     };
     if constexpr (EXACT) {
       h8 fx[TM][4];
@@ -447,28 +463,60 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if constexpr (!CARE) {  // (here, where no product waits for it)
+      if constexpr (ROWS) {
+        // (the work group's threads have them all; the place is formed anew, as 256 x 256
+        // has no register left to hold it)
+        int e = threadIdx.x;
+        asm volatile("" : "+v"(e));
+        const float v = fabsf(ls[e]);
+        rare |= v < 0x1p-100f || v > 0x1p100f;
+      } else {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) rare |= !__builtin_amdgcn_classf(sx[j], 0x10b);  // neither normal nor NaN
+      }
+    }
   };
-  int b = b0;
-  if (b0 < b1) {
+  auto begin = [&]() {
+    if (b0 >= b1) return;
     scales(b0, s0);
     if ((b0 + 1) * kBlock <= a.K)
       share(b0, w0, x0, 0, 1);
     else
       tails(b0, w0, x0);
-  }
+  };
+  auto rest = [&](int b, auto care) {
+    for (bool odd = false; b < b1; ++b, odd = !odd)
+      step(b, odd ? w1 : w0, odd ? x1 : x0, odd ? s1 : s0, odd ? w0 : w1, odd ? x0 : x1, odd ? s0 : s1,
+           std::false_type(), care);
+  };
+  int b = b0;
+  begin();
   for (const int e = min(b1, a.K / kBlock) - 1; b + 1 < e; b += 2) {
-    step(b, w0, x0, s0, w1, x1, s1, std::true_type());
-    step(b + 1, w1, x1, s1, w0, x0, s0, std::true_type());
+    step(b, w0, x0, s0, w1, x1, s1, std::true_type(), std::false_type());
+    step(b + 1, w1, x1, s1, w0, x0, s0, std::true_type(), std::false_type());
   }
-  for (bool odd = false; b < b1; ++b, odd = !odd)  // up to three
-    step(b, odd ? w1 : w0, odd ? x1 : x0, odd ? s1 : s0, odd ? w0 : w1, odd ? x0 : x1, odd ? s0 : s1,
-         std::false_type());
+  rest(b, std::false_type());  // up to three
+  // The whole tile once more where a scale called for it, which finite values of ordinary
+  // sizes never do: 8192 x 11008 x 4096 takes 348 us with and without this. (A choice in
+  // every step takes 280 to 320 registers and spills at 256 x 256.)
+  if (__syncthreads_or(rare)) {
+    int n1 = n0, m1 = m0;  // (unknown to the compiler, which would hold addresses in registers for this)
+    asm("" : "+s"(n1), "+s"(m1));
+    init(n1, m1);
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = f4{0, 0, 0, 0};
+    begin();
+    rest(b0, std::true_type());
+    __syncthreads();
+  }
   // Each wave turns its results through LDS, 16 rows of Y at a time, and stores them
   // row by row, whole lines at a time. Straight from the registers, four results of a
   // lane's row: 3313 x 5770 x 482 bf16 (rows off the 16-byte boundaries) 51 us, now
   // 41; 8192 x 11008 x 4096 394 and 380 us. (Vectors from where a row's own addresses
   // allow them are no faster than one element a lane.)
-  __syncthreads();
   constexpr int EN = BN / WN, PITCH = EN + 4, PER = WN * WM / 4;
   static_assert(PER * 16 * PITCH * 4 <= (BN < BM ? BN : BM) * kBlock, "staged results fit");
   float* own = (float*)(w / PER == 0 ? w0 : w / PER == 1 ? w1 : w / PER == 2 ? x0 : x1) + w % PER * (16 * PITCH);
@@ -621,7 +669,7 @@ __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
           p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[u], fx[u][j], p, 0, 0, 0, 0, 0, 0);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[e] * sw[u][e], sx[u][j], acc[j][e]);
+        for (int e = 0; e < 4; ++e) acc[j][e] = add_scaled(p[e], sw[u][e], sx[u][j], acc[j][e]);
       }
     }
   }
