@@ -385,7 +385,7 @@ size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, 
  *   lse (nullable): log sum e^z of every row and head (-inf for a row of zeros),
  *       seqs * width x heads.
  * A drafted token's keys and values, whatever they hold, reach only the rows that
- * see it; one with a NaN code among its values is NaN as a whole to those. A
+ * see it (a NaN code among them the element it stands in). A
  * token's part in a row, probability times value scale, counts down to about 2^-29 of
  * the row's largest probability times the largest value scale that it sees (of a few
  * tokens around it).

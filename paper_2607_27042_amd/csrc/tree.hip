@@ -24,6 +24,12 @@ constexpr float kLog2E = 1.44269504088896341f;
 // work groups of k_tree that a compute unit's registers and LDS are to hold at once
 constexpr int groups_a_unit(int dp, int tiles) { return dp < 256 && dp * tiles <= 256 ? 2 : 1; }
 
+// The instance whose registers, kept to 128, let a compute unit hold four: one token of 40
+// sequences over 300 (dim 64, f16) 10.8 us, with three 12.4.
+constexpr bool four_a_unit(bool int8, int dp, int tiles, int zq, int zp) {
+  return !int8 && dp == 64 && tiles == 1 && zq < zp;
+}
+
 struct TreeArgs {
   int seqs, width, kv, group, dim, rows;  // rows = width * group: queries of a sequence that share a kv head
   gptq2d_dtype dt;
@@ -117,6 +123,9 @@ struct Tokens {
   f4 ks[2], vs[2];
 };
 
+// the top bits of the bytes that are e4m3's NaNs
+__device__ __forceinline__ uint32_t nan_codes(uint32_t v) { return ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // The table's entries of a wave's next 32 tokens (uniform, looked up ahead of
 // the tokens themselves); an entry that names no page, or tokens from `end` on: -1
 struct Entry {
@@ -186,6 +195,24 @@ __device__ __forceinline__ void fetch_scales(Tokens<DP>& x, const TreeArgs& a, E
   }
 }
 
+// NaN in the results v of N elements from d0 on, for the NaN codes of those drafted tokens
+// first .. end - 1 that query tq sees
+template <int N>
+__device__ __forceinline__ void put_nans(const TreeArgs& a, const int32_t* table, int b, int hkv, int tq, int ctx, int first,
+                                         int end, int d0, float (&v)[N]) {
+  if (d0 >= a.dim) return;
+  const uint64_t sees = a.mask ? a.mask[(int64_t)b * a.width + tq] : ((uint64_t)2 << tq) - 1;
+  for (int x = first; x < end; ++x) {
+    const int pg = x / a.page;
+    const int32_t e = table[pg];
+    if (!((sees >> (x - ctx)) & 1) || e < 0 || e >= a.pages) continue;
+    const uint8_t* p = a.VC + (((int64_t)e * a.kv + hkv) * a.page + (x - pg * a.page)) * a.dim + d0;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if ((p[j] & 0x7f) == 0x7f) v[j] = __uint_as_float(0x7fc00000u);
+  }
+}
+
 // Tokens of a part: the same for all sequences, so that the work groups of long and
 // short ones take alike, as far as the longest one's parts suffice; whole steps.
 // (32 trees of 8, lengths between 8192 and 32768: 278 us, in equal numbers of parts
@@ -230,10 +257,11 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // issue slots, 7 us of the matrix unit); one token over 4096 8.2 us, where a step's
 // latency does.
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
-__global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, four_a_unit(INT8, DP, QT, ZQ, ZP) ? 4 : groups_a_unit(DP, QT)) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
   __shared__ float lm[kWaves][16 * QT], ll[kWaves][16 * QT];
   __shared__ float lo[kWaves][16 * QT][DP + 4];
+  __shared__ int odd[kWaves];
   // parts are the slowest index: work groups go round the XCDs by their number, and
   // the last parts, which few sequences have, are not to meet on a few of them
   const int hkv = blockIdx.x / a.rowblocks, rb = blockIdx.x % a.rowblocks, b = blockIdx.y, split = blockIdx.z;
@@ -301,6 +329,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[t][j] = f4{0, 0, 0, 0};
   }
+  bool found = false;  // a NaN code among the wave's drafted tokens (uniform)
   float minus = -1.0f;  // (unknown to the compiler, which would make a multiply-add with it a subtraction)
   asm("" : "+s"(minus));
 
@@ -312,25 +341,24 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
     const Entry after = look_up(a, table, tok + 2 * kStride, end);
     if constexpr (!INT8) {
       if (tok + kStep > ctx) {
-        // A drafted token whose values hold a NaN code is NaN as a whole, by its scale: a
-        // code would reach the queries that do not see it, as 0 times NaN.
-        auto nan = [&](int h, int i) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int e = 0; e < DP / 64; ++e) top |= (x.v[h][i][e] & 0x7f7f7f7fu) + 0x01010101u;
-          return tok + 16 * h + 4 * g + i >= ctx ? top & 0x80808080u : 0u;
+        // A NaN among a drafted token's codes would reach the queries that do not see it, as
+        // 0 times NaN: it is left out, and those that see it get their NaN at the end.
+        auto nan = [&](int i, int e) {
+          return tok + 16 * (i >> 2) + 4 * g + (i & 3) >= ctx ? nan_codes(x.v[i >> 2][i & 3][e]) : 0u;
         };
         uint32_t any = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) any |= nan(i >> 2, i & 3);
-        // (two halves a query leave no registers for the way around)
-        if (ZQ == 2 || __any(any != 0)) {
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < DP / 64; ++e) any |= nan(i, e);
+        if (__any(any != 0)) {
+          found = true;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (group_max<16>(nan(i >> 2, i & 3)) != 0) {
-              x.vs[i >> 2][i & 3] = __uint_as_float(0x7fc00000u);
 #pragma unroll
-              for (int e = 0; e < DP / 64; ++e) x.v[i >> 2][i & 3][e] = 0;
+            for (int e = 0; e < DP / 64; ++e) {
+              const uint32_t n = nan(i, e);
+              x.v[i >> 2][i & 3][e] &= ~((n << 1) - (n >> 7));
             }
         }
       }
@@ -500,6 +528,9 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
   }
 
   // the waves' parts, in their order
+  if constexpr (!INT8) {
+    if (l == 0) odd[w] = found;
+  }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     sum[t] = quad_sum(sum[t]);
@@ -514,6 +545,9 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
         *(f4*)&lo[w][16 * t + c][(4 * g + i) * NT + j] =
             f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
   __syncthreads();
+  int group = a.group;
+  // (its reciprocal is not to be held from the queries to here)
+  if constexpr (four_a_unit(INT8, DP, QT, ZQ, ZP)) asm("" : "+s"(group));
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * NT;
@@ -535,8 +569,11 @@ __global__ __launch_bounds__(64 * kWaves, groups_a_unit(DP, QT)) void k_tree(Tre
           for (int k = 0; k < 4; ++k) v[j + k] = fmaf(s[k], f[i], v[j + k]);
         }
       }
+      if constexpr (!INT8) {
+        if (odd[0] | odd[1] | odd[2] | odd[3]) put_nans<NT>(a, table, b, hkv, r / group, ctx, max(begin, ctx), end, d0, v);
+      }
       if (a.splits == 1) {
-        const int tk = r / a.group, head = hkv * a.group + r % a.group;
+        const int tk = r / group, head = hkv * group + r % group;
         const int64_t row = (int64_t)b * a.width + tk;
         const bool none = L == 0.0f || tk >= drafted;
         const float inv = 1.0f / L;
