@@ -616,7 +616,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
   float top = ms;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float f = ls == 0.0f ? 0.0f : top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
+  // (-1: an empty part, which is not written; one far below the best is, and may hold a NaN)
+  const float f = ls == 0.0f ? -1.0f : top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
   float L = ls * f;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
@@ -628,11 +629,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_join(TreeArgs a) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int s = s0 + u * G;
-      const float fs = __shfl(f, s & 63);
-      // an empty part is not written; one far below the best is, and may hold a NaN
-      const bool there = s < a.splits && __shfl(ls, s & 63) != 0.0f;
+      const float fs = s < a.splits ? __shfl(f, s) : -1.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += there ? x[u][e] * fs : 0.0f;
+      for (int e = 0; e < E; ++e) v[e] += fs < 0.0f ? 0.0f : x[u][e] * fs;
     }
   }
   if constexpr (G > 1) {
