@@ -498,7 +498,17 @@ def _blocks(v: int) -> int:
     return -(-v // 128)
 
 
-def _enqueue(name: str, args, keep, prepare: bool):
+def _one_device(name: str, tensors, stream) -> None:
+    """The tensors and the stream (None: the current one) of a call have to be the
+    current device's: a launch goes there, wherever its pointers lead."""
+    device = torch.cuda.current_device()
+    for t in (*tensors, stream):
+        if t is not None and t.device.type == "cuda" and t.device.index != device:
+            raise ValueError(f"{name}: a tensor or the stream is on {t.device}, the current device is cuda:{device}")
+
+
+def _enqueue(name: str, args, keep, stream, prepare: bool):
+    _one_device(name, keep, stream)
     fn = getattr(load(), name)
 
     def call(_keep=keep):  # the tensors live as long as the call can be made
@@ -525,7 +535,7 @@ def gptq2d_block_quantize(X, Q, S, QT=None, ST=None, block_rows: int = 1, pow2: 
         qt = _codes(QT, cols, rows, "QT")
         st = _scales(ST, _blocks(cols) if tile else _blocks(rows), _blocks(rows) if tile else cols, "ST")
     args = (rows, cols, _narrow(X), px, ldx, block_rows, int(bool(pow2)), *q, *s, *qt, *st, _stream(stream))
-    return _enqueue("gptq2d_block_quantize", args, (X, Q, S, QT, ST), prepare)
+    return _enqueue("gptq2d_block_quantize", args, (X, Q, S, QT, ST), stream, prepare)
 
 
 def gptq2d_block_matmul_workspace_size(M: int, N: int, K: int) -> int:
@@ -542,7 +552,7 @@ def gptq2d_block_matmul(A, SA, B, SB, C, workspace=None, block_rows: int = 128, 
     c = _mat(C, M, N, "C")
     ws = _space(workspace, gptq2d_block_matmul_workspace_size(M, N, K), "gptq2d_block_matmul")
     args = (M, N, K, *a, *sa, *b, *sb, block_rows, _narrow(C), *c, *ws, _stream(stream))
-    return _enqueue("gptq2d_block_matmul", args, (A, SA, B, SB, C, workspace), prepare)
+    return _enqueue("gptq2d_block_matmul", args, (A, SA, B, SB, C, workspace), stream, prepare)
 
 
 def gptq2d_block_linear_workspace_size(M: int, N: int, K: int) -> int:
@@ -556,7 +566,7 @@ def gptq2d_block_linear(X, W, SW, Y, workspace, pow2: bool = False, stream=None,
     sw = _scales(SW, _blocks(N), _blocks(K), "SW")
     ws = _space(workspace, gptq2d_block_linear_workspace_size(M, N, K), "gptq2d_block_linear")
     args = (M, N, K, _narrow(X, Y), *x, *w, *sw, int(bool(pow2)), *y, *ws, _stream(stream))
-    return _enqueue("gptq2d_block_linear", args, (X, W, SW, Y, workspace), prepare)
+    return _enqueue("gptq2d_block_linear", args, (X, W, SW, Y, workspace), stream, prepare)
 
 
 def gptq2d_block_linear_backward_workspace_size(M: int, N: int, K: int) -> int:
@@ -581,7 +591,7 @@ def gptq2d_block_linear_backward(dY, X, WT, SWT, dX, dW, workspace, pow2: bool =
     dt = _narrow(dY, dX, X if dW is not None else None)
     ws = _space(workspace, gptq2d_block_linear_backward_workspace_size(M, N, K), "gptq2d_block_linear_backward")
     args = (M, N, K, dt, *dy, *x, *wt, *swt, int(bool(pow2)), *dx, *dw, *ws, _stream(stream))
-    return _enqueue("gptq2d_block_linear_backward", args, (dY, X, WT, SWT, dX, dW, workspace), prepare)
+    return _enqueue("gptq2d_block_linear_backward", args, (dY, X, WT, SWT, dX, dW, workspace), stream, prepare)
 
 
 def _cache(KC, VC, KS, VS):
@@ -616,7 +626,7 @@ def gptq2d_cache_append(K, V, slots, KC, VC, KS, VS, stream=None, prepare=False)
     k, v = _mat(K, tokens, heads * dim, "K"), _mat(V, tokens, heads * dim, "V")
     args = (tokens, heads, dim, _narrow(K, V), *k, *v, _ints(slots, (tokens,), torch.int64, "slots"), code, pages, page,
             *tensors, _stream(stream))
-    return _enqueue("gptq2d_cache_append", args, (K, V, slots, KC, VC, KS, VS), prepare)
+    return _enqueue("gptq2d_cache_append", args, (K, V, slots, KC, VC, KS, VS), stream, prepare)
 
 
 def gptq2d_cache_read(slots, KC, VC, KS, VS, K, V, stream=None, prepare=False):
@@ -626,7 +636,7 @@ def gptq2d_cache_read(slots, KC, VC, KS, VS, K, V, stream=None, prepare=False):
     k, v = _mat(K, tokens, heads * dim, "K"), _mat(V, tokens, heads * dim, "V")
     args = (tokens, heads, dim, _narrow(K, V), _ints(slots, (tokens,), torch.int64, "slots"), code, pages, page,
             *tensors, *k, *v, _stream(stream))
-    return _enqueue("gptq2d_cache_read", args, (slots, KC, VC, KS, VS, K, V), prepare)
+    return _enqueue("gptq2d_cache_read", args, (slots, KC, VC, KS, VS, K, V), stream, prepare)
 
 
 def gptq2d_tree_masks(parents, masks, stream=None, prepare=False):
@@ -634,7 +644,7 @@ def gptq2d_tree_masks(parents, masks, stream=None, prepare=False):
     seqs, width = parents.shape
     args = (seqs, width, _ints(parents, (seqs, width), torch.int32, "parents"),
             _ints(masks, (seqs, width), torch.int64, "masks"), _stream(stream))
-    return _enqueue("gptq2d_tree_masks", args, (parents, masks), prepare)
+    return _enqueue("gptq2d_tree_masks", args, (parents, masks), stream, prepare)
 
 
 def gptq2d_tree_attention_workspace_size(seqs: int, width: int, heads: int, kv_heads: int, dim: int) -> int:
@@ -667,7 +677,7 @@ def gptq2d_tree_attention(Q, KC, VC, KS, VS, table, context, drafts, masks, scal
     args = (seqs, width, heads, kv, dim, _narrow(Q, O), *q, code, pages, page, *tensors, *tab, table.shape[1],
             _ints(context, (seqs,), torch.int32, "context"), n, m, float(scale), *o, _ptr(lse), *ws, _stream(stream))
     return _enqueue("gptq2d_tree_attention", args, (Q, KC, VC, KS, VS, table, context, drafts, masks, O, lse, workspace),
-                    prepare)
+                    stream, prepare)
 
 
 def gptq2d_token_logprobs_workspace_size(rows: int, vocab: int, top: int) -> int:
@@ -690,7 +700,8 @@ def gptq2d_token_logprobs(X, target, scale: float, logprob, entropy, lse, ids=No
         best = [_ints(ids, (rows, top), torch.int32, "ids"), _ints(tops, (rows, top), torch.float32, "tops")]
     ws = _space(workspace, gptq2d_token_logprobs_workspace_size(rows, vocab, top), "gptq2d_token_logprobs")
     args = (rows, vocab, _narrow(X), *x, float(scale), y, top, *out, *best, *ws, _stream(stream))
-    return _enqueue("gptq2d_token_logprobs", args, (X, target, logprob, entropy, lse, ids, tops, workspace), prepare)
+    return _enqueue("gptq2d_token_logprobs", args, (X, target, logprob, entropy, lse, ids, tops, workspace), stream,
+                    prepare)
 
 
 def gptq2d_token_logprobs_backward(X, target, scale: float, lse, entropy, g_logprob, g_entropy, dX, stream=None,
@@ -704,7 +715,8 @@ def gptq2d_token_logprobs_backward(X, target, scale: float, lse, entropy, g_logp
     v = [None if t is None else _ints(t, (rows,), torch.float32, w)
          for t, w in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy"))]
     args = (rows, vocab, _narrow(X, dX), *x, float(scale), y, *v, *d, _stream(stream))
-    return _enqueue("gptq2d_token_logprobs_backward", args, (X, target, lse, entropy, g_logprob, g_entropy, dX), prepare)
+    return _enqueue("gptq2d_token_logprobs_backward", args, (X, target, lse, entropy, g_logprob, g_entropy, dX), stream,
+                    prepare)
 
 
 # ---------------------------------------------------------------------------
@@ -799,10 +811,13 @@ def factor_batched(factors, As, Bs, check=True, stream=None, workspace=None):
         gptq2d_factor_batched_check(handles, stream)
 
 
-def _on(stream):
-    """Memory that a call on `stream` uses is taken for that stream, so that none
-    of it goes to other work while the call may still run."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _on(stream, t):
+    """A call runs on `stream` or, without one, on the current stream of tensor t's
+    device. Memory that it uses is taken for that stream, so that none of it goes to
+    other work while the call may still run."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
 
 
 def _bytes(n: int) -> torch.Tensor:
@@ -835,7 +850,7 @@ def block_quantize(X: torch.Tensor, block_rows: int = 128, pow2: bool = False, t
                    stream=None) -> Blocks:
     """X (or its transpose, whose blocks run along X's columns) in e4m3 blocks."""
     rows, cols = X.shape
-    with _on(stream):
+    with _on(stream, X):
         out = Blocks.empty(*((cols, rows) if transposed else (rows, cols)), block_rows)
         pair = (None, None, out.codes, out.scales) if transposed else (out.codes, out.scales)
         gptq2d_block_quantize(X, *pair, block_rows=block_rows, pow2=pow2)
@@ -847,7 +862,7 @@ def block_matmul(A: Blocks, B: Blocks, dtype=torch.bfloat16, stream=None) -> tor
     if A.block_rows != 1:
         raise ValueError("A must be in blocks of 1 x 128")
     (M, K), N = A.codes.shape, B.codes.shape[0]
-    with _on(stream):
+    with _on(stream, A.codes):
         C = torch.empty((M, N), dtype=dtype, device=A.codes.device)
         gptq2d_block_matmul(A.codes, A.scales, B.codes, B.scales, C,
                             _bytes(gptq2d_block_matmul_workspace_size(M, N, K)), block_rows=B.block_rows)
@@ -859,7 +874,7 @@ def block_linear(X: torch.Tensor, W: Blocks, pow2: bool = False, stream=None) ->
     (M, K), N = X.shape, W.codes.shape[0]
     if W.block_rows != 128:
         raise ValueError("W must be in tiles of 128 x 128")
-    with _on(stream):
+    with _on(stream, X):
         Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
         gptq2d_block_linear(X, W.codes, W.scales, Y, _bytes(gptq2d_block_linear_workspace_size(M, N, K)), pow2=pow2)
     return Y
@@ -870,7 +885,7 @@ def block_linear_backward(dY: torch.Tensor, X: torch.Tensor, WT: Blocks, pow2: b
     (M, N), K = dY.shape, X.shape[1]
     if WT.block_rows != 128:
         raise ValueError("WT must be in tiles of 128 x 128")
-    with _on(stream):
+    with _on(stream, dY):
         dX = torch.empty((M, K), dtype=dY.dtype, device=dY.device)
         dW = torch.empty((N, K), dtype=torch.float32, device=dY.device)
         ws = _bytes(gptq2d_block_linear_backward_workspace_size(M, N, K))
@@ -904,10 +919,11 @@ class Cache:
         return torch.where((page < table.shape[1]) & (entry >= 0), slot, -1).reshape(-1)
 
     def append(self, K, V, slots, stream=None) -> None:
-        gptq2d_cache_append(K, V, slots, *self.tensors, stream=stream)
+        with _on(stream, self.KC):
+            gptq2d_cache_append(K, V, slots, *self.tensors)
 
     def read(self, slots, dtype=torch.bfloat16, stream=None):
-        with _on(stream):
+        with _on(stream, self.KC):
             K, V = (torch.empty((slots.shape[0], self.heads * self.dim), dtype=dtype, device=slots.device)
                     for _ in range(2))
             gptq2d_cache_read(slots, *self.tensors, K, V)
@@ -916,7 +932,7 @@ class Cache:
     def attend(self, Q, table, context, masks=None, drafts=None, scale=None, stream=None):
         """(O, lse) of gptq2d_tree_attention; scale defaults to dim^-1/2."""
         seqs, heads = context.shape[0], Q.shape[1] // self.dim
-        with _on(stream):
+        with _on(stream, self.KC):
             O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
             lse = torch.empty((Q.shape[0], heads), dtype=torch.float32, device=Q.device)
             ws = _bytes(gptq2d_tree_attention_workspace_size(seqs, Q.shape[0] // seqs, heads, self.heads, self.dim))
@@ -927,7 +943,7 @@ class Cache:
 
 def tree_masks(parents: torch.Tensor, stream=None) -> torch.Tensor:
     """Masks (int64 bits) of trees of drafted tokens, from their parents (int32)."""
-    with _on(stream):
+    with _on(stream, parents):
         masks = torch.empty(parents.shape, dtype=torch.int64, device=parents.device)
         gptq2d_tree_masks(parents, masks)
     return masks
@@ -944,7 +960,7 @@ class Scores(NamedTuple):
 def token_logprobs(X: torch.Tensor, target=None, scale: float = 1.0, top: int = 0, stream=None) -> Scores:
     """Scores of every row of logits X; ids and tops: the `top` largest."""
     rows, vocab = X.shape
-    with _on(stream):
+    with _on(stream, X):
         out = [torch.empty(rows, dtype=torch.float32, device=X.device) for _ in range(3)]
         best = [torch.empty((rows, top), dtype=dt, device=X.device) if top else None
                 for dt in (torch.int32, torch.float32)]
@@ -956,7 +972,7 @@ def token_logprobs(X: torch.Tensor, target=None, scale: float = 1.0, top: int = 
 def token_logprobs_backward(X: torch.Tensor, target, scores: Scores, g_logprob=None, g_entropy=None, scale: float = 1.0,
                             stream=None) -> torch.Tensor:
     """The gradient of the logits from those of the log probabilities and entropies."""
-    with _on(stream):
+    with _on(stream, X):
         dX = torch.empty_like(X, memory_format=torch.contiguous_format)
         gptq2d_token_logprobs_backward(X, target, scale, scores.lse, scores.entropy, g_logprob, g_entropy, dX)
     return dX
