@@ -911,12 +911,12 @@ class Cache:
 
     def slots(self, table: torch.Tensor, first: torch.Tensor, count: int) -> torch.Tensor:
         """The slots (int64, sequences * count) of positions first[b] .. first[b] +
-        count - 1 of every sequence; -1 past its pages."""
+        count - 1 of every sequence; -1 before the first token and past its pages."""
         at = first.long().unsqueeze(1) + torch.arange(count, device=table.device)
         page = at // self.page_size
-        entry = table.long().gather(1, page.clamp(max=table.shape[1] - 1))
-        slot = entry * self.page_size + at % self.page_size
-        return torch.where((page < table.shape[1]) & (entry >= 0), slot, -1).reshape(-1)
+        table = torch.nn.functional.pad(table.long(), (1, 1), value=-1)  # what lies outside names no page
+        entry = table.gather(1, (page + 1).clamp(0, table.shape[1] - 1))
+        return torch.where(entry >= 0, entry * self.page_size + at % self.page_size, -1).reshape(-1)
 
     def append(self, K, V, slots, stream=None) -> None:
         with _on(stream, self.KC):

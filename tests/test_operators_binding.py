@@ -28,3 +28,14 @@ def test_every_call_checks_its_device(monkeypatch):
     binding._enqueue("f", (1, 2), ("t",), "s", False)
     assert callable(binding._enqueue("f", (1,), ("u",), None, True))
     assert seen == [("f", ("t",), "s"), ("f", ("u",), None)]
+
+
+def test_slots_of_positions_outside():
+    """Positions before the first token, past the table and in pages that are none have no slot."""
+    cache = object.__new__(binding.Cache)
+    cache.page_size = 16
+    table = torch.tensor([[3, 0, -1], [5, 2, 7]], dtype=torch.int32)
+    slots = cache.slots(table, torch.tensor([-3, 46], dtype=torch.int32), 5)
+    assert slots.tolist() == [-1, -1, -1, 48, 49, 7 * 16 + 14, 7 * 16 + 15, -1, -1, -1]
+    assert cache.slots(table, torch.tensor([30, -2 ** 31], dtype=torch.int32), 3).tolist() == [14, 15, -1, -1, -1, -1]
+    assert cache.slots(table[:, :0], torch.tensor([0, 1], dtype=torch.int32), 2).tolist() == [-1] * 4
