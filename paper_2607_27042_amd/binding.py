@@ -9,7 +9,8 @@ The functions named like the C entry points take and return the same things,
 with torch tensors in place of device pointers and Python ints in place of
 handles. ``Factors`` and ``round_matrix`` are conveniences built from them, and
 ``Blocks``, ``Cache``, ``block_*``, ``tree_masks`` and ``token_logprobs*`` those of
-the eight-bit operators: they allocate outputs and workspaces as they go.
+the eight-bit operators: they allocate outputs and workspaces as they go. Of these,
+``block_linear`` (for X) and ``token_logprobs`` (for the logits) take part in autograd.
 """
 from __future__ import annotations
 
@@ -839,6 +840,14 @@ class Blocks(NamedTuple):
         shape = (_blocks(cols), rows) if block_rows == 1 else (_blocks(rows), _blocks(cols))
         return cls(codes, torch.empty(shape, dtype=torch.float32, device=dev), block_rows)
 
+    def transposed(self):
+        """The transpose of a matrix in tiles of 128 x 128 (the same codes and scales)."""
+        if self.block_rows != 128:
+            raise ValueError("only tiles of 128 x 128 have a transpose")
+        out = Blocks.empty(*self.codes.shape[::-1])
+        out.codes.view(torch.uint8).copy_(self.codes.view(torch.uint8).T)
+        return out._replace(scales=self.scales.T.contiguous())
+
     def values(self) -> torch.Tensor:
         """What the codes stand for, in 32 bits."""
         rows, cols = self.codes.shape
@@ -869,12 +878,37 @@ def block_matmul(A: Blocks, B: Blocks, dtype=torch.bfloat16, stream=None) -> tor
     return C
 
 
-def block_linear(X: torch.Tensor, W: Blocks, pow2: bool = False, stream=None) -> torch.Tensor:
-    """X W^T for W in tiles of 128 x 128; X is quantised on the way."""
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, W, pow2, WT):
+        ctx.W, ctx.WT, ctx.pow2 = W, WT, pow2
+        return block_linear(X, W, pow2)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY):
+        N, K = ctx.W.codes.shape
+        M, WT = dY.shape[0], ctx.W.transposed() if ctx.WT is None else ctx.WT
+        dX = torch.empty((M, K), dtype=dY.dtype, device=dY.device)
+        gptq2d_block_linear_backward(dY.contiguous(), None, WT.codes, WT.scales, dX, None,
+                                     _bytes(gptq2d_block_linear_backward_workspace_size(M, N, K)), pow2=ctx.pow2)
+        return dX, None, None, None
+
+
+def block_linear(X: torch.Tensor, W: Blocks, pow2: bool = False, stream=None, WT=None) -> torch.Tensor:
+    """X W^T for W in tiles of 128 x 128; X is quantised on the way. Where X requires
+    a gradient it gets block_linear_backward's, by WT (block_quantize(W,
+    transposed=True); None: W is turned there and then). W's own, of the weights that
+    it holds, is block_linear_backward's dW."""
     (M, K), N = X.shape, W.codes.shape[0]
-    if W.block_rows != 128:
-        raise ValueError("W must be in tiles of 128 x 128")
+    for blocks in (W, WT):
+        if blocks is not None and blocks.block_rows != 128:
+            raise ValueError("W and WT must be in tiles of 128 x 128")
+    if WT is not None and tuple(WT.codes.shape) != (K, N):
+        raise ValueError(f"WT must be {K} x {N}, got {tuple(WT.codes.shape)}")
     with _on(stream, X):
+        if X.requires_grad and torch.is_grad_enabled():
+            return _Linear.apply(X, W, pow2, WT)
         Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
         gptq2d_block_linear(X, W.codes, W.scales, Y, _bytes(gptq2d_block_linear_workspace_size(M, N, K)), pow2=pow2)
     return Y
@@ -957,10 +991,40 @@ class Scores(NamedTuple):
     tops: torch.Tensor | None
 
 
+class _Scores(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, target, scale, top):
+        ctx.set_materialize_grads(False)
+        out = token_logprobs(X, target, scale, top)
+        ctx.save_for_backward(X, target, out.lse, out.entropy)
+        ctx.scale = scale
+        if top:
+            ctx.mark_non_differentiable(out.ids)
+        return tuple(out)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g_logprob, g_entropy, g_lse, g_ids, g_tops):
+        if g_lse is not None or g_tops is not None:
+            raise RuntimeError("token_logprobs has gradients of the log probabilities and entropies only, not of lse or tops")
+        X, target, lse, entropy = ctx.saved_tensors
+        g_logprob, g_entropy = (None if g is None else g.contiguous() for g in (g_logprob, g_entropy))
+        if target is None:
+            g_logprob = None  # (of log probabilities that are 0 by convention)
+        if g_logprob is None and g_entropy is None:
+            return torch.zeros_like(X), None, None, None
+        dX = torch.empty_like(X, memory_format=torch.contiguous_format)
+        gptq2d_token_logprobs_backward(X, target, ctx.scale, lse, entropy, g_logprob, g_entropy, dX)
+        return dX, None, None, None
+
+
 def token_logprobs(X: torch.Tensor, target=None, scale: float = 1.0, top: int = 0, stream=None) -> Scores:
-    """Scores of every row of logits X; ids and tops: the `top` largest."""
+    """Scores of every row of logits X; ids and tops: the `top` largest. Where X
+    requires a gradient, the log probabilities and entropies carry it."""
     rows, vocab = X.shape
     with _on(stream, X):
+        if X.requires_grad and torch.is_grad_enabled():
+            return Scores(*_Scores.apply(X, target, scale, top))
         out = [torch.empty(rows, dtype=torch.float32, device=X.device) for _ in range(3)]
         best = [torch.empty((rows, top), dtype=dt, device=X.device) if top else None
                 for dt in (torch.int32, torch.float32)]
