@@ -1,9 +1,11 @@
 """From calibration to serving: one attention layer and its output head, rounded
 by the library and served in eight bits.
 
-  1. Calibrate. The head's logits are scored (gptq2d_token_logprobs), the scores'
-     gradient (gptq2d_token_logprobs_backward) gives the output side of the
-     two-sided metric, the layer's inputs give the other.
+  1. Calibrate. Sequences of tokens run through the layer and are scored
+     (gptq2d_token_logprobs). What every matrix takes in gives the input side of its
+     two-sided metric, the scores' gradient at what it gives out the other: through
+     the scores (gptq2d_token_logprobs_backward), the head, whose product is in eight
+     bits already (gptq2d_block_linear_backward), and the attention.
   2. Round. W / step is rounded to integers Z under ||A (Z - X) B|| with A and B
      the Cholesky factors of the two Grams (gptq2d_factor, gptq2d_round).
   3. Hold Z in e4m3 tiles with scales that are powers of two, which keep integers
@@ -56,6 +58,28 @@ class Rounded:
         return g.block_linear(x, self.blocks)
 
 
+def calibrate(weights, embed, tokens, target, kv_heads):
+    """Of every matrix: the rows that it takes in, and the gradient of the targets'
+    log probabilities at those that it gives out. tokens, target: sequences x length."""
+    x = embed[tokens.flatten()]
+    q, k, v = ((x @ weights[n].T).requires_grad_() for n in "qkv")
+    seqs, t, dim = *tokens.shape, k.shape[1] // kv_heads
+    split = lambda y: y.view(seqs, t, -1, dim).transpose(1, 2)
+    kk, vv = (split(y).repeat_interleave(q.shape[1] // k.shape[1], 1) for y in (k, v))
+    z = (split(q) @ kk.transpose(2, 3)) * dim ** -0.5
+    ahead = torch.ones(t, t, dtype=torch.bool, device=x.device).triu(1)
+    p = torch.softmax(z.masked_fill(ahead, float("-inf")), -1)
+    attended = (p @ vv).transpose(1, 2).reshape(seqs * t, -1)
+    o = attended @ weights["o"].T
+    h = x + o
+    logits = g.block_linear(h, g.block_quantize(weights["head"]))
+    o.retain_grad()
+    logits.retain_grad()
+    g.token_logprobs(logits, target.flatten()).logprob.sum().backward()
+    return {"q": (x, q.grad), "k": (x, k.grad), "v": (x, v.grad), "o": (attended.detach(), o.grad),
+            "head": (h.detach(), logits.grad)}
+
+
 def plain_attention(q, k, v, kv_heads, context, sees):
     """One sequence, 64 bits: rows of q over `context` tokens and the tree's."""
     t, dim = q.shape[0], k.shape[1] // kv_heads
@@ -77,18 +101,12 @@ def run(width=256, heads=8, kv_heads=2, vocab=1000, prompt=300, page_size=64, se
     weights = {n: w / width ** 0.5 for n, w in weights.items()}
     embed = randn(vocab, width)
 
-    # 1. calibration: tokens through the head, and the gradient of their scores
-    tokens = torch.randint(vocab, (1024,), generator=gen, device="cuda")
-    target = torch.randint(vocab, (1024,), generator=gen, device="cuda")
-    x = embed[tokens]
-    logits = x @ weights["head"].T
-    scores = g.token_logprobs(logits, target)
-    d_logits = g.token_logprobs_backward(logits, target, scores, torch.ones_like(scores.logprob))
-    d_x = d_logits @ weights["head"]
+    # 1. calibration: sequences of tokens, each of which is to say a given one
+    tokens, target = (torch.randint(vocab, (8, 128), generator=gen, device="cuda") for _ in range(2))
+    seen = calibrate(weights, embed, tokens, target, kv_heads)
 
     # 2. and 3.: rounded and held in eight bits
-    rounded = {n: Rounded(w, x, d_logits if n == "head" else (d_x if w.shape[0] == width else randn(1024, kv_width)))
-               for n, w in weights.items()}
+    rounded = {n: Rounded(w, *seen[n]) for n, w in weights.items()}
 
     # 4. a prompt into the cache, then a tree of drafted tokens
     cache = g.Cache(-(-(prompt + 8) // page_size) + 1, kv_heads, page_size, dim)
