@@ -287,7 +287,8 @@ size_t gptq2d_block_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
 /* Enqueues C = A B^T for codes A (M x K, blocks of 1 x 128: SA) and B (N x K,
  * blocks of b_block_rows (1 or 128) x 128: SB); C (M x N) has type dt. Each
  * block's products are summed by themselves and enter the sum, which is held in
- * 32 bits, with the block's two scales. For a 32-bit C the products are summed
+ * 32 bits, with the block's two scales (whose own product may lie outside 32 bits'
+ * range). For a 32-bit C the products are summed
  * in 32 bits throughout; for a 16-bit C inside a block by the eight-bit matrix
  * instruction, whose sum was measured to be off by 1.5e-5 of the sum of
  * magnitudes (3e-4 at most, where few products tower over the others). The
@@ -385,18 +386,19 @@ size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, 
  *   lse (nullable): log sum e^z of every row and head (-inf for a row of zeros),
  *       seqs * width x heads.
  * A drafted token's keys and values, whatever they hold, reach only the rows that
- * see it (a NaN code among them the element it stands in). A
- * token's part in a row, probability times value scale, counts down to about 2^-29 of
- * the row's largest probability times the largest value scale that it sees (of a few
- * tokens around it).
+ * see it (a NaN code among the values only its own element of them). A token's part
+ * in a row, probability times value scale, counts down to about 2^-29 of the row's
+ * largest probability times the largest value scale that it sees (of a few tokens
+ * around it).
  * Sums and the softmax are held in 32 bits. Queries and probabilities enter the
  * products as 16-bit floats (after scaling by a power of two), or as the sum of
- * two where dt is F32. A context past the table's last page ends there; the
- * tokens of an entry that names no page are absent. One token per sequence
- * (width 1) is decoding. 1 <= width <= 64, seqs <= 65535, seqs * width * heads <=
- * 2^24, kv_heads <= 1024. workspace: as sized
- * above, 256-byte aligned, owned by the caller; overlapping calls need distinct
- * ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
+ * two where dt is F32. The same call gives the same bits; a sequence's last bits
+ * depend on the others' lengths, which decide into how many parts its tokens are
+ * split. A context past the table's last page ends there; the tokens of an entry
+ * that names no page are absent. One token per sequence (width 1) is decoding.
+ * 1 <= width <= 64, seqs <= 65535, seqs * width * heads <= 2^24, kv_heads <= 1024.
+ * workspace: as sized above, 256-byte aligned, owned by the caller; overlapping
+ * calls need distinct ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
 gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_heads, int dim,
                                     gptq2d_dtype dt, const void* Q, int64_t ldq, gptq2d_code code,
                                     int64_t pages, int page_size, const void* KC, const void* VC,

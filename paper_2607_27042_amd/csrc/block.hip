@@ -231,7 +231,7 @@ __device__ __forceinline__ u4 tail16(const uint8_t* p, int c, int n) {
 }
 
 // R rows of an operand, from row r0 on, go into LDS 128 codes deep at a time, row
-// by row (128 bytes each). Chunk c of 16 bytes of row r lies at chunk c ^ (r % 8),
+// by row (128 bytes each). Chunk c of 16 bytes of row r lies at chunk c ^ (r / 2 % 8),
 // so that rows read at the same k spread over the banks. Rows past the
 // last are the last one's (their products are not stored).
 template <int R, int THREADS>
@@ -320,8 +320,11 @@ __device__ __forceinline__ void put4(T* p, bool wide, int n, f4 v) {
 // Each 128-deep block is summed by itself and enters the accumulators with its scale.
 // EXACT: the codes are widened to halves (which hold them exactly) and summed
 // by the 16-bit instruction. The eight-bit one aligns its products to about
-// 14 bits below the largest (measured 1.5e-5 of the sum of magnitudes), which
-// is far below a 16-bit result's last place, but not below a 32-bit one's.
+// 14 bits below the largest (measured 1.5e-5 rms of the sum of magnitudes, 3e-4 at
+// most, where few products tower over the others). A 16-bit result's own rounding covers that: off by 2.07e-4
+// (f16) and 1.65e-3 (bf16) rms where only rounded at the end, it is off by 2.07e-4 to
+// 2.15e-4 and 1.65e-3 to 1.67e-3, at K = 128 and 11008 alike, with loud channels or
+// magnitudes over 2^12. A 32-bit result's does not.
 //
 // The whole of a block's codes comes into LDS while the one before it is multiplied.
 // Measured, by tile: 256 x 256 at 8192 x 11008 x 4096 bf16 356 us (2.07 PFLOP/s; a large
@@ -560,7 +563,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(ProductArgs a, int tn,
 // quantises the blocks it takes, two values a lane (K and ldx are even), through
 // LDS of its own. Every work group does that for itself, which for few rows costs
 // less than a launch before this one.
-// Bound by the weights' bytes and one memory latency: 1 x 4096 x 4096 5.8 us, 2.9 TB/s.
+// 256 work groups, one a compute unit, have all blocks of 4096 columns on their way in
+// one turn: what 1 x 4096 x 4096 takes, 5.9 us (2.8 TB/s; in a loop from the last-level
+// cache), is the launch, one memory latency and what follows it.
 template <class T, int TM, bool ROWS, bool EXACT, int FUSED>
 __global__ __launch_bounds__(512) void k_thin(ProductArgs a) {
   constexpr int U = TM == 1 ? 4 : TM == 2 ? 2 : 1;  // (with more, two work groups do not fit a compute unit's registers)

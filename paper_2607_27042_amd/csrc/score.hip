@@ -226,7 +226,7 @@ __device__ __forceinline__ void put_best(Pool& p, const ScoreArgs& a, int64_t ro
 // s1 >= 1 and s2 <= 0, so the entropy log s1 - s2 / s1 cancels nothing.
 // TOP: an element below the limit (the top-th best so far) is none of the best; the
 // first step sets a limit that few pass, so ranking is seldom. Bound by its bytes:
-// 4096 x 128000 bf16 with top 8 222 us, 4.7 TB/s; 2047 x 50257 50 us, 4.1 TB/s, whose
+// 4096 x 128000 bf16 with top 8 212 us in a loop, 4.9 TB/s; 2047 x 50257 50 us, 4.1 TB/s, whose
 // rows start off the 16-byte boundaries. One row of 32000 f32 with top 20, 9.0 us: the
 // first limit and one ranking of candidates (without top 4.4 us).
 template <class T, bool TOP>
@@ -409,7 +409,8 @@ constexpr float kNear = 128.0f;
 
 // One pass, element by element. Rows of logits and gradients that start at the
 // same distance from a 16-byte boundary are moved in 16-byte pieces. Bound by its
-// bytes: 2047 x 50257 bf16 96 us, 4.3 TB/s read and written.
+// bytes: 2047 x 50257 bf16 78 us, 5.3 TB/s read and written (the logits partly from the
+// last-level cache, after the forward pass).
 // A row whose lse is far from zero (or not a 32-bit number at all) is summed again
 // first, relative to its largest logit. Every part of a row does that for itself; where
 // one part's gradients would take the place of logits that another has yet to

@@ -101,10 +101,10 @@ __device__ __forceinline__ float quad_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// log2 of a value scale, rounded up, plus kLevel, in bits 8 to 15: products of e^z and
-// value scales reach 2^5 then, and 2^15 before a reference moves, which halves hold, and
-// stay normal halves down to 2^-19. Scales below 2^-80 count as that, or the sum of the
-// exponentials could overflow.
+// A value scale's level, in bits 8 to 15: log2, rounded up, plus 127. A reference takes it
+// less kLevel: products of e^z and value scales reach 2^5 then, and 2^15 before a
+// reference moves, which halves hold, and are normal halves down to 2^-19 of the largest.
+// Scales below 2^-75 count as that, or the sum of the exponentials could overflow.
 constexpr float kLevel = 132.0f;
 __device__ __forceinline__ uint32_t value_level(float v) {
   return max((__float_as_uint(v) + 0x7fffffu) >> 23, 52u) << 8;
@@ -254,8 +254,8 @@ __device__ __forceinline__ int part_length(const TreeArgs& a, int total, int l) 
 // 32768 tokens (dim 128) 281 us, 5.0 TB/s of cache. With 52 queries a head, 16 trees
 // of 13 over up to 8192 (dim 64, f16) 55 us, the cache's bytes are 19 us of it and
 // the instructions of the softmax and of widening the codes bound it (some 20 us of
-// issue slots, 7 us of the matrix unit); one token over 4096 8.2 us, where a step's
-// latency does.
+// issue slots, 7 us of the matrix unit; the rest is not accounted for); one token over
+// 4096 8.3 us, where the chain of one step does (length, table, codes, scores, values).
 template <bool INT8, int DP, int QT, int ZQ, int ZP>
 __global__ __launch_bounds__(64 * kWaves, four_a_unit(INT8, DP, QT, ZQ, ZP) ? 4 : groups_a_unit(DP, QT)) void k_tree(TreeArgs a) {
   constexpr int KS = DP / 32, NT = DP / 16;
