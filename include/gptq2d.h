@@ -389,7 +389,7 @@ size_t gptq2d_tree_attention_workspace_size(int64_t seqs, int width, int heads, 
  * see it (a NaN code among the values only its own element of them). A token's part
  * in a row, probability times value scale, counts down to about 2^-29 of the row's
  * largest probability times the largest value scale that it sees (of a few tokens
- * around it).
+ * around it; a vector of zeros has scale 1).
  * Sums and the softmax are held in 32 bits. Queries and probabilities enter the
  * products as 16-bit floats (after scaling by a power of two), or as the sum of
  * two where dt is F32. The same call gives the same bits; a sequence's last bits
