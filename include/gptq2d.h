@@ -409,6 +409,114 @@ gptq2d_status gptq2d_tree_attention(int64_t seqs, int width, int heads, int kv_h
                                     size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The end of a serving step: which drafted tokens are kept, their keys and values
+ * moved up in the cache, and page tables after sequences have forked or ended
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of device workspace gptq2d_tree_verify needs (0 on bad sizes). */
+size_t gptq2d_tree_verify_workspace_size(int64_t seqs, int width, int64_t vocab);
+
+/* Enqueues the verification of drafted trees. Row b * width + t of X (seqs * width x
+ * vocab, type F32, F16 or BF16) holds the logits of what follows drafted token t of
+ * sequence b, p = softmax(scale x). Token 0 is decided already and kept; tokens[b *
+ * width + t] (device) are the drafted ones, parents as for gptq2d_tree_masks (device;
+ * NULL: a chain), drafts as for gptq2d_tree_attention (device; NULL: width).
+ *   The tokens that follow the current one, at first token 0, are tested in order; the
+ * first that passes becomes the current one, and so on. With u = uniform[b * width + t]
+ * (device, in [0, 1)), token t with value y passes
+ *   without D, where drafts are certain (the likeliest tokens, say), if
+ *     u (1 - sum of p over those rejected before it) < p(y); not if y was rejected
+ *   with D (seqs * width x vocab, type as X), where the drafts that follow a token
+ *   were drawn independently from q = exp(draft_scale d - draft_lse), d that token's
+ *   row of D and draft_lse (device, seqs * width) its log-sum-exp, if
+ *     u M q(y) < p(y) - beta q(y),
+ *   beta = 0 and M = 1 at first; a rejection makes beta += M, M = sum max(p - beta q, 0)
+ *   without uniform (NULL, D too) if y is the lowest of the largest logits.
+ * The next token is drawn from what is left of p of the last kept token: the first v
+ * with sum over w <= v of r(w) > uniform[b * width] sum r, r being p without the
+ * rejected tokens, or max(p - beta q, 0), or p where that is nothing; without uniform
+ * it is the lowest of the largest logits. Kept and next tokens are distributed as
+ * tokens drawn from p one after another. What decides the next token is held in 64
+ * bits.
+ *   path (device, seqs x width): the kept tokens' places t, in order, -1 after them.
+ *   count (device, seqs): how many they are (0 where drafts is 0: next is -1 then).
+ *   next (device, seqs): the next token.
+ *   logprob (device, seqs x width): log p of drafted token t after the token that it
+ *       follows, 0 for one that follows no drafted token or is not there; at t = 0
+ *       that of the next token.
+ * A token outside the vocabulary does not pass and has log p = -inf. After a row with
+ * a NaN or +inf, or of nothing but -inf, no token passes, next is -1 and log p NaN.
+ * 1 <= width <= 64, seqs <= 65535, vocab <= 2^28. The same call gives the same bits.
+ * workspace: as sized above, 256-byte aligned, owned by the caller; overlapping
+ * calls need distinct ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_tree_verify(int64_t seqs, int width, int64_t vocab, gptq2d_dtype dt,
+                                 const void* X, int64_t ldx, float scale, const int64_t* tokens,
+                                 const int32_t* parents, const int32_t* drafts,
+                                 const float* uniform, const void* D, int64_t ldd,
+                                 float draft_scale, const float* draft_lse, int32_t* path,
+                                 int32_t* count, int64_t* next, float* logprob, void* workspace,
+                                 size_t ws_bytes, void* stream);
+
+/* Enqueues, in the caches of `layers` layers (host arrays of their tensors, which share
+ * a shape and the page tables), the move of kept tokens: of every sequence b the keys
+ * and values at position context[b] + path[b * width + i] go to position context[b] +
+ * i (path as gptq2d_tree_verify gives it, context and table as for
+ * gptq2d_tree_attention). An entry outside [i, width), or whose positions have no page,
+ * moves nothing. The pages of the positions written must be the sequence's own (not
+ * named by another sequence's table). 1 <= layers <= 4096. The arrays may be reused
+ * when the call returns. Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_cache_commit(int layers, int64_t seqs, int width, int heads, int dim,
+                                  int64_t pages, int page_size, void* const* KC, void* const* VC,
+                                  float* const* KS, float* const* VS, const int32_t* table,
+                                  int64_t ldt, int64_t table_width, const int32_t* context,
+                                  const int32_t* path, void* stream);
+
+/* Enqueues, in the caches of `layers` layers, `count` copies of pages: the first
+ * copies[3 i + 2] tokens of page copies[3 i] go to page copies[3 i + 1] (device int32,
+ * as gptq2d_pages_update gives them). A copy that names no page, or the same one
+ * twice, is skipped; a page that is written may not be in another copy. Errors:
+ * INVALID_ARG, HIP. */
+gptq2d_status gptq2d_cache_copy(int layers, int64_t count, int heads, int dim, int64_t pages,
+                                int page_size, void* const* KC, void* const* VC,
+                                float* const* KS, float* const* VS, const int32_t* copies,
+                                void* stream);
+
+/* Bytes of device workspace gptq2d_pages_update needs (0 on bad sizes). */
+size_t gptq2d_pages_update_workspace_size(int64_t rows, int64_t pages);
+
+/* Enqueues the page tables of `rows` sequences from those of `old_rows` sequences
+ * (device int32, table_width entries a sequence): sequences that go on, fork, are cut,
+ * end or begin, in one call.
+ *   length (old_rows): the tokens that the old sequences hold.
+ *   source (rows; NULL: the sequence itself): the old sequence that a new one goes on
+ *       from; one that is none begins a new sequence.
+ *   want (rows): the tokens that the new sequence is to have room for (0 ends it). It
+ *       keeps the first min(length, want) tokens of its source; both are cut to what
+ *       a table has room for.
+ *   held (nullable, pages): pages with an entry other than 0 are held elsewhere; they
+ *       are neither given out nor written.
+ *   out (rows x table_width, not the memory of table): the new tables. Pages whose
+ *       tokens are all kept are shared. The page that the kept tokens end inside stays
+ *       with the lowest row that ends in it if no row keeps it whole and it is not held;
+ *       the others get a copy. Further pages up to want are new. New pages are the
+ *       lowest free ones, row by row, in the order of their entries; entries after
+ *       those, those that none is left for, and kept ones that named no page are -1.
+ *   copies (rows x 3): page, its copy and the tokens to copy, for gptq2d_cache_copy;
+ *       -1, -1, 0 for a row that needs none.
+ *   left (nullable, one): the free pages that are left; below zero the pages that were
+ *       lacking.
+ * Pages named by no new table, and not held, are free. 1 <= rows, old_rows <= 65535,
+ * page_size as for the cache, rows * table_width <= 2^31. workspace: as sized above,
+ * 256-byte aligned, owned by the caller; overlapping calls need distinct ones.
+ * Errors: INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_pages_update(int64_t rows, int64_t old_rows, int64_t table_width,
+                                  const int32_t* table, int64_t ldt, const int32_t* length,
+                                  const int32_t* source, const int32_t* want, const int32_t* held,
+                                  int64_t pages, int page_size, int32_t* out, int64_t ldo,
+                                  int32_t* copies, int32_t* left, void* workspace,
+                                  size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Log probabilities of given tokens: the score of a rounded model, and the
  * gradient that its bases are made from
  *

@@ -92,6 +92,13 @@ def load():
         "gptq2d_tree_attention_workspace_size": (sz, [i64, i32, i32, i32, i32]),
         "gptq2d_tree_attention": (i32, [i64, i32, i32, i32, i32, i32, vp, i64, i32, i64, i32, vp, vp, vp, vp, vp, i64,
                                         i64, vp, vp, vp, ctypes.c_float, vp, i64, vp, vp, sz, vp]),
+        "gptq2d_tree_verify_workspace_size": (sz, [i64, i32, i64]),
+        "gptq2d_tree_verify": (i32, [i64, i32, i64, i32, vp, i64, ctypes.c_float, vp, vp, vp, vp, vp, i64, ctypes.c_float,
+                                     vp, vp, vp, vp, vp, vp, sz, vp]),
+        "gptq2d_cache_commit": (i32, [i32, i64, i32, i32, i32, i64, i32, vp, vp, vp, vp, vp, i64, i64, vp, vp, vp]),
+        "gptq2d_cache_copy": (i32, [i32, i64, i32, i32, i64, i32, vp, vp, vp, vp, vp, vp]),
+        "gptq2d_pages_update_workspace_size": (sz, [i64, i64]),
+        "gptq2d_pages_update": (i32, [i64, i64, i64, vp, i64, vp, vp, vp, vp, i64, i32, vp, i64, vp, vp, vp, sz, vp]),
         "gptq2d_token_logprobs_workspace_size": (sz, [i64, i64, i32]),
         "gptq2d_token_logprobs": (i32, [i64, i64, i32, vp, i64, ctypes.c_float, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
         "gptq2d_token_logprobs_backward": (i32, [i64, i64, i32, vp, i64, ctypes.c_float, vp, vp, vp, vp, vp, vp, i64,
@@ -679,6 +686,97 @@ def gptq2d_tree_attention(Q, KC, VC, KS, VS, table, context, drafts, masks, scal
             _ints(context, (seqs,), torch.int32, "context"), n, m, float(scale), *o, _ptr(lse), *ws, _stream(stream))
     return _enqueue("gptq2d_tree_attention", args, (Q, KC, VC, KS, VS, table, context, drafts, masks, O, lse, workspace),
                     stream, prepare)
+
+
+def gptq2d_tree_verify_workspace_size(seqs: int, width: int, vocab: int) -> int:
+    return int(load().gptq2d_tree_verify_workspace_size(seqs, width, vocab))
+
+
+def gptq2d_tree_verify(X, tokens, parents, drafts, scale: float, uniform, D, draft_lse, draft_scale: float, path, count,
+                       next, logprob, workspace, stream=None, prepare=False):
+    """Which of the drafted tokens (int64, [seqs, width]) are kept, from the logits X
+    (seqs * width x vocab) of what follows each: path (int32, [seqs, width]), count
+    (int32, [seqs]), the next token (int64, [seqs]) and logprob (float32, [seqs,
+    width]). parents (int32, [seqs, width]; None: a chain), drafts (int32, [seqs]; None:
+    width), uniform (float32, [seqs, width]; None: greedy); D and draft_lse (float32,
+    [seqs * width]; None: certain drafts)."""
+    seqs, width = tokens.shape
+    vocab = X.shape[1]
+    x = _mat(X, seqs * width, vocab, "X")
+    d = (ctypes.c_void_p(0), 0) if D is None else _mat(D, seqs * width, vocab, "D")
+    opt = lambda t, shape, dtype, what: None if t is None else _ints(t, shape, dtype, what)
+    both = (seqs, width)
+    args = (seqs, width, vocab, _narrow(X, D), *x, float(scale), _ints(tokens, both, torch.int64, "tokens"),
+            opt(parents, both, torch.int32, "parents"), opt(drafts, (seqs,), torch.int32, "drafts"),
+            opt(uniform, both, torch.float32, "uniform"), *d, float(draft_scale),
+            opt(draft_lse, (seqs * width,), torch.float32, "draft_lse"), _ints(path, both, torch.int32, "path"),
+            _ints(count, (seqs,), torch.int32, "count"), _ints(next, (seqs,), torch.int64, "next"),
+            _ints(logprob, both, torch.float32, "logprob"),
+            *_space(workspace, gptq2d_tree_verify_workspace_size(seqs, width, vocab), "gptq2d_tree_verify"),
+            _stream(stream))
+    return _enqueue("gptq2d_tree_verify", args, (X, tokens, parents, drafts, uniform, D, draft_lse, path, count, next,
+                                                 logprob, workspace), stream, prepare)
+
+
+def _caches(caches):
+    """(pages, heads, page_size, dim), the host arrays of the layers' tensors, and the
+    tensors; the layers' caches have one shape and code."""
+    caches = [tuple(c) for c in caches]
+    if not caches:
+        raise ValueError("no layer's cache is given")
+    first = _cache(*caches[0])
+    for c in caches[1:]:
+        if _cache(*c)[:5] != first[:5]:
+            raise ValueError("the layers' caches must have one shape and code")
+    arrays = tuple((ctypes.c_void_p * len(caches))(*(c[i].data_ptr() for c in caches)) for i in range(4))
+    return first[1:5], arrays, tuple(t for c in caches for t in c)
+
+
+def gptq2d_cache_commit(caches, table, context, path, stream=None, prepare=False):
+    """In the caches (a sequence of (KC, VC, KS, VS), one for each layer), the tokens at
+    positions context[b] + path[b, i] moved to context[b] + i (all int32)."""
+    (pages, heads, page, dim), arrays, tensors = _caches(caches)
+    seqs, width = path.shape
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise TypeError("table must be an int32 matrix")
+    tab = _mat(table, seqs, table.shape[1], "table")
+    args = (len(caches), seqs, width, heads, dim, pages, page, *arrays, *tab, table.shape[1],
+            _ints(context, (seqs,), torch.int32, "context"), _ints(path, (seqs, width), torch.int32, "path"),
+            _stream(stream))
+    return _enqueue("gptq2d_cache_commit", args, (*tensors, table, context, path), stream, prepare)
+
+
+def gptq2d_cache_copy(caches, copies, stream=None, prepare=False):
+    """In the caches (as above), copies (int32, [n, 3]): page, its copy, tokens."""
+    (pages, heads, page, dim), arrays, tensors = _caches(caches)
+    n = copies.shape[0]
+    args = (len(caches), n, heads, dim, pages, page, *arrays, _ints(copies, (n, 3), torch.int32, "copies"),
+            _stream(stream))
+    return _enqueue("gptq2d_cache_copy", args, (*tensors, copies), stream, prepare)
+
+
+def gptq2d_pages_update_workspace_size(rows: int, pages: int) -> int:
+    return int(load().gptq2d_pages_update_workspace_size(rows, pages))
+
+
+def gptq2d_pages_update(table, length, source, want, held, pages: int, page_size: int, out, copies, left, workspace,
+                        stream=None, prepare=False):
+    """The page tables out [rows, width] from table [old rows, width], length [old
+    rows], source [rows] (None: the row itself), want [rows] and held [pages] (None:
+    none); copies [rows, 3], left [1] (may be None). All int32."""
+    rows, old = want.shape[0], length.shape[0]
+    for t in (table, out):
+        if t.dtype != torch.int32 or t.dim() != 2:
+            raise TypeError("table and out must be int32 matrices")
+    width = table.shape[1]
+    opt = lambda t, n, what: None if t is None else _ints(t, (n,), torch.int32, what)
+    args = (rows, old, width, *_mat(table, old, width, "table"), _ints(length, (old,), torch.int32, "length"),
+            opt(source, rows, "source"), _ints(want, (rows,), torch.int32, "want"), opt(held, pages, "held"), pages,
+            page_size, *_mat(out, rows, width, "out"), _ints(copies, (rows, 3), torch.int32, "copies"),
+            opt(left, 1, "left"),
+            *_space(workspace, gptq2d_pages_update_workspace_size(rows, pages), "gptq2d_pages_update"), _stream(stream))
+    return _enqueue("gptq2d_pages_update", args, (table, length, source, want, held, out, copies, left, workspace), stream,
+                    prepare)
 
 
 def gptq2d_token_logprobs_workspace_size(rows: int, vocab: int, top: int) -> int:

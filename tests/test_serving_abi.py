@@ -1,0 +1,160 @@
+"""CPU checks of the entry points that end a serving step: arguments are refused with a
+status and a message before any device is touched; workspace sizes; the binding's own
+checks; the oracle's page tables keep what they promise."""
+import ctypes
+import random
+
+import pytest
+import torch
+
+import serving
+from paper_2607_27042_amd import binding, build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if build.is_stale():
+        build.build()
+    return binding.load()
+
+
+NULL = ctypes.c_void_p(0)
+P = ctypes.c_void_p(4096)  # aligned, never followed: every call here is refused
+F32, F64, BF16 = binding.F32, binding.F64, binding.BF16
+
+
+def refused(status, part):
+    assert status == -1, status
+    assert part in binding.gptq2d_last_error(), binding.gptq2d_last_error()
+
+
+def test_verify_refusals(lib):
+    size = lib.gptq2d_tree_verify_workspace_size
+    assert size(2, 65, 100) == 0 and size(0, 3, 100) == 0 and size(2, 3, 0) == 0 and size(2, 3, 100) > 0
+    ok = dict(seqs=2, width=3, vocab=100, dt=BF16, X=P, ldx=100, scale=1.0, tokens=P, parents=P, drafts=P, u=P, D=P, ldd=100,
+              ds=1.0, dlse=P, path=P, count=P, next=P, lp=P, ws=P, nb=size(2, 3, 100), stream=None)
+    call = lambda **k: lib.gptq2d_tree_verify(*{**ok, **k}.values())
+    refused(call(seqs=-1), "seqs")
+    refused(call(seqs=65536), "seqs")
+    refused(call(width=0), "width")
+    refused(call(width=65), "width")
+    refused(call(vocab=2 ** 28 + 1), "vocab")
+    refused(call(dt=F64), "dtype")
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        refused(call(scale=bad), "scale")
+        refused(call(ds=bad), "draft_scale")
+    refused(call(dlse=NULL), "draft_lse")
+    refused(call(u=NULL), "random numbers")
+    for name in ("X", "tokens", "path", "count", "next", "lp"):
+        refused(call(**{name: NULL}), "NULL")
+    refused(call(ldx=99), "leading dimension")
+    refused(call(ldd=99), "leading dimension")
+    refused(call(X=ctypes.c_void_p(4097)), "aligned")
+    refused(call(next=ctypes.c_void_p(4100)), "aligned")
+    assert call(seqs=0) == 0  # no work
+    assert call(nb=ok["nb"] - 1) == -6 and call(ws=NULL) == -6 and call(ws=ctypes.c_void_p(4100)) == -6
+
+
+def arrays(n, **null):
+    """Host arrays of the layers' tensors; null: name -> the layer whose pointer is other."""
+    out = []
+    for name in ("KC", "VC", "KS", "VS"):
+        a = (ctypes.c_void_p * n)(*[4096] * n)
+        if name in null:
+            a[null[name][0]] = null[name][1]
+        out.append(a)
+    return out
+
+
+def test_commit_and_copy_refusals(lib):
+    def commit(layers=3, seqs=2, width=4, heads=2, dim=64, pages=4, page=16, of=None, table=P, ldt=4, tw=4, context=P, path=P):
+        return lib.gptq2d_cache_commit(layers, seqs, width, heads, dim, pages, page, *(of or arrays(3)), table, ldt, tw, context,
+                                       path, None)
+
+    def copy(layers=3, count=2, heads=2, dim=64, pages=4, page=16, of=None, copies=P):
+        return lib.gptq2d_cache_copy(layers, count, heads, dim, pages, page, *(of or arrays(3)), copies, None)
+
+    for call in (commit, copy):
+        refused(call(layers=0), "layers")
+        refused(call(layers=4097), "layers")
+        refused(call(heads=0), "heads")
+        refused(call(dim=24), "dim")
+        refused(call(page=8), "page_size")
+        refused(call(pages=2 ** 31 // 16), "tokens")
+        refused(call(of=[None] + arrays(3)[1:]), "NULL")
+        refused(call(of=arrays(3, VC=(2, None))), "NULL")
+        refused(call(of=arrays(3, KS=(1, 4104))), "16-byte")
+    refused(commit(seqs=-1), "seqs")
+    refused(commit(width=65), "width")
+    refused(commit(table=NULL), "NULL")
+    refused(commit(path=NULL), "NULL")
+    refused(commit(ldt=3), "table")
+    refused(commit(tw=0), "table")
+    refused(commit(context=ctypes.c_void_p(4098)), "aligned")
+    refused(copy(count=-1), "count")
+    refused(copy(copies=NULL), "NULL")
+    refused(copy(copies=ctypes.c_void_p(4098)), "aligned")
+    assert commit(seqs=0) == 0 and copy(count=0) == 0
+
+
+def test_update_refusals(lib):
+    size = lib.gptq2d_pages_update_workspace_size
+    assert size(0, 5) == 0 and size(5, 0) == 0 and size(5, 100) > 0
+    ok = dict(rows=2, old=3, tw=4, table=P, ldt=4, length=P, source=P, want=P, held=P, pages=10, page=16,
+              out=ctypes.c_void_p(8192), ldo=4, copies=P, left=P, ws=P, nb=size(2, 10), stream=None)
+    call = lambda **k: lib.gptq2d_pages_update(*{**ok, **k}.values())
+    refused(call(rows=0), "rows")
+    refused(call(old=65536), "rows")
+    refused(call(page=24), "page_size")
+    refused(call(pages=0), "tokens")
+    refused(call(pages=2 ** 31 // 16), "tokens")
+    refused(call(tw=0), "table")
+    refused(call(ldt=3), "table")
+    refused(call(ldo=3), "table")
+    refused(call(rows=65535, tw=65536, ldt=65536, ldo=65536), "2^31")
+    for name in ("table", "length", "want", "out", "copies"):
+        refused(call(**{name: NULL}), "NULL")
+    refused(call(rows=4, source=NULL), "sources")
+    refused(call(left=ctypes.c_void_p(4098)), "aligned")
+    refused(call(out=P), "share memory")
+    refused(call(out=ctypes.c_void_p(4096 + 4 * 11)), "share memory")
+    assert call(nb=ok["nb"] - 1) == -6 and call(ws=ctypes.c_void_p(4100)) == -6
+
+
+def test_binding_checks():
+    t = torch.zeros(2, 3)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.gptq2d_tree_verify(t, torch.zeros(1, 2, dtype=torch.long), None, None, 1.0, None, None, None, 1.0, *[None] * 5)
+    with pytest.raises(ValueError, match="no layer"):
+        binding.gptq2d_cache_copy([], torch.zeros(1, 3, dtype=torch.int32))
+    with pytest.raises(TypeError, match="int32"):
+        binding.gptq2d_pages_update(torch.zeros(2, 3), torch.zeros(2), None, torch.zeros(2), None, 5, 16, t, None, None, None)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_oracle_of_page_tables(seed):
+    """No page is written that another row, or somebody else, reads."""
+    rng = random.Random(seed)
+    page, width, rows = 16, 6, 9
+    pages = 80
+    names = rng.sample(range(pages), rows * width)
+    table = [names[i * width:(i + 1) * width] for i in range(rows)]
+    length = [rng.randint(0, width * page) for _ in range(rows)]
+    held = [int(rng.random() < 0.2) for _ in range(pages)]
+    for _ in range(4):
+        source = [rng.randint(-1, rows - 1) for _ in range(rows)]
+        kept = [rng.randint(0, length[s]) if s >= 0 else 0 for s in source]
+        want = [min(k + rng.randint(0, 20), width * page) for k in kept]
+        kept = [min(length[s], w) if s >= 0 else 0 for s, w in zip(source, want)]
+        out, copies, left = serving.pages_update(table, length, source, want, held, pages, page)
+        for i in range(rows):
+            for j in range(-(-want[i] // page)):
+                if (j + 1) * page > kept[i]:  # the row writes here
+                    p = out[i][j]
+                    assert p < 0 or sum(r.count(p) for r in out) == 1 and not held[p]
+            for j in range(kept[i] // page):
+                assert out[i][j] == table[source[i]][j]
+        used = {p for r in out for p in r if p >= 0}
+        assert left < 0 or left == sum(p not in used and not held[p] for p in range(pages))
+        assert not {c[1] for c in copies if c[1] >= 0} & {c[0] for c in copies if c[0] >= 0}
+        table, length = out, want
