@@ -331,6 +331,65 @@ gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq
                                            size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Low-rank adapters of many requests, beside a projection that they share
+ *
+ * `count` adapters of rank R: A (count x R rows of K, row stride lda: adapter a's first
+ * row is row a R) and B (count x N rows of R, row stride ldb), scales (device, 32 bits,
+ * count; NULL: 1). Row m of a batch has the adapter index[m]; a number outside [0, count)
+ * means none. A smaller rank is one with rows of A, or columns of B, of zeros. M, N, K
+ * <= 2^22 (M may be 0), R <= 128, count <= 4096.
+ * ------------------------------------------------------------------------- */
+
+/* int32 numbers that gptq2d_adapter_groups writes for M rows: 2 M + count + 2 (0 on
+ * bad sizes). */
+int64_t gptq2d_adapter_groups_size(int64_t M, int count);
+
+/* Enqueues the order of a batch's rows by adapter, which all its projections use:
+ * groups (device, as sized above) gets the rows, adapter by adapter (those without one
+ * last, each's in the batch's order), each one's adapter, and each adapter's first place.
+ * index: device, M. M (count + 1) <= 2^32. Errors: INVALID_ARG, HIP. */
+gptq2d_status gptq2d_adapter_groups(int64_t M, int count, const int32_t* index, int32_t* groups,
+                                    void* stream);
+
+/* Bytes of device workspace gptq2d_adapters needs (0 on bad sizes). */
+size_t gptq2d_adapters_workspace_size(int64_t M, int64_t N, int64_t K, int R, int count);
+
+/* Enqueues O = Y + scales[a] H B_a^T, H = X A_a^T, with a the row's adapter; a row without
+ * one is Y's. X (M x K), A, B, Y (M x N; nullable: zeros) and O (M x N; may be Y itself)
+ * have type dt (F32, F16 or BF16); Y is what gptq2d_block_linear gives for the projection
+ * that the adapters lie beside. H (nullable, M x R, 32 bits): for the backward pass; zeros
+ * in rows without an adapter. groups: as gptq2d_adapter_groups gave them for the same M
+ * and count. Sums and H are held in 32 bits, O is rounded once. The same call gives the
+ * same bits. workspace: as sized above, 256-byte aligned, owned by the caller;
+ * overlapping calls need distinct ones. Errors: INVALID_ARG, WORKSPACE, HIP. */
+gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count, gptq2d_dtype dt,
+                              const void* X, int64_t ldx, const void* A, int64_t lda,
+                              const void* B, int64_t ldb, const float* scales,
+                              const int32_t* groups, const void* Y, int64_t ldy, void* O,
+                              int64_t ldo, float* H, void* workspace, size_t ws_bytes,
+                              void* stream);
+
+/* Bytes of device workspace gptq2d_adapters_backward needs (0 on bad sizes). */
+size_t gptq2d_adapters_backward_workspace_size(int64_t M, int64_t N, int64_t K, int R, int count);
+
+/* Enqueues the gradients of that call from G (M x N, type dt), the gradient of O (and so
+ * of Y), with H as the forward call gave it:
+ *   P = scales[a] G B_a, dX = D + P A_a (M x K, type dt; D nullable: zeros; dX may be D;
+ *       a row without an adapter is D's)
+ *   dA_a = sum of P^T X, dB_a = scales[a] sum of G^T H over the adapter's rows (32 bits,
+ *       contiguous, count x R x K and count x N x R; zeros for an adapter without rows)
+ * dX, dA and dB are nullable; A is read with dX, B with dX or dA, X with dA, H with dB.
+ * D is what the projection's own backward pass gives. Errors: INVALID_ARG, WORKSPACE,
+ * HIP. */
+gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, int count,
+                                       gptq2d_dtype dt, const void* G, int64_t ldg, const void* X,
+                                       int64_t ldx, const void* A, int64_t lda, const void* B,
+                                       int64_t ldb, const float* scales, const int32_t* groups,
+                                       const float* H, const void* D, int64_t ldd, void* dX,
+                                       int64_t lddx, float* dA, float* dB, void* workspace,
+                                       size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Eight-bit cache of keys and values, and the attention that reads it
  *
  * The cache holds `pages` pages of page_size tokens for `heads` key/value heads

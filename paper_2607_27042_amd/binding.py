@@ -86,6 +86,14 @@ def load():
         "gptq2d_block_linear_backward_workspace_size": (sz, [i64, i64, i64]),
         "gptq2d_block_linear_backward": (i32, [i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64,
                                                vp, i64, vp, sz, vp]),
+        "gptq2d_adapter_groups_size": (i64, [i64, i32]),
+        "gptq2d_adapter_groups": (i32, [i64, i32, vp, vp, vp]),
+        "gptq2d_adapters_workspace_size": (sz, [i64, i64, i64, i32, i32]),
+        "gptq2d_adapters": (i32, [i64, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp,
+                                  vp, sz, vp]),
+        "gptq2d_adapters_backward_workspace_size": (sz, [i64, i64, i64, i32, i32]),
+        "gptq2d_adapters_backward": (i32, [i64, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
+                                           i64, vp, i64, vp, vp, vp, sz, vp]),
         "gptq2d_cache_append": (i32, [i64, i32, i32, i32, vp, i64, vp, i64, vp, i32, i64, i32, vp, vp, vp, vp, vp]),
         "gptq2d_cache_read": (i32, [i64, i32, i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp]),
         "gptq2d_tree_masks": (i32, [i64, i32, vp, vp, vp]),
@@ -600,6 +608,78 @@ def gptq2d_block_linear_backward(dY, X, WT, SWT, dX, dW, workspace, pow2: bool =
     ws = _space(workspace, gptq2d_block_linear_backward_workspace_size(M, N, K), "gptq2d_block_linear_backward")
     args = (M, N, K, dt, *dy, *x, *wt, *swt, int(bool(pow2)), *dx, *dw, *ws, _stream(stream))
     return _enqueue("gptq2d_block_linear_backward", args, (dY, X, WT, SWT, dX, dW, workspace), stream, prepare)
+
+
+def gptq2d_adapter_groups_size(M: int, count: int) -> int:
+    return int(load().gptq2d_adapter_groups_size(M, count))
+
+
+def gptq2d_adapter_groups(index, count: int, groups, stream=None, prepare=False):
+    """The order of a batch's rows by adapter (index: int32, one for each row) into groups
+    (int32, gptq2d_adapter_groups_size numbers)."""
+    M = index.shape[0]
+    size = gptq2d_adapter_groups_size(M, count)
+    args = (M, count, _ints(index, (M,), torch.int32, "index"), _ints(groups, (size,), torch.int32, "groups"),
+            _stream(stream))
+    return _enqueue("gptq2d_adapter_groups", args, (index, groups), stream, prepare)
+
+
+def _adapter_weights(A, B, scales):
+    """(N, K, R, count) and the pointers, with row strides, of A [count, R, K] and B
+    [count, N, R]; scales [count] (float32; None: 1)."""
+    if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+        raise ValueError(f"A must be [count, R, K] and B [count, N, R], got {tuple(A.shape)} and {tuple(B.shape)}")
+    (count, R, K), N = A.shape, B.shape[1]
+    rows = []
+    for t, n, what in ((A, R, "A"), (B, N, "B")):
+        if count > 1 and n > 1 and t.stride(0) != n * t.stride(1):
+            raise ValueError(f"the adapters of {what} must lie behind one another")
+        cols = t.shape[2]
+        ld = t.stride(1) if n > 1 else t.stride(0) if count > 1 else cols
+        rows.append(_mat(t.as_strided((count * n, cols), (ld, t.stride(2) if cols > 1 else 1)), count * n, cols, what))
+    return N, K, R, count, rows[0], rows[1], None if scales is None else _ints(scales, (count,), torch.float32, "scales")
+
+
+def _groups(groups, M: int, count: int):
+    return _ints(groups, (gptq2d_adapter_groups_size(M, count),), torch.int32, "groups")
+
+
+def gptq2d_adapters_workspace_size(M: int, N: int, K: int, R: int, count: int) -> int:
+    return int(load().gptq2d_adapters_workspace_size(M, N, K, R, count))
+
+
+def gptq2d_adapters(X, A, B, scales, groups, Y, O, H, workspace, stream=None, prepare=False):
+    """O = Y + scales[a] (X A[a]^T) B[a]^T for the adapter a of each row; Y (None: zeros) may
+    be O. H (float32, [M, R]; None: not wanted): X A[a]^T, for the backward pass."""
+    N, K, R, count, a, b, sc = _adapter_weights(A, B, scales)
+    M = X.shape[0]
+    y = (ctypes.c_void_p(0), 0) if Y is None else _mat(Y, M, N, "Y")
+    args = (M, N, K, R, count, _narrow(X, A, B, Y, O), *_mat(X, M, K, "X"), *a, *b, sc, _groups(groups, M, count), *y,
+            *_mat(O, M, N, "O"), None if H is None else _ints(H, (M, R), torch.float32, "H"),
+            *_space(workspace, gptq2d_adapters_workspace_size(M, N, K, R, count), "gptq2d_adapters"), _stream(stream))
+    return _enqueue("gptq2d_adapters", args, (X, A, B, scales, groups, Y, O, H, workspace), stream, prepare)
+
+
+def gptq2d_adapters_backward_workspace_size(M: int, N: int, K: int, R: int, count: int) -> int:
+    return int(load().gptq2d_adapters_backward_workspace_size(M, N, K, R, count))
+
+
+def gptq2d_adapters_backward(G, X, A, B, scales, groups, H, D, dX, dA, dB, workspace, stream=None, prepare=False):
+    """From G, the gradient of O: dX = D + that of X through the adapters (D may be None, or
+    dX), dA and dB (float32, shaped like A and B). Any of the three may be None; X is
+    read for dA, H for dB."""
+    N, K, R, count, a, b, sc = _adapter_weights(A, B, scales)
+    M = G.shape[0]
+    none = (ctypes.c_void_p(0), 0)
+    opt = lambda t, cols, what: none if t is None else _mat(t, M, cols, what)
+    grad = lambda t, shape, what: None if t is None else _ints(t, shape, torch.float32, what)
+    args = (M, N, K, R, count, _narrow(G, X, A, B, D, dX), *_mat(G, M, N, "G"), *opt(X, K, "X"), *a, *b, sc,
+            _groups(groups, M, count), grad(H, (M, R), "H"), *opt(D, K, "D"), *opt(dX, K, "dX"),
+            grad(dA, (count, R, K), "dA"), grad(dB, (count, N, R), "dB"),
+            *_space(workspace, gptq2d_adapters_backward_workspace_size(M, N, K, R, count), "gptq2d_adapters_backward"),
+            _stream(stream))
+    return _enqueue("gptq2d_adapters_backward", args, (G, X, A, B, scales, groups, H, D, dX, dA, dB, workspace), stream,
+                    prepare)
 
 
 def _cache(KC, VC, KS, VS):

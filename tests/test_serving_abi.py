@@ -158,3 +158,60 @@ def test_oracle_of_page_tables(seed):
         assert left < 0 or left == sum(p not in used and not held[p] for p in range(pages))
         assert not {c[1] for c in copies if c[1] >= 0} & {c[0] for c in copies if c[0] >= 0}
         table, length = out, want
+
+
+def test_adapters_refusals(lib):
+    size, back = lib.gptq2d_adapters_workspace_size, lib.gptq2d_adapters_backward_workspace_size
+    assert size(0, 8, 8, 4, 2) == 0 and size(8, 8, 8, 129, 2) == 0 and size(8, 8, 8, 4, 2) > 0
+    assert back(0, 8, 8, 4, 2) == 0 and back(8, 8, 8, 4, 5000) == 0 and back(8, 8, 8, 4, 2) > 0
+    assert lib.gptq2d_adapter_groups_size(7, 3) == 19 and lib.gptq2d_adapter_groups_size(-1, 3) == 0
+    refused(lib.gptq2d_adapter_groups(-1, 3, P, P, None), "M")
+    refused(lib.gptq2d_adapter_groups(5, 0, P, P, None), "count")
+    refused(lib.gptq2d_adapter_groups(2 ** 22, 2048, P, P, None), "2^32")
+    refused(lib.gptq2d_adapter_groups(5, 3, NULL, P, None), "NULL")
+    refused(lib.gptq2d_adapter_groups(5, 3, P, ctypes.c_void_p(4098), None), "aligned")
+    shape = dict(M=8, N=16, K=24, R=4, count=2, dt=BF16)
+    ok = dict(**shape, X=P, ldx=24, A=P, lda=24, B=P, ldb=4, scales=P, groups=P, Y=P, ldy=16, O=P, ldo=16, H=P, ws=P,
+              nb=size(8, 16, 24, 4, 2), stream=None)
+    call = lambda **k: lib.gptq2d_adapters(*{**ok, **k}.values())
+    for k in (dict(M=-1), dict(M=2 ** 22 + 1), dict(N=0), dict(K=2 ** 22 + 1)):
+        refused(call(**k), "M, N and K")
+    refused(call(R=0), "R in")
+    refused(call(R=129), "R in")
+    refused(call(count=4097), "count")
+    refused(call(dt=F64), "dtype")
+    for name in ("X", "A", "B", "groups", "O"):
+        refused(call(**{name: NULL}), "NULL")
+    for name in ("ldx", "lda", "ldb", "ldy", "ldo"):
+        refused(call(**{name: ok[name] - 1}), "leading dimension")
+    refused(call(Y=ctypes.c_void_p(4097)), "aligned")
+    refused(call(H=ctypes.c_void_p(4098)), "aligned")
+    assert call(M=0) == 0  # no work
+    assert call(nb=ok["nb"] - 1) == -6 and call(ws=ctypes.c_void_p(4100)) == -6
+    ok = dict(**shape, G=P, ldg=16, X=P, ldx=24, A=P, lda=24, B=P, ldb=4, scales=P, groups=P, H=P, D=P, ldd=24, dX=P, lddx=24,
+              dA=P, dB=P, ws=P, nb=back(8, 16, 24, 4, 2), stream=None)
+    call = lambda **k: lib.gptq2d_adapters_backward(*{**ok, **k}.values())
+    refused(call(R=129), "R in")
+    refused(call(dt=F64), "dtype")
+    refused(call(dX=NULL, dA=NULL, dB=NULL), "no gradient")
+    refused(call(groups=NULL), "NULL")
+    refused(call(G=NULL), "NULL")
+    refused(call(A=NULL), "dX needs A")
+    refused(call(B=NULL), "need B")
+    refused(call(X=NULL), "dA needs X")
+    refused(call(H=NULL), "dB needs H")
+    for name in ("ldg", "ldx", "lda", "ldb", "ldd", "lddx"):
+        refused(call(**{name: ok[name] - 1}), "leading dimension")
+    refused(call(dX=ctypes.c_void_p(4097)), "aligned")
+    refused(call(dB=ctypes.c_void_p(4098)), "aligned")
+    assert call(nb=ok["nb"] - 1) == -6 and call(ws=NULL) == -6
+
+
+def test_adapter_weights():
+    """Adapters behind one another, with a row stride; other layouts are refused."""
+    with pytest.raises(ValueError, match=r"\[count, R, K\]"):
+        binding._adapter_weights(torch.zeros(2, 4, 8), torch.zeros(2, 8, 5), None)
+    with pytest.raises(ValueError, match="behind one another"):
+        binding._adapter_weights(torch.zeros(3, 4, 8)[::2], torch.zeros(2, 8, 4), None)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding._adapter_weights(torch.zeros(2, 4, 8), torch.zeros(2, 8, 4), None)
