@@ -29,11 +29,77 @@ namespace g2d {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVec = 16;                 // elements of a thread and step
+constexpr int kVec = 16;                 // elements of a thread and step in the first pass
 constexpr int kChunk = kThreads * kVec;  // of a work group
+// and step in 64-bit passes
+constexpr int kFew = 4;
+constexpr int kFewChunk = kThreads * kFew;
+constexpr int kTurn = 4;  // steps whose loads are on their way at once
 constexpr int kMaxWidth = 64;
 constexpr int kMaxParts = 64;            // of a row
 constexpr float kLog2E = 1.44269504088896341f;
+constexpr double kLog2E64 = 1.4426950408889634;
+
+// 2^t to about 1e-13 of itself for t in [-1000, 1000], 0 below (NaN: any number), from a table
+// of 2^(k / 256). t is split at the nearest multiple of 1 / 256, which adding 1.5 2^44
+// leaves in the low bits; the rest, |f| <= 1 / 512, needs four terms of its series. The 64-bit
+// terms of the last rows are most of what their pass costs: 64 rows of 128000 with as many
+// of the drafts 20 us, 22 with a polynomial of degree 8 on |f| <= 1 / 2 and no table.
+struct Powers {
+  double at[256];
+  __device__ __forceinline__ void fill() {  // by the first 256 threads; a barrier follows
+    if (threadIdx.x < 256) at[threadIdx.x] = exp2((double)threadIdx.x * 0x1p-8);
+  }
+  __device__ __forceinline__ double of(double t) const {
+    const double big = t + 0x1.8p44, f = t - (big - 0x1.8p44);
+    const uint32_t k = __builtin_bit_cast(u2, big)[0];
+    double p = 0.05550410866482158;
+    p = fma(p, f, 0.2402265069591007);
+    p = fma(p, f, 0.6931471805599453);
+    p *= f;
+    const double e = at[k & 255];
+    u2 b = __builtin_bit_cast(u2, fma(e, p, e));
+    b[1] += (uint32_t)((int32_t)k >> 8) << 20;
+    return t < -1000.0 ? 0.0 : __builtin_bit_cast(double, b);
+  }
+};
+
+// Across a wave without LDS, whose answers would take longer than all else in passes of a
+// few elements a lane: a value moved by a lane pattern, sums of all lanes and of those up
+// to the lane, the value of one lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {  // 0 where the pattern gives none
+  const u2 b = __builtin_bit_cast(u2, x);
+  return __builtin_bit_cast(double, u2{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)b[0], CTRL, ROWS, 0xf, true),
+                                       (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b[1], CTRL, ROWS, 0xf, true)});
+}
+__device__ __forceinline__ double sum_upto(double x) {
+  x += moved<0x111, 0xf>(x);  // rows of 16: 1, 2, 4, 8 lanes up
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);  // the last of rows 0 and 2 to the rows after them
+  x += moved<0x143, 0xc>(x);  // the last of the first half to the second
+  return x;
+}
+__device__ __forceinline__ double at_lane(double x, int lane) {
+  const u2 b = __builtin_bit_cast(u2, x);
+  return __builtin_bit_cast(double, u2{(uint32_t)__builtin_amdgcn_readlane((int)b[0], lane),
+                                       (uint32_t)__builtin_amdgcn_readlane((int)b[1], lane)});
+}
+__device__ __forceinline__ double wave_sum(double x) { return at_lane(sum_upto(x), 63); }
+// a float as a number that orders alike (NaN as -inf), and back
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x == x ? x + 0.0f : -INFINITY);
+  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
+// the largest of all lanes, and the lowest place of those that have it
+__device__ __forceinline__ void wave_top(float& x, int& at) {
+  const uint32_t mine = order_of(x), top = group_max<64>(mine);
+  at = (int)~group_max<64>(mine == top ? ~(uint32_t)at : 0);
+  x = value_of(top);
+}
 
 // of a part of a row: its largest logit, the lowest token that has it, and sums
 // relative to it
@@ -44,15 +110,15 @@ struct alignas(16) Part {
 };
 // of a part of the last row; m, sum: as above, left: the sum of r
 struct alignas(16) Last {
-  double m, sum, left;
-  int64_t at;
+  double m, sum, left, less;  // of drawn drafts: Residue's over and less
+  int32_t at, unused[3];
 };
 // what the scan ends with
 struct alignas(16) State {
   int32_t node;      // -1: none
   int32_t residual;  // r is less than p
   uint64_t gone;     // rejected tokens of the node
-  double beta, m, sum;  // drawn drafts: with the row's largest logit and its sum
+  double beta, m, sum;  // drawn drafts, rejected: beta, the row's largest logit and its sum
 };
 
 struct VerifyArgs {
@@ -74,6 +140,28 @@ struct VerifyArgs {
   Part* part;
   Last* last;
   State* state;
+  // e^(a (x - m)) and e^(ad d - lse); of -inf both are 0
+  __device__ __forceinline__ double p2(const Powers& of, float x, double m) const {
+    const double c = (double)a * kLog2E64;
+    return of.of(fma((double)x, c, -m * c));
+  }
+  __device__ __forceinline__ double q2(const Powers& of, float d, double lse) const {
+    return of.of(fma((double)d, (double)ad * kLog2E64, -lse * kLog2E64));
+  }
+};
+
+// Sums for a drawn draft's residue over some terms f = e^(a (x - m)): of f, and of f and beta
+// q where p > beta q. The sum of max(p - beta q, 0) is over / all - less, with `all` of the
+// whole row, which is known only afterwards; which terms are over is told by a sum that is off by
+// 1e-7, what matters only for terms as near to zero as that.
+struct Residue {
+  double all, over, less;
+  __device__ __forceinline__ void add(double f, double by, double bq) {
+    const bool in = f * by > bq;
+    all += f;
+    over += in ? f : 0.0;
+    less += in ? bq : 0.0;
+  }
 };
 
 __device__ __forceinline__ int drafted(const VerifyArgs& v, int64_t seq) {
@@ -85,26 +173,66 @@ __device__ __forceinline__ int parent_of(const VerifyArgs& v, int64_t seq, int t
   return p >= 0 && p < t ? p : -1;
 }
 
-// Elements first .. first + kVec - 1 of a row, those outside [0, n) as -inf. `first` is
-// kVec elements times something behind a 16-byte boundary where the row allows it.
-template <class T>
-__device__ __forceinline__ void load16(const T* x, int64_t first, int n, float v[kVec]) {
-  constexpr int W = 16 / sizeof(T);
-  struct alignas(16) V { T v[W]; };
-  if (first >= 0 && first + kVec <= n && ((uintptr_t)(x + first) & 15) == 0) {
+// device memory (which the compiler does not see of every pointer here; what it takes for
+// any memory it loads in order with LDS)
+#define G2D_GLOBAL __attribute__((address_space(1)))
+
+// N elements behind a boundary of as many bytes (16 at most), as they are loaded
+template <class T, int N>
+struct Raw {
+  static constexpr int W = N * sizeof(T) < 16 ? N : 16 / sizeof(T);
+  typedef uint32_t V __attribute__((ext_vector_type(W * sizeof(T) / 4)));
+  typedef T E __attribute__((ext_vector_type(W)));
+  V p[N / W];
+  __device__ __forceinline__ void load(const T* x) {
 #pragma unroll
-    for (int i = 0; i < kVec / W; ++i) {
-      const V p = *(const V*)(x + first + i * W);
+    for (int i = 0; i < N / W; ++i) p[i] = *(const G2D_GLOBAL V*)(x + i * W);
+  }
+  __device__ __forceinline__ void values(float v[N]) const {
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[i * W + j] = (float)p.v[j];
+    for (int i = 0; i < N / W; ++i) {
+      const E e = __builtin_bit_cast(E, p[i]);
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i * W + j] = (float)e[j];
     }
+  }
+  static __device__ __forceinline__ bool fits(const T* x, int first, int n) {
+    return first >= 0 && first + N <= n && ((uintptr_t)(x + first) & (sizeof(V) - 1)) == 0;
+  }
+};
+// Elements first .. first + N - 1 of a row, those outside [0, n) as -inf.
+template <int N, class T>
+__device__ __forceinline__ void load_some(const T* x, int first, int n, float v[N]) {
+  if (Raw<T, N>::fits(x, first, n)) {
+    Raw<T, N> r;
+    r.load(x + first);
+    r.values(v);
   } else {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = (float)x[max((int64_t)0, min(first + i, (int64_t)n - 1))];
+    for (int i = 0; i < N; ++i) v[i] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = first + i >= 0 && first + i < n ? v[i] : -INFINITY;
+    for (int i = 0; i < N; ++i)
+      if (first + i >= 0 && first + i < n) v[i] = (float)((const G2D_GLOBAL T*)x)[first + i];
   }
 }
+// kTurn steps of kFew elements from e on, a group's steps behind one another
+template <class T>
+struct Turn {
+  float z[kTurn][kFew];
+  __device__ __forceinline__ void load(const T* x, int e, int n) {
+    typedef Raw<T, kFew> R;
+    if (R::fits(x, e, n) && R::fits(x, e + (kTurn - 1) * kFewChunk, n)) {
+      R r[kTurn];
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) r[k].load(x + e + k * kFewChunk);
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) r[k].values(z[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) load_some<kFew>(x, e + k * kFewChunk, n, z[k]);
+    }
+  }
+};
 template <class T>
 __device__ __forceinline__ int lead_of(const T* x) {
   return (int)(((uintptr_t)x & 15) / sizeof(T));
@@ -117,19 +245,19 @@ __device__ __forceinline__ Part join(Part p, Part q, float a) {
     p = q;
     q = t;
   }
-  if (q.sum != 0.0) p.sum += q.sum * (double)__builtin_amdgcn_exp2f((q.m - p.m) * a * kLog2E);
+  if (q.sum != 0.0) p.sum += q.sum * exp2(((double)q.m - (double)p.m) * (double)a * kLog2E64);
   return p;
 }
 __device__ __forceinline__ Part wave_join(Part p, float a) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const Part q{__shfl_xor(p.m, d), __shfl_xor(p.at, d), __shfl_xor(p.sum, d)};
-    p = (threadIdx.x & d) ? join(q, p, a) : join(p, q, a);
-  }
-  return p;
+  Part q = p;
+  wave_top(q.m, q.at);
+  q.sum = wave_sum(p.sum != 0.0 ? p.sum * exp2(((double)p.m - (double)q.m) * (double)a * kLog2E64) : 0.0);
+  return q;
 }
 
-// Largest logit and sum of a part of every row that tokens follow.
+// Largest logit and sum of a part of every row that tokens follow. Bound by its bytes: 64
+// chains of 8 over 128000 bf16 26 us for 115 MB, 4.4 TB/s (with 64-bit terms, which would spare
+// the last row's own sum, 61 us).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
   __shared__ Part wave[kThreads / 64];
@@ -145,24 +273,42 @@ __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
   const float a2 = v.a * kLog2E;
   float m = -INFINITY, sum = 0.0f;
   int at = 0x7fffffff;
+  // a thread's elements of a step lie in pieces of 16 bytes, the pieces of a group side by
+  // side; the steps inside the row are loaded one ahead
+  constexpr int W = 16 / sizeof(T), N = kVec / W;
+  const int inner = lead > 0 ? 1 : 0, outer = (v.vocab + lead) / kChunk - 1;
+  Raw<T, W> raw[N];
+  auto place = [&](int s, int i) { return s * kChunk + i * kThreads * W + t * W - lead; };
+  auto ahead = [&](int s) {
+    const int c = max(inner, min(s, outer));
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw[i].load(x + place(c, i));
+  };
+  if (inner <= outer) ahead(first);
+#pragma unroll 1
   for (int s = first; s < last; ++s) {
     float z[kVec];
-    const int64_t e = (int64_t)s * kChunk + (int64_t)t * kVec - lead;
-    load16(x, e, v.vocab, z);
+    if (s >= inner && s <= outer) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) raw[i].values(z + i * W);
+      ahead(s + 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_some<W>(x, place(s, i), v.vocab, z + i * W);
+      if (inner <= outer) ahead(s + 1);
+    }
     float top = z[0];
 #pragma unroll
     for (int i = 1; i < kVec; ++i) top = fmaxf(top, z[i]);
     if (top > m) {
       sum *= __builtin_amdgcn_exp2f((m - top) * a2);
       m = top;
-      int k = 0;
 #pragma unroll
-      for (int i = kVec - 1; i >= 0; --i) k = z[i] == top ? i : k;
-      at = (int)(e + k);
+      for (int i = kVec - 1; i >= 0; --i) at = z[i] == top ? place(s, i / W) + i % W : at;
     }
+    const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (z[i] != -INFINITY) sum += __builtin_amdgcn_exp2f((z[i] - m) * a2);  // NaN: NaN
+    for (int i = 0; i < kVec; ++i) sum += __builtin_amdgcn_exp2f((z[i] - ref) * a2);  // NaN: NaN
   }
   Part p = wave_join(Part{m, at, (double)sum}, v.a);
   if (lane == 0) wave[t >> 6] = p;
@@ -170,20 +316,15 @@ __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
   if (t == 0) v.part[blockIdx.x] = join(join(wave[0], wave[1], v.a), join(wave[2], wave[3], v.a), v.a);
 }
 
-constexpr int kWalk = 1024;
-
-__device__ __forceinline__ double wave_sum(double s) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
-  return s;
-}
+constexpr int kWalk = 512;
 
 // The scan of a sequence. All waves go through it alike; where a drawn draft is
 // rejected they share a pass over the row.
 template <class T>
 __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
   __shared__ Part rows[kMaxWidth];
-  __shared__ double sums[kWalk / 64];
+  __shared__ Residue sums[kWalk / 64];
+  __shared__ Powers powers;
   const int64_t seq = blockIdx.x;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   const int n = drafted(v, seq);
@@ -197,6 +338,7 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     p = wave_join(p, v.a);
     if (lane == 0) rows[c] = p;
   }
+  if (v.D) powers.fill();
   __syncthreads();
   const int64_t token = in ? v.tokens[seq * v.width + lane] : -1;
   const T *X = (const T*)v.X + seq * v.width * v.ldx, *D = (const T*)v.D + seq * v.width * v.ldd;
@@ -209,44 +351,39 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     const bool ok = token >= 0 && token < v.vocab;
     const double z = ok ? ((double)(float)X[parent * v.ldx + token] - (double)r.m) * (double)v.a : -INFINITY;
     // of a row of nothing but -inf, or with a NaN or +inf: NaN
-    p = exp(z) / r.sum;
+    p = exp2(z * kLog2E64) / r.sum;
     lp = (float)(z - log(r.sum));
     if (!(r.sum > 0.0)) lp = __uint_as_float(0x7fc00000u), p = (double)lp;
-    if (v.D && ok) q = exp((double)(float)D[parent * v.ldd + token] * (double)v.ad - (double)dlse[parent]);
+    if (v.D && ok) q = exp2(((double)(float)D[parent * v.ldd + token] * (double)v.ad - (double)dlse[parent]) * kLog2E64);
     best = p == p && token == r.at;
   }
   const double u = v.u && in ? (double)v.u[seq * v.width + lane] : 0.0;
-  auto of = [&](double x, int from) { return __shfl(x, from); };
+  auto of = [&](double x, int from) { return at_lane(x, from); };
   int cur = n > 0 ? 0 : -1, kept = n > 0 ? 1 : 0;
   int way = lane == 0 && n > 0 ? 0 : -1;  // lane i: the i-th kept token
-  double beta = 0.0, M = 1.0, gone_p = 0.0, total = 0.0, top = 0.0;
+  double beta = 0.0, M = 1.0, gone_p = 0.0;
   uint64_t gone = 0;
-  bool summed = false;
-  // the sum of the current row and of max(p - beta q, 0), in 64 bits
-  auto pass = [&](bool residual) {
+  // the sum of max(p - beta q, 0) of the current row
+  auto remaining = [&]() {
     const T *x = X + cur * v.ldx, *d = D + cur * v.ldd;
-    double s = 0.0;
     const int lead = lead_of(x);
-    for (int64_t e = (int64_t)t * kVec - lead; e < v.vocab; e += kWalk * kVec) {
-      float z[kVec], y[kVec];
-      load16(x, e, v.vocab, z);
-      if (residual) load16(d, e, v.vocab, y);
-      for (int i = 0; i < kVec; ++i) {
-        if (z[i] == -INFINITY) continue;
-        const double f = exp(((double)z[i] - top) * (double)v.a);
-        if (!residual)
-          s += f;
-        else
-          s += fmax(f / total - beta * exp((double)y[i] * (double)v.ad - (double)dlse[cur]), 0.0);
-      }
+    const double top = (double)rows[cur].m, by = 1.0 / rows[cur].sum, lse = (double)dlse[cur];
+    Residue r{};
+#pragma unroll 1
+    for (int e = t * kFew - lead; e < v.vocab; e += kWalk * kFew) {
+      float z[kFew], y[kFew];
+      load_some<kFew>(x, e, v.vocab, z);
+      load_some<kFew>(d, e, v.vocab, y);
+#pragma unroll
+      for (int i = 0; i < kFew; ++i) r.add(v.p2(powers, z[i], top), by, beta * v.q2(powers, y[i], lse));
     }
-    s = wave_sum(s);
+    r = Residue{wave_sum(r.all), wave_sum(r.over), wave_sum(r.less)};
     __syncthreads();
-    if (lane == 0) sums[w] = s;
+    if (lane == 0) sums[w] = r;
     __syncthreads();
-    s = 0.0;
-    for (int i = 0; i < kWalk / 64; ++i) s += sums[i];
-    return s;
+    r = Residue{};
+    for (int i = 0; i < kWalk / 64; ++i) r.all += sums[i].all, r.over += sums[i].over, r.less += sums[i].less;
+    return fmax(r.over / r.all - r.less, 0.0);
   };
   while (cur >= 0) {
     const uint64_t children = __ballot(parent == cur);
@@ -255,17 +392,15 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
       const int c = __builtin_ctzll(left);
       const double pc = of(p, c);
       if (!v.u) {
-        if (__shfl((int)best, c)) taken = c;
+        if (__ballot(best) >> c & 1) taken = c;
       } else if (v.D) {
-        if (gone != 0) {
-          if (!summed) top = (double)rows[cur].m, total = pass(false), summed = true;
-          M = pass(true);
-        }
+        if (gone != 0) M = remaining();
         const double qc = of(q, c);
         if (of(u, c) * M * qc < pc - beta * qc) taken = c;
         else beta += M;
       } else {
-        const int64_t mine = __shfl(token, c);
+        const int64_t mine = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(token >> 32), c) << 32 |
+                                       (uint32_t)__builtin_amdgcn_readlane((int)token, c));
         const bool again = (__ballot(token == mine) & gone) != 0;
         if (!again && of(u, c) * (1.0 - gone_p) < pc) taken = c;
         else if (!again) gone_p += pc;
@@ -277,10 +412,9 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     cur = taken;
     if (lane == kept) way = cur;
     ++kept;
-    gone = 0, beta = 0.0, M = 1.0, gone_p = 0.0, summed = false;
+    gone = 0, beta = 0.0, M = 1.0, gone_p = 0.0;
   }
   const bool residual = v.u && gone != 0;
-  if (residual && v.D && !summed) top = (double)rows[cur].m, total = pass(false);
   if (w == 0) {
     if (in) {
       v.path[seq * v.width + lane] = way;
@@ -288,7 +422,7 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     }
     if (lane == 0) {
       v.count[seq] = kept;
-      v.state[seq] = State{cur, residual, gone, beta, top, total};
+      v.state[seq] = State{cur, residual, gone, beta, residual ? (double)rows[cur].m : 0.0, residual ? rows[cur].sum : 0.0};
     }
   }
 }
@@ -298,43 +432,30 @@ struct Gone {
   int token[kMaxWidth];
   int n;
 };
-__device__ __forceinline__ void find_gone(const VerifyArgs& v, const State& s, int64_t seq, int64_t first, int64_t end, Gone& g) {
+__device__ __forceinline__ void find_gone(const VerifyArgs& v, const State& s, int64_t seq, int first, int end, Gone& g) {
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
     const int64_t token = s.gone >> lane & 1 ? v.tokens[seq * v.width + lane] : -1;
-    const bool here = token >= first && token < end;
+    const bool here = token >= max(first, 0) && token < end;
     const uint64_t all = __ballot(here);
     if (here) g.token[__popcll(all & ((1ull << lane) - 1))] = (int)token;
     if (lane == 0) g.n = __popcll(all);
   }
 }
 
-// e^(a (x - m)) and what is left of it (relative to the row's sum, for drawn drafts) of a
-// thread's elements
-template <class T>
-__device__ __forceinline__ void remaining(const VerifyArgs& v, const State& s, const Gone& g, const T* x, const T* d, double dlse,
-                                          int64_t e, const float z[kVec], double m, double f[kVec], double r[kVec]) {
-  float y[kVec];
-  const bool drawn = s.residual && v.D;
-  if (drawn) load16(d, e, v.vocab, y);
+__device__ __forceinline__ void without(const Gone& g, int e, double f[kFew]) {
+#pragma unroll 1
+  for (int k = 0; k < g.n; ++k)
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    f[i] = z[i] == -INFINITY ? 0.0 : exp(((double)z[i] - m) * (double)v.a);
-    r[i] = f[i];
-    if (drawn) r[i] = z[i] == -INFINITY ? 0.0 : fmax(f[i] / s.sum - s.beta * exp((double)y[i] * (double)v.ad - dlse), 0.0);
-  }
-  if (s.residual && !v.D)
-    for (int k = 0; k < g.n; ++k)
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) r[i] = e + i == g.token[k] ? 0.0 : r[i];
+    for (int i = 0; i < kFew; ++i) f[i] = e + i == g.token[k] ? 0.0 : f[i];
 }
-
 // Sums of one part of the last row.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   __shared__ Gone gone;
   __shared__ float tops[kThreads / 64];
-  __shared__ double sums[2][kThreads / 64];
+  __shared__ Residue sums[kThreads / 64];
+  __shared__ Powers powers;
   __shared__ int first[kThreads / 64];
   const int64_t seq = blockIdx.x / (uint32_t)v.chunks;
   const int chunk = blockIdx.x - (int)seq * v.chunks, t = threadIdx.x, lane = t & 63;
@@ -343,48 +464,69 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   const int64_t row = seq * v.width + s.node;
   const T *x = (const T*)v.X + row * v.ldx, *d = (const T*)v.D + row * v.ldd;
   const int lead = lead_of(x);
-  const int64_t begin = (int64_t)chunk * v.per - lead, end = min(begin + v.per, (int64_t)v.vocab);
+  const int begin = chunk * v.per - lead, end = min(begin + v.per, v.vocab);
+  const bool drawn = s.residual && v.D;
   find_gone(v, s, seq, begin, end, gone);
+  powers.fill();
+  const bool once = v.per <= kTurn * kFewChunk;  // all of the part in registers
+  Turn<T> turn, other;
+  if (once) turn.load(x, begin + t * kFew, end);
+  if (once && drawn) other.load(d, begin + t * kFew, end);
   float top = -INFINITY;
   int at = 0x7fffffff;
-  for (int64_t e = begin + t * kVec; e < end; e += kChunk) {
-    float z[kVec];
-    load16(x, e, v.vocab, z);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (z[i] > top) top = z[i], at = (int)(e + i);
-  }
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const float o = __shfl_xor(top, k);
-    const int oa = __shfl_xor(at, k);
-    if (o > top || (o == top && oa < at)) top = o, at = oa;
-  }
-  if (lane == 0) tops[t >> 6] = top, first[t >> 6] = at;
-  __syncthreads();
-  for (int k = 0; k < kThreads / 64; ++k)
-    if (tops[k] > top || (tops[k] == top && first[k] < at)) top = tops[k], at = first[k];
-  // the row's own largest where the scan needed it: r is relative to the whole row then
-  const double m = s.residual && v.D ? s.m : (double)top;
-  const double dlse = s.residual && v.D ? (double)v.dlse[row] : 0.0;
-  double all = 0.0, left = 0.0;
   bool bad = false;
-  for (int64_t e = begin + t * kVec; e < end; e += kChunk) {
-    float z[kVec];
-    double f[kVec], r[kVec];
-    load16(x, e, v.vocab, z);
-    remaining(v, s, gone, x, d, dlse, e, z, m, f, r);
+  if (!drawn) {
+    for (int e = begin + t * kFew; e < end; e += kTurn * kFewChunk) {
+      if (e > begin + t * kFew || !once) turn.load(x, e, end);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) all += f[i], left += r[i], bad |= z[i] != z[i] || z[i] == INFINITY;
+      for (int k = 0; k < kTurn; ++k)
+#pragma unroll
+        for (int i = 0; i < kFew; ++i)
+          if (turn.z[k][i] > top) top = turn.z[k][i], at = e + k * kFewChunk + i;
+    }
+    wave_top(top, at);
+    if (lane == 0) tops[t >> 6] = top, first[t >> 6] = at;
   }
-  if (bad) all = NAN;
-  all = wave_sum(all), left = wave_sum(left);
-  if (lane == 0) sums[0][t >> 6] = all, sums[1][t >> 6] = left;
+  __syncthreads();
+  if (!drawn)
+    for (int k = 0; k < kThreads / 64; ++k)
+      if (tops[k] > top || (tops[k] == top && first[k] < at)) top = tops[k], at = first[k];
+  // drawn drafts: the row's own largest, so that its terms can be told from q
+  const double m = drawn ? s.m : top == -INFINITY ? 0.0 : (double)top;
+  const bool some = s.residual && !v.D && gone.n > 0;
+  const double by = drawn ? 1.0 / s.sum : 0.0, lse = drawn ? (double)v.dlse[row] : 0.0;
+  Residue r{};
+  for (int e0 = begin + t * kFew; e0 < end; e0 += kTurn * kFewChunk) {
+    if (!once) turn.load(x, e0, end);
+    if (drawn && !once) other.load(d, e0, end);
+#pragma unroll
+    for (int k = 0; k < kTurn; ++k) {
+      if (e0 - t * kFew + k * kFewChunk >= end) break;
+      double f[kFew];
+#pragma unroll
+      for (int i = 0; i < kFew; ++i) {
+        const float z = turn.z[k][i];
+        f[i] = v.p2(powers, z, m);
+        bad |= z != z || z == INFINITY;
+        if (drawn) r.add(f[i], by, s.beta * v.q2(powers, other.z[k][i], lse));
+        else r.all += f[i];
+      }
+      if (some) {
+        without(gone, e0 + k * kFewChunk, f);
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) r.over += f[i];
+      }
+    }
+  }
+  if (bad) r.all = NAN;
+  if (!drawn && !some) r.over = r.all;
+  r = Residue{wave_sum(r.all), wave_sum(r.over), wave_sum(r.less)};
+  if (lane == 0) sums[t >> 6] = r;
   __syncthreads();
   if (t == 0) {
-    all = left = 0.0;
-    for (int k = 0; k < kThreads / 64; ++k) all += sums[0][k], left += sums[1][k];
-    v.last[blockIdx.x] = Last{m, all, left, at};
+    r = Residue{};
+    for (int k = 0; k < kThreads / 64; ++k) r.all += sums[k].all, r.over += sums[k].over, r.less += sums[k].less;
+    v.last[blockIdx.x] = Last{top == -INFINITY && !drawn ? -INFINITY : m, r.all, r.over, r.less, at, {}};
   }
 }
 
@@ -393,9 +535,10 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
   __shared__ double sums[kThreads / 64];
-  __shared__ int found;
+  __shared__ int found[kThreads / 64];
+  __shared__ Powers powers;
   const int64_t seq = blockIdx.x;
-  const int t = threadIdx.x, lane = t & 63;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   State s = v.state[seq];
   if (s.node < 0) {
     if (t == 0) v.next[seq] = -1, v.logprob[seq * v.width] = 0.0f;
@@ -403,21 +546,15 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   }
   const int64_t row = seq * v.width + s.node;
   const T *x = (const T*)v.X + row * v.ldx, *d = (const T*)v.D + row * v.ldd;
-  Last l{-INFINITY, 0.0, 0.0, 0x7fffffff};
+  Last l{-INFINITY, 0.0, 0.0, 0.0, 0x7fffffff, {}};
   if (lane < v.chunks) l = v.last[seq * v.chunks + lane];
-  double m = l.m, best = l.m;
-  int64_t at = l.at;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const double o = __shfl_xor(best, k);
-    const int64_t oa = __shfl_xor(at, k);
-    if (o > best || (o == best && oa < at)) best = o, at = oa;
-  }
-  const double f = l.sum == 0.0 ? 0.0 : exp((m - best) * (double)v.a);
+  bool drawn = s.residual && v.D;
+  float best = (float)l.m;  // (they are 32-bit numbers)
+  int at = l.at;
+  if (!drawn) wave_top(best, at);
+  else best = (float)s.m;
+  const double f = drawn || best == -INFINITY ? 1.0 : exp2((l.m - (double)best) * ((double)v.a * kLog2E64));
   const double total = wave_sum(l.sum * f);
-  const bool drawn = s.residual && v.D;
-  double left = l.left * (drawn ? 1.0 : f);
-  if (l.left == 0.0) left = 0.0;
   if (!(total > 0.0)) {  // nothing but -inf, or a NaN or +inf
     if (t == 0) v.next[seq] = -1, v.logprob[seq * v.width] = __uint_as_float(0x7fc00000u);
     return;
@@ -425,88 +562,82 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   int64_t chosen = at;
   if (v.u) {
     const double u = (double)v.u[seq * v.width];
-    if (s.residual && !(wave_sum(left) > 0.0)) {  // nothing is left of p: p itself
-      s.residual = 0;
+    double left = drawn ? fmax(l.left / total - l.less, 0.0) : l.left * f;
+    if (s.residual && __ballot(left > 0.0) == 0) {  // nothing is left of p: p itself
+      s.residual = 0, drawn = false;
       left = l.sum * f;
-      if (drawn && l.sum == 0.0) left = 0.0;
     }
     // sums of the parts up to the lane's
-    double upto = left;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const double o = __shfl_up(upto, k);
-      if (lane >= k) upto += o;
-    }
-    const double aim = u * __shfl(upto, 63);
+    const double upto = sum_upto(left), aim = u * at_lane(upto, 63);
     const uint64_t over = __ballot(upto > aim && left > 0.0), some = __ballot(left > 0.0);
-    const int part = over != 0 ? __builtin_ctzll(over) : some != 0 ? 63 - __builtin_clzll(some) : 0;
-    const double before = __shfl(upto - left, part), aim_in = aim - before;
-    const double pm = __shfl(m, part), pf = s.residual && v.D ? 1.0 : __shfl(f, part);
+    const int part = over != 0 ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1);
+    const double before = at_lane(upto - left, part);
+    const double pm = drawn ? s.m : at_lane(l.m, part), pf = at_lane(f, part);
     const int lead = lead_of(x);
-    const int64_t begin = (int64_t)part * v.per - lead, end = min(begin + v.per, (int64_t)v.vocab);
+    const int begin = part * v.per - lead, end = min(begin + v.per, v.vocab);
     find_gone(v, s, seq, begin, end, gone);
-    if (t == 0) found = -1;
+    powers.fill();
     __syncthreads();
-    const double dlse = s.residual && v.D ? (double)v.dlse[row] : 0.0;
+    const double lse = drawn ? (double)v.dlse[row] : 0.0, by = 1.0 / total, aim_in = aim - before;
     double past = 0.0;
-    int late = -1;  // the last token with something left
-    for (int64_t step = begin; step < end; step += kChunk) {
-      const int64_t e = step + t * kVec;
-      float z[kVec];
-      double g[kVec], r[kVec], mine = 0.0;
-      load16(x, e, v.vocab, z);
-      remaining(v, s, gone, x, d, dlse, e, z, pm, g, r);
+    int late = -1, pick = -1;  // the last token with something left, the one looked for
+#pragma unroll 1
+    for (int step = begin; step < end; step += kFewChunk) {
+      const int e = step + t * kFew;
+      float z[kFew];
+      double r[kFew], mine = 0.0;
+      load_some<kFew>(x, e, v.vocab, z);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
+      for (int i = 0; i < kFew; ++i) r[i] = v.p2(powers, z[i], pm);
+      if (drawn) {
+        float y[kFew];
+        load_some<kFew>(d, e, v.vocab, y);
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) r[i] = fmax(fma(r[i], by, -s.beta * v.q2(powers, y[i], lse)), 0.0);
+      } else if (s.residual) {
+        without(gone, e, r);
+      }
+#pragma unroll
+      for (int i = 0; i < kFew; ++i) {
         r[i] *= pf;
         mine += r[i];
-        if (r[i] > 0.0) late = (int)(e + i);
+        if (r[i] > 0.0) late = e + i;
       }
-      double in = mine;
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const double o = __shfl_up(in, k);
-        if (lane >= k) in += o;
-      }
+      const double in = sum_upto(mine);
       __syncthreads();
-      if (lane == 63) sums[t >> 6] = in;
+      if (lane == 63) sums[w] = in;
       __syncthreads();
-      double ahead = past;
-      for (int k = 0; k < (t >> 6); ++k) ahead += sums[k];
-      double sum = ahead + (in - mine);
-      int pick = -1;
+      double sum = past + (in - mine);
+      for (int k = 0; k < w; ++k) sum += sums[k];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
+      for (int i = 0; i < kFew; ++i) {
         sum += r[i];
-        if (pick < 0 && r[i] > 0.0 && sum > aim_in) pick = (int)(e + i);
+        if (pick < 0 && r[i] > 0.0 && sum > aim_in) pick = e + i;
       }
       // the first thread that has one
       const uint64_t has = __ballot(pick >= 0);
-      const int mine_first = has != 0 ? __shfl(pick, __builtin_ctzll(has)) : -1;
-      for (int k = 0; k < kThreads / 64; ++k) {
-        __syncthreads();
-        if (k == t >> 6 && lane == 0 && found < 0 && mine_first >= 0) found = mine_first;
-      }
+      const int one = has != 0 ? __builtin_amdgcn_readlane(pick, __builtin_ctzll(has)) : -1;
+      if (lane == 0) found[w] = one;
       __syncthreads();
-      if (found >= 0) break;
+      pick = -1;
+      for (int k = kThreads / 64 - 1; k >= 0; --k) pick = found[k] >= 0 ? found[k] : pick;
+      if (pick >= 0) break;
       for (int k = 0; k < kThreads / 64; ++k) past += sums[k];
     }
-    chosen = found;
-    if (chosen < 0) {  // the sums' last place: the last one
+    if (pick < 0) {  // the sums' last place: the last one
 #pragma unroll
       for (int k = 1; k < 64; k <<= 1) late = max(late, __shfl_xor(late, k));
       __syncthreads();
-      if (t == 0) found = -1;
+      if (lane == 0) found[w] = late;
       __syncthreads();
-      if (lane == 0) atomicMax(&found, late);
-      __syncthreads();
-      chosen = found;
+      for (int k = 0; k < kThreads / 64; ++k) pick = max(pick, found[k]);
     }
+    chosen = pick;
   }
   if (t == 0) {
     v.next[seq] = chosen;
     v.logprob[seq * v.width] = chosen < 0 ? __uint_as_float(0x7fc00000u)
-                                          : (float)(((double)(float)x[chosen] - best) * (double)v.a - log(total));
+                                          : (float)(((double)(float)x[chosen] - (double)best) * (double)v.a - log(total));
   }
 }
 
@@ -514,10 +645,13 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // parts of a row for the first pass
 int row_parts(int64_t rows, int64_t vocab) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, rows), ceil_div(vocab + 7, kChunk), kMaxParts}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(4096, rows), ceil_div(vocab + 7, kChunk), kMaxParts}));
 }
 // elements of a part of the last row: parts of whole steps, kMaxParts of them at most
-int64_t last_per(int64_t vocab) { return ceil_div(ceil_div(vocab + 7, kMaxParts), kChunk) * kChunk; }
+int64_t last_per(int64_t seqs, int64_t vocab) {
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(2048, seqs)));
+  return ceil_div(ceil_div(vocab + 7, parts), kFewChunk) * kFewChunk;
+}
 
 struct Space {
   size_t part, last, state, all;
@@ -526,7 +660,7 @@ Space space_of(int64_t seqs, int width, int64_t vocab) {
   Space s;
   s.part = 0;
   s.last = s.part + up256((size_t)seqs * width * row_parts(seqs * width, vocab) * sizeof(Part));
-  s.state = s.last + up256((size_t)seqs * ceil_div(vocab + 7, last_per(vocab)) * sizeof(Last));
+  s.state = s.last + up256((size_t)seqs * ceil_div(vocab + 7, last_per(seqs, vocab)) * sizeof(Last));
   s.all = s.state + up256((size_t)seqs * sizeof(State));
   return s;
 }
@@ -569,7 +703,7 @@ gptq2d_status gptq2d_tree_verify(int64_t seqs, int width, int64_t vocab, gptq2d_
   if (!workspace || ws_bytes < sp.all) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
   if (!aligned(workspace, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   char* w = (char*)workspace;
-  const int64_t per = last_per(vocab);
+  const int64_t per = last_per(seqs, vocab);
   VerifyArgs v = {seqs, width, (int)vocab, row_parts(seqs * width, vocab), (int)ceil_div(vocab + 7, per), (int)per, X, ldx,
                   scale, tokens, parents, drafts, uniform, D, ldd, draft_scale, draft_lse, path, count, next, logprob,
                   (Part*)(w + sp.part), (Last*)(w + sp.last), (State*)(w + sp.state)};
