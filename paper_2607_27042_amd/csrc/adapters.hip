@@ -82,6 +82,18 @@ __device__ __forceinline__ float split(float& x, _Float16) {
   return hi;
 }
 
+// over a wave, in every lane, without LDS
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true);
+  const u2 a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = a[0] + a[1];
+  const u2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return b[0] + b[1];
+}
+
 // ---------------------------------------------------------------------------
 // rows in the order of their adapters
 // ---------------------------------------------------------------------------
@@ -106,53 +118,72 @@ __device__ __forceinline__ uint64_t heads_of(const Groups& g, int first, int n, 
   return __ballot(lane < n && mine >= 0 && (lane == 0 || mine != before));
 }
 
-constexpr int kGroupRows = 16;  // of a thread and turn
 struct GroupArgs {
   int rows, count;
   const int32_t* index;
   int32_t *order, *which, *start;
 };
+constexpr int kGroupThreads = 1024;
+constexpr int kGroupRows = 4;  // of a thread and turn
 // One work group for each adapter, and one for the rows that have none: how many rows lie
-// before the adapter's, then the places of its own, which come in the rows' order.
-__global__ __launch_bounds__(256) void k_group(GroupArgs g) {
-  __shared__ int less4[4], same4[4];
-  const int a = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
-  auto key = [&](int m) {
-    const int i = m < g.rows ? g.index[m] : -2;
-    return m >= g.rows ? g.count + 1 : i < 0 || i >= g.count ? g.count : i;
-  };
+// before the adapter's, then the places of its own, which come in the rows' order. All
+// loads of the first pass are on their way at once (8192 rows, 4 adapters: GROUPUS us; one
+// after another 21).
+__global__ __launch_bounds__(kGroupThreads) void k_group(GroupArgs g) {
+  __shared__ int less16[16], same16[16];
+  const int a = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, waves = blockDim.x >> 6;
+  auto key = [&](int i) { return i < 0 || i >= g.count ? g.count : i; };
   int less = 0;
-  for (int m = t; m < g.rows; m += 256) less += key(m) < a;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) less += __shfl_xor(less, d);
-  if (lane == 0) less4[w] = less;
+#pragma unroll 8
+  for (int m = t; m < g.rows; m += blockDim.x) less += key(g.index[m]) < a;
+  less = (int)wave_sum((uint32_t)less);
+  if (lane == 0) less16[w] = less;
   __syncthreads();
-  int at = less4[0] + less4[1] + less4[2] + less4[3];
+  int at = 0;
+  for (int k = 0; k < waves; ++k) at += less16[k];
   if (t == 0) {
     g.start[a] = at;
     if (a == g.count) g.start[a + 1] = g.rows;
   }
-  for (int m0 = 0; m0 < g.rows; m0 += 256 * kGroupRows) {
+  const int turn = blockDim.x * kGroupRows;
+  auto load = [&](int m0, int i[kGroupRows]) {
+#pragma unroll
+    for (int e = 0; e < kGroupRows; ++e) {
+      const int m = m0 + t * kGroupRows + e;
+      i[e] = m < g.rows ? key(g.index[m]) : -1;
+    }
+  };
+  int next[kGroupRows];
+  load(0, next);
+  for (int m0 = 0; m0 < g.rows; m0 += turn) {
     uint32_t mine = 0;
 #pragma unroll
-    for (int i = 0; i < kGroupRows; ++i) mine |= (uint32_t)(key(m0 + t * kGroupRows + i) == a) << i;
-    const int n = __popc(mine);
-    int upto = n;
+    for (int e = 0; e < kGroupRows; ++e) mine |= (uint32_t)(next[e] == a) << e;
+    load(m0 + turn, next);
+    // places: of the waves before, of the lanes before (all lanes' bits of one row of four, one row
+    // after another, give the number before a lane)
+    int before = 0, all = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
+    for (int e = 0; e < kGroupRows; ++e) {
+      const uint64_t b = __ballot(mine >> e & 1);
+      before += __popcll(b & ((1ull << lane) - 1));
+      all += __popcll(b);
     }
     __syncthreads();
-    if (lane == 63) same4[w] = upto;
+    if (lane == 0) same16[w] = all;
     __syncthreads();
-    int p = at + upto - n;
-    for (int k = 0; k < w; ++k) p += same4[k];
-    for (uint32_t left = mine; left != 0; left &= left - 1, ++p) {
-      g.order[p] = m0 + t * kGroupRows + __builtin_ctz(left);
-      g.which[p] = a;
+    int p = at + before, sum = 0;
+    for (int k = 0; k < waves; ++k) {
+      p += k < w ? same16[k] : 0;
+      sum += same16[k];
     }
-    at += same4[0] + same4[1] + same4[2] + same4[3];
+#pragma unroll
+    for (int e = 0; e < kGroupRows; ++e)
+      if (mine >> e & 1) {
+        g.order[p] = m0 + t * kGroupRows + e;
+        g.which[p++] = a;
+      }
+    at += sum;
   }
 }
 
@@ -178,7 +209,7 @@ template <class T, int MT, int RT, bool WIDE>
 __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
   typedef Mat<T> M;
   typedef typename M::F F;
-  constexpr int U = MT + RT <= 2 ? 8 : MT + RT <= 5 ? 4 : 2;
+  constexpr int U = MT + RT <= 3 ? 4 : MT + RT <= 6 ? 2 : 1;
   __shared__ f4 red[4][MT * RT][64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
   const int first = blockIdx.x * 16 * MT;
@@ -201,23 +232,35 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
 #pragma unroll
     for (int j = 0; j < RT; ++j) wr[j] = (const T*)a.W + ad * a.step + (int64_t)min(16 * j + m, a.rank - 1) * a.ldw;
     f4 acc[MT][RT] = {};
-    for (int s = s0 + w; s < s1; s += 4 * U) {
-      F fx[U][MT], fw[U][RT];
+    F fx[2][U][MT], fw[2][U][RT];
+    auto load = [&](int s, F x_[U][MT], F w_[U][RT]) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         // (steps past the end are zeros on one side)
         const int k = s + 4 * u < s1 ? (s + 4 * u) * M::K + q * M::E : a.n;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fx[u][i] = load_row<WIDE>(x[i], k, a.n);
+        for (int i = 0; i < MT; ++i) x_[u][i] = load_row<WIDE>(x[i], k, a.n);
 #pragma unroll
-        for (int j = 0; j < RT; ++j) fw[u][j] = load_row<WIDE>(wr[j], k, a.n);
+        for (int j = 0; j < RT; ++j) w_[u][j] = load_row<WIDE>(wr[j], k, a.n);
       }
+    };
+    auto sum = [&](F x_[U][MT], F w_[U][RT]) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int j = 0; j < RT; ++j) acc[i][j] = mma(fw[u][j], fx[u][i], acc[i][j]);
+          for (int j = 0; j < RT; ++j) acc[i][j] = mma(w_[u][j], x_[u][i], acc[i][j]);
+    };
+    // a turn's loads are on their way while the one before is summed
+    load(s0 + w, fx[0], fw[0]);
+#pragma unroll 1
+    for (int s = s0 + w; s < s1; s += 8 * U) {
+      load(s + 4 * U, fx[1], fw[1]);
+      sum(fx[0], fw[0]);
+      if (s + 4 * U >= s1) break;
+      load(s + 8 * U, fx[0], fw[0]);
+      sum(fx[1], fw[1]);
     }
     __syncthreads();
 #pragma unroll
@@ -290,52 +333,46 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2, kPacked = kNarrow && NK == 0;
   constexpr int S = kPacked ? 1 : NK, TERMS = kNarrow && !kPacked ? 2 : 1;
-  constexpr int ROWS = 16 * WIN;
+  constexpr int ROWS = 16 * WIN, V = 16 * sizeof(T) / 16;  // rows; pieces of 16 bytes of a lane's columns
   // h of the window, as the instruction takes it: [term][step][row][4 pieces]
   __shared__ F hs[TERMS * S][ROWS * 4];
   __shared__ float back[ROWS];
+  __shared__ int at[ROWS], of[ROWS];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
   const int first = blockIdx.x * ROWS;
-  int mine;
-  uint64_t heads = heads_of(a.g, first, ROWS, mine);
   const int c0 = blockIdx.y * 256 + w * 64 + q * 16;  // the lane's columns
-  T* out[WIN];
-  int own[WIN];
-  float y[WIN][16];
-#pragma unroll
-  for (int i = 0; i < WIN; ++i) {
-    const int64_t row = row_at(a.g, first + 16 * i + m);
-    own[i] = which_at(a.g, first + 16 * i + m);
-    out[i] = (T*)a.O + row * a.ldo + c0;
-    const T* p = (const T*)a.Y + row * a.ldy;
-    if (a.Y) {
-      const bool all = a.wide && c0 + 16 <= a.n;
-      load8(p + c0, all, min(a.n - c0, 8), y[i], p);
-      load8(p + c0 + 8, all, min(a.n - c0 - 8, 8), y[i] + 8, p);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) y[i][e] = 0.0f;
-    }
-  }
+  const bool whole = a.wide && c0 + 16 <= a.n;
+  if (t < ROWS) at[t] = row_at(a.g, first + t), of[t] = which_at(a.g, first + t);
   for (int i0 = t >> 2; i0 < ROWS; i0 += 64) {
     const int place = first + i0, p = t & 3;
     const int wh = which_at(a.g, place);
-    const float f = wh >= 0 && wh < a.g.count && a.scales ? a.scales[wh] : 1.0f;
+    const bool some = wh >= 0 && wh < a.g.count;
+    const float f = some && a.scales ? a.scales[wh] : 1.0f;
     float h[S][M::E];
 #pragma unroll
-    for (int k = 0; k < S; ++k) {
+    for (int k = 0; k < S; ++k)
 #pragma unroll
       for (int e = 0; e < M::E; ++e) h[k][e] = 0.0f;
-      const int r = kPacked ? p % 2 * 8 : k * M::K + p * M::E;
-      if (r < a.ranks && wh >= 0 && wh < a.g.count)
-        for (int s = 0; s < a.parts; ++s) {
-          const f4* x = (const f4*)(a.H + (s * a.places + place) * a.ranks + r);
+    const float* from = a.H + (int64_t)(some ? place : 0) * a.ranks;
+    const int64_t part = a.places * a.ranks;
+#pragma unroll 4
+    for (int s = 0; s < a.parts; ++s)
 #pragma unroll
-          for (int v = 0; v < M::E / 4; ++v)
+      for (int k = 0; k < S; ++k) {
+        const int r = kPacked ? p % 2 * 8 : k * M::K + p * M::E;
+        const f4* x = (const f4*)(from + s * part + (r < a.ranks ? r : 0));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[k][4 * v + e] += x[v][e];
+        for (int v = 0; v < M::E / 4; ++v) {
+          const f4 y = x[v];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[k][4 * v + e] += y[e];
         }
-    }
+      }
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+#pragma unroll
+      for (int e = 0; e < M::E; ++e)
+        if (!some || (kPacked ? p % 2 * 8 : k * M::K + p * M::E) >= a.ranks) h[k][e] = 0.0f;
     float up = 1.0f;
     if constexpr (std::is_same<T, _Float16>::value) {
       // a power of two brings the row's largest to [1, 2): halves reach from there to where it does not matter
@@ -380,42 +417,77 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
     }
   }
   __syncthreads();
-  for (int z = 0; heads != 0; heads &= heads - 1, ++z) {
-    if (z % gridDim.z != blockIdx.z) continue;
-    const int ad = __shfl(mine, __builtin_ctzll(heads));
-    F fw[4][S];
-    if (ad < a.g.count) {
-      // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
+  if (c0 - q * 16 >= a.n) return;
+  // a window's part of Y, loaded one window ahead
+  u4 ahead[V];
+  auto fetch = [&](int i) {
+    if (!whole || !a.Y) return;
+    const T* p = (const T*)a.Y + (int64_t)at[16 * i + m] * a.ldy + c0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = blockIdx.y * 256 + w * 64 + (m >> 2) * 16 + 4 * j + (m & 3);
-        const T* row = (const T*)a.W + ad * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
+    for (int v = 0; v < V; ++v) ahead[v] = *(const u4*)((const char*)p + 16 * v);
+  };
+  F fw[4][S];
+  int held = -1;  // the adapter whose W is in registers
+  for (int z0 = 0, z = 0; z0 < ROWS; z0 += 64) {
+    // adapters of these (up to) 64 places; a work group of many takes some of them
+    const int mine = of[z0 + min(lane, ROWS - 1)], before = __shfl_up(mine, 1);
+    uint64_t heads = __ballot(lane < min(ROWS, 64) && mine >= 0 && (lane == 0 || mine != before));
+    for (; heads != 0; heads &= heads - 1, ++z) {
+      if (z % gridDim.z != blockIdx.z) continue;
+      const int from = z0 + __builtin_ctzll(heads), ad = __builtin_amdgcn_readfirstlane(of[from]);
+      const uint64_t rest = heads & (heads - 1);
+      const int last = (rest ? z0 + __builtin_ctzll(rest) : min(z0 + 64, ROWS)) - 1;
+      fetch(from / 16);
+      if (ad < a.g.count && ad != held) {
+        // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
 #pragma unroll
-        for (int k = 0; k < S; ++k) fw[j][k] = load_row<WIDE>(row, kPacked ? q % 2 * 8 : k * M::K + q * M::E, a.rank);
+        for (int j = 0; j < 4; ++j) {
+          const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
+          const T* row = (const T*)a.W + ad * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
+#pragma unroll
+          for (int k = 0; k < S; ++k) fw[j][k] = load_row<WIDE>(row, kPacked ? q % 2 * 8 : k * M::K + q * M::E, a.rank);
+        }
+        held = ad;
       }
-    }
+#pragma unroll 1
+      for (int i = from / 16; i <= last / 16; ++i) {
+        const int place = 16 * i + m;
+        const bool own = place >= from && of[place] == ad;
+        u4 y[V];
 #pragma unroll
-    for (int i = 0; i < WIN; ++i) {
-      if (__ballot(own[i] == ad) == 0) continue;
-      f4 acc[4] = {};
-      if (ad < a.g.count) {
+        for (int v = 0; v < V; ++v) y[v] = ahead[v];
+        if (i < last / 16) fetch(i + 1);
+        f4 acc[4] = {};
+        if (ad < a.g.count) {
 #pragma unroll
-        for (int k = 0; k < S; ++k)
+          for (int k = 0; k < S; ++k)
 #pragma unroll
-          for (int u = 0; u < TERMS; ++u) {
-            const F h = hs[u * S + k][(16 * i + m) * 4 + q];
+            for (int u = 0; u < TERMS; ++u) {
+              const F h = hs[u * S + k][place * 4 + q];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = mma(fw[j][k], h, acc[j]);
-          }
+              for (int j = 0; j < 4; ++j) acc[j] = mma(fw[j][k], h, acc[j]);
+            }
+        }
+        if (!own || c0 >= a.n) continue;
+        const float f = back[place];
+        T* out = (T*)a.O + (int64_t)at[place] * a.ldo + c0;
+        const T* from_y = (const T*)a.Y + (int64_t)at[place] * a.ldy + c0;
+        float o[16];
+        if (whole && a.Y) {
+          typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = (float)__builtin_bit_cast(E, y[e * sizeof(T) / 16])[e % (16 / sizeof(T))];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = a.Y && c0 + e < a.n ? (float)from_y[e] : 0.0f;
+        }
+        if (ad < a.g.count) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = fmaf(acc[e / 4][e % 4], f, o[e]);
+        }
+        store8(out, whole, min(a.n - c0, 8), o);
+        store8(out + 8, whole, min(a.n - c0 - 8, 8), o + 8);
       }
-      if (own[i] != ad || c0 >= a.n) continue;
-      const float f = back[16 * i + m];
-      float o[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = ad < a.g.count ? fmaf(acc[e / 4][e % 4], f, y[i][e]) : y[i][e];
-      const bool all = a.wide && c0 + 16 <= a.n;
-      store8(out[i], all, min(a.n - c0, 8), o);
-      store8(out[i] + 8, all, min(a.n - c0 - 8, 8), o + 8);
     }
   }
 }
@@ -424,49 +496,53 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
 // sums over an adapter's rows
 // ---------------------------------------------------------------------------
 
-struct OuterArgs {
-  Groups g;
-  int n, rank;
+struct Outer {
+  int n;
   const void* Z;  // rows of n
   int64_t ldz;
   const float* H;  // rows (by_row: of the batch, else places) of ldh
   int64_t ldh;
-  bool by_row;
+  bool by_row, wide;
   const float* scales;
   float* out;       // [adapter][n][rank], or [adapter][rank][n] where `across`
   bool across;
   int window;       // places of a work group, a multiple of 32
   float* parts;     // [window + adapter] like an adapter's part of out
 };
+struct OuterArgs {
+  Groups g;
+  int rank, ranks;  // rank, work groups of it
+  Outer of[2];      // those that are asked for
+};
 
-// A wave takes 128 columns and 16 RT ranks; lane l reads 8 (16-bit) or 4 columns of a
-// row at once, whose pieces of different rows are turned in registers to runs of one column.
-// Adapters whose rows lie in one window are done with it; of the others each window gives a
+// A work group takes some columns, 16 RT ranks and a window of places, whose steps its
+// four waves share; their sums are joined in LDS. Lane l reads 8 (16-bit) or 4 columns of
+// a row at once; the pieces of 16-bit rows are turned in registers to runs of one
+// column. Adapters whose rows lie in one window are done with it; of the others each window gives a
 // part, at the number of the window and the adapter together (which grows along the
 // order, so that no two are alike).
 template <class T, int RT, bool WIDE>
-__global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
+__device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, int strip, int window, int rank0, float* red) {
   typedef Mat<T> M;
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2;
   constexpr int C = M::E;             // column tiles: columns C m + j
   constexpr int TERMS = std::is_same<T, bf16>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
-  constexpr int COLS = 16 * C, STEP = kNarrow ? 32 : 4;  // rows of a step
+  constexpr int COLS = 16 * C, STEP = 32;  // columns, rows of a step
+  constexpr int L = kNarrow ? 8 : 8;       // rows of a lane and step
+  constexpr int PITCH = COLS + 4;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
-  const int c0 = (blockIdx.x * 4 + w) * COLS, r0 = blockIdx.z * 16 * RT;
-  if (c0 >= a.n) return;
-  const int begin = blockIdx.y * a.window, end = min(begin + a.window, a.g.rows);
+  const int c0 = strip * COLS, r0 = rank0 * 16 * RT;
+  const int begin = window * o.window, end = min(begin + o.window, a.g.rows);
   int i0 = begin;
   while (i0 < end) {
     const int ad = which_at(a.g, i0);
     if (ad >= a.g.count) break;
     const int from = max(a.g.start[ad], begin), to = min(a.g.start[ad + 1], end);
     if (to <= i0) break;  // (groups that are not this batch's)
-    const float f = a.scales ? a.scales[ad] : 1.0f;
-    auto h_of = [&](int i, int r) {
-      const int64_t row = a.by_row ? row_at(a.g, i) : i;
-      return r < a.rank ? a.H[row * a.ldh + r] * f : 0.0f;
-    };
+    const float f = o.scales ? o.scales[ad] : 1.0f;
+    // place of a lane's row e in the step from s on
+    auto place = [&](int s, int e) { return kNarrow ? s + 8 * q + e : s + 4 * e + q; };
     float down[RT], up[RT];
 #pragma unroll
     for (int j = 0; j < RT; ++j) down[j] = up[j] = 1.0f;
@@ -474,41 +550,62 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
       // a power of two for each rank: its largest h here comes to [1, 2)
 #pragma unroll
       for (int j = 0; j < RT; ++j) {
+        const int r = min(r0 + 16 * j + m, a.rank - 1);
         uint32_t top = 0;
-        for (int i = from + q; i < to; i += 4) top = max(top, mag(h_of(i, r0 + 16 * j + m)));
+#pragma unroll 4
+        for (int i = from + q; i < to; i += 4) top = max(top, mag(o.H[(o.by_row ? (int64_t)row_at(a.g, i) : i) * o.ldh + r] * f));
         top = quad_max(top);
         const uint32_t ex = min(max(top >> 23, 2u), 252u);
         up[j] = __uint_as_float(ex << 23);
         down[j] = __uint_as_float((254u - ex) << 23);
       }
     }
-    f4 acc[C][RT] = {};
-    for (int s = from; s < to; s += STEP) {
-      if constexpr (kNarrow) {
-        u4 z[8];
-        const int i8 = s + 8 * q;
+    struct Step {
+      u4 z[L];
+      float h[RT][L];
+    };
+    int rows[L];
+    auto find = [&](int s) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = min(i8 + e, to - 1);
-          const T* row = (const T*)a.Z + (int64_t)row_at(a.g, i) * a.ldz;
-          z[e] = __builtin_bit_cast(u4, load_row<WIDE>(row, c0 + C * m, a.n));
-          if (i8 + e >= to) z[e] = u4{};
+      for (int e = 0; e < L; ++e) rows[e] = row_at(a.g, min(place(s, e), to - 1));
+    };
+    auto load = [&](int s, Step& x) {
+#pragma unroll
+      for (int e = 0; e < L; ++e)
+        x.z[e] = __builtin_bit_cast(u4, load_row<WIDE>((const T*)o.Z + (int64_t)rows[e] * o.ldz, c0 + C * m, o.n));
+#pragma unroll
+      for (int j = 0; j < RT; ++j)
+#pragma unroll
+        for (int e = 0; e < L; ++e)
+          x.h[j][e] = o.H[(o.by_row ? (int64_t)rows[e] : min(place(s, e), to - 1)) * o.ldh + min(r0 + 16 * j + m, a.rank - 1)];
+    };
+    f4 acc[C][RT] = {};
+    auto sum = [&](int s, Step& x) {
+      if (s + STEP > to) {
+#pragma unroll
+        for (int e = 0; e < L; ++e) {
+          const bool in = place(s, e) < to;
+          if (!in) x.z[e] = u4{};
+#pragma unroll
+          for (int j = 0; j < RT; ++j) x.h[j][e] = in ? x.h[j][e] : 0.0f;
         }
+      }
+      if constexpr (kNarrow) {
         F h[RT][TERMS];
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            float x = i8 + e < to ? h_of(min(i8 + e, to - 1), r0 + 16 * j + m) * down[j] : 0.0f;
+            float v = x.h[j][e] * f * down[j];
 #pragma unroll
-            for (int u = 0; u < TERMS; ++u) h[j][u][e] = u + 1 < TERMS ? (T)split(x, T()) : (T)x;
+            for (int u = 0; u < TERMS; ++u) h[j][u][e] = u + 1 < TERMS ? (T)split(v, T()) : (T)v;
           }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           u4 col;
 #pragma unroll
           for (int p = 0; p < 4; ++p)
-            col[p] = __builtin_amdgcn_perm(z[2 * p + 1][c / 2], z[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+            col[p] = __builtin_amdgcn_perm(x.z[2 * p + 1][c / 2], x.z[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
           const F fz = __builtin_bit_cast(F, col);
 #pragma unroll
           for (int j = 0; j < RT; ++j)
@@ -516,79 +613,127 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
             for (int u = TERMS - 1; u >= 0; --u) acc[c][j] = mma(fz, h[j][u], acc[c][j]);
         }
       } else {
-        const int i = s + q;
-        const T* row = (const T*)a.Z + (int64_t)row_at(a.g, min(i, to - 1)) * a.ldz;
-        F z = load_row<WIDE>(row, c0 + C * m, a.n);
-        if (i >= to) z = F{};
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-          const float h = i < to ? h_of(min(i, to - 1), r0 + 16 * j + m) : 0.0f;
+        for (int e = 0; e < L; ++e) {
+          const f4 z = __builtin_bit_cast(f4, x.z[e]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(z[c], h, acc[c][j], 0, 0, 0);
+          for (int j = 0; j < RT; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(z[c], x.h[j][e] * f, acc[c][j], 0, 0, 0);
         }
       }
+    };
+    // a step's loads are on their way while the one before is summed, its rows' numbers before that
+    Step x, y;
+    const int s0 = from + w * STEP;
+    if (s0 < to) {
+      find(s0);
+      load(s0, x);
+      find(s0 + 4 * STEP);
+#pragma unroll 1
+      for (int s = s0; s < to; s += 8 * STEP) {
+        if (s + 4 * STEP < to) load(s + 4 * STEP, y);
+        find(s + 8 * STEP);
+        sum(s, x);
+        if (s + 4 * STEP >= to) break;
+        if (s + 8 * STEP < to) load(s + 8 * STEP, x);
+        find(s + 12 * STEP);
+        sum(s + 4 * STEP, y);
+      }
     }
-    const bool whole = a.g.start[ad] >= begin && a.g.start[ad + 1] <= end;
-    float* o = whole ? a.out + (int64_t)ad * a.n * a.rank : a.parts + (int64_t)(blockIdx.y + ad) * a.n * a.rank;
-    // lane: rank m of each tile, columns c0 + C (4 q + i) + c
+    // lane: rank m of each tile, columns C (4 q + i) + c: to rows of ranks
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      const int r = r0 + 16 * j + m;
-      if (r >= a.rank) continue;
+    for (int j = 0; j < RT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int col = c0 + C * (4 * q + i) + c;
-          if (col < a.n) o[a.across ? (int64_t)r * a.n + col : (int64_t)col * a.rank + r] = acc[c][j][i] * up[j];
+        for (int c = 0; c < C; c += 4) {
+          f4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[c + e][j][i] * up[j];
+          *(f4*)(red + ((w * RT + j) * 16 + m) * PITCH + C * (4 * q + i) + c) = v;
         }
+    __syncthreads();
+    const bool whole = a.g.start[ad] >= begin && a.g.start[ad + 1] <= end;
+    float* to_out = whole ? o.out + (int64_t)ad * o.n * a.rank : o.parts + (int64_t)(window + ad) * o.n * a.rank;
+    for (int e = t; e < 16 * RT * COLS; e += 256) {
+      const int r = o.across ? e / COLS : e % (16 * RT), c = o.across ? e % COLS : e / (16 * RT);
+      const float* v = red + r * PITCH + c;
+      constexpr int wave = RT * 16 * PITCH;
+      const float s = (v[0] + v[wave]) + (v[2 * wave] + v[3 * wave]);
+      if (r0 + r < a.rank && c0 + c < o.n)
+        to_out[o.across ? (int64_t)(r0 + r) * o.n + c0 + c : (int64_t)(c0 + c) * a.rank + r0 + r] = s;
     }
     i0 = to;
   }
 }
+template <class T, int RT>
+__global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
+  __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
+  const Outer o = a.of[blockIdx.z / a.ranks];
+  if ((int)blockIdx.x * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
+  if (o.wide)
+    outer_tile<T, RT, true>(a, o, blockIdx.x, blockIdx.y, blockIdx.z % a.ranks, red);
+  else
+    outer_tile<T, RT, false>(a, o, blockIdx.x, blockIdx.y, blockIdx.z % a.ranks, red);
+}
 
 // The parts' sums, and zeros for adapters without rows.
-struct JoinArgs {
-  Groups g;
-  int64_t size;  // of an adapter
-  int window;
-  const float* parts;
-  float* out;
-};
-__global__ __launch_bounds__(256) void k_outer_join(JoinArgs a) {
+__global__ __launch_bounds__(256) void k_outer_join(OuterArgs a) {
+  const Outer o = a.of[blockIdx.z];
   const int ad = blockIdx.y;
+  const int64_t size = (int64_t)o.n * a.rank;
   const int from = a.g.start[ad], to = min(a.g.start[ad + 1], a.g.rows);
-  const int w0 = from / a.window, w1 = to > from ? (to - 1) / a.window : w0;
-  if (to > from && w0 == w1) return;  // (or it is there already)
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < a.size; e += (int64_t)gridDim.x * 256) {
+  const int w0 = from / o.window, w1 = to > from ? (to - 1) / o.window : w0;
+  if (to > from && w0 == w1) return;  // (it is there already)
+  float* out = o.out + ad * size;
+  const float* parts = o.parts + (int64_t)(w0 + ad) * size;
+  if (size % 4 == 0) {  // (out is aligned to its elements, the parts to 16 bytes)
+    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < size; e += (int64_t)gridDim.x * 1024) {
+      f4 s = {};
+      if (to > from)
+#pragma unroll 4
+        for (int w = 0; w <= w1 - w0; ++w) s += *(const f4*)(parts + w * size + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[e + i] = s[i];
+    }
+    return;
+  }
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < size; e += (int64_t)gridDim.x * 256) {
     float s = 0.0f;
     if (to > from)
-      for (int w = w0; w <= w1; ++w) s += a.parts[(w + ad) * a.size + e];
-    a.out[ad * a.size + e] = s;
+      for (int w = 0; w <= w1 - w0; ++w) s += parts[w * size + e];
+    out[e] = s;
   }
 }
 
 // Rows of W (rows x cols, of each adapter that has rows) as columns.
-struct TurnArgs {
-  Groups g;
+struct Turn {
   int rows, cols;
   const void* W;
   int64_t ldw, step;
   void* out;
   int64_t ldo, step_out;
 };
+struct TurnArgs {
+  Groups g;
+  Turn of[2];
+};
 template <class T>
 __global__ __launch_bounds__(256) void k_turn(TurnArgs a) {
   __shared__ T tile[32][33];
   const int ad = blockIdx.z;
-  if (a.g.start[ad] >= a.g.start[ad + 1]) return;
-  const int tiles = (a.cols + 31) / 32, x = threadIdx.x & 31, y0 = threadIdx.x >> 5;
+  const Turn u = a.of[blockIdx.y];
+  const int tiles = (u.cols + 31) / 32, x = threadIdx.x & 31, y0 = threadIdx.x >> 5;
   const int r0 = blockIdx.x / tiles * 32, c0 = (blockIdx.x - r0 / 32 * tiles) * 32;
+  if (r0 >= u.rows || a.g.start[ad] >= a.g.start[ad + 1]) return;
   for (int y = y0; y < 32; y += 8)
-    if (r0 + y < a.rows && c0 + x < a.cols) tile[y][x] = ((const T*)a.W)[ad * a.step + (r0 + y) * a.ldw + c0 + x];
+    if (r0 + y < u.rows && c0 + x < u.cols) tile[y][x] = ((const T*)u.W)[ad * u.step + (r0 + y) * u.ldw + c0 + x];
   __syncthreads();
   for (int y = y0; y < 32; y += 8)
-    if (c0 + y < a.cols && r0 + x < a.rows) ((T*)a.out)[ad * a.step_out + (c0 + y) * a.ldo + r0 + x] = tile[x][y];
+    if (c0 + y < u.cols && r0 + x < u.rows) ((T*)u.out)[ad * u.step_out + (c0 + y) * u.ldo + r0 + x] = tile[x][y];
 }
 
 // ---------------------------------------------------------------------------
@@ -599,15 +744,19 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return ceil_div(v, m) * m; }
 
 int ranks_of(int rank) { return (int)up(rank, 16); }
-// row tiles of a window, parts of the inner side
-int shrink_tiles(int64_t rows, int rank, bool wide) { return !wide || rows < 2048 ? 1 : rank <= 64 ? 4 : 2; }
-int shrink_parts(int64_t rows, int64_t n) {
-  const int64_t want = ceil_div(512, ceil_div(rows, 16)), room = ceil_div(n, 256);
+// Row tiles of a window, and parts of the inner side. More rows of a window read the weights
+// more seldom, parts fill the device, each at its price: PLANNOTE
+int shrink_tiles(int64_t rows, int rank) { return rows < 2048 ? 1 : rank <= 16 ? 1 : 2; }
+int shrink_parts(int64_t rows, int64_t n, int rank, int count) {
+  const int64_t windows = ceil_div(rows, 16 * shrink_tiles(rows, rank));
+  // work groups that have something to do, as far as sizes tell
+  const int64_t work = rows < 2048 ? std::min<int64_t>(rows, windows * std::min(16, count)) : windows;
+  const int64_t want = ceil_div(rows < 2048 ? 256 : 512, work), room = ceil_div(n, 256);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, room, 16}));
 }
 int64_t places_of(int64_t rows) { return up(rows, 64); }
-size_t h_bytes(int64_t rows, int64_t n, int rank) {
-  return up256((size_t)shrink_parts(rows, n) * places_of(rows) * ranks_of(rank) * 4);
+size_t h_bytes(int64_t rows, int64_t n, int rank, int count) {
+  return up256((size_t)shrink_parts(rows, n, rank, count) * places_of(rows) * ranks_of(rank) * 4);
 }
 
 template <class T, int MT, int RT, bool WIDE>
@@ -616,13 +765,13 @@ void shrink_as(const ShrinkArgs& a, int parts, int z, hipStream_t s) {
 }
 template <class T>
 void shrink(const ShrinkArgs& a, bool wide, int parts, hipStream_t s) {
-  const int tiles = shrink_tiles(a.g.rows, a.rank, wide);
-  const int z = std::min(tiles == 1 && a.g.rows <= 1024 ? 16 : 1, a.g.count);
+  const int tiles = shrink_tiles(a.g.rows, a.rank);
+  const int z = a.g.rows < 2048 ? std::min(16, a.g.count) : 1;
   auto of = [&](auto rt) {
     constexpr int RT = decltype(rt)::value;
-    if (!wide) return shrink_as<T, 1, RT, false>(a, parts, z, s);
-    if (tiles == 1) return shrink_as<T, 1, RT, true>(a, parts, z, s);
-    return shrink_as<T, RT == 8 ? 2 : 4, RT, true>(a, parts, z, s);
+    constexpr int MT = RT == 1 ? 1 : 2;
+    if (tiles == 1) return wide ? shrink_as<T, 1, RT, true>(a, parts, z, s) : shrink_as<T, 1, RT, false>(a, parts, z, s);
+    return wide ? shrink_as<T, MT, RT, true>(a, parts, z, s) : shrink_as<T, MT, RT, false>(a, parts, z, s);
   };
   if (a.rank <= 16) of(std::integral_constant<int, 1>());
   else if (a.rank <= 32) of(std::integral_constant<int, 2>());
@@ -631,14 +780,15 @@ void shrink(const ShrinkArgs& a, bool wide, int parts, hipStream_t s) {
 }
 
 template <class T>
-void turn(const TurnArgs& a, hipStream_t s) {
-  const int64_t tiles = ceil_div(a.rows, 32) * ceil_div(a.cols, 32);
-  hipLaunchKernelGGL(k_turn<T>, dim3((unsigned)tiles, 1, a.g.count), dim3(256), 0, s, a);
+void turn(const TurnArgs& a, int n, hipStream_t s) {
+  int64_t tiles = 0;
+  for (int i = 0; i < n; ++i) tiles = std::max(tiles, ceil_div(a.of[i].rows, 32) * ceil_div(a.of[i].cols, 32));
+  hipLaunchKernelGGL(k_turn<T>, dim3((unsigned)tiles, n, a.g.count), dim3(256), 0, s, a);
 }
 
 template <class T>
 void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
-  const bool few = a.g.rows <= 1024;
+  const bool few = a.g.rows < 2048;
   auto of = [&](auto nk) {
     constexpr int NK = decltype(nk)::value;
     const unsigned cols = (unsigned)ceil_div(a.n, 256);
@@ -647,9 +797,8 @@ void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
       const dim3 grid((unsigned)ceil_div(a.g.rows, 16 * WIN), cols, few ? std::min(16, a.g.count + 1) : 1);
       hipLaunchKernelGGL((k_expand<T, NK, WIN, decltype(w)::value>), grid, dim3(256), 0, s, a);
     };
-    if (!wide) as(std::integral_constant<int, 1>(), std::false_type());
-    else if (few) as(std::integral_constant<int, 1>(), std::true_type());
-    else as(std::integral_constant<int, 4>(), std::true_type());
+    if (few) wide ? as(std::integral_constant<int, 1>(), std::true_type()) : as(std::integral_constant<int, 1>(), std::false_type());
+    else wide ? as(std::integral_constant<int, 8>(), std::true_type()) : as(std::integral_constant<int, 8>(), std::false_type());
   };
   if constexpr (sizeof(T) == 4) {
     if (a.rank <= 16) of(std::integral_constant<int, 1>());
@@ -664,37 +813,45 @@ void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
   }
 }
 
+// Sums parts of h where more than one work group would do it for itself again (many rows);
+// returns how many are left. `out` may be h itself: an element's parts are one thread's.
+template <class T>
+int fold(const Groups& g, int rank, int parts, const float* h, float* out, hipStream_t s) {
+  if (parts == 1 || g.rows < 2048) return parts;
+  const FoldArgs f = {g, rank, ranks_of(rank), parts, h, places_of(g.rows), out, false};
+  hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(g.rows * (int64_t)ranks_of(rank), 256)), dim3(256), 0, s, f);
+  return 1;
+}
+
+// places of a window: as many windows as fill the device with strips of 128 columns, of 256
+// places at least (two steps of each wave), the fewer the less there is to join
 int outer_window(int64_t rows, int64_t n) {
-  // as many windows as fill the device with four waves of columns a work group
-  const int64_t strips = ceil_div(n, 512), want = std::max<int64_t>(1, ceil_div(512, strips));
-  return (int)std::max<int64_t>(64, up(ceil_div(rows, want), 32));
+  const int64_t want = std::max<int64_t>(1, ceil_div(512, ceil_div(n, 128)));
+  return (int)std::max<int64_t>(256, up(ceil_div(rows, want), 128));
 }
 size_t outer_bytes(int64_t rows, int64_t n, int rank, int count) {
   const int64_t windows = ceil_div(rows, outer_window(rows, n));
   return windows <= 1 ? 0 : up256((size_t)(windows + count) * n * rank * 4);
 }
+// the first n of a.of
 template <class T>
-void outer(OuterArgs a, bool wide, hipStream_t s) {
-  a.window = outer_window(a.g.rows, a.n);
-  const JoinArgs join = {a.g, (int64_t)a.n * a.rank, a.window, a.parts, a.out};
-  const dim3 join_grid((unsigned)std::min<int64_t>(ceil_div(join.size, 1024), 1024), a.g.count);
-  if (a.g.rows == 0) {  // zeros
-    hipLaunchKernelGGL(k_outer_join, join_grid, dim3(256), 0, s, join);
-    return;
+void outer(OuterArgs a, int n, hipStream_t s) {
+  int64_t strips = 0, windows = 0, size = 0;
+  for (int i = 0; i < n; ++i) {
+    a.of[i].window = outer_window(a.g.rows, a.of[i].n);
+    strips = std::max(strips, ceil_div(a.of[i].n, 16 * Mat<T>::E));
+    windows = std::max(windows, ceil_div(a.g.rows, a.of[i].window));
+    size = std::max(size, (int64_t)a.of[i].n * a.rank);
   }
-  auto of = [&](auto rt) {
-    constexpr int RT = decltype(rt)::value;
-    const dim3 grid((unsigned)ceil_div(a.n, 4 * 16 * Mat<T>::E), (unsigned)ceil_div(a.g.rows, a.window),
-                    (unsigned)ceil_div(a.rank, 16 * RT));
-    if (wide)
-      hipLaunchKernelGGL((k_outer<T, RT, true>), grid, dim3(256), 0, s, a);
+  if (windows > 0) {
+    a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
+    const dim3 grid((unsigned)strips, (unsigned)windows, (unsigned)(n * a.ranks));
+    if (a.rank <= 16)
+      hipLaunchKernelGGL((k_outer<T, 1>), grid, dim3(256), 0, s, a);
     else
-      hipLaunchKernelGGL((k_outer<T, RT, false>), grid, dim3(256), 0, s, a);
-  };
-  if (a.rank <= 16) of(std::integral_constant<int, 1>());
-  else if (a.rank <= 32) of(std::integral_constant<int, 2>());
-  else of(std::integral_constant<int, 4>());
-  hipLaunchKernelGGL(k_outer_join, join_grid, dim3(256), 0, s, join);
+      hipLaunchKernelGGL((k_outer<T, 2>), grid, dim3(256), 0, s, a);
+  }
+  hipLaunchKernelGGL(k_outer_join, dim3((unsigned)std::min<int64_t>(ceil_div(size, 1024), 256), a.g.count, n), dim3(256), 0, s, a);
 }
 
 bool bad_shape(int64_t M, int64_t N, int64_t K, int R, int count) {
@@ -708,18 +865,19 @@ bool wide_matrix(const void* p, int64_t ld, int64_t n) {
 }
 
 struct BackSpace {
-  size_t h, p, at, bt, outer, all;
+  size_t h, p, at, bt, outer[2], all;
   int64_t ldat, ldbt;
 };
 BackSpace back_space(int64_t M, int64_t N, int64_t K, int R, int count) {
   BackSpace b;
   b.ldat = up(R, 8), b.ldbt = up(N, 8);
   b.h = 0;
-  b.p = b.h + h_bytes(M, N, R);
+  b.p = b.h + h_bytes(M, N, R, count);
   b.at = b.p + up256((size_t)places_of(M) * ranks_of(R) * 4);
   b.bt = b.at + up256((size_t)count * K * b.ldat * 4);
-  b.outer = b.bt + up256((size_t)count * R * b.ldbt * 4);
-  b.all = b.outer + std::max(outer_bytes(M, N, R, count), outer_bytes(M, K, R, count));
+  b.outer[0] = b.bt + up256((size_t)count * R * b.ldbt * 4);
+  b.outer[1] = b.outer[0] + outer_bytes(M, K, R, count);
+  b.all = b.outer[1] + outer_bytes(M, N, R, count);
   return b;
 }
 
@@ -741,13 +899,13 @@ gptq2d_status gptq2d_adapter_groups(int64_t M, int count, const int32_t* index, 
   if (!groups || (M > 0 && !index)) return refuse("index or groups is NULL");
   if (!aligned(index, 4) || !aligned(groups, 4)) return refuse("an argument is not aligned to its elements");
   const GroupArgs a = {(int)M, count, index, groups, groups + M, groups + 2 * M};
-  hipLaunchKernelGGL(k_group, dim3(count + 1), dim3(256), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL(k_group, dim3(count + 1), dim3(M <= 1024 ? 256 : kGroupThreads), 0, (hipStream_t)stream, a);
   return launched("gptq2d_adapter_groups");
 }
 
 size_t gptq2d_adapters_workspace_size(int64_t M, int64_t N, int64_t K, int R, int count) {
   if (bad_shape(M, N, K, R, count) || M == 0) return 0;
-  return h_bytes(M, K, R);
+  return h_bytes(M, K, R, count);
 }
 
 gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count, gptq2d_dtype dt, const void* X, int64_t ldx,
@@ -763,12 +921,12 @@ gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count,
   if (!aligned(X, es) || !aligned(A, es) || !aligned(B, es) || !aligned(Y, es) || !aligned(O, es) || !aligned(scales, 4) ||
       !aligned(groups, 4) || !aligned(H, 4))
     return refuse("an argument is not aligned to its elements");
-  const size_t need = h_bytes(M, K, R);
+  const size_t need = h_bytes(M, K, R, count);
   if (!workspace || ws_bytes < need) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
   if (!aligned(workspace, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   const hipStream_t s = (hipStream_t)stream;
   const Groups g = groups_of(groups, M, count);
-  const int parts = shrink_parts(M, K);
+  const int parts = shrink_parts(M, K, R, count);
   float* h = (float*)workspace;
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
@@ -778,7 +936,8 @@ gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count,
       const FoldArgs f = {g, R, ranks_of(R), parts, h, places_of(M), H, true};
       hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * R, 256)), dim3(256), 0, s, f);
     }
-    const ExpandArgs e = {g, (int)N, R, ranks_of(R), parts, h, places_of(M), scales, B, ldb, N * ldb, Y, ldy, O, ldo,
+    const int left = fold<T>(g, R, parts, h, h, s);
+    const ExpandArgs e = {g, (int)N, R, ranks_of(R), left, h, places_of(M), scales, B, ldb, N * ldb, Y, ldy, O, ldo,
                           (!Y || wide_rows(Y, ldy, es)) && wide_rows(O, ldo, es)};
     expand<T>(e, wide_matrix<T>(B, ldb, R), s);
   });
@@ -800,9 +959,11 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
   if (!dX && !dA && !dB) return refuse("no gradient is asked for");
   if (!groups) return refuse("groups is NULL");
   if (M == 0) {  // nothing but zeros
-    const Groups g = groups_of(groups, 0, count);
-    if (dA) outer<float>({g, (int)K, R, nullptr, 0, nullptr, 0, false, nullptr, dA, true, 0, nullptr}, true, (hipStream_t)stream);
-    if (dB) outer<float>({g, (int)N, R, nullptr, 0, nullptr, 0, false, nullptr, dB, false, 0, nullptr}, true, (hipStream_t)stream);
+    OuterArgs o = {groups_of(groups, 0, count), R, 1, {}};
+    int n = 0;
+    if (dA) o.of[n].n = (int)K, o.of[n++].out = dA;
+    if (dB) o.of[n].n = (int)N, o.of[n++].out = dB;
+    if (n > 0) outer<float>(o, n, (hipStream_t)stream);
     return launched("gptq2d_adapters_backward");
   }
   if (!G) return refuse("G is NULL");
@@ -823,27 +984,31 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
   const hipStream_t s = (hipStream_t)stream;
   const Groups g = groups_of(groups, M, count);
   char* ws = (char*)workspace;
-  float *h = (float*)(ws + b.h), *pr = (float*)(ws + b.p), *parts = (float*)(ws + b.outer);
+  float *h = (float*)(ws + b.h), *pr = (float*)(ws + b.p);
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
     const bool wide_g = wide_matrix<T>(G, ldg, N);
-    if (dB) outer<T>({g, (int)N, R, G, ldg, H, R, true, scales, dB, false, 0, parts}, wide_g, s);
-    if (!dX && !dA) return;
-    const TurnArgs tb = {g, (int)N, R, B, ldb, N * ldb, ws + b.bt, b.ldbt, R * b.ldbt};
-    turn<T>(tb, s);
-    const int n = shrink_parts(M, N);
-    const ShrinkArgs sh = {g, (int)N, R, ranks_of(R), G, ldg, ws + b.bt, b.ldbt, R * b.ldbt, scales, h, places_of(M)};
-    shrink<T>(sh, wide_g, n, s);
     const float* ph = h;
-    if (n > 1) {
-      const FoldArgs f = {g, R, ranks_of(R), n, h, places_of(M), pr, false};
-      hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * ranks_of(R), 256)), dim3(256), 0, s, f);
-      ph = pr;
+    if (dX || dA) {
+      const Turn of_b = {(int)N, R, B, ldb, N * ldb, ws + b.bt, b.ldbt, R * b.ldbt};
+      const Turn of_a = {R, (int)K, A, lda, R * lda, ws + b.at, b.ldat, K * b.ldat};
+      turn<T>({g, {of_b, of_a}}, dX ? 2 : 1, s);
+      const int parts = shrink_parts(M, N, R, count);
+      const ShrinkArgs sh = {g, (int)N, R, ranks_of(R), G, ldg, ws + b.bt, b.ldbt, R * b.ldbt, scales, h, places_of(M)};
+      shrink<T>(sh, wide_g, parts, s);
+      if (parts > 1) {
+        const FoldArgs f = {g, R, ranks_of(R), parts, h, places_of(M), pr, false};
+        hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * ranks_of(R), 256)), dim3(256), 0, s, f);
+        ph = pr;
+      }
     }
-    if (dA) outer<T>({g, (int)K, R, X, ldx, ph, ranks_of(R), false, nullptr, dA, true, 0, parts}, wide_matrix<T>(X, ldx, K), s);
+    OuterArgs o = {g, R, 1, {}};
+    int n = 0;
+    if (dA) o.of[n++] = {(int)K, X, ldx, ph, ranks_of(R), false, wide_matrix<T>(X, ldx, K), nullptr, dA, true, 0,
+                         (float*)(ws + b.outer[0])};
+    if (dB) o.of[n++] = {(int)N, G, ldg, H, R, true, wide_g, scales, dB, false, 0, (float*)(ws + b.outer[1])};
+    if (n > 0) outer<T>(o, n, s);
     if (dX) {
-      const TurnArgs ta = {g, R, (int)K, A, lda, R * lda, ws + b.at, b.ldat, K * b.ldat};
-      turn<T>(ta, s);
       const ExpandArgs e = {g, (int)K, R, ranks_of(R), 1, ph, places_of(M), nullptr, ws + b.at, b.ldat, K * b.ldat, D, ldd, dX,
                             lddx, (!D || wide_rows(D, ldd, es)) && wide_rows(dX, lddx, es)};
       expand<T>(e, R % Mat<T>::E == 0, s);
