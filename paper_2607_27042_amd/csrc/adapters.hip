@@ -51,6 +51,9 @@ __device__ __forceinline__ f4 mma(f4 a, f4 b, f4 c) {
   return c;
 }
 
+// 16 bytes at any element (the memory takes them off their boundary as well, in two lines)
+typedef u4 u4_near __attribute__((aligned(2)));
+
 // Elements k .. k + E - 1 of a row of n, zeros past its end. WIDE: rows start on 16-byte
 // boundaries and n is a multiple of E.
 template <bool WIDE, class T>
@@ -61,10 +64,14 @@ __device__ __forceinline__ typename Mat<T>::F load_row(const T* row, int k, int 
     f = __builtin_bit_cast(F, *(const u4*)(row + (k < n ? k : 0)));
     if (k >= n) f = F{};
   } else {
+    if (k + Mat<T>::E <= n) {
+      f = __builtin_bit_cast(F, *(const u4_near*)(row + k));
+    } else {
+      f = F{};
 #pragma unroll
-    for (int i = 0; i < Mat<T>::E; ++i) f[i] = row[min(k + i, n - 1)];
-#pragma unroll
-    for (int i = 0; i < Mat<T>::E; ++i) f[i] = k + i < n ? f[i] : (T)0.0f;
+      for (int i = 0; i < Mat<T>::E; ++i)
+        if (k + i < n) f[i] = row[k + i];
+    }
   }
   return f;
 }
@@ -126,64 +133,80 @@ struct GroupArgs {
 constexpr int kGroupThreads = 1024;
 constexpr int kGroupRows = 4;  // of a thread and turn
 // One work group for each adapter, and one for the rows that have none: how many rows lie
-// before the adapter's, then the places of its own, which come in the rows' order. All
-// loads of the first pass are on their way at once (8192 rows, 4 adapters: GROUPUS us; one
-// after another 21).
+// before the adapter's, and the places of its own, which come in the rows' order. Up to
+// 16384 rows are looked at once (8192 rows, 4 adapters: GROUPUS us; turn by turn 9.6, row by row 21).
+template <int TURNS>
 __global__ __launch_bounds__(kGroupThreads) void k_group(GroupArgs g) {
-  __shared__ int less16[16], same16[16];
+  __shared__ int less16[16], count64[64];
   const int a = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, waves = blockDim.x >> 6;
+  const bool many = g.rows > (int)blockDim.x * kGroupRows * TURNS;
   auto key = [&](int i) { return i < 0 || i >= g.count ? g.count : i; };
-  int less = 0;
+  // turn u of the rows from m0 on: rows in fours along the threads
+  auto row = [&](int m0, int u, int e) { return m0 + (u * (int)blockDim.x + t) * kGroupRows + e; };
+  int less = 0, at = 0;
+  if (many) {
 #pragma unroll 8
-  for (int m = t; m < g.rows; m += blockDim.x) less += key(g.index[m]) < a;
-  less = (int)wave_sum((uint32_t)less);
-  if (lane == 0) less16[w] = less;
-  __syncthreads();
-  int at = 0;
-  for (int k = 0; k < waves; ++k) at += less16[k];
-  if (t == 0) {
-    g.start[a] = at;
-    if (a == g.count) g.start[a + 1] = g.rows;
+    for (int m = t; m < g.rows; m += blockDim.x) less += key(g.index[m]) < a;
+    less = (int)wave_sum((uint32_t)less);
+    if (lane == 0) less16[w] = less;
+    __syncthreads();
+    for (int k = 0; k < waves; ++k) at += less16[k];
   }
-  const int turn = blockDim.x * kGroupRows;
-  auto load = [&](int m0, int i[kGroupRows]) {
+  for (int m0 = 0; m0 < g.rows || m0 == 0; m0 += (int)blockDim.x * kGroupRows * TURNS) {
+    int k[TURNS][kGroupRows];
 #pragma unroll
-    for (int e = 0; e < kGroupRows; ++e) {
-      const int m = m0 + t * kGroupRows + e;
-      i[e] = m < g.rows ? key(g.index[m]) : -1;
-    }
-  };
-  int next[kGroupRows];
-  load(0, next);
-  for (int m0 = 0; m0 < g.rows; m0 += turn) {
+    for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+      for (int e = 0; e < kGroupRows; ++e) k[u][e] = row(m0, u, e) < g.rows ? key(g.index[row(m0, u, e)]) : 0x7fffffff;
     uint32_t mine = 0;
+    int before[TURNS];
 #pragma unroll
-    for (int e = 0; e < kGroupRows; ++e) mine |= (uint32_t)(next[e] == a) << e;
-    load(m0 + turn, next);
-    // places: of the waves before, of the lanes before (all lanes' bits of one row of four, one row
-    // after another, give the number before a lane)
-    int before = 0, all = 0;
+    for (int u = 0; u < TURNS; ++u) {
+      // the bits of the lanes of each of four rows: how many lie before the lane's, and all
+      int all = 0;
+      before[u] = 0;
 #pragma unroll
-    for (int e = 0; e < kGroupRows; ++e) {
-      const uint64_t b = __ballot(mine >> e & 1);
-      before += __popcll(b & ((1ull << lane) - 1));
-      all += __popcll(b);
-    }
-    __syncthreads();
-    if (lane == 0) same16[w] = all;
-    __syncthreads();
-    int p = at + before, sum = 0;
-    for (int k = 0; k < waves; ++k) {
-      p += k < w ? same16[k] : 0;
-      sum += same16[k];
-    }
-#pragma unroll
-    for (int e = 0; e < kGroupRows; ++e)
-      if (mine >> e & 1) {
-        g.order[p] = m0 + t * kGroupRows + e;
-        g.which[p++] = a;
+      for (int e = 0; e < kGroupRows; ++e) {
+        if (!many) less += k[u][e] < a;
+        mine |= (uint32_t)(k[u][e] == a) << (u * kGroupRows + e);
+        const uint64_t b = __ballot(k[u][e] == a);
+        before[u] += __popcll(b & ((1ull << lane) - 1));
+        all += __popcll(b);
       }
-    at += sum;
+      if (m0 > 0 && u == 0) __syncthreads();
+      if (lane == 0) count64[u * 16 + w] = all;
+    }
+    if (!many) {
+      less = (int)wave_sum((uint32_t)less);
+      if (lane == 0) less16[w] = less;
+    }
+    __syncthreads();
+    if (!many)
+      for (int k = 0; k < waves; ++k) at += less16[k];
+    // of turns and waves, in that order, those before
+    const int n = lane % 16 < waves && lane < TURNS * 16 ? count64[lane] : 0;
+    int upto = n;
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xa, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xc, 0xf, true);
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) {
+      int p = at + before[u] + __builtin_amdgcn_readlane(upto - n, u * 16 + w);
+#pragma unroll
+      for (int e = 0; e < kGroupRows; ++e)
+        if (mine >> (u * kGroupRows + e) & 1) {
+          g.order[p] = row(m0, u, e);
+          g.which[p++] = a;
+        }
+    }
+    if (m0 == 0 && t == 0) {
+      g.start[a] = at;
+      if (a == g.count) g.start[a + 1] = g.rows;
+    }
+    at += __builtin_amdgcn_readlane(upto, 63);
   }
 }
 
@@ -209,7 +232,7 @@ template <class T, int MT, int RT, bool WIDE>
 __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
   typedef Mat<T> M;
   typedef typename M::F F;
-  constexpr int U = MT + RT <= 3 ? 4 : MT + RT <= 6 ? 2 : 1;
+  constexpr int U = MT + RT <= 3 ? 4 : 2;
   __shared__ f4 red[4][MT * RT][64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
   const int first = blockIdx.x * 16 * MT;
@@ -233,11 +256,18 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
     for (int j = 0; j < RT; ++j) wr[j] = (const T*)a.W + ad * a.step + (int64_t)min(16 * j + m, a.rank - 1) * a.ldw;
     f4 acc[MT][RT] = {};
     F fx[2][U][MT], fw[2][U][RT];
-    auto load = [&](int s, F x_[U][MT], F w_[U][RT]) {
+    // A wave takes two steps in a row (128 bytes of a row), then the next wave's turn. Windows begin at
+    // different steps: rows that lie a power of two apart have the same columns in the same
+    // channels of memory.
+    const int n = s1 - s0, turns = (n + 7) / 8, shift = (int)(blockIdx.x * 5u % (unsigned)turns);
+    auto load = [&](int i, F x_[U][MT], F w_[U][RT]) {  // steps i .. i + U - 1 of the wave's
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        // (steps past the end are zeros on one side)
-        const int k = s + 4 * u < s1 ? (s + 4 * u) * M::K + q * M::E : a.n;
+        int turn = (i + u) / 2 + shift;
+        turn -= turn >= turns ? turns : 0;
+        const int s = turn * 8 + 2 * w + (i + u) % 2;
+        // (steps past the end are zeros)
+        const int k = s < n && i + u < 2 * turns ? (s0 + s) * M::K + q * M::E : a.n;
 #pragma unroll
         for (int i = 0; i < MT; ++i) x_[u][i] = load_row<WIDE>(x[i], k, a.n);
 #pragma unroll
@@ -253,13 +283,13 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
           for (int j = 0; j < RT; ++j) acc[i][j] = mma(w_[u][j], x_[u][i], acc[i][j]);
     };
     // a turn's loads are on their way while the one before is summed
-    load(s0 + w, fx[0], fw[0]);
+    load(0, fx[0], fw[0]);
 #pragma unroll 1
-    for (int s = s0 + w; s < s1; s += 8 * U) {
-      load(s + 4 * U, fx[1], fw[1]);
+    for (int i = 0; i < 2 * turns; i += 2 * U) {
+      load(i + U, fx[1], fw[1]);
       sum(fx[0], fw[0]);
-      if (s + 4 * U >= s1) break;
-      load(s + 8 * U, fx[0], fw[0]);
+      if (i + U >= 2 * turns) break;
+      load(i + 2 * U, fx[0], fw[0]);
       sum(fx[1], fw[1]);
     }
     __syncthreads();
@@ -321,7 +351,6 @@ struct ExpandArgs {
   int64_t ldy;
   void* O;
   int64_t ldo;
-  bool wide;  // Y and O are moved in 16-byte pieces
 };
 
 // NK: steps of the inner side, of M::K each; 0: of 16-bit types one step that has both
@@ -341,8 +370,30 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
   const int first = blockIdx.x * ROWS;
   const int c0 = blockIdx.y * 256 + w * 64 + q * 16;  // the lane's columns
-  const bool whole = a.wide && c0 + 16 <= a.n;
+  const bool whole = c0 + 16 <= a.n;
   if (t < ROWS) at[t] = row_at(a.g, first + t), of[t] = which_at(a.g, first + t);
+  F fw[4][S];
+  int held = -1;  // the adapter whose W is in registers
+  auto hold = [&](int ad) {
+    if (ad >= a.g.count || ad == held) return;
+    held = ad;
+    // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
+      const T* row = (const T*)a.W + ad * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
+#pragma unroll
+      for (int k = 0; k < S; ++k) fw[j][k] = load_row<WIDE>(row, kPacked ? q % 2 * 8 : k * M::K + q * M::E, a.rank);
+    }
+  };
+  {
+    // W of the work group's first adapter is on its way while h is laid out
+    int mine;
+    uint64_t heads = heads_of(a.g, first, min(ROWS, 64), mine);
+    for (int z = 0; z < (int)blockIdx.z && heads != 0; ++z) heads &= heads - 1;
+    if (heads == 0 && gridDim.z > 1 && ROWS <= 64) return;  // the window has no more of them
+    if (heads != 0) hold(__builtin_amdgcn_readlane(mine, __builtin_ctzll(heads)));
+  }
   for (int i0 = t >> 2; i0 < ROWS; i0 += 64) {
     const int place = first + i0, p = t & 3;
     const int wh = which_at(a.g, place);
@@ -353,7 +404,7 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
     for (int k = 0; k < S; ++k)
 #pragma unroll
       for (int e = 0; e < M::E; ++e) h[k][e] = 0.0f;
-    const float* from = a.H + (int64_t)(some ? place : 0) * a.ranks;
+    const float* from = a.H + (int64_t)place * a.ranks;  // (read where there is none, too: nothing waits for which)
     const int64_t part = a.places * a.ranks;
 #pragma unroll 4
     for (int s = 0; s < a.parts; ++s)
@@ -418,16 +469,15 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
   }
   __syncthreads();
   if (c0 - q * 16 >= a.n) return;
-  // a window's part of Y, loaded one window ahead
-  u4 ahead[V];
-  auto fetch = [&](int i) {
+  // a window's part of Y, loaded some windows ahead
+  constexpr int AHEAD = WIN >= 4 ? 3 : 1;
+  u4 ahead[AHEAD][V];
+  auto fetch = [&](int i, u4 to[V]) {
     if (!whole || !a.Y) return;
-    const T* p = (const T*)a.Y + (int64_t)at[16 * i + m] * a.ldy + c0;
+    const T* p = (const T*)a.Y + (int64_t)at[16 * min(i, WIN - 1) + m] * a.ldy + c0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) ahead[v] = *(const u4*)((const char*)p + 16 * v);
+    for (int v = 0; v < V; ++v) to[v] = *(const u4_near*)((const char*)p + 16 * v);
   };
-  F fw[4][S];
-  int held = -1;  // the adapter whose W is in registers
   for (int z0 = 0, z = 0; z0 < ROWS; z0 += 64) {
     // adapters of these (up to) 64 places; a work group of many takes some of them
     const int mine = of[z0 + min(lane, ROWS - 1)], before = __shfl_up(mine, 1);
@@ -437,26 +487,21 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
       const int from = z0 + __builtin_ctzll(heads), ad = __builtin_amdgcn_readfirstlane(of[from]);
       const uint64_t rest = heads & (heads - 1);
       const int last = (rest ? z0 + __builtin_ctzll(rest) : min(z0 + 64, ROWS)) - 1;
-      fetch(from / 16);
-      if (ad < a.g.count && ad != held) {
-        // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
-          const T* row = (const T*)a.W + ad * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
-#pragma unroll
-          for (int k = 0; k < S; ++k) fw[j][k] = load_row<WIDE>(row, kPacked ? q % 2 * 8 : k * M::K + q * M::E, a.rank);
-        }
-        held = ad;
-      }
+      for (int b = 0; b < AHEAD; ++b) fetch(from / 16 + b, ahead[b]);
+      hold(ad);
 #pragma unroll 1
       for (int i = from / 16; i <= last / 16; ++i) {
         const int place = 16 * i + m;
         const bool own = place >= from && of[place] == ad;
         u4 y[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) y[v] = ahead[v];
-        if (i < last / 16) fetch(i + 1);
+        for (int v = 0; v < V; ++v) y[v] = ahead[0][v];
+#pragma unroll
+        for (int b = 0; b + 1 < AHEAD; ++b)
+#pragma unroll
+          for (int v = 0; v < V; ++v) ahead[b][v] = ahead[b + 1][v];
+        if (i + AHEAD <= last / 16) fetch(i + AHEAD, ahead[AHEAD - 1]);
         f4 acc[4] = {};
         if (ad < a.g.count) {
 #pragma unroll
@@ -485,8 +530,20 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = fmaf(acc[e / 4][e % 4], f, o[e]);
         }
-        store8(out, whole, min(a.n - c0, 8), o);
-        store8(out + 8, whole, min(a.n - c0 - 8, 8), o + 8);
+        if (whole) {
+          typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            E x;
+#pragma unroll
+            for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = (T)o[v * 16 / sizeof(T) + e];
+            *(u4_near*)((char*)out + 16 * v) = __builtin_bit_cast(u4, x);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (c0 + e < a.n) out[e] = (T)o[e];
+        }
       }
     }
   }
@@ -543,23 +600,11 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     const float f = o.scales ? o.scales[ad] : 1.0f;
     // place of a lane's row e in the step from s on
     auto place = [&](int s, int e) { return kNarrow ? s + 8 * q + e : s + 4 * e + q; };
-    float down[RT], up[RT];
+    // f16: sums are kept relative to a power of two for each rank, that of its largest h so
+    // far, so that the halves of an h reach from there to where it does not matter
+    uint32_t ex[RT];
 #pragma unroll
-    for (int j = 0; j < RT; ++j) down[j] = up[j] = 1.0f;
-    if constexpr (std::is_same<T, _Float16>::value) {
-      // a power of two for each rank: its largest h here comes to [1, 2)
-#pragma unroll
-      for (int j = 0; j < RT; ++j) {
-        const int r = min(r0 + 16 * j + m, a.rank - 1);
-        uint32_t top = 0;
-#pragma unroll 4
-        for (int i = from + q; i < to; i += 4) top = max(top, mag(o.H[(o.by_row ? (int64_t)row_at(a.g, i) : i) * o.ldh + r] * f));
-        top = quad_max(top);
-        const uint32_t ex = min(max(top >> 23, 2u), 252u);
-        up[j] = __uint_as_float(ex << 23);
-        down[j] = __uint_as_float((254u - ex) << 23);
-      }
-    }
+    for (int j = 0; j < RT; ++j) ex[j] = 2;
     struct Step {
       u4 z[L];
       float h[RT][L];
@@ -592,11 +637,27 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
       }
       if constexpr (kNarrow) {
         F h[RT][TERMS];
+        if constexpr (std::is_same<T, _Float16>::value) {
+#pragma unroll
+          for (int j = 0; j < RT; ++j) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, mag(x.h[j][e] * f));
+            top = max(ex[j], min(quad_max(top) >> 23, 252u));
+            if (__ballot(top != ex[j]) != 0) {
+              const float by = top - ex[j] > 126u ? 0.0f : __uint_as_float((127u - (top - ex[j])) << 23);
+#pragma unroll
+              for (int c = 0; c < C; ++c) acc[c][j] *= by;
+              ex[j] = top;
+            }
+          }
+        }
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            float v = x.h[j][e] * f * down[j];
+            float v = x.h[j][e] * f;
+            if constexpr (std::is_same<T, _Float16>::value) v *= __uint_as_float((254u - ex[j]) << 23);
 #pragma unroll
             for (int u = 0; u < TERMS; ++u) h[j][u][e] = u + 1 < TERMS ? (T)split(v, T()) : (T)v;
           }
@@ -652,7 +713,8 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
         for (int c = 0; c < C; c += 4) {
           f4 v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = acc[c + e][j][i] * up[j];
+          for (int e = 0; e < 4; ++e)
+            v[e] = std::is_same<T, _Float16>::value ? acc[c + e][j][i] * __uint_as_float(ex[j] << 23) : acc[c + e][j][i];
           *(f4*)(red + ((w * RT + j) * 16 + m) * PITCH + C * (4 * q + i) + c) = v;
         }
     __syncthreads();
@@ -669,15 +731,14 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     i0 = to;
   }
 }
-template <class T, int RT>
+template <class T, int RT, bool WIDE>
 __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
-  const Outer o = a.of[blockIdx.z / a.ranks];
-  if ((int)blockIdx.x * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
-  if (o.wide)
-    outer_tile<T, RT, true>(a, o, blockIdx.x, blockIdx.y, blockIdx.z % a.ranks, red);
-  else
-    outer_tile<T, RT, false>(a, o, blockIdx.x, blockIdx.y, blockIdx.z % a.ranks, red);
+  const Outer o = a.of[blockIdx.z];
+  // every eighth work group runs on the same die: the ranks of a strip follow one another there
+  const int k = blockIdx.x >> 3, strip = k / a.ranks * 8 + (blockIdx.x & 7);
+  if (strip * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
+  outer_tile<T, RT, WIDE>(a, o, strip, blockIdx.y, k % a.ranks, red);
 }
 
 // The parts' sums, and zeros for adapters without rows.
@@ -798,7 +859,8 @@ void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
       hipLaunchKernelGGL((k_expand<T, NK, WIN, decltype(w)::value>), grid, dim3(256), 0, s, a);
     };
     if (few) wide ? as(std::integral_constant<int, 1>(), std::true_type()) : as(std::integral_constant<int, 1>(), std::false_type());
-    else wide ? as(std::integral_constant<int, 8>(), std::true_type()) : as(std::integral_constant<int, 8>(), std::false_type());
+    else wide ? as(std::integral_constant<int, NK >= 2 ? 4 : 8>(), std::true_type())
+              : as(std::integral_constant<int, NK >= 2 ? 4 : 8>(), std::false_type());
   };
   if constexpr (sizeof(T) == 4) {
     if (a.rank <= 16) of(std::integral_constant<int, 1>());
@@ -824,32 +886,37 @@ int fold(const Groups& g, int rank, int parts, const float* h, float* out, hipSt
 }
 
 // places of a window: as many windows as fill the device with strips of 128 columns, of 256
-// places at least (two steps of each wave), the fewer the less there is to join
-int outer_window(int64_t rows, int64_t n) {
-  const int64_t want = std::max<int64_t>(1, ceil_div(512, ceil_div(n, 128)));
-  return (int)std::max<int64_t>(256, up(ceil_div(rows, want), 128));
+// places at least (two steps of each wave): fewer windows are fewer sums to join
+int outer_window(int64_t rows, int64_t n, int rank) {
+  const int64_t groups = 2 * ceil_div(n, 128) * (rank <= 16 ? 1 : ceil_div(rank, 32));
+  return (int)std::max<int64_t>(256, up(ceil_div(rows, std::max<int64_t>(1, ceil_div(768, groups))), 128));
 }
 size_t outer_bytes(int64_t rows, int64_t n, int rank, int count) {
-  const int64_t windows = ceil_div(rows, outer_window(rows, n));
+  const int64_t windows = ceil_div(rows, outer_window(rows, n, rank));
   return windows <= 1 ? 0 : up256((size_t)(windows + count) * n * rank * 4);
 }
 // the first n of a.of
 template <class T>
 void outer(OuterArgs a, int n, hipStream_t s) {
   int64_t strips = 0, windows = 0, size = 0;
+  bool wide = true;
   for (int i = 0; i < n; ++i) {
-    a.of[i].window = outer_window(a.g.rows, a.of[i].n);
+    a.of[i].window = outer_window(a.g.rows, a.of[i].n, a.rank);
     strips = std::max(strips, ceil_div(a.of[i].n, 16 * Mat<T>::E));
     windows = std::max(windows, ceil_div(a.g.rows, a.of[i].window));
     size = std::max(size, (int64_t)a.of[i].n * a.rank);
+    wide = wide && a.of[i].wide;
   }
   if (windows > 0) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
-    const dim3 grid((unsigned)strips, (unsigned)windows, (unsigned)(n * a.ranks));
-    if (a.rank <= 16)
-      hipLaunchKernelGGL((k_outer<T, 1>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_outer<T, 2>), grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)n);
+    auto as = [&](auto rt, auto w) {
+      hipLaunchKernelGGL((k_outer<T, decltype(rt)::value, decltype(w)::value>), grid, dim3(256), 0, s, a);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    if (a.rank <= 16) wide ? as(one, std::true_type()) : as(one, std::false_type());
+    else wide ? as(two, std::true_type()) : as(two, std::false_type());
   }
   hipLaunchKernelGGL(k_outer_join, dim3((unsigned)std::min<int64_t>(ceil_div(size, 1024), 256), a.g.count, n), dim3(256), 0, s, a);
 }
@@ -899,7 +966,12 @@ gptq2d_status gptq2d_adapter_groups(int64_t M, int count, const int32_t* index, 
   if (!groups || (M > 0 && !index)) return refuse("index or groups is NULL");
   if (!aligned(index, 4) || !aligned(groups, 4)) return refuse("an argument is not aligned to its elements");
   const GroupArgs a = {(int)M, count, index, groups, groups + M, groups + 2 * M};
-  hipLaunchKernelGGL(k_group, dim3(count + 1), dim3(M <= 1024 ? 256 : kGroupThreads), 0, (hipStream_t)stream, a);
+  // as many threads as rows want, in one turn where that is enough
+  const dim3 threads(M <= 1024 ? 256 : kGroupThreads);
+  if (M <= 4096)
+    hipLaunchKernelGGL(k_group<1>, dim3(count + 1), threads, 0, (hipStream_t)stream, a);
+  else
+    hipLaunchKernelGGL(k_group<4>, dim3(count + 1), threads, 0, (hipStream_t)stream, a);
   return launched("gptq2d_adapter_groups");
 }
 
@@ -937,8 +1009,7 @@ gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count,
       hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * R, 256)), dim3(256), 0, s, f);
     }
     const int left = fold<T>(g, R, parts, h, h, s);
-    const ExpandArgs e = {g, (int)N, R, ranks_of(R), left, h, places_of(M), scales, B, ldb, N * ldb, Y, ldy, O, ldo,
-                          (!Y || wide_rows(Y, ldy, es)) && wide_rows(O, ldo, es)};
+    const ExpandArgs e = {g, (int)N, R, ranks_of(R), left, h, places_of(M), scales, B, ldb, N * ldb, Y, ldy, O, ldo};
     expand<T>(e, wide_matrix<T>(B, ldb, R), s);
   });
   return launched("gptq2d_adapters");
@@ -1010,7 +1081,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
     if (n > 0) outer<T>(o, n, s);
     if (dX) {
       const ExpandArgs e = {g, (int)K, R, ranks_of(R), 1, ph, places_of(M), nullptr, ws + b.at, b.ldat, K * b.ldat, D, ldd, dX,
-                            lddx, (!D || wide_rows(D, ldd, es)) && wide_rows(dX, lddx, es)};
+                            lddx};
       expand<T>(e, R % Mat<T>::E == 0, s);
     }
   });
