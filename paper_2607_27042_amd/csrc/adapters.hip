@@ -51,29 +51,37 @@ __device__ __forceinline__ f4 mma(f4 a, f4 b, f4 c) {
   return c;
 }
 
-// 16 bytes at any element (the memory takes them off their boundary as well, in two lines)
+// 16 bytes at any element (memory takes them off their boundary as well, in two lines)
 typedef u4 u4_near __attribute__((aligned(2)));
 
-// Elements k .. k + E - 1 of a row of n, zeros past its end. WIDE: rows start on 16-byte
-// boundaries and n is a multiple of E.
-template <bool WIDE, class T>
+// Elements k .. k + E - 1 of a row of n, in two halves: the load, without a branch and with
+// nothing done to what it brings (a wave that would set it to zero there, or choose between two
+// loads, would wait for it there), and what is left to do where it is used and the row ends
+// among these elements or before them.
+template <class T>
 __device__ __forceinline__ typename Mat<T>::F load_row(const T* row, int k, int n) {
-  typedef typename Mat<T>::F F;
-  F f;
-  if constexpr (WIDE) {
-    f = __builtin_bit_cast(F, *(const u4*)(row + (k < n ? k : 0)));
-    if (k >= n) f = F{};
+  typename Mat<T>::F f;
+  if (n >= Mat<T>::E) f = __builtin_bit_cast(typename Mat<T>::F, *(const u4_near*)(row + min(k, n - Mat<T>::E)));
+  return f;
+}
+template <class T>
+__device__ __forceinline__ void end_row(typename Mat<T>::F& f, const T* row, int k, int n) {
+  typedef unsigned __int128 B;
+  constexpr int E = Mat<T>::E, bits = 8 * sizeof(T);
+  if (k + E <= n) return;
+  B b = __builtin_bit_cast(B, f);
+  if (n >= E) {  // the row's last E elements: those before k are shifted out, zeros in
+    const int d = k - (n - E);
+    b = d < E ? b >> (bits * d) : 0;
   } else {
-    if (k + Mat<T>::E <= n) {
-      f = __builtin_bit_cast(F, *(const u4_near*)(row + k));
-    } else {
-      f = F{};
-#pragma unroll
-      for (int i = 0; i < Mat<T>::E; ++i)
-        if (k + i < n) f[i] = row[k + i];
+    b = 0;
+#pragma unroll 1
+    for (int i = n - 1; i >= k; --i) {
+      typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type U;
+      b = b << bits | __builtin_bit_cast(U, row[i]);
     }
   }
-  return f;
+  f = __builtin_bit_cast(typename Mat<T>::F, b);
 }
 
 // what of x (or, near the type's smallest number, of all that is summed with it) T holds
@@ -228,7 +236,7 @@ struct ShrinkArgs {
 
 // A work group takes a window of 16 MT rows and a part of the inner side, whose steps its
 // four waves share; their sums are joined in LDS.
-template <class T, int MT, int RT, bool WIDE>
+template <class T, int MT, int RT>
 __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
   typedef Mat<T> M;
   typedef typename M::F F;
@@ -256,41 +264,45 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
     for (int j = 0; j < RT; ++j) wr[j] = (const T*)a.W + ad * a.step + (int64_t)min(16 * j + m, a.rank - 1) * a.ldw;
     f4 acc[MT][RT] = {};
     F fx[2][U][MT], fw[2][U][RT];
-    // A wave takes two steps in a row (128 bytes of a row), then the next wave's turn. Windows begin at
-    // different steps: rows that lie a power of two apart have the same columns in the same
-    // channels of memory.
-    const int n = s1 - s0, turns = (n + 7) / 8, shift = (int)(blockIdx.x * 5u % (unsigned)turns);
+    // a wave takes two steps in a row (128 bytes of a row of 16-bit numbers), then the next one
+    const int n = s1 - s0, all = (n + 7) / 8 * 2;
+    auto step = [&](int i) { return (i & ~1) * 4 + 2 * w + (i & 1); };  // the wave's i-th
     auto load = [&](int i, F x_[U][MT], F w_[U][RT]) {  // steps i .. i + U - 1 of the wave's
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int turn = (i + u) / 2 + shift;
-        turn -= turn >= turns ? turns : 0;
-        const int s = turn * 8 + 2 * w + (i + u) % 2;
-        // (steps past the end are zeros)
-        const int k = s < n && i + u < 2 * turns ? (s0 + s) * M::K + q * M::E : a.n;
+        const int k = (s0 + min(step(i + u), n - 1)) * M::K + q * M::E;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x_[u][i] = load_row<WIDE>(x[i], k, a.n);
+        for (int i = 0; i < MT; ++i) x_[u][i] = load_row(x[i], k, a.n);
 #pragma unroll
-        for (int j = 0; j < RT; ++j) w_[u][j] = load_row<WIDE>(wr[j], k, a.n);
+        for (int j = 0; j < RT; ++j) w_[u][j] = load_row(wr[j], k, a.n);
       }
     };
-    auto sum = [&](F x_[U][MT], F w_[U][RT]) {
+    auto sum = [&](int i, F x_[U][MT], F w_[U][RT]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        const int s = step(i + u), k0 = (s0 + s) * M::K;
+        if (i + u >= all || s >= n) continue;
+        if (k0 + M::K > a.n) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) end_row(x_[u][i], x[i], k0 + q * M::E, a.n);
+#pragma unroll
+          for (int j = 0; j < RT; ++j) end_row(w_[u][j], wr[j], k0 + q * M::E, a.n);
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < RT; ++j) acc[i][j] = mma(w_[u][j], x_[u][i], acc[i][j]);
+      }
     };
     // a turn's loads are on their way while the one before is summed
     load(0, fx[0], fw[0]);
 #pragma unroll 1
-    for (int i = 0; i < 2 * turns; i += 2 * U) {
+    for (int i = 0; i < all; i += 2 * U) {
       load(i + U, fx[1], fw[1]);
-      sum(fx[0], fw[0]);
-      if (i + U >= 2 * turns) break;
+      sum(i, fx[0], fw[0]);
+      if (i + U >= all) break;
       load(i + 2 * U, fx[0], fw[0]);
-      sum(fx[1], fw[1]);
+      sum(i + U, fx[1], fw[1]);
     }
     __syncthreads();
 #pragma unroll
@@ -311,6 +323,106 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
         *(f4*)(a.H + ((int64_t)blockIdx.y * a.places + first + 16 * i + m) * a.ranks + r) = s;
       }
     }
+  }
+}
+
+// The same for many rows: a work group takes 64 rows and a part of the inner side, which come
+// through a ring of LDS buffers of 128 bytes of each row, loaded without registers in
+// between, BUFS - 1 of them ahead; a wave sums 16 rows. The pieces of a row are dealt out so that
+// the 16 rows that are read at once lie in different banks. (The rows' direct way to the
+// registers takes 64 bytes of each of 16 rows at a time, and has each wave load the weights anew:
+// 8192 x 4096, rank 16, 22.8 us there, SHRINK16 here; 4096 x 4096, rank 64, 21.9 and SHRINK64.)
+// For rows on 16-byte boundaries, of whole pieces.
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until N of the wave's loads are on their way
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+}
+typedef __attribute__((address_space(3))) void lds_void;
+template <int RT>
+constexpr int shrink_bufs() { return RT == 1 ? 12 : RT == 2 ? 10 : RT == 4 ? 8 : 6; }
+template <class T, int RT>
+__global__ __launch_bounds__(256) void k_shrink_many(ShrinkArgs a) {
+  typedef Mat<T> M;
+  typedef typename M::F F;
+  constexpr int BUFS = shrink_bufs<RT>(), ROWS = 64 + 16 * RT;
+  constexpr int CHUNK = 128 / sizeof(T);               // elements of a row in a buffer
+  constexpr int XL = 2, WL = RT == 1 ? 1 : RT / 2;     // a wave's loads of X and W (eight rows each)
+  __shared__ alignas(16) char ring[BUFS][ROWS * 128];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
+  const int first = blockIdx.x * 64;
+  int mine;
+  uint64_t heads = heads_of(a.g, first, 64, mine);
+  const int own = which_at(a.g, first + 16 * w + m);
+  // the lane's place in a load: row lane / 8 of eight, piece lane % 8 of it, changed by the row
+  const int lr = lane >> 3, piece = (lane & 7) ^ lr;
+  const char* x[XL];
+#pragma unroll
+  for (int i = 0; i < XL; ++i) x[i] = (const char*)((const T*)a.X + (int64_t)row_at(a.g, first + 16 * w + 8 * i + lr) * a.ldx);
+  const int chunks = (a.n + CHUNK - 1) / CHUNK;
+  const int s0 = (int)((int64_t)chunks * blockIdx.y / gridDim.y), s1 = (int)((int64_t)chunks * (blockIdx.y + 1) / gridDim.y);
+  const int most = (int)((a.n * sizeof(T) - 16));  // the last piece of a row
+  for (; heads != 0; heads &= heads - 1) {
+    const int ad = __builtin_amdgcn_readlane(mine, __builtin_ctzll(heads));
+    if (ad >= a.g.count) continue;
+    const char* wr[WL];
+#pragma unroll
+    for (int i = 0; i < WL; ++i)
+      wr[i] = (const char*)((const T*)a.W + ad * a.step + (int64_t)min((w * WL + i) * 8 + lr, a.rank - 1) * a.ldw);
+    auto load = [&](int s) {
+      char* b = ring[(s - s0) % BUFS];
+      const int at = min(s * 128 + piece * 16, most);
+#pragma unroll
+      for (int i = 0; i < XL; ++i)
+        __builtin_amdgcn_global_load_lds((const void*)(x[i] + at), (lds_void*)(b + (16 * w + 8 * i) * 128), 16, 0, 0);
+      if (RT > 1 || w < 2) {
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+          __builtin_amdgcn_global_load_lds((const void*)(wr[i] + at), (lds_void*)(b + (64 + (w * WL + i) * 8) * 128), 16, 0, 0);
+      }
+    };
+    f4 acc[RT] = {};
+    wait_loads<0>();
+    asm volatile("s_barrier" ::: "memory");  // the last adapter's buffers are read
+#pragma unroll 1
+    for (int s = s0; s < min(s0 + BUFS - 1, s1); ++s) load(s);
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+      if (s + BUFS - 1 > s1) wait_loads<0>();
+      else if (RT > 1 || w < 2) wait_loads<(BUFS - 2) * (XL + WL)>();
+      else wait_loads<(BUFS - 2) * XL>();
+      // every wave's part of this buffer is there, and every wave has read the one that is filled next
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (s + BUFS - 1 < s1) load(s + BUFS - 1);
+      const char* b = ring[(s - s0) % BUFS];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {  // (two steps of the instruction)
+        const int p = ((4 * k + q) ^ (m & 7)) * 16;
+        F fx = *(const F*)(b + (16 * w + m) * 128 + p);
+        F fw[RT];
+#pragma unroll
+        for (int j = 0; j < RT; ++j) fw[j] = *(const F*)(b + (64 + 16 * j + m) * 128 + p);
+        if ((s + 1) * CHUNK > a.n && s * CHUNK + (4 * k + q) * M::E >= a.n) {
+          fx = F{};
+#pragma unroll
+          for (int j = 0; j < RT; ++j) fw[j] = F{};
+        }
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[j] = mma(fw[j], fx, acc[j]);
+      }
+    }
+    const float f = a.scales ? a.scales[ad] : 1.0f;
+    if (own == ad) {
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        const int r = 16 * j + 4 * q;
+        if (r >= a.ranks) continue;
+        f4 s = acc[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = r + e < a.rank ? s[e] * f : 0.0f;
+        *(f4*)(a.H + ((int64_t)blockIdx.y * a.places + first + 16 * w + m) * a.ranks + r) = s;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
@@ -356,8 +468,13 @@ struct ExpandArgs {
 // NK: steps of the inner side, of M::K each; 0: of 16-bit types one step that has both
 // halves of 16 h. A work group takes 16 WIN rows and 256 columns, a wave 64 of them. Four
 // tiles' rows of W are dealt out so that a lane ends with 16 consecutive columns.
-template <class T, int NK, int WIN, bool WIDE>
-__global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
+// waves of a SIMD that an instance's registers are held down to
+template <class T, int NK>
+constexpr int expand_waves() {
+  return sizeof(T) == 2 ? (NK == 1 ? 3 : NK <= 2 ? 4 : 2) : NK == 1 ? 4 : NK == 2 ? 3 : NK == 4 ? 2 : 1;
+}
+template <class T, int NK, int WIN>
+__global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandArgs a) {
   typedef Mat<T> M;
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2, kPacked = kNarrow && NK == 0;
@@ -368,22 +485,31 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
   __shared__ float back[ROWS];
   __shared__ int at[ROWS], of[ROWS];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
-  const int first = blockIdx.x * ROWS;
-  const int c0 = blockIdx.y * 256 + w * 64 + q * 16;  // the lane's columns
+  const int strips = (a.n + 255) / 256, window = blockIdx.x / (uint32_t)strips, strip = blockIdx.x - window * strips;
+  const int first = window * ROWS;
+  const int c0 = strip * 256 + w * 64 + q * 16;  // the lane's columns
   const bool whole = c0 + 16 <= a.n;
   if (t < ROWS) at[t] = row_at(a.g, first + t), of[t] = which_at(a.g, first + t);
   F fw[4][S];
   int held = -1;  // the adapter whose W is in registers
+  auto inner = [&](int k) { return kPacked ? q % 2 * 8 : k * M::K + q * M::E; };  // a lane's elements of step k
+  // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
+  auto w_row = [&](int j) {
+    const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
+    return (const T*)a.W + held * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
+  };
   auto hold = [&](int ad) {
     if (ad >= a.g.count || ad == held) return;
     held = ad;
-    // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
-      const T* row = (const T*)a.W + ad * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int k = 0; k < S; ++k) fw[j][k] = load_row<WIDE>(row, kPacked ? q % 2 * 8 : k * M::K + q * M::E, a.rank);
+      for (int k = 0; k < S; ++k) fw[j][k] = load_row(w_row(j), inner(k), a.rank);
+    if (a.rank % (kPacked ? 16 : M::K) != 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < S; ++k) end_row(fw[j][k], w_row(j), inner(k), a.rank);
     }
   };
   {
@@ -470,7 +596,7 @@ __global__ __launch_bounds__(256) void k_expand(ExpandArgs a) {
   __syncthreads();
   if (c0 - q * 16 >= a.n) return;
   // a window's part of Y, loaded some windows ahead
-  constexpr int AHEAD = WIN >= 4 ? 3 : 1;
+  constexpr int AHEAD = WIN == 1 || NK == 8 ? 1 : 3;
   u4 ahead[AHEAD][V];
   auto fetch = [&](int i, u4 to[V]) {
     if (!whole || !a.Y) return;
@@ -559,7 +685,7 @@ struct Outer {
   int64_t ldz;
   const float* H;  // rows (by_row: of the batch, else places) of ldh
   int64_t ldh;
-  bool by_row, wide;
+  bool by_row;
   const float* scales;
   float* out;       // [adapter][n][rank], or [adapter][rank][n] where `across`
   bool across;
@@ -578,7 +704,7 @@ struct OuterArgs {
 // column. Adapters whose rows lie in one window are done with it; of the others each window gives a
 // part, at the number of the window and the adapter together (which grows along the
 // order, so that no two are alike).
-template <class T, int RT, bool WIDE>
+template <class T, int RT>
 __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, int strip, int window, int rank0, float* red) {
   typedef Mat<T> M;
   typedef typename M::F F;
@@ -617,7 +743,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     auto load = [&](int s, Step& x) {
 #pragma unroll
       for (int e = 0; e < L; ++e)
-        x.z[e] = __builtin_bit_cast(u4, load_row<WIDE>((const T*)o.Z + (int64_t)rows[e] * o.ldz, c0 + C * m, o.n));
+        x.z[e] = __builtin_bit_cast(u4, load_row((const T*)o.Z + (int64_t)rows[e] * o.ldz, c0 + C * m, o.n));
 #pragma unroll
       for (int j = 0; j < RT; ++j)
 #pragma unroll
@@ -626,6 +752,14 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     };
     f4 acc[C][RT] = {};
     auto sum = [&](int s, Step& x) {
+      if (c0 + COLS > o.n && c0 + C * m < o.n) {  // the last columns (those past them are not written)
+#pragma unroll
+        for (int e = 0; e < L; ++e) {
+          F f = __builtin_bit_cast(F, x.z[e]);
+          end_row(f, (const T*)o.Z + (int64_t)row_at(a.g, min(place(s, e), to - 1)) * o.ldz, c0 + C * m, o.n);
+          x.z[e] = __builtin_bit_cast(u4, f);
+        }
+      }
       if (s + STEP > to) {
 #pragma unroll
         for (int e = 0; e < L; ++e) {
@@ -731,14 +865,14 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     i0 = to;
   }
 }
-template <class T, int RT, bool WIDE>
+template <class T, int RT>
 __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
   const Outer o = a.of[blockIdx.z];
   // every eighth work group runs on the same die: the ranks of a strip follow one another there
   const int k = blockIdx.x >> 3, strip = k / a.ranks * 8 + (blockIdx.x & 7);
   if (strip * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
-  outer_tile<T, RT, WIDE>(a, o, strip, blockIdx.y, k % a.ranks, red);
+  outer_tile<T, RT>(a, o, strip, blockIdx.y, k % a.ranks, red);
 }
 
 // The parts' sums, and zeros for adapters without rows.
@@ -805,34 +939,46 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return ceil_div(v, m) * m; }
 
 int ranks_of(int rank) { return (int)up(rank, 16); }
-// Row tiles of a window, and parts of the inner side. More rows of a window read the weights
-// more seldom, parts fill the device, each at its price: PLANNOTE
-int shrink_tiles(int64_t rows, int rank) { return rows < 2048 ? 1 : rank <= 16 ? 1 : 2; }
+// Few rows: windows of 16 for whose adapters there is a work group each. Otherwise a work group
+// takes its window's adapters one after another.
+constexpr int kFew = 2048;
+constexpr int kManyGroups = 256;  // work groups of many rows
+// Row tiles of a window: more rows read the weights more seldom.
+int shrink_tiles(int64_t rows, int rank) { return rows < kFew || rank <= 16 ? 1 : 2; }
+// Parts of the inner side, which fill the device. Few rows: four at most, which what reads h
+// sums (64 rows of 4096, 48 adapters of rank 16, a call: 2 / 4 / 8 / 16 parts 16.0 / 14.9 / 15.7 / 17.8 us,
+// one row 11.9 / 11.7 / 11.7 / 12.4).
 int shrink_parts(int64_t rows, int64_t n, int rank, int count) {
-  const int64_t windows = ceil_div(rows, 16 * shrink_tiles(rows, rank));
-  // work groups that have something to do, as far as sizes tell
-  const int64_t work = rows < 2048 ? std::min<int64_t>(rows, windows * std::min(16, count)) : windows;
-  const int64_t want = ceil_div(rows < 2048 ? 256 : 512, work), room = ceil_div(n, 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, room, 16}));
+  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, 256);
+  // an adapter begins inside a window or at its end
+  const int64_t want = rows < kFew ? std::min<int64_t>(4, ceil_div(256, std::min(rows, windows + count - 1)))
+                                   : std::min<int64_t>(16, ceil_div(kManyGroups, ceil_div(rows, 64)));
+  return (int)std::max<int64_t>(1, std::min(want, room));
 }
 int64_t places_of(int64_t rows) { return up(rows, 64); }
 size_t h_bytes(int64_t rows, int64_t n, int rank, int count) {
   return up256((size_t)shrink_parts(rows, n, rank, count) * places_of(rows) * ranks_of(rank) * 4);
 }
 
-template <class T, int MT, int RT, bool WIDE>
-void shrink_as(const ShrinkArgs& a, int parts, int z, hipStream_t s) {
-  hipLaunchKernelGGL((k_shrink<T, MT, RT, WIDE>), dim3((unsigned)ceil_div(a.g.rows, 16 * MT), parts, z), dim3(256), 0, s, a);
-}
 template <class T>
-void shrink(const ShrinkArgs& a, bool wide, int parts, hipStream_t s) {
+void shrink(const ShrinkArgs& a, int parts, hipStream_t s) {
+  if (a.g.rows >= kFew && wide_rows(a.X, a.ldx, sizeof(T)) && wide_rows(a.W, a.ldw, sizeof(T)) && a.n % Mat<T>::E == 0 &&
+      a.n >= 128) {
+    const dim3 grid((unsigned)ceil_div(a.g.rows, 64), parts);
+    if (a.rank <= 16) hipLaunchKernelGGL((k_shrink_many<T, 1>), grid, dim3(256), 0, s, a);
+    else if (a.rank <= 32) hipLaunchKernelGGL((k_shrink_many<T, 2>), grid, dim3(256), 0, s, a);
+    else if (a.rank <= 64) hipLaunchKernelGGL((k_shrink_many<T, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_shrink_many<T, 8>), grid, dim3(256), 0, s, a);
+    return;
+  }
   const int tiles = shrink_tiles(a.g.rows, a.rank);
-  const int z = a.g.rows < 2048 ? std::min(16, a.g.count) : 1;
+  const dim3 grid((unsigned)ceil_div(a.g.rows, 16 * tiles), parts, a.g.rows < kFew ? std::min(16, a.g.count) : 1);
   auto of = [&](auto rt) {
     constexpr int RT = decltype(rt)::value;
-    constexpr int MT = RT == 1 ? 1 : 2;
-    if (tiles == 1) return wide ? shrink_as<T, 1, RT, true>(a, parts, z, s) : shrink_as<T, 1, RT, false>(a, parts, z, s);
-    return wide ? shrink_as<T, MT, RT, true>(a, parts, z, s) : shrink_as<T, MT, RT, false>(a, parts, z, s);
+    if (tiles == 1)
+      hipLaunchKernelGGL((k_shrink<T, 1, RT>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_shrink<T, 2, RT>), grid, dim3(256), 0, s, a);
   };
   if (a.rank <= 16) of(std::integral_constant<int, 1>());
   else if (a.rank <= 32) of(std::integral_constant<int, 2>());
@@ -848,19 +994,17 @@ void turn(const TurnArgs& a, int n, hipStream_t s) {
 }
 
 template <class T>
-void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
-  const bool few = a.g.rows < 2048;
+void expand(const ExpandArgs& a, hipStream_t s) {
+  const bool few = a.g.rows < kFew;
   auto of = [&](auto nk) {
-    constexpr int NK = decltype(nk)::value;
-    const unsigned cols = (unsigned)ceil_div(a.n, 256);
-    auto as = [&](auto win, auto w) {
-      constexpr int WIN = decltype(win)::value;
-      const dim3 grid((unsigned)ceil_div(a.g.rows, 16 * WIN), cols, few ? std::min(16, a.g.count + 1) : 1);
-      hipLaunchKernelGGL((k_expand<T, NK, WIN, decltype(w)::value>), grid, dim3(256), 0, s, a);
-    };
-    if (few) wide ? as(std::integral_constant<int, 1>(), std::true_type()) : as(std::integral_constant<int, 1>(), std::false_type());
-    else wide ? as(std::integral_constant<int, NK >= 2 ? 4 : 8>(), std::true_type())
-              : as(std::integral_constant<int, NK >= 2 ? 4 : 8>(), std::false_type());
+    // windows of 64 rows (4096 x 11008, rank 64, a call: 32 / 64 rows 95 / 83 us; 128 take too many registers)
+    constexpr int NK = decltype(nk)::value, WIN = 4;
+    const int64_t strips = ceil_div(a.n, 256);
+    if (few)
+      hipLaunchKernelGGL((k_expand<T, NK, 1>), dim3((unsigned)(ceil_div(a.g.rows, 16) * strips), 1, std::min(16, a.g.count + 1)),
+                         dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_expand<T, NK, WIN>), dim3((unsigned)(ceil_div(a.g.rows, 16 * WIN) * strips)), dim3(256), 0, s, a);
   };
   if constexpr (sizeof(T) == 4) {
     if (a.rank <= 16) of(std::integral_constant<int, 1>());
@@ -879,7 +1023,7 @@ void expand(const ExpandArgs& a, bool wide, hipStream_t s) {
 // returns how many are left. `out` may be h itself: an element's parts are one thread's.
 template <class T>
 int fold(const Groups& g, int rank, int parts, const float* h, float* out, hipStream_t s) {
-  if (parts == 1 || g.rows < 2048) return parts;
+  if (parts == 1 || g.rows < kFew) return parts;
   const FoldArgs f = {g, rank, ranks_of(rank), parts, h, places_of(g.rows), out, false};
   hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(g.rows * (int64_t)ranks_of(rank), 256)), dim3(256), 0, s, f);
   return 1;
@@ -899,24 +1043,19 @@ size_t outer_bytes(int64_t rows, int64_t n, int rank, int count) {
 template <class T>
 void outer(OuterArgs a, int n, hipStream_t s) {
   int64_t strips = 0, windows = 0, size = 0;
-  bool wide = true;
   for (int i = 0; i < n; ++i) {
     a.of[i].window = outer_window(a.g.rows, a.of[i].n, a.rank);
     strips = std::max(strips, ceil_div(a.of[i].n, 16 * Mat<T>::E));
     windows = std::max(windows, ceil_div(a.g.rows, a.of[i].window));
     size = std::max(size, (int64_t)a.of[i].n * a.rank);
-    wide = wide && a.of[i].wide;
   }
   if (windows > 0) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
     const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)n);
-    auto as = [&](auto rt, auto w) {
-      hipLaunchKernelGGL((k_outer<T, decltype(rt)::value, decltype(w)::value>), grid, dim3(256), 0, s, a);
-    };
-    const std::integral_constant<int, 1> one;
-    const std::integral_constant<int, 2> two;
-    if (a.rank <= 16) wide ? as(one, std::true_type()) : as(one, std::false_type());
-    else wide ? as(two, std::true_type()) : as(two, std::false_type());
+    if (a.rank <= 16)
+      hipLaunchKernelGGL((k_outer<T, 1>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_outer<T, 2>), grid, dim3(256), 0, s, a);
   }
   hipLaunchKernelGGL(k_outer_join, dim3((unsigned)std::min<int64_t>(ceil_div(size, 1024), 256), a.g.count, n), dim3(256), 0, s, a);
 }
@@ -926,11 +1065,6 @@ bool bad_shape(int64_t M, int64_t N, int64_t K, int R, int count) {
   return M < 0 || M > top || N < 1 || N > top || K < 1 || K > top || R < 1 || R > kMaxRank || count < 1 || count > 4096;
 }
 Groups groups_of(const int32_t* g, int64_t M, int count) { return {g, g + M, g + 2 * M, (int)M, count}; }
-template <class T>
-bool wide_matrix(const void* p, int64_t ld, int64_t n) {
-  return wide_rows(p, ld, sizeof(T)) && n % Mat<T>::E == 0;
-}
-
 struct BackSpace {
   size_t h, p, at, bt, outer[2], all;
   int64_t ldat, ldbt;
@@ -1003,14 +1137,14 @@ gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count,
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
     const ShrinkArgs sh = {g, (int)K, R, ranks_of(R), X, ldx, A, lda, R * lda, nullptr, h, places_of(M)};
-    shrink<T>(sh, wide_matrix<T>(X, ldx, K) && wide_matrix<T>(A, lda, K), parts, s);
+    shrink<T>(sh, parts, s);
     if (H) {
       const FoldArgs f = {g, R, ranks_of(R), parts, h, places_of(M), H, true};
       hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * R, 256)), dim3(256), 0, s, f);
     }
     const int left = fold<T>(g, R, parts, h, h, s);
     const ExpandArgs e = {g, (int)N, R, ranks_of(R), left, h, places_of(M), scales, B, ldb, N * ldb, Y, ldy, O, ldo};
-    expand<T>(e, wide_matrix<T>(B, ldb, R), s);
+    expand<T>(e, s);
   });
   return launched("gptq2d_adapters");
 }
@@ -1058,7 +1192,6 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
   float *h = (float*)(ws + b.h), *pr = (float*)(ws + b.p);
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
-    const bool wide_g = wide_matrix<T>(G, ldg, N);
     const float* ph = h;
     if (dX || dA) {
       const Turn of_b = {(int)N, R, B, ldb, N * ldb, ws + b.bt, b.ldbt, R * b.ldbt};
@@ -1066,7 +1199,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
       turn<T>({g, {of_b, of_a}}, dX ? 2 : 1, s);
       const int parts = shrink_parts(M, N, R, count);
       const ShrinkArgs sh = {g, (int)N, R, ranks_of(R), G, ldg, ws + b.bt, b.ldbt, R * b.ldbt, scales, h, places_of(M)};
-      shrink<T>(sh, wide_g, parts, s);
+      shrink<T>(sh, parts, s);
       if (parts > 1) {
         const FoldArgs f = {g, R, ranks_of(R), parts, h, places_of(M), pr, false};
         hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(M * ranks_of(R), 256)), dim3(256), 0, s, f);
@@ -1075,14 +1208,14 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
     }
     OuterArgs o = {g, R, 1, {}};
     int n = 0;
-    if (dA) o.of[n++] = {(int)K, X, ldx, ph, ranks_of(R), false, wide_matrix<T>(X, ldx, K), nullptr, dA, true, 0,
+    if (dA) o.of[n++] = {(int)K, X, ldx, ph, ranks_of(R), false, nullptr, dA, true, 0,
                          (float*)(ws + b.outer[0])};
-    if (dB) o.of[n++] = {(int)N, G, ldg, H, R, true, wide_g, scales, dB, false, 0, (float*)(ws + b.outer[1])};
+    if (dB) o.of[n++] = {(int)N, G, ldg, H, R, true, scales, dB, false, 0, (float*)(ws + b.outer[1])};
     if (n > 0) outer<T>(o, n, s);
     if (dX) {
       const ExpandArgs e = {g, (int)K, R, ranks_of(R), 1, ph, places_of(M), nullptr, ws + b.at, b.ldat, K * b.ldat, D, ldd, dX,
                             lddx};
-      expand<T>(e, R % Mat<T>::E == 0, s);
+      expand<T>(e, s);
     }
   });
   return launched("gptq2d_adapters_backward");
