@@ -142,7 +142,7 @@ constexpr int kGroupThreads = 1024;
 constexpr int kGroupRows = 4;  // of a thread and turn
 // One work group for each adapter, and one for the rows that have none: how many rows lie
 // before the adapter's, and the places of its own, which come in the rows' order. Up to
-// 16384 rows are looked at once (8192 rows, 4 adapters: GROUPUS us; turn by turn 9.6, row by row 21).
+// 16384 rows are looked at once (8192 rows, 4 adapters: 6.7 us; turn by turn 9.6, row by row 21).
 template <int TURNS>
 __global__ __launch_bounds__(kGroupThreads) void k_group(GroupArgs g) {
   __shared__ int less16[16], count64[64];
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
 // between, BUFS - 1 of them ahead; a wave sums 16 rows. The pieces of a row are dealt out so that
 // the 16 rows that are read at once lie in different banks. (The rows' direct way to the
 // registers takes 64 bytes of each of 16 rows at a time, and has each wave load the weights anew:
-// 8192 x 4096, rank 16, 22.8 us there, SHRINK16 here; 4096 x 4096, rank 64, 21.9 and SHRINK64.)
+// 8192 x 4096, rank 16, 22.8 us there, 20.8 here; 4096 x 4096, rank 64, 21.9 and 16.4.)
 // For rows on 16-byte boundaries, of whole pieces.
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until N of the wave's loads are on their way
