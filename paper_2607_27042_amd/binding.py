@@ -8,9 +8,10 @@ missing library is an error, never a fallback.
 The functions named like the C entry points take and return the same things,
 with torch tensors in place of device pointers and Python ints in place of
 handles. ``Factors`` and ``round_matrix`` are conveniences built from them, and
-``Blocks``, ``Cache``, ``block_*``, ``tree_masks`` and ``token_logprobs*`` those of
-the eight-bit operators: they allocate outputs and workspaces as they go. Of these,
-``block_linear`` (for X) and ``token_logprobs`` (for the logits) take part in autograd.
+``Blocks``, ``Cache``, ``block_*``, ``adapter*``, ``tree_*``, ``cache_*``, ``pages_update``
+and ``token_logprobs*`` those of the operators around a rounded model: they allocate
+outputs and workspaces as they go. Of these, ``block_linear`` (for X), ``adapters`` (for X,
+A, B and Y) and ``token_logprobs`` (for the logits) take part in autograd.
 """
 from __future__ import annotations
 
@@ -1105,6 +1106,69 @@ def block_linear_backward(dY: torch.Tensor, X: torch.Tensor, WT: Blocks, pow2: b
     return dX, dW
 
 
+def adapter_groups(index: torch.Tensor, count: int, stream=None) -> torch.Tensor:
+    """The order of a batch's rows by adapter (index: int32, outside [0, count): none), which
+    all projections of the batch use."""
+    with _on(stream, index):
+        groups = torch.empty(gptq2d_adapter_groups_size(index.shape[0], count), dtype=torch.int32, device=index.device)
+        gptq2d_adapter_groups(index, count, groups)
+    return groups
+
+
+class _Adapters(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, A, B, Y, scales, groups):
+        (M, K), (count, N, R) = X.shape, B.shape
+        O = torch.empty((M, N), dtype=X.dtype, device=X.device)
+        H = torch.empty((M, R), dtype=torch.float32, device=X.device)
+        gptq2d_adapters(X, A, B, scales, groups, Y, O, H, _bytes(gptq2d_adapters_workspace_size(M, N, K, R, count)))
+        ctx.save_for_backward(X, A, B, scales, groups, H)
+        return O
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, G):
+        X, A, B, scales, groups, H = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        dX = dA = dB = None
+        if any(want[:3]):
+            dX, dA, dB = adapters_backward(G.contiguous(), X, A, B, groups, H, scales, wants=want[:3])
+        # (32-bit sums, rounded once to what they are the gradients of)
+        dA, dB = (None if d is None else d.to(t.dtype) for d, t in ((dA, A), (dB, B)))
+        return dX, dA, dB, G if want[3] else None, None, None
+
+
+def adapters(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, groups: torch.Tensor, Y=None, scales=None,
+             stream=None) -> torch.Tensor:
+    """Y + scales[a] (X A[a]^T) B[a]^T for the adapter a of each row (A: [count, R, K], B:
+    [count, N, R], scales: float32 [count], None: 1; Y None: zeros); groups as
+    adapter_groups gives it. X, A, B and Y get their gradients, scales none."""
+    (M, K), (count, N, R) = X.shape, B.shape
+    with _on(stream, X):
+        if torch.is_grad_enabled():
+            if scales is not None and scales.requires_grad:
+                raise ValueError("scales have no gradient here: they must not require one")
+            if any(t is not None and t.requires_grad for t in (X, A, B, Y)):
+                return _Adapters.apply(X, A, B, Y, scales, groups)
+        O = torch.empty((M, N), dtype=X.dtype, device=X.device)
+        gptq2d_adapters(X, A, B, scales, groups, Y, O, None, _bytes(gptq2d_adapters_workspace_size(M, N, K, R, count)))
+    return O
+
+
+def adapters_backward(G: torch.Tensor, X, A: torch.Tensor, B: torch.Tensor, groups: torch.Tensor, H, scales=None, D=None,
+                      wants=(True, True, True), stream=None):
+    """(dX, dA, dB) of adapters from G, the gradient of what it gave, with H = X A[a]^T as the
+    forward call gave it and D, which is added to dX; None where not wanted."""
+    M, (count, N, R), K = G.shape[0], B.shape, A.shape[2]
+    with _on(stream, G):
+        new = lambda want, shape, dtype: torch.empty(shape, dtype=dtype, device=G.device) if want else None
+        dX = new(wants[0], (M, K), G.dtype)
+        dA, dB = new(wants[1], (count, R, K), torch.float32), new(wants[2], (count, N, R), torch.float32)
+        gptq2d_adapters_backward(G, X if wants[1] else None, A, B, scales, groups, H if wants[2] else None, D, dX, dA, dB,
+                                 _bytes(gptq2d_adapters_backward_workspace_size(M, N, K, R, count)))
+    return dX, dA, dB
+
+
 class Cache:
     """A paged eight-bit cache of keys and values (code: torch.float8_e4m3fn or
     torch.int8). Pages are the caller's to hand out: table (int32, sequences x
@@ -1159,6 +1223,65 @@ def tree_masks(parents: torch.Tensor, stream=None) -> torch.Tensor:
         masks = torch.empty(parents.shape, dtype=torch.int64, device=parents.device)
         gptq2d_tree_masks(parents, masks)
     return masks
+
+
+class Verified(NamedTuple):
+    path: torch.Tensor
+    count: torch.Tensor
+    next: torch.Tensor
+    logprob: torch.Tensor
+
+
+def tree_verify(X: torch.Tensor, tokens: torch.Tensor, parents=None, drafts=None, scale: float = 1.0, uniform=None, D=None,
+                draft_lse=None, draft_scale: float = 1.0, stream=None) -> Verified:
+    """Which drafted tokens are kept, and the token after them (gptq2d_tree_verify); D without
+    draft_lse is scored first."""
+    with _on(stream, X):
+        if D is not None and draft_lse is None:
+            draft_lse = token_logprobs(D.detach(), None, draft_scale).lse
+        both, dev = tuple(tokens.shape), X.device
+        out = Verified(torch.empty(both, dtype=torch.int32, device=dev), torch.empty(both[0], dtype=torch.int32, device=dev),
+                       torch.empty(both[0], dtype=torch.int64, device=dev), torch.empty(both, dtype=torch.float32, device=dev))
+        gptq2d_tree_verify(X, tokens, parents, drafts, scale, uniform, D, draft_lse, draft_scale, *out,
+                           _bytes(gptq2d_tree_verify_workspace_size(*both, X.shape[1])))
+    return out
+
+
+def _tensors(caches):
+    return [c.tensors if isinstance(c, Cache) else c for c in caches]
+
+
+def cache_commit(caches, table: torch.Tensor, context: torch.Tensor, path: torch.Tensor, stream=None) -> None:
+    """In every layer's Cache, the tokens kept of each sequence's tree moved to where the next step
+    expects them: context[b] + path[b, i] to context[b] + i."""
+    with _on(stream, path):
+        gptq2d_cache_commit(_tensors(caches), table, context, path)
+
+
+def cache_copy(caches, copies: torch.Tensor, stream=None) -> None:
+    """In every layer's Cache, the copies of pages that pages_update asks for."""
+    with _on(stream, copies):
+        gptq2d_cache_copy(_tensors(caches), copies)
+
+
+class Pages(NamedTuple):
+    table: torch.Tensor
+    copies: torch.Tensor
+    left: torch.Tensor
+
+
+def pages_update(table: torch.Tensor, length: torch.Tensor, want: torch.Tensor, pages: int, page_size: int, source=None,
+                 held=None, stream=None) -> Pages:
+    """The page tables of sequences that go on (from those in source; None: from themselves), fork,
+    end (want 0) or begin, with room for want tokens; the copies for cache_copy; the free
+    pages left (below zero: lacking)."""
+    with _on(stream, table):
+        rows, dev = want.shape[0], table.device
+        out = Pages(torch.empty((rows, table.shape[1]), dtype=torch.int32, device=dev),
+                    torch.empty((rows, 3), dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.int32, device=dev))
+        gptq2d_pages_update(table, length, source, want, held, pages, page_size, *out,
+                            _bytes(gptq2d_pages_update_workspace_size(rows, pages)))
+    return out
 
 
 class Scores(NamedTuple):

@@ -1,0 +1,159 @@
+"""The operators of a serving step as they are used together: a shared eight-bit projection
+with the adapters of several requests, drafted trees attended and scored, verified,
+committed in every layer's cache, and the sequences forked."""
+import pytest
+import torch
+
+import serving
+from paper_2607_27042_amd import binding as g
+
+pytestmark = pytest.mark.gpu
+
+LAYERS, SEQS, WIDTH, WIDE, HEADS, KV, DIM, PAGE, VOCAB, COUNT = 2, 4, 7, 128, 4, 2, 32, 16, 501, 3
+
+
+class Model:
+    """A few layers of attention without anything else, rounded, with adapters at the queries."""
+
+    def __init__(self, seed=0):
+        r = torch.Generator(device="cuda")
+        r.manual_seed(seed)
+        self.r = r
+        randn = lambda *s: torch.randn(*s, generator=r, device="cuda")
+        self.embed = randn(VOCAB, WIDE).to(torch.bfloat16)
+        mat = lambda n, k: g.block_quantize(randn(n, k) / k ** 0.5)
+        self.q = [mat(HEADS * DIM, WIDE) for _ in range(LAYERS)]
+        self.k = [mat(KV * DIM, WIDE) for _ in range(LAYERS)]
+        self.v = [mat(KV * DIM, WIDE) for _ in range(LAYERS)]
+        self.o = [mat(WIDE, HEADS * DIM) for _ in range(LAYERS)]
+        self.head = mat(VOCAB, WIDE)
+        self.A = (randn(COUNT, 8, WIDE) / WIDE ** 0.5).to(torch.bfloat16)
+        self.B = randn(COUNT, HEADS * DIM, 8).to(torch.bfloat16)
+
+    def step(self, caches, table, context, words, index, masks, drafts=None):
+        """Logits of words (seqs x t, behind context tokens each), whose keys and values are cached."""
+        t = words.shape[1]
+        groups = g.adapter_groups(index.repeat_interleave(t), COUNT)
+        h = self.embed[words.flatten()]
+        for i, cache in enumerate(caches):
+            q = g.adapters(h, self.A, self.B, groups, g.block_linear(h, self.q[i]))
+            cache.append(g.block_linear(h, self.k[i]), g.block_linear(h, self.v[i]), cache.slots(table, context, t))
+            attended, _ = cache.attend(q, table, context, masks, drafts)
+            h = h + g.block_linear(attended, self.o[i])
+        return g.block_linear(h, self.head)
+
+
+def tokens_of(caches, table, length):
+    """The keys and values of a sequence's first tokens, layer by layer."""
+    out = []
+    for cache in caches:
+        out += cache.read(cache.slots(table.view(1, -1), torch.zeros(1, dtype=torch.int32, device="cuda"), length))
+    return out
+
+
+def test_serving_steps():
+    m = Model()
+    r, ints = m.r, lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    pages = 40
+    caches = [g.Cache(pages, KV, PAGE, DIM) for _ in range(LAYERS)]
+    held = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    held[0] = 1
+    index = ints([0, 2, -1, 1])
+    # prompts of several lengths, in pages that an update hands out
+    prompt = [21, 16, 33, 5]
+    table = torch.full((SEQS, 6), -1, dtype=torch.int32, device="cuda")
+    none = ints([0] * SEQS)
+    state = g.pages_update(table, none, ints([p + WIDTH for p in prompt]), pages, PAGE, held=held)
+    assert int(state.left) == pages - 1 - sum(-(-(p + WIDTH) // PAGE) for p in prompt)
+    table, context = state.table, ints(prompt)
+    words = [torch.randint(VOCAB, (p,), generator=r, device="cuda") for p in prompt]
+    for b in range(SEQS):  # one prompt after the other, in trees of chains
+        for i in range(0, prompt[b], 8):
+            some = words[b][i:i + 8].view(1, -1)
+            m.step(caches, table[b:b + 1], ints([i]), some, index[b:b + 1], None)
+    text = [w.tolist() for w in words]
+    last = torch.randint(VOCAB, (SEQS,), generator=r, device="cuda")  # decided, not yet cached
+    parents = ints([[-1, 0, 0, 1, 1, 2, 3]] * SEQS)
+    masks = g.tree_masks(parents)
+    for step in range(4):
+        drafts = ints([WIDTH, WIDTH - 2, WIDTH, 1 + step])
+        tree = torch.randint(VOCAB, (SEQS, WIDTH), generator=r, device="cuda")
+        tree[:, 0] = last
+        X = m.step(caches, table, context, tree, index, masks, drafts)
+        # the likeliest after token 0 and after token 1, so that some are kept
+        tree[:, 1] = X.view(SEQS, WIDTH, VOCAB)[:, 0].argmax(1)
+        X = m.step(caches, table, context, tree, index, masks, drafts)
+        tree[:, 4] = X.view(SEQS, WIDTH, VOCAB)[:, 1].argmax(1)
+        X = m.step(caches, table, context, tree, index, masks, drafts)
+        uniform = 0.2 * torch.rand(SEQS, WIDTH, generator=r, device="cuda") if step % 2 else None
+        kept = g.tree_verify(X, tree, parents, drafts, 2.0, uniform)
+        ref = serving.verify(X, tree, parents, drafts, 2.0, uniform)
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(kept[:3], ref[:3]))
+        before = [tokens_of(caches, table[b], int(context[b]) + WIDTH) for b in range(SEQS)]
+        g.cache_commit(caches, table, context, kept.path)
+        old = context
+        context = context + kept.count
+        for b in range(SEQS):
+            n, path = int(old[b]), [int(p) for p in kept.path[b] if p >= 0]
+            at = list(range(n)) + [n + p for p in path]
+            for a, e in zip(tokens_of(caches, table[b], len(at)), before[b]):
+                assert torch.equal(a, e[at])
+            text[b] += [int(tree[b, p]) for p in path]
+        last = kept.next
+        # every sequence goes on; in the last step two go on from the first, one ends and begins anew
+        source = ints([0, 0, 2, -1]) if step == 2 else ints([0, 1, 2, 3])
+        want = torch.where(source >= 0, context[source.clamp(min=0).long()] + WIDTH, WIDTH)
+        if step == 2:
+            want[2] = 0
+        new = g.pages_update(table, context, want, pages, PAGE, source=source, held=held)
+        assert int(new.left) >= 0
+        ref = serving.pages_update(table.tolist(), context.tolist(), source.tolist(), want.tolist(), held.tolist(), pages, PAGE)
+        assert (new.table.tolist(), new.copies.tolist(), int(new.left)) == ref
+        old = [tokens_of(caches, table[max(s, 0)], int(context[max(s, 0)])) for s in source.tolist()]
+        g.cache_copy(caches, new.copies)
+        table = new.table
+        if step == 2:
+            context = torch.where(source >= 0, context[source.clamp(min=0).long()], 0)
+            context[2] = 0
+            text = [list(text[0]), list(text[0]), [], []]
+            last = last[source.clamp(min=0).long()]
+            index = index[source.clamp(min=0).long()]
+        for b in range(SEQS):
+            n = int(context[b])
+            if n:
+                assert all(torch.equal(a, e[:n]) for a, e in zip(tokens_of(caches, table[b], n), old[b]))
+        if step == 2:  # the third has no pages: begin it, too
+            new = g.pages_update(table, context, ints([int(w) + WIDTH for w in context]), pages, PAGE, held=held)
+            assert new.copies.tolist() == [[-1, -1, 0]] * SEQS
+            table = new.table
+    # what the caches hold at the end is what a cache holds that was given each text at once
+    for b in range(SEQS):
+        n = int(context[b])
+        assert n == len(text[b])
+    fresh = [g.Cache(pages, KV, PAGE, DIM) for _ in range(LAYERS)]
+    t = torch.arange(6, dtype=torch.int32, device="cuda").view(1, -1)
+    h = m.embed[torch.tensor(text[0], device="cuda")]
+    fresh[0].append(g.block_linear(h, m.k[0]), g.block_linear(h, m.v[0]), fresh[0].slots(t, ints([0]), len(text[0])))
+    for a, e in zip(tokens_of(caches[:1], table[0], len(text[0])), tokens_of(fresh[:1], t[0], len(text[0]))):
+        # (products of other numbers of rows run on other routes, whose sums differ by their last places; a code is a sixteenth)
+        assert bool(((a - e).abs() <= 2.0 ** -3 * e.abs() + 2.0 ** -3).all())
+
+
+def test_conveniences():
+    """Allocating forms give what the entry points give; a draft's own scores are made on the way."""
+    r = torch.Generator(device="cuda")
+    r.manual_seed(1)
+    X, D = (torch.randn(10, 100, generator=r, device="cuda") for _ in range(2))
+    tokens = torch.randint(100, (2, 5), generator=r, device="cuda")
+    u = torch.rand(2, 5, generator=r, device="cuda")
+    got = g.tree_verify(X, tokens, uniform=u, D=D, draft_scale=0.7)
+    lse = g.token_logprobs(D, scale=0.7).lse
+    ref = serving.verify(X, tokens, None, None, 1.0, u, D, lse, 0.7)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(got[:3], ref[:3]))
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    again = g.tree_verify(X, tokens, uniform=u, D=D, draft_scale=0.7, stream=stream)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    with pytest.raises(ValueError, match="one shape"):
+        g.cache_copy([g.Cache(4, 1, 16, 16), g.Cache(5, 1, 16, 16)], torch.zeros(1, 3, dtype=torch.int32, device="cuda"))
