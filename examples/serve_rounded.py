@@ -15,6 +15,12 @@ by the library and served in eight bits.
      (gptq2d_tree_attention), and every product with a rounded matrix is
      gptq2d_block_linear.
   5. Score the drafted tokens, beside the same layer unrounded.
+  6. Verify the tree (gptq2d_tree_verify), move the kept tokens' keys and values up
+     (gptq2d_cache_commit), and go on with two continuations, which share the pages that are
+     full and have a copy each of the last one (gptq2d_pages_update, gptq2d_cache_copy).
+  7. Give back some of what rounding took: low-rank adapters of two requests beside the
+     rounded head (gptq2d_adapters), fitted to its calibration targets through
+     gptq2d_adapters_backward.
 
     python examples/serve_rounded.py [--width 256] [--vocab 1000] [--prompt 300]
 """
@@ -91,6 +97,44 @@ def plain_attention(q, k, v, kv_heads, context, sees):
     return torch.einsum("htx,xhd->thd", p, v).reshape(t, -1)
 
 
+def decide(cache, table, prompt, words, parents, logits, gen, spare=4):
+    """The tree's kept tokens, committed in a copy of the cache (with pages to spare), and the
+    tables of two continuations of them."""
+    width, before = parents.shape[1], cache
+    cache = g.Cache(before.KC.shape[0] + spare, cache.heads, cache.page_size, cache.dim, cache.KC.dtype)
+    for new, old in zip(cache.tensors, before.tensors):
+        new.view(torch.uint8)[:old.shape[0]] = old.view(torch.uint8)
+    context = torch.tensor([prompt], dtype=torch.int32, device="cuda")
+    uniform = torch.rand(1, width, generator=gen, device="cuda")
+    kept = g.tree_verify(logits, words[prompt:].view(1, -1).long(), parents, uniform=uniform)
+    g.cache_commit([cache], table, context, kept.path)
+    length = context + kept.count
+    twice = torch.zeros(2, dtype=torch.int32, device="cuda")
+    pages = g.pages_update(table, length, (length + width).repeat(2), cache.KC.shape[0], cache.page_size, source=twice)
+    g.cache_copy([cache], pages.copies)
+    return kept, pages, length, cache
+
+
+def tune(head, h, target, index, count=2, rank=8, steps=4, rate=0.5):
+    """Adapters beside a rounded head, by gradient steps on the targets' log probabilities;
+    index: the adapter (the request's) of every row. Their gradients of the last step come back too."""
+    N, K = head.blocks.codes.shape
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    A = (torch.randn(count, rank, K, generator=gen, device="cuda") / K ** 0.5).to(h.dtype).requires_grad_()
+    B = torch.zeros(count, N, rank, dtype=h.dtype, device="cuda", requires_grad=True)
+    groups = g.adapter_groups(index, count)
+    with torch.no_grad():
+        Y = head(h)
+    for _ in range(steps):
+        loss = -g.token_logprobs(g.adapters(h, A, B, groups, Y), target).logprob.mean()
+        grads = torch.autograd.grad(loss, (A, B))
+        with torch.no_grad():
+            for t, d in zip((A, B), grads):
+                t -= rate * d
+    return A.detach(), B.detach(), groups, grads
+
+
 def run(width=256, heads=8, kv_heads=2, vocab=1000, prompt=300, page_size=64, seed=0, dtype=torch.bfloat16):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
@@ -132,7 +176,14 @@ def run(width=256, heads=8, kv_heads=2, vocab=1000, prompt=300, page_size=64, se
     a = plain_attention(he[prompt:] @ w["q"].T, he @ w["k"].T, he @ w["v"].T, kv_heads, prompt, sees)
     ref = (he[prompt:] + a @ w["o"].T) @ w["head"].T
     exact = torch.log_softmax(ref, 1).gather(1, child.unsqueeze(1))[:, 0]
-    return {"served": served, "unrounded": exact, "logits": out, "reference": ref, "rounded": rounded,
+    kept, pages, length, later = decide(cache, table, prompt, words, parents, out, gen)
+    head_in = seen["head"][0].to(dtype)
+    index = (torch.arange(head_in.shape[0], device="cuda") * 2 // head_in.shape[0]).to(torch.int32)
+    A, B, groups, grads = tune(rounded["head"], head_in, target.flatten(), index)
+    tuned = g.adapters(head_in, A, B, groups, rounded["head"](head_in))
+    return {"kept": kept, "pages": pages, "length": length, "later": later, "adapters": (A, B, groups, index, grads), "tuned": tuned,
+            "head_in": head_in, "words": words, "parents": parents, "target": target,
+            "served": served, "unrounded": exact, "logits": out, "reference": ref, "rounded": rounded,
             "weights": weights, "cache": cache, "k": k, "v": v, "table": table, "prompt": prompt}
 
 
@@ -150,6 +201,13 @@ def main():
     for a, b, e, t in zip(r["served"].logprob.tolist(), r["unrounded"].tolist(), r["served"].entropy.tolist(),
                           r["served"].ids.tolist()):
         print(f"  {a:9.4f} / {b:9.4f}   entropy {e:.3f}   most likely {t}")
+    kept = r["kept"]
+    print(f"kept {int(kept.count)} of the tree's tokens (places {kept.path[0, :int(kept.count)].tolist()}), then token "
+          f"{int(kept.next)}; pages of two continuations {r['pages'].table.tolist()}, {int(r['pages'].left)} left")
+    target = r["target"].flatten()
+    plain = g.token_logprobs(r["rounded"]["head"](r["head_in"]), target).logprob.mean()
+    print(f"calibration targets: mean log probability {float(plain):.4f} of the rounded head, "
+          f"{float(g.token_logprobs(r['tuned'], target).logprob.mean()):.4f} with its adapters")
 
 
 if __name__ == "__main__":
