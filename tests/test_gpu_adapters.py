@@ -164,6 +164,16 @@ def test_many_rows(M, N, K, R, count, dtype):
     Problem(M, N, K, R, count, dtype, seed=M + R, index=index).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K,R,count", [(2, 2688, 384, 4, 1), (70, 1408, 632, 1, 12), (20, 300, 200, 2, 3), (33, 130, 70, 7, 2),
+                                           (40, 5, 300, 16, 2), (40, 300, 3, 16, 2), (9, 7, 6, 5, 2), (50, 260, 9, 9, 3),
+                                           (2100, 136, 200, 3, 4), (2100, 300, 5, 16, 2), (2100, 6, 256, 40, 2),
+                                           (2100, 264, 260, 65, 2)])
+def test_short_sides(M, N, K, R, count, dtype):
+    """Sides shorter than the pieces that rows are read in, and ends inside them."""
+    Problem(M, N, K, R, count, dtype, seed=N + R).check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [1, 8, 10])
 def test_views(dtype, pad):
