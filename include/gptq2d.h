@@ -337,7 +337,7 @@ gptq2d_status gptq2d_block_linear_backward(int64_t M, int64_t N, int64_t K, gptq
  * row is row a R) and B (count x N rows of R, row stride ldb), scales (device, 32 bits,
  * count; NULL: 1). Row m of a batch has the adapter index[m]; a number outside [0, count)
  * means none. A smaller rank is one with rows of A, or columns of B, of zeros. M, N, K
- * <= 2^22 (M may be 0), R <= 128, count <= 4096.
+ * <= 2^22 (M may be 0), M N and M K <= 2^37, R <= 128, count <= 4096.
  * ------------------------------------------------------------------------- */
 
 /* int32 numbers that gptq2d_adapter_groups writes for M rows: 2 M + count + 2 (0 on

@@ -699,8 +699,8 @@ struct Outer {
 };
 struct OuterArgs {
   Groups g;
-  int rank, ranks;  // rank, work groups of it
-  Outer of[2];      // those that are asked for
+  int rank, ranks, deal;  // rank, work groups of it, and those that share a window's adapters
+  Outer of[2];            // those that are asked for
 };
 
 // A work group takes some columns, 16 RT ranks and a window of places, whose steps its
@@ -710,7 +710,8 @@ struct OuterArgs {
 // part, at the number of the window and the adapter together (which grows along the
 // order, so that no two are alike).
 template <class T, int RT, bool SHORT>
-__device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, int strip, int window, int rank0, float* red) {
+__device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, int strip, int window, int rank0, int share,
+                                           float* red) {
   typedef Mat<T> M;
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2;
@@ -728,6 +729,11 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     if (ad >= a.g.count) break;
     const int from = max(a.g.start[ad], begin), to = min(a.g.start[ad + 1], end);
     if (to <= i0) break;  // (groups that are not this batch's)
+    if (share-- != 0) {
+      i0 = to;
+      continue;
+    }
+    share = a.deal - 1;
     const float f = o.scales ? o.scales[ad] : 1.0f;
     // place of a lane's row e in the step from s on
     auto place = [&](int s, int e) { return kNarrow ? s + 8 * q + e : s + 4 * e + q; };
@@ -857,7 +863,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
           *(f4*)(red + ((w * RT + j) * 16 + m) * PITCH + C * (4 * q + i) + c) = v;
         }
     __syncthreads();
-    const bool whole = a.g.start[ad] >= begin && a.g.start[ad + 1] <= end;
+    const bool whole = a.g.rows <= o.window || (a.g.start[ad] >= begin && a.g.start[ad + 1] <= end);
     float* to_out = whole ? o.out + (int64_t)ad * o.n * a.rank : o.parts + (int64_t)(window + ad) * o.n * a.rank;
     for (int e = t; e < 16 * RT * COLS; e += 256) {
       const int r = o.across ? e / COLS : e % (16 * RT), c = o.across ? e % COLS : e / (16 * RT);
@@ -873,11 +879,12 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
 template <class T, int RT, bool SHORT>
 __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
-  const Outer o = a.of[blockIdx.z];
+  const int which = blockIdx.z / (uint32_t)a.deal;
+  const Outer o = a.of[which];
   // every eighth work group runs on the same die: the ranks of a strip follow one another there
   const int k = blockIdx.x >> 3, strip = k / a.ranks * 8 + (blockIdx.x & 7);
   if (strip * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
-  outer_tile<T, RT, SHORT>(a, o, strip, blockIdx.y, k % a.ranks, red);
+  outer_tile<T, RT, SHORT>(a, o, strip, blockIdx.y, k % a.ranks, blockIdx.z - which * a.deal, red);
 }
 
 // The parts' sums, and zeros for adapters without rows.
@@ -885,7 +892,7 @@ __global__ __launch_bounds__(256) void k_outer_join(OuterArgs a) {
   const Outer o = a.of[blockIdx.z];
   const int ad = blockIdx.y;
   const int64_t size = (int64_t)o.n * a.rank;
-  const int from = a.g.start[ad], to = min(a.g.start[ad + 1], a.g.rows);
+  const int from = max(a.g.start[ad], 0), to = min(a.g.start[ad + 1], a.g.rows);
   const int w0 = from / o.window, w1 = to > from ? (to - 1) / o.window : w0;
   if (to > from && w0 == w1) return;  // (it is there already)
   float* out = o.out + ad * size;
@@ -953,16 +960,17 @@ int shrink_tiles(int64_t rows, int rank) { return rows < kFew || rank <= 16 ? 1 
 // Parts of the inner side, which fill the device. Few rows: four at most, which what reads h
 // sums (64 rows of 4096, 48 adapters of rank 16, a call: 2 / 4 / 8 / 16 parts 16.0 / 14.9 / 15.7 / 17.8 us,
 // one row 11.9 / 11.7 / 11.7 / 12.4).
-int shrink_parts(int64_t rows, int64_t n, int rank, int count) {
-  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, 256);
+// `apart`: their sums take a launch of their own, which a short side does without.
+int shrink_parts(int64_t rows, int64_t n, int rank, int count, bool apart) {
+  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, apart && rows < kFew ? 1024 : 256);
   // an adapter begins inside a window or at its end
   const int64_t want = rows < kFew ? std::min<int64_t>(4, ceil_div(256, std::min(rows, windows + count - 1)))
                                    : std::min<int64_t>(16, ceil_div(kManyGroups, ceil_div(rows, 64)));
   return (int)std::max<int64_t>(1, std::min(want, room));
 }
 int64_t places_of(int64_t rows) { return up(rows, 64); }
-size_t h_bytes(int64_t rows, int64_t n, int rank, int count) {
-  return up256((size_t)shrink_parts(rows, n, rank, count) * places_of(rows) * ranks_of(rank) * 4);
+size_t h_bytes(int64_t rows, int64_t n, int rank, int count, bool apart) {
+  return up256((size_t)shrink_parts(rows, n, rank, count, apart) * places_of(rows) * ranks_of(rank) * 4);
 }
 
 template <class T>
@@ -1071,7 +1079,10 @@ void outer(OuterArgs a, int n, hipStream_t s) {
   }
   if (windows > 0) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
-    const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)n);
+    // few work groups: a window's adapters at the same time
+    const int64_t groups = up(strips, 8) * a.ranks * windows * n;
+    a.deal = (int)std::max<int64_t>(1, std::min<int64_t>({a.g.count, 8, 1024 / groups}));
+    const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)(n * a.deal));
     auto as = [&](auto rt, auto brief) {
       hipLaunchKernelGGL((k_outer<T, decltype(rt)::value, decltype(brief)::value>), grid, dim3(256), 0, s, a);
     };
@@ -1084,8 +1095,9 @@ void outer(OuterArgs a, int n, hipStream_t s) {
 }
 
 bool bad_shape(int64_t M, int64_t N, int64_t K, int R, int count) {
-  const int64_t top = (int64_t)1 << 22;
-  return M < 0 || M > top || N < 1 || N > top || K < 1 || K > top || R < 1 || R > kMaxRank || count < 1 || count > 4096;
+  const int64_t top = (int64_t)1 << 22, all = (int64_t)1 << 37;  // (work groups of 64 rows and 256 columns: 2^32 work items at most)
+  return M < 0 || M > top || N < 1 || N > top || K < 1 || K > top || M * N > all || M * K > all || R < 1 || R > kMaxRank ||
+         count < 1 || count > 4096;
 }
 Groups groups_of(const int32_t* g, int64_t M, int count) { return {g, g + M, g + 2 * M, (int)M, count}; }
 struct BackSpace {
@@ -1096,7 +1108,7 @@ BackSpace back_space(int64_t M, int64_t N, int64_t K, int R, int count) {
   BackSpace b;
   b.ldat = up(R, 8), b.ldbt = up(N, 8);
   b.h = 0;
-  b.p = b.h + h_bytes(M, N, R, count);
+  b.p = b.h + h_bytes(M, N, R, count, true);
   b.at = b.p + up256((size_t)places_of(M) * ranks_of(R) * 4);
   b.bt = b.at + up256((size_t)count * K * b.ldat * 4);
   b.outer[0] = b.bt + up256((size_t)count * R * b.ldbt * 4);
@@ -1134,14 +1146,14 @@ gptq2d_status gptq2d_adapter_groups(int64_t M, int count, const int32_t* index, 
 
 size_t gptq2d_adapters_workspace_size(int64_t M, int64_t N, int64_t K, int R, int count) {
   if (bad_shape(M, N, K, R, count) || M == 0) return 0;
-  return h_bytes(M, K, R, count);
+  return h_bytes(M, K, R, count, false);
 }
 
 gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count, gptq2d_dtype dt, const void* X, int64_t ldx,
                               const void* A, int64_t lda, const void* B, int64_t ldb, const float* scales,
                               const int32_t* groups, const void* Y, int64_t ldy, void* O, int64_t ldo, float* H,
                               void* workspace, size_t ws_bytes, void* stream) {
-  if (bad_shape(M, N, K, R, count)) return refuse("M, N and K must lie in [1, 2^22] (M may be 0), R in [1, 128], count in [1, 4096]");
+  if (bad_shape(M, N, K, R, count)) return refuse("M, N and K must lie in [1, 2^22] (M may be 0), M N and M K in [0, 2^37], R in [1, 128], count in [1, 4096]");
   if (!narrow_dtype(dt)) return refuse("bad dtype");
   if (M == 0) return GPTQ2D_OK;
   if (!X || !A || !B || !groups || !O) return refuse("X, A, B, groups or O is NULL");
@@ -1150,12 +1162,12 @@ gptq2d_status gptq2d_adapters(int64_t M, int64_t N, int64_t K, int R, int count,
   if (!aligned(X, es) || !aligned(A, es) || !aligned(B, es) || !aligned(Y, es) || !aligned(O, es) || !aligned(scales, 4) ||
       !aligned(groups, 4) || !aligned(H, 4))
     return refuse("an argument is not aligned to its elements");
-  const size_t need = h_bytes(M, K, R, count);
+  const size_t need = h_bytes(M, K, R, count, false);
   if (!workspace || ws_bytes < need) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace missing or too small");
   if (!aligned(workspace, 256)) return refuse(GPTQ2D_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   const hipStream_t s = (hipStream_t)stream;
   const Groups g = groups_of(groups, M, count);
-  const int parts = shrink_parts(M, K, R, count);
+  const int parts = shrink_parts(M, K, R, count, false);
   float* h = (float*)workspace;
   with_type(dt, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
@@ -1182,12 +1194,12 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
                                        int64_t ldb, const float* scales, const int32_t* groups, const float* H, const void* D,
                                        int64_t ldd, void* dX, int64_t lddx, float* dA, float* dB, void* workspace,
                                        size_t ws_bytes, void* stream) {
-  if (bad_shape(M, N, K, R, count)) return refuse("M, N and K must lie in [1, 2^22] (M may be 0), R in [1, 128], count in [1, 4096]");
+  if (bad_shape(M, N, K, R, count)) return refuse("M, N and K must lie in [1, 2^22] (M may be 0), M N and M K in [0, 2^37], R in [1, 128], count in [1, 4096]");
   if (!narrow_dtype(dt)) return refuse("bad dtype");
   if (!dX && !dA && !dB) return refuse("no gradient is asked for");
   if (!groups) return refuse("groups is NULL");
   if (M == 0) {  // nothing but zeros
-    OuterArgs o = {groups_of(groups, 0, count), R, 1, {}};
+    OuterArgs o = {groups_of(groups, 0, count), R, 1, 1, {}};
     int n = 0;
     if (dA) o.of[n].n = (int)K, o.of[n++].out = dA;
     if (dB) o.of[n].n = (int)N, o.of[n++].out = dB;
@@ -1220,7 +1232,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
       const Turn of_b = {(int)N, R, B, ldb, N * ldb, ws + b.bt, b.ldbt, R * b.ldbt};
       const Turn of_a = {R, (int)K, A, lda, R * lda, ws + b.at, b.ldat, K * b.ldat};
       turn<T>({g, {of_b, of_a}}, dX ? 2 : 1, s);
-      const int parts = shrink_parts(M, N, R, count);
+      const int parts = shrink_parts(M, N, R, count, true);
       const ShrinkArgs sh = {g, (int)N, R, ranks_of(R), G, ldg, ws + b.bt, b.ldbt, R * b.ldbt, scales, h, places_of(M)};
       shrink<T>(sh, parts, s);
       if (parts > 1) {
@@ -1229,7 +1241,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
         ph = pr;
       }
     }
-    OuterArgs o = {g, R, 1, {}};
+    OuterArgs o = {g, R, 1, 1, {}};
     int n = 0;
     if (dA) o.of[n++] = {(int)K, X, ldx, ph, ranks_of(R), false, nullptr, dA, true, 0,
                          (float*)(ws + b.outer[0])};

@@ -215,3 +215,15 @@ def test_adapter_weights():
         binding._adapter_weights(torch.zeros(3, 4, 8)[::2], torch.zeros(2, 8, 4), None)
     with pytest.raises(ValueError, match="device tensor"):
         binding._adapter_weights(torch.zeros(2, 4, 8), torch.zeros(2, 8, 4), None)
+
+
+def test_adapter_sizes(lib):
+    """Batches whose work groups would be too many are refused, and have no workspace."""
+    args = lambda M, N, K: (M, N, K, 4, 2, binding.BF16, P, K, P, K, P, 4, NULL, P, NULL, N, P, N, NULL, P, 1 << 60, None)
+    back = lambda M, N, K: (M, N, K, 4, 2, binding.BF16, P, N, P, K, P, K, P, 4, NULL, P, P, NULL, K, P, K, P, P, P, 1 << 60, None)
+    for M, N, K in ((1 << 20, 1 << 18, 8), (1 << 20, 8, 1 << 18), (1 << 22, 8, (1 << 15) + 1)):
+        refused(lib.gptq2d_adapters(*args(M, N, K)), "2^37")
+        refused(lib.gptq2d_adapters_backward(*back(M, N, K)), "2^37")
+        assert lib.gptq2d_adapters_workspace_size(M, N, K, 4, 2) == 0
+        assert lib.gptq2d_adapters_backward_workspace_size(M, N, K, 4, 2) == 0
+    assert lib.gptq2d_adapters_workspace_size(1 << 22, 8, 1 << 15, 4, 2) > 0
