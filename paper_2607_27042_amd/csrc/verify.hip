@@ -215,21 +215,21 @@ __device__ __forceinline__ void load_some(const T* x, int first, int n, float v[
       if (first + i >= 0 && first + i < n) v[i] = (float)((const G2D_GLOBAL T*)x)[first + i];
   }
 }
-// kTurn steps of kFew elements from e on, a group's steps behind one another
-template <class T>
+// STEPS steps of kFew elements from e on, a group's steps behind one another
+template <class T, int STEPS = kTurn>
 struct Turn {
-  float z[kTurn][kFew];
+  float z[STEPS][kFew];
   __device__ __forceinline__ void load(const T* x, int e, int n) {
     typedef Raw<T, kFew> R;
-    if (R::fits(x, e, n) && R::fits(x, e + (kTurn - 1) * kFewChunk, n)) {
-      R r[kTurn];
+    if (R::fits(x, e, n) && R::fits(x, e + (STEPS - 1) * kFewChunk, n)) {
+      R r[STEPS];
 #pragma unroll
-      for (int k = 0; k < kTurn; ++k) r[k].load(x + e + k * kFewChunk);
+      for (int k = 0; k < STEPS; ++k) r[k].load(x + e + k * kFewChunk);
 #pragma unroll
-      for (int k = 0; k < kTurn; ++k) r[k].values(z[k]);
+      for (int k = 0; k < STEPS; ++k) r[k].values(z[k]);
     } else {
 #pragma unroll
-      for (int k = 0; k < kTurn; ++k) load_some<kFew>(x, e + k * kFewChunk, n, z[k]);
+      for (int k = 0; k < STEPS; ++k) load_some<kFew>(x, e + k * kFewChunk, n, z[k]);
     }
   }
 };
@@ -530,11 +530,13 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   }
 }
 
-// The next token of a sequence: its part of the row, then its place there.
-template <class T>
+// The next token of a sequence: its part of the row, then its place there, STEPS steps at
+// once: a part of 4096 waits once for memory and for the other waves' sums (64 rows of 128000
+// 7.6 us, step by step 10.0; parts of one step 4.2 us, as four 6.8).
+template <class T, int STEPS>
 __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
-  __shared__ double sums[kThreads / 64];
+  __shared__ double sums[STEPS][kThreads / 64];
   __shared__ int found[kThreads / 64];
   __shared__ Powers powers;
   const int64_t seq = blockIdx.x;
@@ -582,47 +584,54 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
     double past = 0.0;
     int late = -1, pick = -1;  // the last token with something left, the one looked for
 #pragma unroll 1
-    for (int step = begin; step < end; step += kFewChunk) {
-      const int e = step + t * kFew;
-      float z[kFew];
-      double r[kFew], mine = 0.0;
-      load_some<kFew>(x, e, v.vocab, z);
+    for (int step = begin; step < end; step += STEPS * kFewChunk) {
+      Turn<T, STEPS> turn, other;
+      turn.load(x, step + t * kFew, end);
+      if (drawn) other.load(d, step + t * kFew, end);
+      double r[STEPS][kFew], before_in[STEPS];
 #pragma unroll
-      for (int i = 0; i < kFew; ++i) r[i] = v.p2(powers, z[i], pm);
-      if (drawn) {
-        float y[kFew];
-        load_some<kFew>(d, e, v.vocab, y);
+      for (int k = 0; k < STEPS; ++k) {
+        const int e = step + k * kFewChunk + t * kFew;
+        double mine = 0.0;
 #pragma unroll
-        for (int i = 0; i < kFew; ++i) r[i] = fmax(fma(r[i], by, -s.beta * v.q2(powers, y[i], lse)), 0.0);
-      } else if (s.residual) {
-        without(gone, e, r);
+        for (int i = 0; i < kFew; ++i) r[k][i] = v.p2(powers, turn.z[k][i], pm);
+        if (drawn) {
+#pragma unroll
+          for (int i = 0; i < kFew; ++i) r[k][i] = fmax(fma(r[k][i], by, -s.beta * v.q2(powers, other.z[k][i], lse)), 0.0);
+        } else if (s.residual) {
+          without(gone, e, r[k]);
+        }
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) {
+          r[k][i] *= pf;
+          mine += r[k][i];
+          if (r[k][i] > 0.0) late = e + i;
+        }
+        const double in = sum_upto(mine);
+        before_in[k] = in - mine;
+        if (lane == 63) sums[k][w] = in;
       }
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kFew; ++i) {
-        r[i] *= pf;
-        mine += r[i];
-        if (r[i] > 0.0) late = e + i;
-      }
-      const double in = sum_upto(mine);
-      __syncthreads();
-      if (lane == 63) sums[w] = in;
-      __syncthreads();
-      double sum = past + (in - mine);
-      for (int k = 0; k < w; ++k) sum += sums[k];
+      for (int k = 0; k < STEPS; ++k) {
+        double sum = past + before_in[k];
+        for (int i = 0; i < kThreads / 64; ++i) {
+          const double all = sums[k][i];
+          if (i < w) sum += all;
+          past += all;
+        }
 #pragma unroll
-      for (int i = 0; i < kFew; ++i) {
-        sum += r[i];
-        if (pick < 0 && r[i] > 0.0 && sum > aim_in) pick = e + i;
+        for (int i = 0; i < kFew; ++i) {
+          sum += r[k][i];
+          if (pick < 0 && r[k][i] > 0.0 && sum > aim_in) pick = step + k * kFewChunk + t * kFew + i;
+        }
       }
-      // the first thread that has one
-      const uint64_t has = __ballot(pick >= 0);
-      const int one = has != 0 ? __builtin_amdgcn_readlane(pick, __builtin_ctzll(has)) : -1;
-      if (lane == 0) found[w] = one;
+      // the lowest (of none: -1, as a number without sign the largest)
+      pick = (int)~group_max<64>(~(uint32_t)pick);
+      if (lane == 0) found[w] = pick;
       __syncthreads();
-      pick = -1;
-      for (int k = kThreads / 64 - 1; k >= 0; --k) pick = found[k] >= 0 ? found[k] : pick;
+      for (int k = 0; k < kThreads / 64; ++k) pick = (int)min((uint32_t)pick, (uint32_t)found[k]);
       if (pick >= 0) break;
-      for (int k = 0; k < kThreads / 64; ++k) past += sums[k];
     }
     if (pick < 0) {  // the sums' last place: the last one
 #pragma unroll
@@ -713,7 +722,10 @@ gptq2d_status gptq2d_tree_verify(int64_t seqs, int width, int64_t vocab, gptq2d_
     if (width > 1) hipLaunchKernelGGL(k_rows<T>, dim3((unsigned)(seqs * width * v.parts)), dim3(kThreads), 0, s, v);
     hipLaunchKernelGGL(k_walk<T>, dim3((unsigned)seqs), dim3(kWalk), 0, s, v);
     hipLaunchKernelGGL(k_last<T>, dim3((unsigned)(seqs * v.chunks)), dim3(kThreads), 0, s, v);
-    hipLaunchKernelGGL(k_next<T>, dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
+    if (per == kFewChunk)
+      hipLaunchKernelGGL((k_next<T, 1>), dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
+    else
+      hipLaunchKernelGGL((k_next<T, kTurn>), dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
   });
   return launched("gptq2d_tree_verify");
 }
