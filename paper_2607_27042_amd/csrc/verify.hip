@@ -449,8 +449,8 @@ __device__ __forceinline__ void without(const Gone& g, int e, double f[kFew]) {
 #pragma unroll
     for (int i = 0; i < kFew; ++i) f[i] = e + i == g.token[k] ? 0.0 : f[i];
 }
-// Sums of one part of the last row.
-template <class T>
+// Sums of one part of the last row, STEPS steps at once.
+template <class T, int STEPS>
 __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   __shared__ Gone gone;
   __shared__ float tops[kThreads / 64];
@@ -468,18 +468,18 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   const bool drawn = s.residual && v.D;
   find_gone(v, s, seq, begin, end, gone);
   powers.fill();
-  const bool once = v.per <= kTurn * kFewChunk;  // all of the part in registers
-  Turn<T> turn, other;
+  const bool once = v.per <= STEPS * kFewChunk;  // all of the part in registers
+  Turn<T, STEPS> turn, other;
   if (once) turn.load(x, begin + t * kFew, end);
   if (once && drawn) other.load(d, begin + t * kFew, end);
   float top = -INFINITY;
   int at = 0x7fffffff;
   bool bad = false;
   if (!drawn) {
-    for (int e = begin + t * kFew; e < end; e += kTurn * kFewChunk) {
+    for (int e = begin + t * kFew; e < end; e += STEPS * kFewChunk) {
       if (e > begin + t * kFew || !once) turn.load(x, e, end);
 #pragma unroll
-      for (int k = 0; k < kTurn; ++k)
+      for (int k = 0; k < STEPS; ++k)
 #pragma unroll
         for (int i = 0; i < kFew; ++i)
           if (turn.z[k][i] > top) top = turn.z[k][i], at = e + k * kFewChunk + i;
@@ -496,11 +496,11 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   const bool some = s.residual && !v.D && gone.n > 0;
   const double by = drawn ? 1.0 / s.sum : 0.0, lse = drawn ? (double)v.dlse[row] : 0.0;
   Residue r{};
-  for (int e0 = begin + t * kFew; e0 < end; e0 += kTurn * kFewChunk) {
+  for (int e0 = begin + t * kFew; e0 < end; e0 += STEPS * kFewChunk) {
     if (!once) turn.load(x, e0, end);
     if (drawn && !once) other.load(d, e0, end);
 #pragma unroll
-    for (int k = 0; k < kTurn; ++k) {
+    for (int k = 0; k < STEPS; ++k) {
       if (e0 - t * kFew + k * kFewChunk >= end) break;
       double f[kFew];
 #pragma unroll
@@ -721,11 +721,13 @@ gptq2d_status gptq2d_tree_verify(int64_t seqs, int width, int64_t vocab, gptq2d_
     using T = std::remove_pointer_t<decltype(p)>;
     if (width > 1) hipLaunchKernelGGL(k_rows<T>, dim3((unsigned)(seqs * width * v.parts)), dim3(kThreads), 0, s, v);
     hipLaunchKernelGGL(k_walk<T>, dim3((unsigned)seqs), dim3(kWalk), 0, s, v);
-    hipLaunchKernelGGL(k_last<T>, dim3((unsigned)(seqs * v.chunks)), dim3(kThreads), 0, s, v);
-    if (per == kFewChunk)
-      hipLaunchKernelGGL((k_next<T, 1>), dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
-    else
-      hipLaunchKernelGGL((k_next<T, kTurn>), dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
+    auto end = [&](auto steps) {
+      constexpr int STEPS = decltype(steps)::value;
+      hipLaunchKernelGGL((k_last<T, STEPS>), dim3((unsigned)(seqs * v.chunks)), dim3(kThreads), 0, s, v);
+      hipLaunchKernelGGL((k_next<T, STEPS>), dim3((unsigned)seqs), dim3(kThreads), 0, s, v);
+    };
+    if (per == kFewChunk) end(std::integral_constant<int, 1>());
+    else end(std::integral_constant<int, kTurn>());
   });
   return launched("gptq2d_tree_verify");
 }
