@@ -40,17 +40,19 @@ constexpr int kMaxParts = 64;            // of a row
 constexpr float kLog2E = 1.44269504088896341f;
 constexpr double kLog2E64 = 1.4426950408889634;
 
-// 2^t to about 1e-13 of itself for t in [-1000, 1000], 0 below (NaN: any number), from a table
-// of 2^(k / 256). t is split at the nearest multiple of 1 / 256, which adding 1.5 2^44
+// 2^t to about 1e-13 of itself for t in [-1000, 1000], 0 far below (and for NaN), from a
+// table of 2^(k / 256). t is split at the nearest multiple of 1 / 256, which adding 1.5 2^44
 // leaves in the low bits; the rest, |f| <= 1 / 512, needs four terms of its series. The 64-bit
 // terms of the last rows are most of what their pass costs: 64 rows of 128000 with as many
-// of the drafts 20 us, 22 with a polynomial of degree 8 on |f| <= 1 / 2 and no table.
+// of the drafts 18.6 us; with a comparison in place of the lower bound and the exponent's
+// own instruction 20.5, with a polynomial of degree 8 on |f| <= 1 / 2 and no table 22.
 struct Powers {
   double at[256];
   __device__ __forceinline__ void fill() {  // by the first 256 threads; a barrier follows
     if (threadIdx.x < 256) at[threadIdx.x] = exp2((double)threadIdx.x * 0x1p-8);
   }
   __device__ __forceinline__ double of(double t) const {
+    t = fmax(t, -5000.0);
     const double big = t + 0x1.8p44, f = t - (big - 0x1.8p44);
     const uint32_t k = __builtin_bit_cast(u2, big)[0];
     double p = 0.05550410866482158;
@@ -58,9 +60,7 @@ struct Powers {
     p = fma(p, f, 0.6931471805599453);
     p *= f;
     const double e = at[k & 255];
-    u2 b = __builtin_bit_cast(u2, fma(e, p, e));
-    b[1] += (uint32_t)((int32_t)k >> 8) << 20;
-    return t < -1000.0 ? 0.0 : __builtin_bit_cast(double, b);
+    return __builtin_amdgcn_ldexp(fma(e, p, e), (int32_t)k >> 8);
   }
 };
 
@@ -159,8 +159,10 @@ struct Residue {
   __device__ __forceinline__ void add(double f, double by, double bq) {
     const bool in = f * by > bq;
     all += f;
-    over += in ? f : 0.0;
-    less += in ? bq : 0.0;
+    if (in) {  // (a branch: choosing the terms takes four instructions more than it does)
+      over += f, less += bq;
+      asm volatile("" : "+v"(over));
+    }
   }
 };
 
@@ -532,7 +534,7 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
 
 // The next token of a sequence: its part of the row, then its place there, STEPS steps at
 // once: a part of 4096 waits once for memory and for the other waves' sums (64 rows of 128000
-// 7.6 us, step by step 10.0; parts of one step 4.2 us, as four 6.8).
+// 7.4 us, step by step 10.0; parts of one step 4.1 us, as four 6.8).
 template <class T, int STEPS>
 __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
