@@ -700,6 +700,7 @@ struct Outer {
 struct OuterArgs {
   Groups g;
   int rank, ranks, deal;  // rank, work groups of it, and those that share a window's adapters
+  bool alone;             // one window, few adapters: nothing to join
   Outer of[2];            // those that are asked for
 };
 
@@ -884,6 +885,20 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   // every eighth work group runs on the same die: the ranks of a strip follow one another there
   const int k = blockIdx.x >> 3, strip = k / a.ranks * 8 + (blockIdx.x & 7);
   if (strip * 16 * Mat<T>::E >= o.n || (int)blockIdx.y * o.window >= a.g.rows) return;
+  if (a.alone) {
+    // zeros for adapters without rows
+    constexpr int COLS = 16 * Mat<T>::E;
+    const int lane = threadIdx.x & 63, ad = min(lane, a.g.count - 1), c0 = strip * COLS, r0 = k % a.ranks * 16 * RT;
+    uint64_t none = __ballot(lane < a.g.count && lane % a.deal == (int)blockIdx.z - which * a.deal &&
+                             a.g.start[ad] >= a.g.start[ad + 1]);
+    for (; none != 0; none &= none - 1) {
+      float* out = o.out + (int64_t)__builtin_ctzll(none) * o.n * a.rank;
+      for (int e = threadIdx.x; e < 16 * RT * COLS; e += 256) {
+        const int r = o.across ? e / COLS : e % (16 * RT), c = o.across ? e % COLS : e / (16 * RT);
+        if (r0 + r < a.rank && c0 + c < o.n) out[o.across ? (int64_t)(r0 + r) * o.n + c0 + c : (int64_t)(c0 + c) * a.rank + r0 + r] = 0.0f;
+      }
+    }
+  }
   outer_tile<T, RT, SHORT>(a, o, strip, blockIdx.y, k % a.ranks, blockIdx.z - which * a.deal, red);
 }
 
@@ -1056,8 +1071,10 @@ int fold(const Groups& g, int rank, int parts, const float* h, float* out, hipSt
 }
 
 // places of a window: as many windows as fill the device with strips of 128 columns, of 256
-// places at least (two steps of each wave): fewer windows are fewer sums to join
+// places at least (two steps of each wave): fewer windows are fewer sums to join, and of a single one
+// (up to 512 places) there is nothing to join
 int outer_window(int64_t rows, int64_t n, int rank) {
+  if (rows <= 512) return 512;
   const int64_t groups = 2 * ceil_div(n, 128) * (rank <= 16 ? 1 : ceil_div(rank, 32));
   return (int)std::max<int64_t>(256, up(ceil_div(rows, std::max<int64_t>(1, ceil_div(768, groups))), 128));
 }
@@ -1081,6 +1098,7 @@ void outer(OuterArgs a, int n, hipStream_t s) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
     // few work groups: a window's adapters at the same time
     const int64_t groups = up(strips, 8) * a.ranks * windows * n;
+    a.alone = windows == 1 && a.g.count <= 64;
     a.deal = (int)std::max<int64_t>(1, std::min<int64_t>({a.g.count, 8, 1024 / groups}));
     const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)(n * a.deal));
     auto as = [&](auto rt, auto brief) {
@@ -1091,7 +1109,8 @@ void outer(OuterArgs a, int n, hipStream_t s) {
     if (a.rank <= 16) brief ? as(one, std::true_type()) : as(one, std::false_type());
     else brief ? as(two, std::true_type()) : as(two, std::false_type());
   }
-  hipLaunchKernelGGL(k_outer_join, dim3((unsigned)std::min<int64_t>(ceil_div(size, 1024), 256), a.g.count, n), dim3(256), 0, s, a);
+  if (!a.alone)
+    hipLaunchKernelGGL(k_outer_join, dim3((unsigned)std::min<int64_t>(ceil_div(size, 1024), 256), a.g.count, n), dim3(256), 0, s, a);
 }
 
 bool bad_shape(int64_t M, int64_t N, int64_t K, int R, int count) {
@@ -1199,7 +1218,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
   if (!dX && !dA && !dB) return refuse("no gradient is asked for");
   if (!groups) return refuse("groups is NULL");
   if (M == 0) {  // nothing but zeros
-    OuterArgs o = {groups_of(groups, 0, count), R, 1, 1, {}};
+    OuterArgs o = {groups_of(groups, 0, count), R, 1, 1, false, {}};
     int n = 0;
     if (dA) o.of[n].n = (int)K, o.of[n++].out = dA;
     if (dB) o.of[n].n = (int)N, o.of[n++].out = dB;
@@ -1241,7 +1260,7 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
         ph = pr;
       }
     }
-    OuterArgs o = {g, R, 1, 1, {}};
+    OuterArgs o = {g, R, 1, 1, false, {}};
     int n = 0;
     if (dA) o.of[n++] = {(int)K, X, ldx, ph, ranks_of(R), false, nullptr, dA, true, 0,
                          (float*)(ws + b.outer[0])};
