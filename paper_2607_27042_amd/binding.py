@@ -1142,7 +1142,10 @@ def adapters(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, groups: torch.Te
              stream=None) -> torch.Tensor:
     """Y + scales[a] (X A[a]^T) B[a]^T for the adapter a of each row (A: [count, R, K], B:
     [count, N, R], scales: float32 [count], None: 1; Y None: zeros); groups as
-    adapter_groups gives it. X, A, B and Y get their gradients, scales none."""
+    adapter_groups gives it. X, A, B and Y get their gradients, scales none. Before a
+    backward pass is captured into a graph, let go of what was computed eagerly from the same
+    leaves: torch keeps a leaf's gradient on the stream of the first, and a capture may not
+    wait for that."""
     (M, K), (count, N, R) = X.shape, B.shape
     with _on(stream, X):
         if torch.is_grad_enabled():

@@ -281,7 +281,7 @@ __device__ __forceinline__ void scan_all(const UpdateArgs& a, const uint32_t* ma
 
 // All of it in one launch: every work group marks all pages and finds all free ones for
 // itself, in LDS, and writes its share of the rows. (Marks shared through memory have to be
-// cleared, made, and looked at by launches of their own: 256 rows of 130 entries over 9729
+// cleared, made, and looked at by launches of their own: 256 rows of 130 entries over 9281
 // pages 20 us in four launches, 15 here.)
 constexpr int kOnePages = 28672, kOneRows = 1024;
 struct Found {

@@ -174,6 +174,14 @@ def test_short_sides(M, N, K, R, count, dtype):
     Problem(M, N, K, R, count, dtype, seed=N + R).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K,R,count", [(30, 40, 24, 8, 64), (30, 40, 24, 8, 65), (512, 136, 260, 20, 64), (513, 136, 260, 20, 64),
+                                           (512, 300, 70, 33, 2), (300, 64, 1100, 16, 300), (1500, 1030, 64, 5, 9)])
+def test_adapters_of_a_window(M, N, K, R, count, dtype):
+    """Many adapters in a window, one window or several, adapters without rows."""
+    Problem(M, N, K, R, count, dtype, seed=M + count).check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [1, 8, 10])
 def test_views(dtype, pad):

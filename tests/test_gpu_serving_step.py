@@ -157,3 +157,60 @@ def test_conveniences():
     assert all(torch.equal(a, b) for a, b in zip(got, again))
     with pytest.raises(ValueError, match="one shape"):
         g.cache_copy([g.Cache(4, 1, 16, 16), g.Cache(5, 1, 16, 16)], torch.zeros(1, 3, dtype=torch.int32, device="cuda"))
+
+
+def test_two_graphs():
+    """The end of a step captured in two graphs that share a workspace, replayed one after the
+    other between eager work, against the same calls on copies."""
+    seqs, width, vocab, pages = 3, 6, 3001, 20
+    r = torch.Generator(device="cuda")
+    r.manual_seed(2)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    tensors = lambda c: [t.view(torch.uint8) if t.dtype != torch.float32 else t for x in c for t in x.tensors]
+    caches = [g.Cache(pages, KV, PAGE, DIM) for _ in range(LAYERS)]
+    X = torch.empty(seqs * width, vocab, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.empty(seqs, width, dtype=torch.int64, device="cuda")
+    u = torch.empty(seqs, width, device="cuda")
+    table, source = ints([[0, 1, 2, -1], [3, 4, 5, -1], [6, 7, 8, -1]]), ints([0, 0, 2])
+    context, want = ints([20, 9, 30]), ints([40, 40, 40])
+    path, count = ints([[0] * width] * seqs), ints([0] * seqs)
+    after = torch.empty(seqs, dtype=torch.int64, device="cuda")
+    logprob = torch.empty(seqs, width, device="cuda")
+    length, out, copies, left = torch.empty_like(context), torch.empty_like(table), ints([[0] * 3] * seqs), ints([0])
+    size = max(g.gptq2d_tree_verify_workspace_size(seqs, width, vocab), g.gptq2d_pages_update_workspace_size(seqs, pages))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    for t in (X, tokens, u):
+        t.zero_()
+    torch.cuda.synchronize()
+    decide, turn = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(decide):
+        g.gptq2d_tree_verify(X, tokens, None, None, 1.0, u, None, None, 1.0, path, count, after, logprob, ws)
+        g.gptq2d_cache_commit([c.tensors for c in caches], table, context, path)
+        torch.add(context, count, out=length)
+    with torch.cuda.graph(turn):
+        g.gptq2d_pages_update(table, length, source, want, None, pages, PAGE, out, copies, left, ws)
+        g.gptq2d_cache_copy([c.tensors for c in caches], copies)
+    for _ in range(4):
+        X.copy_(3 * torch.randn(X.shape, generator=r, device="cuda"))
+        tokens.copy_(X.view(seqs, width, vocab).argmax(2).roll(1, 1))
+        u.copy_(torch.rand(u.shape, generator=r, device="cuda"))
+        for t in tensors(caches):
+            t.copy_(torch.randint(0, 256, t.shape, generator=r, device="cuda"))
+        others = [g.Cache(pages, KV, PAGE, DIM) for _ in range(LAYERS)]
+        for a, b in zip(tensors(others), tensors(caches)):
+            a.copy_(b)
+        torch.cuda.synchronize()
+        decide.replay()
+        turn.replay()
+        kept = g.tree_verify(X, tokens, uniform=u)
+        g.cache_commit(others, table, context, kept.path)
+        new = g.pages_update(table, context + kept.count, want, pages, PAGE, source=source)
+        g.cache_copy(others, new.copies)
+        torch.cuda.synchronize()
+        ref = serving.verify(X, tokens, None, None, 1.0, u)
+        assert all(torch.equal(a.cpu(), b) for a, b in zip((path, count, after), ref[:3]))
+        assert all(torch.equal(a, b) for a, b in zip((path, count, after, logprob), kept))
+        assert torch.equal(out, new.table) and torch.equal(copies, new.copies) and int(left) == int(new.left)
+        ref = serving.pages_update(table.tolist(), length.tolist(), source.tolist(), want.tolist(), [0] * pages, pages, PAGE)
+        assert (out.tolist(), copies.tolist(), int(left)) == ref
+        assert all(torch.equal(a, b) for a, b in zip(tensors(caches), tensors(others)))

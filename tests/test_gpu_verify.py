@@ -105,6 +105,27 @@ def test_drawn_drafts(dtype, vocab, chain):
     assert int(got[1].max()) > 2  # something was kept
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mode", ["certain", "drawn", "greedy"])
+@pytest.mark.parametrize("seqs,width,vocab", [(3, 4, 70001), (2, 3, 128000), (2, 3, 250001), (2, 3, 300008), (600, 2, 6001)])
+def test_long_rows(dtype, mode, seqs, width, vocab):
+    """Parts of the last row of several steps: of fewer than a turn has, of as many, of more."""
+    r = gen(vocab + width)
+    X = logits(r, seqs * width, vocab, dtype)
+    if mode != "drawn":
+        tokens = likely(X, torch.zeros(seqs, width), tree(r, seqs, width), r)
+        check(X, tokens, None, None, 1.0, torch.rand(seqs, width, generator=r, device="cuda") if mode == "certain" else None)
+        return
+    D = (X.float() + torch.randn(X.shape, generator=r, device="cuda")).to(X.dtype)
+    lse = torch.logsumexp(D.double(), 1).float()
+    q = torch.softmax(D.float(), 1).view(seqs, width, vocab)[:, :-1].reshape(-1, vocab)
+    u = torch.rand(seqs, width, generator=r, device="cuda")
+    tokens = torch.randint(vocab, (seqs, width), generator=r, device="cuda")
+    cut = torch.rand(q.shape[0], 1, generator=r, device="cuda")
+    tokens[:, 1:] = torch.searchsorted(q.cumsum(1), cut).clamp(max=vocab - 1).view(seqs, -1)
+    check(X, tokens, None, None, 1.0, u, D, lse, 1.0)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [1, 9, 5000, 33333])
 def test_greedy(dtype, vocab):
