@@ -966,20 +966,28 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return ceil_div(v, m) * m; }
 
 int ranks_of(int rank) { return (int)up(rank, 16); }
-// Few rows: windows of 16 for whose adapters there is a work group each. Otherwise a work group
+// Sums over a long side of few rows: windows of 16 for whose adapters there are work groups each.
+// Of many rows, and of fewer along so long a side that what windows of 16 read of W is most
+// (1800 x 11008, rank 64, a call: 77 so, 62 as of many; 1200 x 4096, rank 16, 33 and 38), a work group
 // takes its window's adapters one after another.
 constexpr int kFew = 2048;
+bool many_rows(int64_t rows, int64_t n, int rank) { return rows >= kFew || (rows >= kFew / 2 && n * rank >= 3 << 17); }
 constexpr int kManyGroups = 256;  // work groups of many rows
+// Work groups for the adapters of a window of 16: as many as a window has on average and one (a
+// work group too many costs its launch: 1358 x 4224, 38 adapters, 27 us, with 16 for each 36).
+int adapter_groups(int64_t rows, int count) {
+  return (int)std::min<int64_t>({16, count, ceil_div(count, ceil_div(rows, 16)) + 1});
+}
 // Row tiles of a window: more rows read the weights more seldom.
-int shrink_tiles(int64_t rows, int rank) { return rows < kFew || rank <= 16 ? 1 : 2; }
+int shrink_tiles(int64_t rows, int64_t n, int rank) { return !many_rows(rows, n, rank) || rank <= 16 ? 1 : 2; }
 // Parts of the inner side, which fill the device. Few rows: four at most, which what reads h
 // sums (64 rows of 4096, 48 adapters of rank 16, a call: 2 / 4 / 8 / 16 parts 16.0 / 14.9 / 15.7 / 17.8 us,
 // one row 11.9 / 11.7 / 11.7 / 12.4).
 // `apart`: their sums take a launch of their own, which a short side does without.
 int shrink_parts(int64_t rows, int64_t n, int rank, int count, bool apart) {
-  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, apart && rows < kFew ? 1024 : 256);
+  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, apart && !many_rows(rows, n, rank) ? 1024 : 256);
   // an adapter begins inside a window or at its end
-  const int64_t want = rows < kFew ? std::min<int64_t>(4, ceil_div(256, std::min(rows, windows + count - 1)))
+  const int64_t want = !many_rows(rows, n, rank) ? std::min<int64_t>(4, ceil_div(256, std::min(rows, windows + count - 1)))
                                    : std::min<int64_t>(16, ceil_div(kManyGroups, ceil_div(rows, 64)));
   return (int)std::max<int64_t>(1, std::min(want, room));
 }
@@ -990,7 +998,8 @@ size_t h_bytes(int64_t rows, int64_t n, int rank, int count, bool apart) {
 
 template <class T>
 void shrink(const ShrinkArgs& a, int parts, hipStream_t s) {
-  if (a.g.rows >= kFew && wide_rows(a.X, a.ldx, sizeof(T)) && wide_rows(a.W, a.ldw, sizeof(T)) && a.n % Mat<T>::E == 0 &&
+  const bool many = many_rows(a.g.rows, a.n, a.rank);
+  if (many && wide_rows(a.X, a.ldx, sizeof(T)) && wide_rows(a.W, a.ldw, sizeof(T)) && a.n % Mat<T>::E == 0 &&
       a.n >= 128) {
     const dim3 grid((unsigned)ceil_div(a.g.rows, 64), parts);
     if (a.rank <= 16) hipLaunchKernelGGL((k_shrink_many<T, 1>), grid, dim3(256), 0, s, a);
@@ -1000,8 +1009,8 @@ void shrink(const ShrinkArgs& a, int parts, hipStream_t s) {
     return;
   }
   const bool brief = a.n < Mat<T>::E;
-  const int tiles = brief ? 1 : shrink_tiles(a.g.rows, a.rank);
-  const dim3 grid((unsigned)ceil_div(a.g.rows, 16 * tiles), parts, a.g.rows < kFew ? std::min(16, a.g.count) : 1);
+  const int tiles = brief ? 1 : shrink_tiles(a.g.rows, a.n, a.rank);
+  const dim3 grid((unsigned)ceil_div(a.g.rows, 16 * tiles), parts, many ? 1 : adapter_groups(a.g.rows, a.g.count));
   auto of = [&](auto rt) {
     constexpr int RT = decltype(rt)::value;
     if (brief)
@@ -1026,15 +1035,17 @@ void turn(const TurnArgs& a, int n, hipStream_t s) {
 
 template <class T>
 void expand(const ExpandArgs& a, hipStream_t s) {
-  const bool few = a.g.rows < kFew;
+  // Windows of 64 rows (4096 x 11008, rank 64, a call: 32 / 64 rows 95 / 83 us; 128 take too many registers),
+  // of 16 where that leaves the device without work (600 x 4096, rank 16, 22 us, of 64 28; 1200 x 11008 33 and 28;
+  // 1100 x 2048, rank 64, 32 and 36, but of rank 128 37 and 34: so many rows of W are better read for 64).
+  const bool few = ceil_div(a.g.rows, 64) * ceil_div(a.n, 256) < (a.rank > 64 ? 128 : 400);
   auto of = [&](auto nk) {
-    // windows of 64 rows (4096 x 11008, rank 64, a call: 32 / 64 rows 95 / 83 us; 128 take too many registers)
     constexpr int NK = decltype(nk)::value, WIN = 4;
     const int64_t strips = ceil_div(a.n, 256);
     auto as = [&](auto win, auto brief) {
       constexpr int W = decltype(win)::value;
       hipLaunchKernelGGL((k_expand<T, NK, W, decltype(brief)::value>),
-                         dim3((unsigned)(ceil_div(a.g.rows, 16 * W) * strips), 1, few ? std::min(16, a.g.count + 1) : 1), dim3(256),
+                         dim3((unsigned)(ceil_div(a.g.rows, 16 * W) * strips), 1, few ? adapter_groups(a.g.rows, a.g.count + 1) : 1), dim3(256),
                          0, s, a);
     };
     const std::integral_constant<int, 1> one;
@@ -1060,11 +1071,11 @@ void expand(const ExpandArgs& a, hipStream_t s) {
   }
 }
 
-// Sums parts of h where more than one work group would do it for itself again (many rows);
+// Sums parts of h where there are many, or many work groups would do it for themselves again;
 // returns how many are left. `out` may be h itself: an element's parts are one thread's.
 template <class T>
 int fold(const Groups& g, int rank, int parts, const float* h, float* out, hipStream_t s) {
-  if (parts == 1 || g.rows < kFew) return parts;
+  if (parts == 1 || (parts <= 4 && g.rows < kFew)) return parts;
   const FoldArgs f = {g, rank, ranks_of(rank), parts, h, places_of(g.rows), out, false};
   hipLaunchKernelGGL(k_fold, dim3((unsigned)ceil_div(g.rows * (int64_t)ranks_of(rank), 256)), dim3(256), 0, s, f);
   return 1;
