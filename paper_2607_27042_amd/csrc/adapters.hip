@@ -51,6 +51,20 @@ __device__ __forceinline__ f4 mma(f4 a, f4 b, f4 c) {
   return c;
 }
 
+// the same with the fragments of N tiles: the 32-bit steps of one would wait for one another
+template <int N, class F>
+__device__ __forceinline__ void mma_each(const F (&w)[N], F x, f4 (&acc)[N]) {
+  if constexpr (std::is_same<F, f4>::value) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[j][i], x[i], acc[j], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = mma(w[j], x, acc[j]);
+  }
+}
+
 // 16 bytes at any element (memory takes them off their boundary as well, in two lines)
 typedef u4 u4_near __attribute__((aligned(2)));
 
@@ -294,9 +308,10 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
           for (int j = 0; j < RT; ++j) end_row<SHORT>(w_[u][j], wr[j], k0 + q * M::E, a.n);
         }
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < RT; ++j) acc[i][j] = mma(w_[u][j], x_[u][i], acc[i][j]);
+        for (int i = 0; i < MT; ++i) {
+          F (&rows)[RT] = *(F(*)[RT])w_[u];
+          mma_each(rows, x_[u][i], acc[i]);
+        }
       }
     };
     // a turn's loads are on their way while the one before is summed
@@ -411,8 +426,7 @@ __global__ __launch_bounds__(256) void k_shrink_many(ShrinkArgs a) {
 #pragma unroll
           for (int j = 0; j < RT; ++j) fw[j] = F{};
         }
-#pragma unroll
-        for (int j = 0; j < RT; ++j) acc[j] = mma(fw[j], fx, acc[j]);
+        mma_each(fw, fx, acc);
       }
     }
     const float f = a.scales ? a.scales[ad] : 1.0f;
@@ -760,7 +774,8 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
       for (int j = 0; j < RT; ++j)
 #pragma unroll
         for (int e = 0; e < L; ++e)
-          x.h[j][e] = o.H[(o.by_row ? (int64_t)rows[e] : min(place(s, e), to - 1)) * o.ldh + min(r0 + 16 * j + m, a.rank - 1)];
+          x.h[j][e] = *(const float*)((const char*)o.H + ((uint32_t)(o.by_row ? rows[e] : min(place(s, e), to - 1)) * (uint32_t)o.ldh +
+                                                          (uint32_t)min(r0 + 16 * j + m, a.rank - 1)) * 4u);
     };
     f4 acc[C][RT] = {};
     auto sum = [&](int s, Step& x) {
@@ -877,8 +892,10 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     i0 = to;
   }
 }
+// (32 bits: registers for two waves of a SIMD, 4096 x 2048, rank 64, gradients 113 us, for one 129; three
+// 16-bit terms of 32 ranks do not fit them)
 template <class T, int RT, bool SHORT>
-__global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
+__global__ __launch_bounds__(256, (RT == 2 && sizeof(T) == 4 ? 2 : 1)) void k_outer(OuterArgs a) {
   __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
   const int which = blockIdx.z / (uint32_t)a.deal;
   const Outer o = a.of[which];
@@ -985,10 +1002,21 @@ int shrink_tiles(int64_t rows, int64_t n, int rank) { return !many_rows(rows, n,
 // one row 11.9 / 11.7 / 11.7 / 12.4).
 // `apart`: their sums take a launch of their own, which a short side does without.
 int shrink_parts(int64_t rows, int64_t n, int rank, int count, bool apart) {
-  const int64_t windows = ceil_div(rows, 16), room = ceil_div(n, apart && !many_rows(rows, n, rank) ? 1024 : 256);
+  const bool many = many_rows(rows, n, rank);
+  const int64_t room = ceil_div(n, apart && !many ? 1024 : 256);
+  if (many) {
+    // a work group has a compute unit for itself: rounds of them, each of its share of the side (in pieces
+    // of 64) and what it takes to begin (4787 rows of 4096, rank 128, 32 bits, a call: three parts 122 us,
+    // four, which begin a second round, 156; 5000 rows of 11008, rank 16, 16 bits 64 and 71)
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t p = 1; p <= std::min<int64_t>(16, room); ++p) {
+      const int64_t takes = ceil_div(ceil_div(rows, 64) * p, kManyGroups) * (ceil_div(n, 64 * p) + 6) + p;
+      if (takes < least) least = takes, best = p;
+    }
+    return (int)best;
+  }
   // an adapter begins inside a window or at its end
-  const int64_t want = !many_rows(rows, n, rank) ? std::min<int64_t>(4, ceil_div(256, std::min(rows, windows + count - 1)))
-                                   : std::min<int64_t>(16, ceil_div(kManyGroups, ceil_div(rows, 64)));
+  const int64_t want = std::min<int64_t>(4, ceil_div(256, std::min(rows, ceil_div(rows, 16) + count - 1)));
   return (int)std::max<int64_t>(1, std::min(want, room));
 }
 int64_t places_of(int64_t rows) { return up(rows, 64); }
