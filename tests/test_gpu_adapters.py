@@ -182,6 +182,23 @@ def test_adapters_of_a_window(M, N, K, R, count, dtype):
     Problem(M, N, K, R, count, dtype, seed=M + count).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K,R,count", [(1100, 40, 6200, 64, 3), (1030, 6200, 48, 20, 5), (300, 7100, 72, 100, 4), (1025, 6161, 6157, 65, 2),
+                                           (2500, 100, 8200, 16, 2)])
+def test_long_sides(M, N, K, R, count, dtype):
+    """Long sides of few rows, which are taken as of many, in both directions."""
+    Problem(M, N, K, R, count, dtype, seed=M + R).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1000, 2100])
+def test_crowded_window(M, dtype):
+    """Most rows have one adapter, a few windows many more than their share."""
+    index = torch.zeros(M, dtype=torch.int64, device="cuda")
+    index[-40:] = torch.arange(40, device="cuda") - 1
+    Problem(M, 300, 200, 16, 39, dtype, seed=M, index=index).check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [1, 8, 10])
 def test_views(dtype, pad):
