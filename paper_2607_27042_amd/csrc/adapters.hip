@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void k_shrink(ShrinkArgs a) {
 // between, BUFS - 1 of them ahead; a wave sums 16 rows. The pieces of a row are dealt out so that
 // the 16 rows that are read at once lie in different banks. (The rows' direct way to the
 // registers takes 64 bytes of each of 16 rows at a time, and has each wave load the weights anew:
-// 8192 x 4096, rank 16, 22.8 us there, 20.8 here; 4096 x 4096, rank 64, 21.9 and 16.4.)
+// 8192 x 4096, rank 16, 22.8 us there, 17.3 here; 4096 x 4096, rank 64, 21.9 and 15.7.)
 // For rows on 16-byte boundaries, of whole pieces.
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until N of the wave's loads are on their way
@@ -359,7 +359,9 @@ __device__ __forceinline__ void wait_loads() {  // until N of the wave's loads a
 }
 typedef __attribute__((address_space(3))) void lds_void;
 template <int RT>
-constexpr int shrink_bufs() { return RT == 1 ? 12 : RT == 2 ? 10 : RT == 4 ? 8 : 6; }
+constexpr int shrink_bufs() {  // two work groups' fit a compute unit (5756 x 2816, rank 64, 32 bits, a call: 77 us; one with twice the buffers 116)
+  return RT == 1 ? 7 : RT == 2 ? 6 : RT == 4 ? 4 : 3;
+}
 template <class T, int RT>
 __global__ __launch_bounds__(256) void k_shrink_many(ShrinkArgs a) {
   typedef Mat<T> M;
@@ -989,7 +991,7 @@ int ranks_of(int rank) { return (int)up(rank, 16); }
 // takes its window's adapters one after another.
 constexpr int kFew = 2048;
 bool many_rows(int64_t rows, int64_t n, int rank) { return rows >= kFew || (rows >= kFew / 2 && n * rank >= 3 << 17); }
-constexpr int kManyGroups = 256;  // work groups of many rows
+constexpr int kManyGroups = 512;  // work groups of many rows that run at once
 // Work groups for the adapters of a window of 16: as many as a window has on average and one (a
 // work group too many costs its launch: 1358 x 4224, 38 adapters, 27 us, with 16 for each 36).
 int adapter_groups(int64_t rows, int count) {
@@ -1005,9 +1007,9 @@ int shrink_parts(int64_t rows, int64_t n, int rank, int count, bool apart) {
   const bool many = many_rows(rows, n, rank);
   const int64_t room = ceil_div(n, apart && !many ? 1024 : 256);
   if (many) {
-    // a work group has a compute unit for itself: rounds of them, each of its share of the side (in pieces
-    // of 64) and what it takes to begin (4787 rows of 4096, rank 128, 32 bits, a call: three parts 122 us,
-    // four, which begin a second round, 156; 5000 rows of 11008, rank 16, 16 bits 64 and 71)
+    // rounds of the work groups that run at once, each of its share of the side (in pieces
+    // of 64) and what it takes to begin (4787 rows of 4096, rank 128, 32 bits, a call, with half as many at
+    // once: three parts 122 us, four, which begin a second round, 156)
     int64_t best = 1, least = INT64_MAX;
     for (int64_t p = 1; p <= std::min<int64_t>(16, room); ++p) {
       const int64_t takes = ceil_div(ceil_div(rows, 64) * p, kManyGroups) * (ceil_div(n, 64 * p) + 6) + p;
