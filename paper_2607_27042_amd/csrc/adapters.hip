@@ -492,7 +492,7 @@ struct ExpandArgs {
 // waves of a SIMD that an instance's registers are held down to
 template <class T, int NK>
 constexpr int expand_waves() {
-  return sizeof(T) == 2 ? (NK == 1 ? 3 : NK <= 2 ? 4 : 2) : NK == 1 ? 4 : NK == 2 ? 3 : NK == 4 ? 2 : 1;
+  return sizeof(T) == 2 ? (NK == 1 ? 3 : NK <= 2 ? 4 : 2) : NK == 1 ? 4 : NK == 2 ? 3 : 2;
 }
 template <class T, int NK, int WIN, bool SHORT>
 __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandArgs a) {
@@ -987,10 +987,10 @@ int64_t up(int64_t v, int64_t m) { return ceil_div(v, m) * m; }
 int ranks_of(int rank) { return (int)up(rank, 16); }
 // Sums over a long side of few rows: windows of 16 for whose adapters there are work groups each.
 // Of many rows, and of fewer along so long a side that what windows of 16 read of W is most
-// (1800 x 11008, rank 64, a call: 77 so, 62 as of many; 1200 x 4096, rank 16, 33 and 38), a work group
-// takes its window's adapters one after another.
+// (1500 x 11008, rank 16, a call: 35 us so, 30 as of many; 1100 x 4096, rank 64, 28.3 and 26.6, rank 32 19.5 and 22),
+// a work group takes its window's adapters one after another.
 constexpr int kFew = 2048;
-bool many_rows(int64_t rows, int64_t n, int rank) { return rows >= kFew || (rows >= kFew / 2 && n * rank >= 3 << 17); }
+bool many_rows(int64_t rows, int64_t n, int rank) { return rows >= kFew || (rows >= kFew / 2 && n * rank >= 5 << 15); }
 constexpr int kManyGroups = 512;  // work groups of many rows that run at once
 // Work groups for the adapters of a window of 16: as many as a window has on average and one (a
 // work group too many costs its launch: 1358 x 4224, 38 adapters, 27 us, with 16 for each 36).
@@ -1139,7 +1139,7 @@ void outer(OuterArgs a, int n, hipStream_t s) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
     // few work groups: a window's adapters at the same time
     const int64_t groups = up(strips, 8) * a.ranks * windows * n;
-    a.alone = windows == 1 && a.g.count <= 64;
+    a.alone = windows == 1 && a.g.count <= 8;
     a.deal = (int)std::max<int64_t>(1, std::min<int64_t>({a.g.count, 8, 1024 / groups}));
     const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)(n * a.deal));
     auto as = [&](auto rt, auto brief) {
