@@ -856,14 +856,13 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
       load(s0, x);
       find(s0 + 4 * STEP);
 #pragma unroll 1
-      for (int s = s0; s < to; s += 8 * STEP) {
+      for (int s = s0;;) {  // (x and y in turn, without copies: twice the code, which small calls wait for, and 80 registers more)
         if (s + 4 * STEP < to) load(s + 4 * STEP, y);
         find(s + 8 * STEP);
         sum(s, x);
-        if (s + 4 * STEP >= to) break;
-        if (s + 8 * STEP < to) load(s + 8 * STEP, x);
-        find(s + 12 * STEP);
-        sum(s + 4 * STEP, y);
+        s += 4 * STEP;
+        if (s >= to) break;
+        x = y;
       }
     }
     // lane: rank m of each tile, columns C (4 q + i) + c: to rows of ranks
@@ -894,10 +893,10 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     i0 = to;
   }
 }
-// (32 bits: registers for two waves of a SIMD, 4096 x 2048, rank 64, gradients 113 us, for one 129; three
-// 16-bit terms of 32 ranks do not fit them)
+// (registers for three waves of a SIMD, two for 32 ranks: 8192 x 4096, rank 16, gradients 101.0 us, with two
+// 102.6; 4096 x 2048, rank 64, 32 bits, 112, with one 129)
 template <class T, int RT, bool SHORT>
-__global__ __launch_bounds__(256, (RT == 2 && sizeof(T) == 4 ? 2 : 1)) void k_outer(OuterArgs a) {
+__global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void k_outer(OuterArgs a) {
   __shared__ float red[4 * RT * 16 * (16 * Mat<T>::E + 4)];
   const int which = blockIdx.z / (uint32_t)a.deal;
   const Outer o = a.of[which];
@@ -932,13 +931,13 @@ __global__ __launch_bounds__(256) void k_outer_join(OuterArgs a) {
   float* out = o.out + ad * size;
   const float* parts = o.parts + (int64_t)(w0 + ad) * size;
   if (size % 4 == 0) {  // (out is aligned to its elements, the parts to 16 bytes)
+    typedef f4 f4_near __attribute__((aligned(4)));
     for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < size; e += (int64_t)gridDim.x * 1024) {
       f4 s = {};
       if (to > from)
 #pragma unroll 4
         for (int w = 0; w <= w1 - w0; ++w) s += *(const f4*)(parts + w * size + e);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) out[e + i] = s[i];
+      *(f4_near*)(out + e) = s;
     }
     return;
   }
@@ -1138,8 +1137,8 @@ void outer(OuterArgs a, int n, hipStream_t s) {
   if (windows > 0) {
     a.ranks = a.rank <= 16 ? 1 : (int)ceil_div(a.rank, 32);
     // few work groups: a window's adapters at the same time
-    const int64_t groups = up(strips, 8) * a.ranks * windows * n;
-    a.alone = windows == 1 && a.g.count <= 8;
+    const int64_t groups = strips * a.ranks * windows * n;
+    a.alone = windows == 1 && a.g.count <= 64 && a.g.count * size <= 1 << 20;
     a.deal = (int)std::max<int64_t>(1, std::min<int64_t>({a.g.count, 8, 1024 / groups}));
     const dim3 grid((unsigned)(up(strips, 8) * a.ranks), (unsigned)windows, (unsigned)(n * a.deal));
     auto as = [&](auto rt, auto brief) {
