@@ -468,6 +468,7 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   const int lead = lead_of(x);
   const int begin = chunk * v.per - lead, end = min(begin + v.per, v.vocab);
   const bool drawn = s.residual && v.D;
+  const float ld = drawn ? v.dlse[row] : 0.0f;
   find_gone(v, s, seq, begin, end, gone);
   powers.fill();
   const bool once = v.per <= STEPS * kFewChunk;  // all of the part in registers
@@ -496,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
   // drawn drafts: the row's own largest, so that its terms can be told from q
   const double m = drawn ? s.m : top == -INFINITY ? 0.0 : (double)top;
   const bool some = s.residual && !v.D && gone.n > 0;
-  const double by = drawn ? 1.0 / s.sum : 0.0, lse = drawn ? (double)v.dlse[row] : 0.0;
+  const double by = drawn ? 1.0 / s.sum : 0.0, lse = (double)ld;
   Residue r{};
   for (int e0 = begin + t * kFew; e0 < end; e0 += STEPS * kFewChunk) {
     if (!once) turn.load(x, e0, end);
@@ -540,9 +541,14 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
   __shared__ double sums[STEPS][kThreads / 64];
   __shared__ int found[kThreads / 64];
+  __shared__ float logit;
   __shared__ Powers powers;
   const int64_t seq = blockIdx.x;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  // (parts of a sequence without a row are not what they were: they are not used)
+  Last l{-INFINITY, 0.0, 0.0, 0.0, 0x7fffffff, {}};
+  if (lane < v.chunks) l = v.last[seq * v.chunks + lane];
+  const float u32 = v.u ? v.u[seq * v.width] : 0.0f;
   State s = v.state[seq];
   if (s.node < 0) {
     if (t == 0) v.next[seq] = -1, v.logprob[seq * v.width] = 0.0f;
@@ -550,8 +556,6 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   }
   const int64_t row = seq * v.width + s.node;
   const T *x = (const T*)v.X + row * v.ldx, *d = (const T*)v.D + row * v.ldd;
-  Last l{-INFINITY, 0.0, 0.0, 0.0, 0x7fffffff, {}};
-  if (lane < v.chunks) l = v.last[seq * v.chunks + lane];
   bool drawn = s.residual && v.D;
   float best = (float)l.m;  // (they are 32-bit numbers)
   int at = l.at;
@@ -564,8 +568,9 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
     return;
   }
   int64_t chosen = at;
+  float value = best;  // its logit
   if (v.u) {
-    const double u = (double)v.u[seq * v.width];
+    const double u = (double)u32;
     double left = drawn ? fmax(l.left / total - l.less, 0.0) : l.left * f;
     if (s.residual && __ballot(left > 0.0) == 0) {  // nothing is left of p: p itself
       s.residual = 0, drawn = false;
@@ -579,10 +584,11 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
     const double pm = drawn ? s.m : at_lane(l.m, part), pf = at_lane(f, part);
     const int lead = lead_of(x);
     const int begin = part * v.per - lead, end = min(begin + v.per, v.vocab);
+    const double lse = drawn ? (double)v.dlse[row] : 0.0;
     find_gone(v, s, seq, begin, end, gone);
     powers.fill();
     __syncthreads();
-    const double lse = drawn ? (double)v.dlse[row] : 0.0, by = 1.0 / total, aim_in = aim - before;
+    const double by = 1.0 / total, aim_in = aim - before;
     double past = 0.0;
     int late = -1, pick = -1;  // the last token with something left, the one looked for
 #pragma unroll 1
@@ -633,8 +639,16 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
       if (lane == 0) found[w] = pick;
       __syncthreads();
       for (int k = 0; k < kThreads / 64; ++k) pick = (int)min((uint32_t)pick, (uint32_t)found[k]);
-      if (pick >= 0) break;
+      if (pick >= 0) {  // (the thread that has it has its logit)
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+          for (int i = 0; i < kFew; ++i)
+            if (step + k * kFewChunk + t * kFew + i == pick) logit = turn.z[k][i];
+        break;
+      }
     }
+    const bool known = pick >= 0;
     if (pick < 0) {  // the sums' last place: the last one
 #pragma unroll
       for (int k = 1; k < 64; k <<= 1) late = max(late, __shfl_xor(late, k));
@@ -643,12 +657,14 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
       __syncthreads();
       for (int k = 0; k < kThreads / 64; ++k) pick = max(pick, found[k]);
     }
+    __syncthreads();
     chosen = pick;
+    value = known ? logit : pick >= 0 ? (float)x[pick] : 0.0f;
   }
   if (t == 0) {
     v.next[seq] = chosen;
     v.logprob[seq * v.width] = chosen < 0 ? __uint_as_float(0x7fc00000u)
-                                          : (float)(((double)(float)x[chosen] - (double)best) * (double)v.a - log(total));
+                                          : (float)(((double)value - (double)best) * (double)v.a - log(total));
   }
 }
 
