@@ -535,7 +535,7 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
 
 // The next token of a sequence: its part of the row, then its place there, STEPS steps at
 // once: a part of 4096 waits once for memory and for the other waves' sums (64 rows of 128000
-// 7.4 us, step by step 10.0; parts of one step 4.1 us, as four 6.8).
+// 7.5 us, step by step 10.0; parts of one step 3.7 us, as four 6.8).
 template <class T, int STEPS>
 __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
