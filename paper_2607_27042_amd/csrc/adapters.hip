@@ -491,8 +491,8 @@ struct ExpandArgs {
   int64_t ldo;
 };
 
-// NK: steps of the inner side, of M::K each; 0: of 16-bit types one step that has both
-// halves of 16 h. A work group takes 16 WIN rows and 256 columns, a wave 64 of them. Four
+// NK: steps of the inner side, of M::K each; 0: of 16-bit types steps that have two of the
+// numbers that each of 16 h is the sum of. A work group takes 16 WIN rows and 256 columns, a wave 64 of them. Four
 // tiles' rows of W are dealt out so that a lane ends with 16 consecutive columns.
 // waves of a SIMD that an instance's registers are held down to
 template <class T, int NK>
@@ -504,7 +504,10 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
   typedef Mat<T> M;
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2, kPacked = kNarrow && NK == 0;
-  constexpr int S = kPacked ? 1 : NK, TERMS = kNarrow && !kPacked ? 2 : 1;
+  constexpr int S = kPacked ? 1 : NK;
+  // numbers that an h is the sum of (bf16: 24 bits in three, with two of which outputs were off by 2^-17 of
+  // their terms), and instructions of a step that these take
+  constexpr int NUMBERS = std::is_same<T, bf16>::value ? 3 : kNarrow ? 2 : 1, TERMS = kPacked ? (NUMBERS + 1) / 2 : NUMBERS;
   constexpr int ROWS = 16 * WIN, V = 16 * sizeof(T) / 16;  // rows; pieces of 16 bytes of a lane's columns
   // h of the window, as the instruction takes it: [term][step][row][4 pieces]
   __shared__ F hs[TERMS * S][ROWS * 4];
@@ -603,18 +606,21 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
         for (int e = 0; e < 4; ++e) v[e] = h[k][e];
         hs[k][i0 * 4 + p] = v;
       } else {
-        F hi, lo;
+        F v[NUMBERS + 1] = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float x = h[k][e];
-          hi[e] = (T)split(x, T());
-          lo[e] = (T)x;
+#pragma unroll
+          for (int u = 0; u < NUMBERS; ++u) v[u][e] = u + 1 < NUMBERS ? (T)split(x, T()) : (T)x;
         }
-        if constexpr (kPacked) {
-          hs[0][i0 * 4 + p] = p < 2 ? hi : lo;
-        } else {
-          hs[k][i0 * 4 + p] = hi;
-          hs[S + k][i0 * 4 + p] = lo;
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u) {
+          if constexpr (kPacked) {
+            const u4 first = __builtin_bit_cast(u4, v[2 * u]), second = __builtin_bit_cast(u4, v[2 * u + 1]);
+            hs[u * S + k][i0 * 4 + p] = __builtin_bit_cast(F, p < 2 ? first : second);
+          } else {
+            hs[u * S + k][i0 * 4 + p] = v[u];
+          }
         }
       }
     }
