@@ -11,8 +11,10 @@
 // few, one after another.
 //
 // Inner products of 16-bit inputs are summed by the 16-bit matrix instruction in 32
-// bits. h and p stay 32-bit: where the instruction takes them in, they are the sum of 16-bit
-// numbers, so that no rounding of theirs shows in a result.
+// bits. h and p stay 32-bit: where the instruction takes them in, each is the sum of three bf16
+// numbers, which hold its 24 bits whatever its size, and an f16 number beside it is the sum of
+// two, its 11 bits. (As halves of f16, relative to the largest h of a row or of an adapter's rows,
+// an h 2^-25 of that was nothing, and those in between lost bits to it.)
 #include <math.h>
 
 #include <algorithm>
@@ -103,17 +105,20 @@ __device__ __forceinline__ void end_row(typename Mat<T>::F& f, const T* row, int
   f = __builtin_bit_cast(typename Mat<T>::F, b);
 }
 
-// what of x (or, near the type's smallest number, of all that is summed with it) T holds
-// and what it does not; infinities leave nothing
-__device__ __forceinline__ float split(float& x, bf16) {
+// Takes the first eight bits of x off it: x becomes the rest; infinities leave nothing.
+__device__ __forceinline__ float split(float& x) {
   const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
   x = x == hi ? 0.0f : x - hi;
   return hi;
 }
-__device__ __forceinline__ float split(float& x, _Float16) {
-  const float hi = (float)(_Float16)x;
-  x = x == hi ? 0.0f : x - hi;
-  return hi;
+// eight f16 as the sums of two bf16 each
+__device__ __forceinline__ void split(h8 x, b8& hi, b8& lo) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float v = (float)x[e];
+    hi[e] = (bf16)split(v);
+    lo[e] = (bf16)v;
+  }
 }
 
 // over a wave, in every lane, without LDS
@@ -497,7 +502,7 @@ struct ExpandArgs {
 // waves of a SIMD that an instance's registers are held down to
 template <class T, int NK>
 constexpr int expand_waves() {
-  return sizeof(T) == 2 ? (NK == 1 ? 3 : NK <= 2 ? 4 : 2) : NK == 1 ? 4 : NK == 2 ? 3 : 2;
+  return std::is_same<T, _Float16>::value ? (NK <= 1 ? 3 : 2) : sizeof(T) == 2 ? (NK == 1 ? 3 : NK <= 2 ? 4 : 2) : NK == 1 ? 4 : NK == 2 ? 3 : 2;
 }
 template <class T, int NK, int WIN, bool SHORT>
 __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandArgs a) {
@@ -505,12 +510,14 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2, kPacked = kNarrow && NK == 0;
   constexpr int S = kPacked ? 1 : NK;
-  // numbers that an h is the sum of (bf16: 24 bits in three, with two of which outputs were off by 2^-17 of
-  // their terms), and instructions of a step that these take
-  constexpr int NUMBERS = std::is_same<T, bf16>::value ? 3 : kNarrow ? 2 : 1, TERMS = kPacked ? (NUMBERS + 1) / 2 : NUMBERS;
+  // what the instruction multiplies; the numbers that an h and an f16 of W are the sums of. Of a
+  // packed step bf16 has two of an h's three in one instruction, f16 both of W's
+  typedef typename std::conditional<kNarrow, b8, F>::type P;
+  constexpr bool kHalves = std::is_same<T, _Float16>::value;
+  constexpr int NUMBERS = kNarrow ? 3 : 1, TERMS = kPacked && !kHalves ? 2 : NUMBERS, OF_W = kHalves && !kPacked ? 2 : 1;
   constexpr int ROWS = 16 * WIN, V = 16 * sizeof(T) / 16;  // rows; pieces of 16 bytes of a lane's columns
   // h of the window, as the instruction takes it: [term][step][row][4 pieces]
-  __shared__ F hs[TERMS * S][ROWS * 4];
+  __shared__ P hs[TERMS * S][ROWS * 4];
   __shared__ float back[ROWS];
   __shared__ int at[ROWS], of[ROWS];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
@@ -520,16 +527,37 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
   const bool whole = c0 + 16 <= a.n;
   if (t < ROWS) at[t] = row_at(a.g, first + t), of[t] = which_at(a.g, first + t);
   F fw[4][S];
+  P numbers[4][kHalves ? S * OF_W : 1];  // of an f16 W
   int held = -1;  // the adapter whose W is in registers
+  bool fresh = false;
   auto inner = [&](int k) { return kPacked ? q % 2 * 8 : k * M::K + q * M::E; };  // a lane's elements of step k
   // rows of tile j: lane m has column 16 (m / 4) + 4 j + m % 4 of the wave's
   auto w_row = [&](int j) {
     const int c = c0 - q * 16 + (m >> 2) * 16 + 4 * j + (m & 3);
     return (const T*)a.W + held * a.step + (int64_t)min(c, a.n - 1) * a.ldw;
   };
-  auto hold = [&](int ad) {
+  auto take = [&]() __attribute__((always_inline)) {  // what hold has loaded
+    if constexpr (kHalves) {
+      if (!fresh) return;
+      fresh = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          P hi, lo;
+          split(fw[j][k], hi, lo);
+          if constexpr (kPacked) {
+            const u4 first = __builtin_bit_cast(u4, hi), second = __builtin_bit_cast(u4, lo);
+            numbers[j][k] = __builtin_bit_cast(P, q < 2 ? first : second);
+          } else {
+            numbers[j][k * OF_W] = hi, numbers[j][k * OF_W + 1] = lo;
+          }
+        }
+    }
+  };
+  auto hold = [&](int ad) __attribute__((always_inline)) {
     if (ad >= a.g.count || ad == held) return;
-    held = ad;
+    held = ad, fresh = true;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -540,6 +568,7 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
 #pragma unroll
         for (int k = 0; k < S; ++k) end_row<SHORT>(fw[j][k], w_row(j), inner(k), a.rank);
     }
+    if (S > 1) take();  // (as loaded and as numbers they would not fit the registers)
   };
   {
     // W of the work group's first adapter is on its way while h is laid out
@@ -579,25 +608,7 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
 #pragma unroll
       for (int e = 0; e < M::E; ++e)
         if (!some || (kPacked ? p % 2 * 8 : k * M::K + p * M::E) >= a.ranks) h[k][e] = 0.0f;
-    float up = 1.0f;
-    if constexpr (std::is_same<T, _Float16>::value) {
-      // a power of two brings the row's largest to [1, 2): halves reach from there to where it does not matter
-      uint32_t top = 0;
-#pragma unroll
-      for (int k = 0; k < S; ++k)
-#pragma unroll
-        for (int e = 0; e < M::E; ++e) top = max(top, mag(h[k][e]));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-      const uint32_t ex = min(max(top >> 23, 2u), 252u);
-      up = __uint_as_float(ex << 23);
-      const float down = __uint_as_float((254u - ex) << 23);
-#pragma unroll
-      for (int k = 0; k < S; ++k)
-#pragma unroll
-        for (int e = 0; e < M::E; ++e) h[k][e] *= down;
-    }
-    if (p == 0) back[i0] = up * f;
+    if (p == 0) back[i0] = f;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       if constexpr (!kNarrow) {
@@ -606,18 +617,19 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
         for (int e = 0; e < 4; ++e) v[e] = h[k][e];
         hs[k][i0 * 4 + p] = v;
       } else {
-        F v[NUMBERS + 1] = {};
+        P v[4] = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float x = h[k][e];
-#pragma unroll
-          for (int u = 0; u < NUMBERS; ++u) v[u][e] = u + 1 < NUMBERS ? (T)split(x, T()) : (T)x;
+          v[0][e] = (bf16)split(x);
+          v[1][e] = (bf16)split(x);
+          v[2][e] = (bf16)x;
         }
 #pragma unroll
         for (int u = 0; u < TERMS; ++u) {
-          if constexpr (kPacked) {
+          if constexpr (kPacked && !kHalves) {
             const u4 first = __builtin_bit_cast(u4, v[2 * u]), second = __builtin_bit_cast(u4, v[2 * u + 1]);
-            hs[u * S + k][i0 * 4 + p] = __builtin_bit_cast(F, p < 2 ? first : second);
+            hs[u * S + k][i0 * 4 + p] = __builtin_bit_cast(P, p < 2 ? first : second);
           } else {
             hs[u * S + k][i0 * 4 + p] = v[u];
           }
@@ -648,6 +660,7 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
 #pragma unroll
       for (int b = 0; b < AHEAD; ++b) fetch(from / 16 + b, ahead[b]);
       hold(ad);
+      take();
 #pragma unroll 1
       for (int i = from / 16; i <= last / 16; ++i) {
         const int place = 16 * i + m;
@@ -666,9 +679,14 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
           for (int k = 0; k < S; ++k)
 #pragma unroll
             for (int u = 0; u < TERMS; ++u) {
-              const F h = hs[u * S + k][place * 4 + q];
+              const P h = hs[u * S + k][place * 4 + q];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) acc[j] = mma(fw[j][k], h, acc[j]);
+              for (int o = 0; o < OF_W; ++o)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if constexpr (kHalves) acc[j] = mma(numbers[j][k * OF_W + o], h, acc[j]);
+                  else acc[j] = mma(fw[j][k], h, acc[j]);
+                }
             }
         }
         if (!own || c0 >= a.n) continue;
@@ -744,7 +762,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
   typedef typename M::F F;
   constexpr bool kNarrow = sizeof(T) == 2;
   constexpr int C = M::E;             // column tiles: columns C m + j
-  constexpr int TERMS = std::is_same<T, bf16>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
+  constexpr bool kHalves = std::is_same<T, _Float16>::value;
   constexpr int COLS = 16 * C, STEP = 32;  // columns, rows of a step
   constexpr int L = kNarrow ? 8 : 8;       // rows of a lane and step
   constexpr int PITCH = COLS + 4;
@@ -765,11 +783,6 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
     const float f = o.scales ? o.scales[ad] : 1.0f;
     // place of a lane's row e in the step from s on
     auto place = [&](int s, int e) { return kNarrow ? s + 8 * q + e : s + 4 * e + q; };
-    // f16: sums are kept relative to a power of two for each rank, that of its largest h so
-    // far, so that the halves of an h reach from there to where it does not matter
-    uint32_t ex[RT];
-#pragma unroll
-    for (int j = 0; j < RT; ++j) ex[j] = 2;
     struct Step {
       u4 z[L];
       float h[RT][L];
@@ -810,30 +823,15 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
         }
       }
       if constexpr (kNarrow) {
-        F h[RT][TERMS];
-        if constexpr (std::is_same<T, _Float16>::value) {
-#pragma unroll
-          for (int j = 0; j < RT; ++j) {
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, mag(x.h[j][e] * f));
-            top = max(ex[j], min(quad_max(top) >> 23, 252u));
-            if (__ballot(top != ex[j]) != 0) {
-              const float by = top - ex[j] > 126u ? 0.0f : __uint_as_float((127u - (top - ex[j])) << 23);
-#pragma unroll
-              for (int c = 0; c < C; ++c) acc[c][j] *= by;
-              ex[j] = top;
-            }
-          }
-        }
+        b8 h[RT][3];
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             float v = x.h[j][e] * f;
-            if constexpr (std::is_same<T, _Float16>::value) v *= __uint_as_float((254u - ex[j]) << 23);
-#pragma unroll
-            for (int u = 0; u < TERMS; ++u) h[j][u][e] = u + 1 < TERMS ? (T)split(v, T()) : (T)v;
+            h[j][0][e] = (bf16)split(v);
+            h[j][1][e] = (bf16)split(v);
+            h[j][2][e] = (bf16)v;
           }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
@@ -841,11 +839,15 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
 #pragma unroll
           for (int p = 0; p < 4; ++p)
             col[p] = __builtin_amdgcn_perm(x.z[2 * p + 1][c / 2], x.z[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-          const F fz = __builtin_bit_cast(F, col);
+          b8 z[2];
+          if constexpr (kHalves) split(__builtin_bit_cast(h8, col), z[0], z[1]);
+          else z[0] = __builtin_bit_cast(b8, col);
 #pragma unroll
           for (int j = 0; j < RT; ++j)
 #pragma unroll
-            for (int u = TERMS - 1; u >= 0; --u) acc[c][j] = mma(fz, h[j][u], acc[c][j]);
+            for (int u = 2; u >= 0; --u)
+#pragma unroll
+              for (int o = kHalves ? 1 : 0; o >= 0; --o) acc[c][j] = mma(z[o], h[j][u], acc[c][j]);
         }
       } else {
 #pragma unroll
@@ -887,7 +889,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
           f4 v;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            v[e] = std::is_same<T, _Float16>::value ? acc[c + e][j][i] * __uint_as_float(ex[j] << 23) : acc[c + e][j][i];
+            v[e] = acc[c + e][j][i];
           *(f4*)(red + ((w * RT + j) * 16 + m) * PITCH + C * (4 * q + i) + c) = v;
         }
     __syncthreads();
