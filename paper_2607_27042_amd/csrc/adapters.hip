@@ -105,10 +105,13 @@ __device__ __forceinline__ void end_row(typename Mat<T>::F& f, const T* row, int
   f = __builtin_bit_cast(typename Mat<T>::F, b);
 }
 
-// Takes the first eight bits of x off it: x becomes the rest; infinities leave nothing.
+// Takes the first eight bits of x off it: x becomes the rest. Both have its sign and neither is
+// zero unless x is (what bf16 holds whole is taken as the number before it), so that the sum
+// of what an infinite factor gives with each is infinite too.
 __device__ __forceinline__ float split(float& x) {
-  const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-  x = x == hi ? 0.0f : x - hi;
+  const uint32_t b = __float_as_uint(x);
+  const float hi = __uint_as_float((b - (x != 0.0f ? 1u : 0u)) & 0xffff0000u);
+  x -= hi;
   return hi;
 }
 // eight f16 as the sums of two bf16 each

@@ -10,6 +10,8 @@ the last rounding hides nothing.
 
 Loud ranks and rows, whose other factor is zero, may take nothing from the others: what is
 allowed goes by the sum of the magnitudes of a result's own terms."""
+import math
+
 import pytest
 import torch
 
@@ -161,3 +163,22 @@ def test_loud_rows(M, N, K, R, count, dtype):
     p.X[at == 1] = 0.0
     O, _ = p.forward(Y=False)
     componentwise(p, dtype, O, H, *p.backward(H, D=False))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_infinities_stay(dtype):
+    """An infinite h or gradient beside numbers that fewer bits hold gives infinities, not NaN."""
+    M, N, K, R = 40, 72, 64, 4
+    p = Problem(M, N, K, R, 1, dtype, seed=3, index=torch.zeros(M, dtype=torch.int32, device="cuda"), scales=False)
+    p.A.fill_(1.0)
+    p.B.fill_(0.5)
+    p.X.fill_(1.0)
+    p.G.fill_(1.0)
+    p.X[3, 5], p.X[4, 6] = math.inf, -math.inf
+    O, H = p.forward(Y=False)
+    assert bool((O[3] == math.inf).all()) and bool((O[4] == -math.inf).all()) and bool((O[5:] == 128.0).all())
+    p.X.fill_(1.0)
+    p.G[7, 2] = math.inf
+    dX, dA, dB = p.backward(torch.ones(M, R, device="cuda"), D=False)
+    assert bool((dX[7] == math.inf).all()) and bool((dX[8:] == 144.0).all()) and bool((dA == math.inf).all())
+    assert bool((dB[0, 2] == math.inf).all()) and bool((dB[0, 3:] == 40.0).all())
