@@ -40,7 +40,7 @@ constexpr int kMaxParts = 64;            // of a row
 constexpr float kLog2E = 1.44269504088896341f;
 constexpr double kLog2E64 = 1.4426950408889634;
 
-// 2^t to about 1e-13 of itself for t in [-1000, 1000], 0 far below (and for NaN), from a
+// 2^t to about 1e-13 of itself for t in [-1000, 1000], 0 or infinity down to -5000 and up to 5000, from a
 // table of 2^(k / 256). t is split at the nearest multiple of 1 / 256, which adding 1.5 2^44
 // leaves in the low bits; the rest, |f| <= 1 / 512, needs four terms of its series. The 64-bit
 // terms of the last rows are most of what their pass costs: 64 rows of 128000 with as many
@@ -52,7 +52,6 @@ struct Powers {
     if (threadIdx.x < 256) at[threadIdx.x] = exp2((double)threadIdx.x * 0x1p-8);
   }
   __device__ __forceinline__ double of(double t) const {
-    t = fmax(t, -5000.0);
     const double big = t + 0x1.8p44, f = t - (big - 0x1.8p44);
     const uint32_t k = __builtin_bit_cast(u2, big)[0];
     double p = 0.05550410866482158;
@@ -140,13 +139,14 @@ struct VerifyArgs {
   Part* part;
   Last* last;
   State* state;
-  // e^(a (x - m)) and e^(ad d - lse); of -inf both are 0
+  // e^(a (x - m)) and e^(ad d - lse); of -inf both are 0. Differences first (a d is exact): with m
+  // a log2(e) rounded before x was taken from it, the largest logit's own term would be 1 only as
+  // long as m a is below 2^50 or so.
   __device__ __forceinline__ double p2(const Powers& of, float x, double m) const {
-    const double c = (double)a * kLog2E64;
-    return of.of(fma((double)x, c, -m * c));
+    return of.of(fmax(((double)x - m) * ((double)a * kLog2E64), -5000.0));  // (NaN: 0)
   }
   __device__ __forceinline__ double q2(const Powers& of, float d, double lse) const {
-    return of.of(fma((double)d, (double)ad * kLog2E64, -lse * kLog2E64));
+    return of.of(fmin(fmax(fma((double)d, (double)ad, -lse) * kLog2E64, -5000.0), 5000.0));
   }
 };
 

@@ -1,0 +1,75 @@
+"""gptq2d_tree_verify at scales and logits of any size, against the scan in 64 bits, whose
+products of a 32-bit logit and a 32-bit scale are exact and whose differences are rounded
+once. What is kept and next has to be equal, log probabilities are bounded as in
+test_gpu_verify.py."""
+import math
+
+import pytest
+import torch
+
+import serving
+from test_gpu_verify import check, gen, likely, logits, tree
+
+pytestmark = pytest.mark.gpu
+
+
+def f32(x):
+    return float(torch.tensor(x, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("mode", ["certain", "drawn", "greedy"])
+@pytest.mark.parametrize("scale", [1e7, 1e10, 1e12, 1e14, 1e18, 1e30, 2e38])
+def test_large_scales(scale, mode):
+    """Cold samplers: of logits in [1, 30] the largest ones alone are left, of those near zero some more."""
+    r = gen(int(math.log2(scale)))
+    seqs, width, scale = 6, 5, f32(scale)
+    for vocab in (40, 5000):
+        X = 1.0 + 29.0 * torch.rand(seqs * width, vocab, generator=r, device="cuda")
+        X[:, ::3] = X.max(1, keepdim=True).values  # many of the same
+        near = torch.rand(seqs * width, vocab, generator=r, device="cuda") * (4.0 / scale)
+        X = torch.where((torch.arange(seqs * width, device="cuda") % 2 == 0).unsqueeze(1), X, near)
+        parents = tree(r, seqs, width)
+        tokens = likely(X, torch.zeros(seqs, width), parents, r)
+        u = torch.rand(seqs, width, generator=r, device="cuda") if mode != "greedy" else None
+        D = logits(r, seqs * width, vocab, "f32") if mode == "drawn" else None
+        lse = torch.logsumexp(D.double(), 1).float() if mode == "drawn" else None
+        got = check(X, tokens, parents, None, scale, u, D, lse)
+        assert int(got[2].min()) >= 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [0.5, 0.75, 1.0])
+@pytest.mark.parametrize("mode", ["certain", "drawn", "greedy"])
+def test_lowest_values(dtype, scale, mode):
+    """Masks of the type's lowest value: in part of a row, in all of it (then every token is as likely)."""
+    r = gen(17)
+    seqs, width = 6, 4
+    for vocab in (33, 4100):
+        X = logits(r, seqs * width, vocab, dtype)
+        low = torch.finfo(X.dtype).min
+        X.view(seqs, width, vocab)[1, 0] = low
+        X.view(seqs, width, vocab)[2] = low
+        X.view(seqs, width, vocab)[3, :, ::2] = low
+        X.view(seqs, width, vocab)[4, 0, :30] = -math.inf
+        X.view(seqs, width, vocab)[4, 0, 30:] = low
+        tokens = torch.randint(vocab, (seqs, width), generator=r, device="cuda")
+        u = torch.rand(seqs, width, generator=r, device="cuda") if mode != "greedy" else None
+        D = logits(r, seqs * width, vocab, dtype) if mode == "drawn" else None
+        lse = torch.logsumexp(D.double(), 1).float() if mode == "drawn" else None
+        got = check(X, tokens, None, None, scale, u, D, lse)
+        assert int(got[2].min()) >= 0
+
+
+def test_far_drafts():
+    """A draft's logits far from zero, and rows of it that are infinite or empty where nothing is drawn from them."""
+    r = gen(19)
+    seqs, width, vocab = 8, 5, 900
+    X = logits(r, seqs * width, vocab, "f32")
+    D = X + 0.5 * torch.randn(X.shape, generator=r, device="cuda") + 2.0 ** 14
+    D[width:2 * width] -= 2.0 ** 15
+    lse = torch.logsumexp(D.double(), 1).float()
+    D[2 * width:3 * width, 7:] = -math.inf
+    lse[2 * width:3 * width] = torch.logsumexp(D[2 * width:3 * width].double(), 1).float()
+    tokens = torch.randint(7, (seqs, width), generator=r, device="cuda")
+    parents = tree(r, seqs, width, 4)
+    check(X, tokens, parents, None, 1.0, torch.rand(seqs, width, generator=r, device="cuda"), D, lse)
