@@ -272,7 +272,9 @@ __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
   const int lead = lead_of(x);
   const int steps = (v.vocab + lead + kChunk - 1) / kChunk;
   const int first = (int)((int64_t)steps * part / v.parts), last = (int)((int64_t)steps * (part + 1) / v.parts);
-  const float a2 = v.a * kLog2E;
+  // (never infinite: the largest logit's own term would be that times 0. What is too small then matters
+  // for differences below 2^-120.)
+  const float a2 = fminf(v.a * kLog2E, 0x1.fffffep127f);
   float m = -INFINITY, sum = 0.0f;
   int at = 0x7fffffff;
   // a thread's elements of a step lie in pieces of 16 bytes, the pieces of a group side by

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import serving
-from test_gpu_verify import check, gen, likely, logits, tree
+from test_gpu_verify import call, check, gen, likely, logits, tree
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +73,25 @@ def test_far_drafts():
     tokens = torch.randint(7, (seqs, width), generator=r, device="cuda")
     parents = tree(r, seqs, width, 4)
     check(X, tokens, parents, None, 1.0, torch.rand(seqs, width, generator=r, device="cuda"), D, lse)
+
+
+@pytest.mark.parametrize("mode", ["certain", "greedy"])
+@pytest.mark.parametrize("scale", [2.5e38, 3.0e38, torch.finfo(torch.float32).max])
+def test_largest_scales(scale, mode):
+    """As cold as 32 bits go: the scale times log2(e) has no 32-bit number."""
+    r = gen(23)
+    seqs, width, vocab, scale = 6, 5, 300, f32(scale)
+    X = logits(r, seqs * width, vocab, "f32")
+    X[:, ::3] = X.max(1, keepdim=True).values
+    parents = tree(r, seqs, width)
+    tokens = likely(X, torch.zeros(seqs, width), parents, r)
+    tokens[:, 1:3] = 3  # one of the largest
+    u = torch.rand(seqs, width, generator=r, device="cuda") if mode == "certain" else None
+    # (every logit below the largest is further from it than 32 bits tell: log p = -inf in 32 bits, if not in 64)
+    got = call(X, tokens, parents, None, scale, u)
+    ref = serving.verify(X, tokens, parents, None, scale, u)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(got[:3], ref[:3]))
+    a, b = got[3].cpu(), ref[3].float()
+    assert torch.equal(torch.isinf(a), torch.isinf(b)) and not bool(torch.isnan(a).any())
+    fine = torch.isfinite(b)
+    assert bool(((a[fine] - b[fine]).abs() <= 2.0 ** -24 * (48 + b[fine].abs())).all())
