@@ -1271,14 +1271,15 @@ gptq2d_status gptq2d_adapters_backward(int64_t M, int64_t N, int64_t K, int R, i
                                        size_t ws_bytes, void* stream) {
   if (bad_shape(M, N, K, R, count)) return refuse("M, N and K must lie in [1, 2^22] (M may be 0), M N and M K in [0, 2^37], R in [1, 128], count in [1, 4096]");
   if (!narrow_dtype(dt)) return refuse("bad dtype");
-  if (!dX && !dA && !dB) return refuse("no gradient is asked for");
+  if (M > 0 && !dX && !dA && !dB) return refuse("no gradient is asked for");  // (of no rows dX may be NULL)
   if (!groups) return refuse("groups is NULL");
   if (M == 0) {  // nothing but zeros
+    if (!dA && !dB) return GPTQ2D_OK;
     OuterArgs o = {groups_of(groups, 0, count), R, 1, 1, false, {}};
     int n = 0;
     if (dA) o.of[n].n = (int)K, o.of[n++].out = dA;
     if (dB) o.of[n].n = (int)N, o.of[n++].out = dB;
-    if (n > 0) outer<float>(o, n, (hipStream_t)stream);
+    outer<float>(o, n, (hipStream_t)stream);
     return launched("gptq2d_adapters_backward");
   }
   if (!G) return refuse("G is NULL");

@@ -227,3 +227,12 @@ def test_adapter_sizes(lib):
         assert lib.gptq2d_adapters_workspace_size(M, N, K, 4, 2) == 0
         assert lib.gptq2d_adapters_backward_workspace_size(M, N, K, 4, 2) == 0
     assert lib.gptq2d_adapters_workspace_size(1 << 22, 8, 1 << 15, 4, 2) > 0
+
+
+def test_gradients_of_no_rows(lib):
+    """An empty batch's tensors have no memory: a dX of no rows is nothing to do, not nothing asked for."""
+    args = lambda M, dX: (M, 16, 24, 4, 2, BF16, NULL, 16, NULL, 24, P, 24, P, 4, P, P, NULL, NULL, 0, dX, 24, NULL, NULL, NULL,
+                          0, None)
+    assert lib.gptq2d_adapters_backward(*args(0, NULL)) == 0
+    assert lib.gptq2d_adapters_backward(*args(0, P)) == 0
+    refused(lib.gptq2d_adapters_backward(*args(8, NULL)), "no gradient")
