@@ -153,6 +153,8 @@ def _layout(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
     outside the tensor or another row."""
     if t.dim() != 2 or tuple(t.shape) != (rows, cols):
         raise ValueError(f"{what} must be {rows} x {cols}, got {tuple(t.shape)}")
+    if rows == 0:
+        return cols  # nothing is touched (and an expanded tensor of no rows counts as contiguous)
     if t.stride(1) != 1 and cols > 1:
         raise ValueError(f"{what} must be row-major with unit column stride")
     ld = t.stride(0) if rows > 1 else cols

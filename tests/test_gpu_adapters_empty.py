@@ -22,3 +22,11 @@ def test_no_rows(wants, dtype):
         assert (t.grad is not None) == w
         if w:
             assert t.grad.shape == t.shape and int(torch.count_nonzero(t.grad)) == 0
+
+
+def test_expanded_gradient_of_no_rows():
+    """The gradient of a sum over no rows has no strides."""
+    X, A, B = (torch.randn(s, device="cuda").requires_grad_() for s in ((0, 64), (3, 8, 64), (3, 96, 8)))
+    groups = g.adapter_groups(torch.empty(0, dtype=torch.int32, device="cuda"), 3)
+    g.adapters(X, A, B, groups).sum().backward()
+    assert X.grad.shape == (0, 64) and int(torch.count_nonzero(A.grad)) == 0 and int(torch.count_nonzero(B.grad)) == 0
