@@ -1144,11 +1144,14 @@ def adapters(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, groups: torch.Te
              stream=None) -> torch.Tensor:
     """Y + scales[a] (X A[a]^T) B[a]^T for the adapter a of each row (A: [count, R, K], B:
     [count, N, R], scales: float32 [count], None: 1; Y None: zeros); groups as
-    adapter_groups gives it. X, A, B and Y get their gradients, scales none. Before a
+    adapter_groups gives it. X, A, B and Y get their gradients, scales none; forward-mode tangents
+    are refused. Before a
     backward pass is captured into a graph, let go of what was computed eagerly from the same
     leaves: torch keeps a leaf's gradient on the stream of the first, and a capture may not
     wait for that."""
     (M, K), (count, N, R) = X.shape, B.shape
+    if any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in (X, A, B, Y, scales)):
+        raise NotImplementedError("adapters has no forward-mode derivative: its inputs must not carry tangents")
     with _on(stream, X):
         if torch.is_grad_enabled():
             if scales is not None and scales.requires_grad:
@@ -1240,7 +1243,8 @@ class Verified(NamedTuple):
 def tree_verify(X: torch.Tensor, tokens: torch.Tensor, parents=None, drafts=None, scale: float = 1.0, uniform=None, D=None,
                 draft_lse=None, draft_scale: float = 1.0, stream=None) -> Verified:
     """Which drafted tokens are kept, and the token after them (gptq2d_tree_verify); D without
-    draft_lse is scored first."""
+    draft_lse is scored first. Nothing of it takes part in autograd, whatever X requires:
+    token_logprobs gives log probabilities that do."""
     with _on(stream, X):
         if D is not None and draft_lse is None:
             draft_lse = token_logprobs(D.detach(), None, draft_scale).lse

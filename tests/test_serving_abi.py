@@ -236,3 +236,15 @@ def test_gradients_of_no_rows(lib):
     assert lib.gptq2d_adapters_backward(*args(0, NULL)) == 0
     assert lib.gptq2d_adapters_backward(*args(0, P)) == 0
     refused(lib.gptq2d_adapters_backward(*args(8, NULL)), "no gradient")
+
+
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("which", range(5))
+def test_adapters_refuse_tangents(which, grad):
+    """No derivative is lost without a word: there is no forward-mode one."""
+    tensors = [torch.zeros(5, 8), torch.zeros(2, 4, 8), torch.zeros(2, 6, 4), torch.zeros(5, 6), torch.ones(2)]
+    with torch.autograd.forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        tensors[which] = torch.autograd.forward_ad.make_dual(tensors[which], torch.ones_like(tensors[which]))
+        X, A, B, Y, scales = tensors
+        with pytest.raises(NotImplementedError, match="tangents"):
+            binding.adapters(X, A, B, None, Y, scales)
