@@ -503,8 +503,9 @@ size_t gptq2d_tree_verify_workspace_size(int64_t seqs, int width, int64_t vocab)
  *   logprob (device, seqs x width): log p of drafted token t after the token that it
  *       follows, 0 for one that follows no drafted token or is not there; at t = 0
  *       that of the next token.
- * A token outside the vocabulary does not pass and has log p = -inf. After a row with
- * a NaN or +inf, or of nothing but -inf, no token passes, next is -1 and log p NaN.
+ * A token outside the vocabulary (padding, say) has log p = -inf; all else is as if it
+ * were not there. After a row with a NaN or +inf, or of nothing but -inf, no token
+ * passes, next is -1 and log p NaN.
  * 1 <= width <= 64, seqs <= 65535, vocab <= 2^28. The same call gives the same bits.
  * workspace: as sized above, 256-byte aligned, owned by the caller; overlapping
  * calls need distinct ones. Errors: INVALID_ARG, WORKSPACE, HIP. */

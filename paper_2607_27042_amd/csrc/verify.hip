@@ -361,6 +361,7 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     if (v.D && ok) q = exp2(((double)(float)D[parent * v.ldd + token] * (double)v.ad - (double)dlse[parent]) * kLog2E64);
     best = p == p && token == r.at;
   }
+  const uint64_t words = __ballot(token >= 0 && token < v.vocab);
   const double u = v.u && in ? (double)v.u[seq * v.width + lane] : 0.0;
   auto of = [&](double x, int from) { return at_lane(x, from); };
   int cur = n > 0 ? 0 : -1, kept = n > 0 ? 1 : 0;
@@ -398,6 +399,8 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
       if (!v.u) {
         if (__ballot(best) >> c & 1) taken = c;
       } else if (v.D) {
+        // (what is no token was not drawn from q: that it does not pass says nothing of the others)
+        if (!(words >> c & 1)) continue;
         if (gone != 0) M = remaining();
         const double qc = of(q, c);
         if (of(u, c) * M * qc < pc - beta * qc) taken = c;

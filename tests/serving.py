@@ -60,6 +60,8 @@ def verify(X, tokens, parents, drafts, scale, uniform, D=None, draft_lse=None, d
                 way.append(t)
                 continue
             if D is not None:
+                if not 0 <= y < vocab:  # not drawn from q: no rejection
+                    continue
                 if lp is not None:
                     beta += 1.0 if not gone else float((lp.exp() - beta * q[b, cur]).clamp(min=0).sum())
                 gone.append(y)
