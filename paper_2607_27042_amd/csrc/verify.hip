@@ -577,92 +577,101 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   if (v.u) {
     const double u = (double)u32;
     double left = drawn ? fmax(l.left / total - l.less, 0.0) : l.left * f;
-    if (s.residual && __ballot(left > 0.0) == 0) {  // nothing is left of p: p itself
-      s.residual = 0, drawn = false;
-      left = l.sum * f;
-    }
-    // sums of the parts up to the lane's
-    const double upto = sum_upto(left), aim = u * at_lane(upto, 63);
-    const uint64_t over = __ballot(upto > aim && left > 0.0), some = __ballot(left > 0.0);
-    const int part = over != 0 ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1);
-    const double before = at_lane(upto - left, part);
-    const double pm = drawn ? s.m : at_lane(l.m, part), pf = at_lane(f, part);
-    const int lead = lead_of(x);
-    const int begin = part * v.per - lead, end = min(begin + v.per, v.vocab);
-    const double lse = drawn ? (double)v.dlse[row] : 0.0;
-    find_gone(v, s, seq, begin, end, gone);
     powers.fill();
-    __syncthreads();
-    const double by = 1.0 / total, aim_in = aim - before;
-    double past = 0.0;
-    int late = -1, pick = -1;  // the last token with something left, the one looked for
+    int pick;
+    bool known;
 #pragma unroll 1
-    for (int step = begin; step < end; step += STEPS * kFewChunk) {
-      Turn<T, STEPS> turn, other;
-      turn.load(x, step + t * kFew, end);
-      if (drawn) other.load(d, step + t * kFew, end);
-      double r[STEPS][kFew], before_in[STEPS];
+    for (;;) {
+      if (s.residual && __ballot(left > 0.0) == 0) {  // nothing is left of p: p itself
+        s.residual = 0, drawn = false;
+        left = l.sum * f;
+      }
+      // sums of the parts up to the lane's
+      const double upto = sum_upto(left), aim = u * at_lane(upto, 63);
+      const uint64_t over = __ballot(upto > aim && left > 0.0), some = __ballot(left > 0.0);
+      const int part = over != 0 ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1);
+      const double before = at_lane(upto - left, part);
+      const double pm = drawn ? s.m : at_lane(l.m, part), pf = at_lane(f, part);
+      const int lead = lead_of(x);
+      const int begin = part * v.per - lead, end = min(begin + v.per, v.vocab);
+      const double lse = drawn ? (double)v.dlse[row] : 0.0;
+      find_gone(v, s, seq, begin, end, gone);
+      __syncthreads();
+      const double by = 1.0 / total, aim_in = aim - before;
+      double past = 0.0;
+      int late = -1;  // the last token with something left
+      pick = -1;
+#pragma unroll 1
+      for (int step = begin; step < end; step += STEPS * kFewChunk) {
+        Turn<T, STEPS> turn, other;
+        turn.load(x, step + t * kFew, end);
+        if (drawn) other.load(d, step + t * kFew, end);
+        double r[STEPS][kFew], before_in[STEPS];
 #pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
-        const int e = step + k * kFewChunk + t * kFew;
-        double mine = 0.0;
+        for (int k = 0; k < STEPS; ++k) {
+          const int e = step + k * kFewChunk + t * kFew;
+          double mine = 0.0;
 #pragma unroll
-        for (int i = 0; i < kFew; ++i) r[k][i] = v.p2(powers, turn.z[k][i], pm);
-        if (drawn) {
+          for (int i = 0; i < kFew; ++i) r[k][i] = v.p2(powers, turn.z[k][i], pm);
+          if (drawn) {
 #pragma unroll
-          for (int i = 0; i < kFew; ++i) r[k][i] = fmax(fma(r[k][i], by, -s.beta * v.q2(powers, other.z[k][i], lse)), 0.0);
-        } else if (s.residual) {
-          without(gone, e, r[k]);
+            for (int i = 0; i < kFew; ++i) r[k][i] = fmax(fma(r[k][i], by, -s.beta * v.q2(powers, other.z[k][i], lse)), 0.0);
+          } else if (s.residual) {
+            without(gone, e, r[k]);
+          }
+#pragma unroll
+          for (int i = 0; i < kFew; ++i) {
+            r[k][i] *= pf;
+            mine += r[k][i];
+            if (r[k][i] > 0.0) late = e + i;
+          }
+          const double in = sum_upto(mine);
+          before_in[k] = in - mine;
+          if (lane == 63) sums[k][w] = in;
         }
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kFew; ++i) {
-          r[k][i] *= pf;
-          mine += r[k][i];
-          if (r[k][i] > 0.0) late = e + i;
+        for (int k = 0; k < STEPS; ++k) {
+          double sum = past + before_in[k];
+          for (int i = 0; i < kThreads / 64; ++i) {
+            const double all = sums[k][i];
+            if (i < w) sum += all;
+            past += all;
+          }
+#pragma unroll
+          for (int i = 0; i < kFew; ++i) {
+            sum += r[k][i];
+            if (pick < 0 && r[k][i] > 0.0 && sum > aim_in) pick = step + k * kFewChunk + t * kFew + i;
+          }
         }
-        const double in = sum_upto(mine);
-        before_in[k] = in - mine;
-        if (lane == 63) sums[k][w] = in;
+        // the lowest (of none: -1, as a number without sign the largest)
+        pick = (int)~group_max<64>(~(uint32_t)pick);
+        if (lane == 0) found[w] = pick;
+        __syncthreads();
+        for (int k = 0; k < kThreads / 64; ++k) pick = (int)min((uint32_t)pick, (uint32_t)found[k]);
+        if (pick >= 0) {  // (the thread that has it has its logit)
+#pragma unroll
+          for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+            for (int i = 0; i < kFew; ++i)
+              if (step + k * kFewChunk + t * kFew + i == pick) logit = turn.z[k][i];
+          break;
+        }
+      }
+      known = pick >= 0;
+      if (pick < 0) {  // the sums' last place: the last one
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) late = max(late, __shfl_xor(late, k));
+        __syncthreads();
+        if (lane == 0) found[w] = late;
+        __syncthreads();
+        for (int k = 0; k < kThreads / 64; ++k) pick = max(pick, found[k]);
       }
       __syncthreads();
-#pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
-        double sum = past + before_in[k];
-        for (int i = 0; i < kThreads / 64; ++i) {
-          const double all = sums[k][i];
-          if (i < w) sum += all;
-          past += all;
-        }
-#pragma unroll
-        for (int i = 0; i < kFew; ++i) {
-          sum += r[k][i];
-          if (pick < 0 && r[k][i] > 0.0 && sum > aim_in) pick = step + k * kFewChunk + t * kFew + i;
-        }
-      }
-      // the lowest (of none: -1, as a number without sign the largest)
-      pick = (int)~group_max<64>(~(uint32_t)pick);
-      if (lane == 0) found[w] = pick;
-      __syncthreads();
-      for (int k = 0; k < kThreads / 64; ++k) pick = (int)min((uint32_t)pick, (uint32_t)found[k]);
-      if (pick >= 0) {  // (the thread that has it has its logit)
-#pragma unroll
-        for (int k = 0; k < STEPS; ++k)
-#pragma unroll
-          for (int i = 0; i < kFew; ++i)
-            if (step + k * kFewChunk + t * kFew + i == pick) logit = turn.z[k][i];
-        break;
-      }
+      if (pick >= 0 || !s.residual) break;
+      // what a part has left was the rounding of its sums (p and beta q alike to their last places): without it
+      if (lane == part) left = 0.0;
     }
-    const bool known = pick >= 0;
-    if (pick < 0) {  // the sums' last place: the last one
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) late = max(late, __shfl_xor(late, k));
-      __syncthreads();
-      if (lane == 0) found[w] = late;
-      __syncthreads();
-      for (int k = 0; k < kThreads / 64; ++k) pick = max(pick, found[k]);
-    }
-    __syncthreads();
     chosen = pick;
     value = known ? logit : pick >= 0 ? (float)x[pick] : 0.0f;
   }

@@ -95,3 +95,30 @@ def test_largest_scales(scale, mode):
     assert torch.equal(torch.isinf(a), torch.isinf(b)) and not bool(torch.isnan(a).any())
     fine = torch.isfinite(b)
     assert bool(((a[fine] - b[fine]).abs() <= 2.0 ** -24 * (48 + b[fine].abs())).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [8, 5000])
+def test_drafts_like_the_target(vocab, dtype):
+    """Drafts whose q is p to its last place or nearly: what is left of p after a rejection is
+    nothing, or what sums round to. The next token is one that has something of p."""
+    r = gen(29)
+    seqs, V = 65535 if vocab == 8 else 6000, vocab
+    for n in (1, 2, 3, 5, 6):
+        # n tokens of one size and a last one of next to nothing (the other way round for the draft)
+        X = torch.full((seqs, 2, V), -math.inf, device="cuda")
+        X[..., :n], X[..., n] = 0.0, -(17.0 + 2.0 * torch.rand(seqs, 1, generator=r, device="cuda"))
+        X = X.to(serving.DTYPE[dtype])
+        size = n + torch.exp(X[:, 0, n].double())  # of the row
+        lse = torch.log(size).float()
+        off = torch.randint(-40, 41, (seqs,), generator=r, device="cuda").double() * 2.0 ** -52
+        D = torch.full((seqs, 2, V), -math.inf, device="cuda")
+        D[..., :n] = (lse.double() - torch.log(size) + off).float().view(seqs, 1, 1)
+        D[..., n] = 5.0
+        D = D.to(X.dtype)
+        tokens = torch.full((seqs, 2), n, device="cuda")
+        u = 0.4 + 0.5 * torch.rand(seqs, 2, generator=r, device="cuda")
+        _, count, after, logprob = call(X.view(-1, V), tokens, None, None, 1.0, u, D.view(-1, V),
+                                        lse.unsqueeze(1).expand(-1, 2).flatten())
+        assert bool((count == 1).all())
+        assert bool(((after >= 0) & (after <= n)).all()) and bool(torch.isfinite(logprob).all())
