@@ -361,7 +361,6 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     if (v.D && ok) q = exp2(((double)(float)D[parent * v.ldd + token] * (double)v.ad - (double)dlse[parent]) * kLog2E64);
     best = p == p && token == r.at;
   }
-  const uint64_t words = __ballot(token >= 0 && token < v.vocab);
   const double u = v.u && in ? (double)v.u[seq * v.width + lane] : 0.0;
   auto of = [&](double x, int from) { return at_lane(x, from); };
   int cur = n > 0 ? 0 : -1, kept = n > 0 ? 1 : 0;
@@ -391,7 +390,8 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
     return fmax(r.over / r.all - r.less, 0.0);
   };
   while (cur >= 0) {
-    const uint64_t children = __ballot(parent == cur);
+    // (what is no token was not drawn from q: that it does not pass says nothing of the others)
+    const uint64_t children = __ballot(parent == cur && token >= 0 && token < v.vocab);
     int taken = -1;
     for (uint64_t left = children; left != 0; left &= left - 1) {
       const int c = __builtin_ctzll(left);
@@ -399,8 +399,6 @@ __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
       if (!v.u) {
         if (__ballot(best) >> c & 1) taken = c;
       } else if (v.D) {
-        // (what is no token was not drawn from q: that it does not pass says nothing of the others)
-        if (!(words >> c & 1)) continue;
         if (gone != 0) M = remaining();
         const double qc = of(q, c);
         if (of(u, c) * M * qc < pc - beta * qc) taken = c;
@@ -577,7 +575,6 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   if (v.u) {
     const double u = (double)u32;
     double left = drawn ? fmax(l.left / total - l.less, 0.0) : l.left * f;
-    powers.fill();
     int pick;
     bool known;
 #pragma unroll 1
@@ -596,6 +593,7 @@ __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
       const int begin = part * v.per - lead, end = min(begin + v.per, v.vocab);
       const double lse = drawn ? (double)v.dlse[row] : 0.0;
       find_gone(v, s, seq, begin, end, gone);
+      powers.fill();
       __syncthreads();
       const double by = 1.0 / total, aim_in = aim - before;
       double past = 0.0;
