@@ -576,9 +576,9 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
   {
     // W of the work group's first adapter is on its way while h is laid out
     int mine;
-    uint64_t heads = heads_of(a.g, first, min(ROWS, 64), mine);
+    uint64_t heads = heads_of(a.g, first, ROWS, mine);
     for (int z = 0; z < (int)blockIdx.z && heads != 0; ++z) heads &= heads - 1;
-    if (heads == 0 && gridDim.z > 1 && ROWS <= 64) return;  // the window has no more of them
+    if (heads == 0 && gridDim.z > 1) return;  // the window has no more of them
     if (heads != 0) hold(__builtin_amdgcn_readlane(mine, __builtin_ctzll(heads)));
   }
   for (int i0 = t >> 2; i0 < ROWS; i0 += 64) {
@@ -651,78 +651,76 @@ __global__ __launch_bounds__(256, (expand_waves<T, NK>())) void k_expand(ExpandA
 #pragma unroll
     for (int v = 0; v < V; ++v) to[v] = *(const u4_near*)((const char*)p + 16 * v);
   };
-  for (int z0 = 0, z = 0; z0 < ROWS; z0 += 64) {
-    // adapters of these (up to) 64 places; a work group of many takes some of them
-    const int mine = of[z0 + min(lane, ROWS - 1)], before = __shfl_up(mine, 1);
-    uint64_t heads = __ballot(lane < min(ROWS, 64) && mine >= 0 && (lane == 0 || mine != before));
-    for (; heads != 0; heads &= heads - 1, ++z) {
-      if (z % gridDim.z != blockIdx.z) continue;
-      const int from = z0 + __builtin_ctzll(heads), ad = __builtin_amdgcn_readfirstlane(of[from]);
-      const uint64_t rest = heads & (heads - 1);
-      const int last = (rest ? z0 + __builtin_ctzll(rest) : min(z0 + 64, ROWS)) - 1;
+  // the window's adapters; a work group of many takes some of them
+  const int mine = of[min(lane, ROWS - 1)], before = __shfl_up(mine, 1);
+  uint64_t heads = __ballot(lane < ROWS && mine >= 0 && (lane == 0 || mine != before));
+  for (int z = 0; heads != 0; heads &= heads - 1, ++z) {
+    if (z % gridDim.z != blockIdx.z) continue;
+    const int from = __builtin_ctzll(heads), ad = __builtin_amdgcn_readfirstlane(of[from]);
+    const uint64_t rest = heads & (heads - 1);
+    const int last = (rest ? __builtin_ctzll(rest) : ROWS) - 1;
 #pragma unroll
-      for (int b = 0; b < AHEAD; ++b) fetch(from / 16 + b, ahead[b]);
-      hold(ad);
-      take();
+    for (int b = 0; b < AHEAD; ++b) fetch(from / 16 + b, ahead[b]);
+    hold(ad);
+    take();
 #pragma unroll 1
-      for (int i = from / 16; i <= last / 16; ++i) {
-        const int place = 16 * i + m;
-        const bool own = place >= from && of[place] == ad;
-        u4 y[V];
+    for (int i = from / 16; i <= last / 16; ++i) {
+      const int place = 16 * i + m;
+      const bool own = place >= from && of[place] == ad;
+      u4 y[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) y[v] = ahead[0][v];
+      for (int v = 0; v < V; ++v) y[v] = ahead[0][v];
 #pragma unroll
-        for (int b = 0; b + 1 < AHEAD; ++b)
+      for (int b = 0; b + 1 < AHEAD; ++b)
 #pragma unroll
-          for (int v = 0; v < V; ++v) ahead[b][v] = ahead[b + 1][v];
-        if (i + AHEAD <= last / 16) fetch(i + AHEAD, ahead[AHEAD - 1]);
-        f4 acc[4] = {};
-        if (ad < a.g.count) {
+        for (int v = 0; v < V; ++v) ahead[b][v] = ahead[b + 1][v];
+      if (i + AHEAD <= last / 16) fetch(i + AHEAD, ahead[AHEAD - 1]);
+      f4 acc[4] = {};
+      if (ad < a.g.count) {
 #pragma unroll
-          for (int k = 0; k < S; ++k)
+        for (int k = 0; k < S; ++k)
 #pragma unroll
-            for (int u = 0; u < TERMS; ++u) {
-              const P h = hs[u * S + k][place * 4 + q];
+          for (int u = 0; u < TERMS; ++u) {
+            const P h = hs[u * S + k][place * 4 + q];
 #pragma unroll
-              for (int o = 0; o < OF_W; ++o)
+            for (int o = 0; o < OF_W; ++o)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  if constexpr (kHalves) acc[j] = mma(numbers[j][k * OF_W + o], h, acc[j]);
-                  else acc[j] = mma(fw[j][k], h, acc[j]);
-                }
-            }
-        }
-        if (!own || c0 >= a.n) continue;
-        const float f = back[place];
-        T* out = (T*)a.O + (int64_t)at[place] * a.ldo + c0;
-        const T* from_y = (const T*)a.Y + (int64_t)at[place] * a.ldy + c0;
-        float o[16];
-        if (whole && a.Y) {
-          typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = (float)__builtin_bit_cast(E, y[e * sizeof(T) / 16])[e % (16 / sizeof(T))];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = a.Y && c0 + e < a.n ? (float)from_y[e] : 0.0f;
-        }
-        if (ad < a.g.count) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = fmaf(acc[e / 4][e % 4], f, o[e]);
-        }
-        if (whole) {
-          typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            E x;
-#pragma unroll
-            for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = (T)o[v * 16 / sizeof(T) + e];
-            *(u4_near*)((char*)out + 16 * v) = __builtin_bit_cast(u4, x);
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (kHalves) acc[j] = mma(numbers[j][k * OF_W + o], h, acc[j]);
+                else acc[j] = mma(fw[j][k], h, acc[j]);
+              }
           }
-        } else {
+      }
+      if (!own || c0 >= a.n) continue;
+      const float f = back[place];
+      T* out = (T*)a.O + (int64_t)at[place] * a.ldo + c0;
+      const T* from_y = (const T*)a.Y + (int64_t)at[place] * a.ldy + c0;
+      float o[16];
+      if (whole && a.Y) {
+        typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (c0 + e < a.n) out[e] = (T)o[e];
+        for (int e = 0; e < 16; ++e) o[e] = (float)__builtin_bit_cast(E, y[e * sizeof(T) / 16])[e % (16 / sizeof(T))];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = a.Y && c0 + e < a.n ? (float)from_y[e] : 0.0f;
+      }
+      if (ad < a.g.count) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = fmaf(acc[e / 4][e % 4], f, o[e]);
+      }
+      if (whole) {
+        typedef T E __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          E x;
+#pragma unroll
+          for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = (T)o[v * 16 / sizeof(T) + e];
+          *(u4_near*)((char*)out + 16 * v) = __builtin_bit_cast(u4, x);
         }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (c0 + e < a.n) out[e] = (T)o[e];
       }
     }
   }
@@ -767,7 +765,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, const Outer& o, i
   constexpr int C = M::E;             // column tiles: columns C m + j
   constexpr bool kHalves = std::is_same<T, _Float16>::value;
   constexpr int COLS = 16 * C, STEP = 32;  // columns, rows of a step
-  constexpr int L = kNarrow ? 8 : 8;       // rows of a lane and step
+  constexpr int L = 8;                     // rows of a lane and step
   constexpr int PITCH = COLS + 4;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, m = lane & 15, q = lane >> 4;
   const int c0 = strip * COLS, r0 = rank0 * 16 * RT;
