@@ -44,8 +44,9 @@ constexpr double kLog2E64 = 1.4426950408889634;
 // table of 2^(k / 256). t is split at the nearest multiple of 1 / 256, which adding 1.5 2^44
 // leaves in the low bits; the rest, |f| <= 1 / 512, needs four terms of its series. The 64-bit
 // terms of the last rows are most of what their pass costs: 64 rows of 128000 with as many
-// of the drafts 18.6 us; with a comparison in place of the lower bound and the exponent's
-// own instruction 20.5, with a polynomial of degree 8 on |f| <= 1 / 2 and no table 22.
+// of the drafts 19.4 us, 18.7 with the scaled maximum rounded before it is taken off. (There, with
+// a comparison in place of the lower bound and the exponent's own instruction 20.5, with a
+// polynomial of degree 8 on |f| <= 1 / 2 and no table 22.)
 struct Powers {
   double at[256];
   __device__ __forceinline__ void fill() {  // by the first 256 threads; a barrier follows
@@ -258,7 +259,7 @@ __device__ __forceinline__ Part wave_join(Part p, float a) {
 }
 
 // Largest logit and sum of a part of every row that tokens follow. Bound by its bytes: 64
-// chains of 8 over 128000 bf16 26 us for 115 MB, 4.4 TB/s (with 64-bit terms, which would spare
+// chains of 8 over 128000 bf16 28 us for 115 MB, 4.1 TB/s (with 64-bit terms, which would spare
 // the last row's own sum, 61 us).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
@@ -322,8 +323,10 @@ __global__ __launch_bounds__(kThreads) void k_rows(VerifyArgs v) {
 
 constexpr int kWalk = 512;
 
-// The scan of a sequence. All waves go through it alike; where a drawn draft is
-// rejected they share a pass over the row.
+// The scan of a sequence. All waves go through it alike; where a drawn draft is rejected and
+// another follows the same token they share a pass over the row, one work group with nothing
+// loaded ahead: 16 trees of 13, three followers each, over 128000 bf16 126 us with 2.9 tokens
+// kept and 195 with 1.9, over 50257 f16 50; a chain, which has no such pass, 7.7.
 template <class T>
 __global__ __launch_bounds__(kWalk) void k_walk(VerifyArgs v) {
   __shared__ Part rows[kMaxWidth];
@@ -538,7 +541,7 @@ __global__ __launch_bounds__(kThreads) void k_last(VerifyArgs v) {
 
 // The next token of a sequence: its part of the row, then its place there, STEPS steps at
 // once: a part of 4096 waits once for memory and for the other waves' sums (64 rows of 128000
-// 7.5 us, step by step 10.0; parts of one step 3.7 us, as four 6.8).
+// 7.8 us, step by step 10.0; parts of one step 3.7 us, as four 6.8).
 template <class T, int STEPS>
 __global__ __launch_bounds__(kThreads) void k_next(VerifyArgs v) {
   __shared__ Gone gone;
