@@ -59,7 +59,7 @@ def products(p, left, right):
     return out, size
 
 
-def judge(got, low, size, rest, dtype):
+def expect(got, low, size, rest, dtype):
     """got = low + rest, rounded, with low of n products."""
     far = 2.0 ** -24 * (max(3, NUMBERS[dtype]) * USED + 4) * size
     want = low + rest.double()
@@ -79,7 +79,7 @@ def test_h(M, N, K, R, count, dtype):
     p.Y.copy_(-o)
     O, H = p.forward()
     assert torch.equal(H.double(), h)
-    judge(O, o, size, p.Y, dtype)
+    expect(O, o, size, p.Y, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
@@ -95,7 +95,7 @@ def test_p(M, N, K, R, count, dtype):
     dx, size = products(p, pr, p.A.transpose(1, 2))
     p.D.copy_(-dx)
     dX = p.backward(None, wants=(True, False, False))[0]
-    judge(dX, dx, size, p.D, dtype)
+    expect(dX, dx, size, p.D, dtype)
 
 
 def componentwise(p, dtype, O, H, dX, dA, dB):
